@@ -98,7 +98,11 @@ typedef enum {
     LAST_OP_INTERSECT_REFERENCE = 2,
     LAST_OP_SHORTEST_PATH = 3,
     LAST_OP_LOCAL_LOG_LIKELIHOOD = 4,
-    LAST_OP_LOSS = 5
+    LAST_OP_LOSS = 5,
+    LAST_OP_RESIDUAL_NORM_GRAD = 6,    /* this and the following: last_layer_workspace_bytes */
+    LAST_OP_PRODUCT = 7,
+    LAST_OP_PRODUCT_GRAD_INPUT = 8,
+    LAST_OP_PRODUCT_GRAD_WEIGHT = 9
 } last_op_t;
 
 /* Context dependency (Section 3): the full n-gram one in closed form (Figure 1a
@@ -244,6 +248,110 @@ last_status_t last_shortest_path(const last_weights_t* weights, const int32_t* l
                                  int32_t* labels, int32_t* states, float* score,
                                  int32_t* item_status,
                                  void* ws, size_t ws_bytes, void* hip_stream);
+
+/* ---- The layer between an encoder's frames and the lattice.
+ *
+ * A model's encoder hands frames to the lattice as f[b][t][hidden] or as arc weights, and takes df back.  These calls are
+ * what stands between: a root-mean-square norm with the residual's addition, a product with bias, activation and residual
+ * in one kernel, and activations kept in 8 bits for the backward pass (Section 4.2 is about what differentiation has to
+ * keep).  A feed-forward block is last_residual_norm, last_product (which keeps what its activation is applied to) and
+ * last_product with the residual; its gradient is last_product_grad_weight and last_product_grad_input twice and
+ * last_residual_norm_grad.
+ *
+ * Matrices hold a row for each frame, row b*T + t: `data` (dev) with `pitch` elements from a row to the next (columns are
+ * contiguous; pitch * size at most 4 MiB).  Types LAST_F32, LAST_BF16 and LAST_F16 are plain.  LAST_I8 (two's complement)
+ * and LAST_E4M3 (OCP 8-bit floats, 4 exponent bits, largest 448) are codes in blocks of 32 columns; `scales` (dev) holds a
+ * byte k for each block, `scale_pitch` bytes from a row to the next: a code q stands for q * 2^(k-127), k = 255 for NaN.
+ * The scale is the smallest power of two, from 2^-127, at which the block's largest magnitude does not pass the largest
+ * code (127, 448), codes are rounded to nearest even, and a block with an infinity or a NaN stands for NaN altogether.
+ * Any alignment of at least an element's is taken.  16-byte alignment of data and pitch is what is fast; products lay
+ * operands without it out in the workspace first.
+ *
+ * Frames: lengths (dev int32 [B], or NULL: all frames exist).  Frames t >= lengths[b] do not exist: what stands there is
+ * not read into any result, rows of results are zeros (codes 0, scale bytes 0) and sums over frames pass them by.  Lengths
+ * are taken as clamped to [0, T] (the lattice calls on them report a bad one).  T = 0 is allowed.
+ *
+ * Sums, norms and activations are in float32, each result is rounded once, to nearest even.  Results do not depend on
+ * timing: there are no atomics.  Results may not overlap operands, except that the element-wise calls (last_residual_norm,
+ * last_residual_norm_grad, last_kept_grad) may write s over x or over residual, dx over dy or over ds, in the same type
+ * and pitch. */
+typedef enum { LAST_F32 = 0, LAST_BF16 = 1, LAST_F16 = 2, LAST_I8 = 3, LAST_E4M3 = 4 } last_type_t;
+
+/* relu; silu: v / (1 + e^-v); gelu: v (1 + erf(v / sqrt 2)) / 2; tanh */
+typedef enum {
+    LAST_ACT_NONE = 0, LAST_ACT_RELU = 1, LAST_ACT_SILU = 2, LAST_ACT_GELU = 3, LAST_ACT_TANH = 4
+} last_activation_t;
+
+typedef struct {
+    int32_t B, T;
+    const int32_t* lengths;
+} last_frames_t;
+
+typedef struct {
+    void* data;
+    int32_t type;              /* last_type_t */
+    int64_t pitch;             /* elements */
+    uint8_t* scales;           /* LAST_I8, LAST_E4M3 only */
+    int64_t scale_pitch;
+} last_matrix_t;
+
+/* s = x + residual, inv = 1 / sqrt(mean over the H columns of s^2 + eps), y = s * inv * gain.  gain: dev float32 [H], H up
+ * to 16384.  residual may be NULL (then s = x); results that are NULL are not written: s (type of x), y (F32, BF16 or F16),
+ * kept (y in 8 bits), inv (dev float32 [B*T], what the gradient needs).  x and residual: F32, BF16 or F16, the same. */
+last_status_t last_residual_norm(const last_frames_t* frames, int32_t H, const last_matrix_t* x,
+                                 const last_matrix_t* residual, const float* gain, float eps,
+                                 const last_matrix_t* s, const last_matrix_t* y, const last_matrix_t* kept,
+                                 float* inv, void* hip_stream);
+
+/* The gradient: with u = gain * dy,  dx = inv * (u - s * inv^2 * mean(u * s)) + ds, which is that of x and of the residual
+ * alike; dgain[h] = sum over frames of dy * s * inv.  ds (or NULL): the gradient that reaches s by other ways.  dgain (dev
+ * float32 [H], written) may be NULL.  dy: F32, BF16 or F16; s: the same type, or BF16 or F16 beside dy in F32, or kept in 8
+ * bits (LAST_I8, LAST_E4M3); dx: F32, BF16 or F16, and ds of its type.  Workspace: LAST_OP_RESIDUAL_NORM_GRAD, N = 1. */
+last_status_t last_residual_norm_grad(const last_frames_t* frames, int32_t H, const last_matrix_t* dy,
+                                      const last_matrix_t* s, const float* gain, const float* inv,
+                                      const last_matrix_t* ds, const last_matrix_t* dx, float* dgain,
+                                      void* ws, size_t ws_bytes, void* hip_stream);
+
+/* h = x W^T + bias, y = act(h) + residual.  x: B*T rows of K, w: N rows of K, both BF16, both F16 or both E4M3 (with
+ * scales along K; products of codes and scales are exact, sums float32).  bias (dev float32 [N]) and residual (type of y;
+ * any of the three plain ones where y is in 8 bits) may be NULL.  y: F32, BF16, F16, or 8 bits (I8, E4M3).  kept (or
+ * NULL): h in 8 bits, what the gradient of the activation needs.  Workspace: LAST_OP_PRODUCT, a = x, b = w. */
+last_status_t last_product(const last_frames_t* frames, int32_t N, int32_t K, const last_matrix_t* x,
+                           const last_matrix_t* w, const float* bias, last_activation_t act,
+                           const last_matrix_t* residual, const last_matrix_t* y, const last_matrix_t* kept,
+                           void* ws, size_t ws_bytes, void* hip_stream);
+
+/* dx = (dy W) * act'(kept): the gradient of the product's input, and through the activation that made that input of
+ * `kept` (B*T rows of K in 8 bits; NULL with LAST_ACT_NONE).  dy: B*T rows of N and w: N rows of K, both BF16 or both F16;
+ * dx: F32, BF16 or F16.  Workspace: LAST_OP_PRODUCT_GRAD_INPUT, a = dy, b = w. */
+last_status_t last_product_grad_input(const last_frames_t* frames, int32_t N, int32_t K, const last_matrix_t* dy,
+                                      const last_matrix_t* w, const last_matrix_t* kept, last_activation_t act,
+                                      const last_matrix_t* dx, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* dw = dy^T act(x) (N rows of K: F32, BF16 or F16), dbias[n] = sum over frames of dy (dev float32 [N], or NULL).  dy: BF16
+ * or F16; x: the same type (act LAST_ACT_NONE), or kept in 8 bits, whose activation is formed again, rounded to dy's type.
+ * Workspace: LAST_OP_PRODUCT_GRAD_WEIGHT, a = dy, b = x. */
+last_status_t last_product_grad_weight(const last_frames_t* frames, int32_t N, int32_t K, const last_matrix_t* dy,
+                                       const last_matrix_t* x, last_activation_t act, const last_matrix_t* dw,
+                                       float* dbias, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Scratch bytes of a call above (LAST_OP_RESIDUAL_NORM_GRAD ... LAST_OP_PRODUCT_GRAD_WEIGHT) on operands of these types,
+ * pitches and alignments (a and b as named there; their data is not read).  At least 256; 0 on invalid arguments. */
+size_t last_layer_workspace_bytes(int32_t op, const last_frames_t* frames, int32_t N, int32_t K,
+                                  const last_matrix_t* a, const last_matrix_t* b);
+
+/* x (F32, BF16 or F16; B*T rows of H) in 8 bits. */
+last_status_t last_keep(const last_frames_t* frames, int32_t H, const last_matrix_t* x, const last_matrix_t* kept,
+                        void* hip_stream);
+
+/* y = act(kept), F32, BF16 or F16: what was kept, and what was made of it. */
+last_status_t last_kept_values(const last_frames_t* frames, int32_t H, const last_matrix_t* kept,
+                               last_activation_t act, const last_matrix_t* y, void* hip_stream);
+
+/* dx = dy * act'(kept): the gradient of an activation alone.  dy, dx: F32, BF16 or F16. */
+last_status_t last_kept_grad(const last_frames_t* frames, int32_t H, const last_matrix_t* dy,
+                             const last_matrix_t* kept, last_activation_t act, const last_matrix_t* dx,
+                             void* hip_stream);
 
 /* For callers that cannot allocate device memory (code under HIP graph capture,
  * tight serving loops, harnesses that forbid hipMalloc): last_shortest_distance

@@ -20,6 +20,7 @@ LAST_LOG, LAST_TROPICAL = 0, 1
 OP_SHORTEST_DISTANCE, OP_ARC_POSTERIORS, OP_INTERSECT_REFERENCE, OP_SHORTEST_PATH = 0, 1, 2, 3
 OP_LOCAL_LOG_LIKELIHOOD = 4
 OP_LOSS = 5
+OP_RESIDUAL_NORM_GRAD, OP_PRODUCT, OP_PRODUCT_GRAD_INPUT, OP_PRODUCT_GRAD_WEIGHT = 6, 7, 8, 9
 WEIGHTS_DENSE, WEIGHTS_SHARED_EMB = 0, 1
 
 EXPORTS = ["last_workspace_bytes", "last_shortest_distance", "last_arc_posteriors",
@@ -27,7 +28,9 @@ EXPORTS = ["last_workspace_bytes", "last_shortest_distance", "last_arc_posterior
            "last_version", "last_kernel_variant", "last_hip_error_string",
            "last_shortest_distance_static", "last_set_option", "last_get_option",
            "last_local_log_likelihood", "last_probe_bandwidth", "last_globally_normalized_loss",
-           "last_verify_placement", "last_least_workspace_bytes"]
+           "last_verify_placement", "last_least_workspace_bytes", "last_residual_norm", "last_residual_norm_grad",
+           "last_product", "last_product_grad_input", "last_product_grad_weight", "last_layer_workspace_bytes",
+           "last_keep", "last_kept_values", "last_kept_grad"]
 PROBE_READ, PROBE_COPY, PROBE_READ_ROWS, PROBE_READ_COLUMNS = 0, 1, 2, 3
 OPT_FORCE_SOLO, OPT_CLUSTER_GENERATION, OPT_CLUSTER_VITERBI, OPT_SPIN_LIMIT, OPT_FUSED_FRAMES_PER_TILE = 0, 1, 2, 3, 4
 OPT_FUSED_KEEP_MARGINALS = 5
@@ -49,6 +52,15 @@ class LastGrads(ctypes.Structure):
     _fields_ = [("dw", ctypes.c_void_p), ("df", ctypes.c_void_p), ("de", ctypes.c_void_p),
                 ("dW", ctypes.c_void_p), ("accumulate", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class LastFrames(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("lengths", ctypes.c_void_p)]
+
+
+class LastMatrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int32), ("pitch", ctypes.c_int64),
+                ("scales", ctypes.c_void_p), ("scale_pitch", ctypes.c_int64)]
 
 
 class LastError(RuntimeError):
@@ -106,6 +118,20 @@ def load_library():
     lib.last_set_option.argtypes = [i32, i32]
     lib.last_get_option.restype = i32
     lib.last_get_option.argtypes = [i32]
+    f32, fr, mx = ctypes.c_float, ctypes.POINTER(LastFrames), ctypes.POINTER(LastMatrix)
+    for name, arguments in (
+            ("last_residual_norm", [fr, i32, mx, mx, vp, f32, mx, mx, mx, vp, vp]),
+            ("last_residual_norm_grad", [fr, i32, mx, mx, vp, vp, mx, mx, vp, vp, sz, vp]),
+            ("last_product", [fr, i32, i32, mx, mx, vp, i32, mx, mx, mx, vp, sz, vp]),
+            ("last_product_grad_input", [fr, i32, i32, mx, mx, mx, i32, mx, vp, sz, vp]),
+            ("last_product_grad_weight", [fr, i32, i32, mx, mx, i32, mx, vp, vp, sz, vp]),
+            ("last_keep", [fr, i32, mx, mx, vp]),
+            ("last_kept_values", [fr, i32, mx, i32, mx, vp]),
+            ("last_kept_grad", [fr, i32, mx, mx, i32, mx, vp])):
+        getattr(lib, name).restype = i32
+        getattr(lib, name).argtypes = arguments
+    lib.last_layer_workspace_bytes.restype = sz
+    lib.last_layer_workspace_bytes.argtypes = [i32, fr, i32, i32, mx, mx]
     lib.last_kernel_variant.restype = i32
     lib.last_kernel_variant.argtypes = [ctypes.POINTER(LastWeights), ctypes.POINTER(LastContext), i32]
     _lib = lib
@@ -432,3 +458,230 @@ def last_shortest_path(w, lengths, order=1, item_status=None):
                                   _ptr(states), _ptr(score), _ptr(item_status), _ptr(ws),
                                   ws.numel(), _stream()))
     return labels, states, score
+
+
+# ---- the layer between an encoder's frames and the lattice
+
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "tanh": 4}
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3, torch.float8_e4m3fn: 4}
+_EIGHT = (torch.int8, torch.float8_e4m3fn)
+
+
+class Kept(tuple):
+    """Values in 8 bits: (codes, scales), codes int8 or float8_e4m3fn [..., H], scales uint8 [..., ceil(H / 32)]; a code q
+    in a block of 32 columns with scale byte k stands for q * 2^(k - 127), k = 255 for NaN (see include/last.h)."""
+
+    def __new__(cls, codes, scales):
+        return super().__new__(cls, (codes, scales))
+
+    codes = property(lambda self: self[0])
+    scales = property(lambda self: self[1])
+
+    @classmethod
+    def empty(cls, shape, dtype, device):
+        return cls(torch.empty(shape, dtype=dtype, device=device),
+                   torch.empty((*shape[:-1], (shape[-1] + 31) // 32), dtype=torch.uint8, device=device))
+
+
+class Norm(tuple):
+    """(y, s, inv, kept) of last_residual_norm; what was not asked for is None."""
+
+    def __new__(cls, y, s, inv, kept):
+        return super().__new__(cls, (y, s, inv, kept))
+
+    y = property(lambda self: self[0])
+    s = property(lambda self: self[1])
+    inv = property(lambda self: self[2])
+    kept = property(lambda self: self[3])
+
+
+def _pitch(t, name):
+    """Elements from a row of t [R, H] or [B, T, H] to the next: the columns are contiguous, the rows evenly spaced."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2:
+        pitch = strides[0] if shape[0] > 1 else max(strides[0], shape[1])
+    elif len(shape) == 3:
+        B, T, H = shape
+        pitch = strides[1] if T > 1 else strides[0] if B > 1 else H
+        if B > 1 and T > 1 and strides[0] != T * pitch:
+            pitch = -1
+    else:
+        raise ValueError("%s must be [rows, columns] or [B, T, columns]" % name)
+    if pitch < shape[-1] or (strides[-1] != 1 and shape[-1] != 1):
+        raise ValueError("%s must have contiguous columns and evenly spaced rows" % name)
+    return pitch
+
+
+def _matrix(t, name, rows=None, columns=None):
+    """LastMatrix of a device tensor or a Kept, whose shape is checked against `rows` (leading sizes) and `columns`."""
+    codes, scales = t if isinstance(t, Kept) else (t, None)
+    if not isinstance(codes, torch.Tensor) or not codes.is_cuda or codes.dtype not in _TYPES:
+        raise TypeError("%s must be a device tensor of a supported type" % name)
+    if (codes.dtype in _EIGHT) != (scales is not None):
+        raise TypeError("%s: values in 8 bits are a Kept of codes and scales" % name)
+    shape = codes.shape
+    if (rows is not None and shape[:-1] != rows) or (columns is not None and shape[-1] != columns):
+        raise ValueError("%s has shape %s: expected %s" % (name, tuple(shape), (*(rows or ("...",)), columns)))
+    if scales is None:
+        return LastMatrix(codes.data_ptr(), _TYPES[codes.dtype], _pitch(codes, name), None, 0)
+    if not isinstance(scales, torch.Tensor) or not scales.is_cuda or scales.dtype != torch.uint8 \
+            or scales.shape != (*shape[:-1], (shape[-1] + 31) // 32):
+        raise TypeError("the scales of %s must be device uint8 [..., ceil(columns / 32)]" % name)
+    return LastMatrix(codes.data_ptr(), _TYPES[codes.dtype], _pitch(codes, name), scales.data_ptr(), _pitch(scales, name))
+
+
+def _opt(t, name, rows, columns):
+    return None if t is None else _matrix(t, name, rows, columns)
+
+
+def _vector(t, n, name):
+    if t is None:
+        return None
+    _dev_tensor(t, torch.float32, name)
+    if t.numel() != n:
+        raise ValueError("%s must have %d elements" % (name, n))
+    return t.data_ptr()
+
+
+def _frames(t, lengths, name):
+    """(LastFrames, leading sizes) of a tensor or Kept [R, H] or [B, T, H]; with lengths it is the latter."""
+    t = t[0] if isinstance(t, Kept) else t
+    if not isinstance(t, torch.Tensor) or t.dim() not in (2, 3):
+        raise TypeError("%s must be a device tensor [rows, columns] or [B, T, columns]" % name)
+    if lengths is None:
+        rows = t.shape[0] if t.dim() == 2 else t.shape[0] * t.shape[1]
+        return LastFrames(1, rows, None), t.shape[:-1]
+    _dev_tensor(lengths, torch.int32, "lengths")
+    if t.dim() != 3 or lengths.shape != t.shape[:1]:
+        raise ValueError("with lengths [B], %s must be [B, T, columns]" % name)
+    return LastFrames(t.shape[0], t.shape[1], lengths.data_ptr()), t.shape[:-1]
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError("unknown activation %r: one of %s" % (name, ", ".join(ACTIVATIONS)))
+    return ACTIVATIONS[name]
+
+
+def _result(shape, dtype, device):
+    return Kept.empty(shape, dtype, device) if dtype in _EIGHT else torch.empty(shape, dtype=dtype, device=device)
+
+
+def _layer_scratch(op, frames, N, K, a, b, device):
+    nbytes = load_library().last_layer_workspace_bytes(op, frames, N, K, a, b)
+    if nbytes == 0:
+        raise LastError(6, "combination not supported")
+    return workspace(nbytes, device)
+
+
+def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=None, keep=None):
+    """Root-mean-square norm of s = x + residual: a Norm (y, s, inv, kept), y = s * inv * gain of `dtype` (default: that of
+    x), s (None without a residual, where it is x), inv [rows] float32 for the gradient, and, with `keep` torch.int8 or
+    torch.float8_e4m3fn, y in 8 bits as a Kept.  With `keep` and no `dtype`, y itself is None.  x: [rows, H], or [B, T, H] with
+    lengths [B] of which the frames past the end are zeros in every result."""
+    lib = load_library()
+    fr, rows = _frames(x, lengths, "x")
+    H = x.shape[-1]
+    mx, mr = _matrix(x, "x"), _opt(residual, "residual", rows, H)
+    s = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = None if keep is not None and dtype is None else torch.empty(x.shape, dtype=dtype or x.dtype, device=x.device)
+    kept = None if keep is None else _result(x.shape, keep, x.device)
+    inv = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _check(lib.last_residual_norm(fr, H, mx, mr, _vector(gain, H, "gain"), eps, _opt(s, "s", rows, H), _opt(y, "y", rows, H),
+                                  _opt(kept, "keep", rows, H), inv.data_ptr(), _stream()))
+    return Norm(y, s, inv, kept)
+
+
+def last_residual_norm_grad(dy, s, gain, inv, ds=None, lengths=None, dtype=None):
+    """(dx, dgain): the gradient of x and of the residual alike, of `dtype` (default: that of ds, or of s, or, s being a
+    Kept, of dy), and dgain [H] float32.  s and inv as last_residual_norm returned them, s maybe in 8 bits (a Kept); ds:
+    the gradient that reaches s by other ways."""
+    lib = load_library()
+    fr, rows = _frames(dy, lengths, "dy")
+    H, device = dy.shape[-1], dy.device
+    if dtype is None:
+        dtype = ds.dtype if ds is not None else dy.dtype if isinstance(s, Kept) else s.dtype
+    dx = torch.empty(dy.shape, dtype=dtype, device=device)
+    dgain = torch.empty(H, dtype=torch.float32, device=device)
+    m = [_matrix(dy, "dy"), _matrix(s, "s", rows, H), _opt(ds, "ds", rows, H), _matrix(dx, "dx")]
+    ws = _layer_scratch(OP_RESIDUAL_NORM_GRAD, fr, 1, H, None, None, device)
+    _check(lib.last_residual_norm_grad(fr, H, m[0], m[1], _vector(gain, H, "gain"), _vector(inv, fr.B * fr.T, "inv"), m[2], m[3],
+                                       dgain.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
+    return dx, dgain
+
+
+def last_product(x, w, bias=None, activation="none", residual=None, lengths=None, dtype=None, keep=None):
+    """(y, kept): y = act(x w^T + bias) + residual, w [N, K], x [rows, K] or [B, T, K]: both bfloat16, float16, or both a Kept
+    of float8_e4m3fn.  `dtype` of y: default that of x (bfloat16 for a Kept); torch.int8 or torch.float8_e4m3fn make it a Kept.
+    `keep`: such a type to keep what the activation is applied to in (kept, a Kept), or None."""
+    lib = load_library()
+    fr, rows = _frames(x, lengths, "x")
+    N, K = (w[0] if isinstance(w, Kept) else w).shape
+    mx, mw = _matrix(x, "x", rows, K), _matrix(w, "w", (N,), K)
+    device = x[0].device
+    if dtype is None:
+        dtype = torch.bfloat16 if isinstance(x, Kept) else x.dtype
+    y = _result((*rows, N), dtype, device)
+    kept = None if keep is None else _result((*rows, N), keep, device)
+    ws = _layer_scratch(OP_PRODUCT, fr, N, K, mx, mw, device)
+    _check(lib.last_product(fr, N, K, mx, mw, _vector(bias, N, "bias"), _activation(activation),
+                            _opt(residual, "residual", rows, N), _matrix(y, "y"), _opt(kept, "keep", rows, N),
+                            ws.data_ptr(), ws.numel(), _stream()))
+    return y, kept
+
+
+def last_product_grad_input(dy, w, kept=None, activation="none", lengths=None, dtype=None):
+    """dx = (dy w) * act'(kept), of `dtype` (default: that of dy): the gradient of a product's input and, with `kept` [.., K],
+    through the activation that made this input of what was kept."""
+    lib = load_library()
+    fr, rows = _frames(dy, lengths, "dy")
+    N, K = w.shape
+    mdy, mw, mk = _matrix(dy, "dy", rows, N), _matrix(w, "w", (N,), K), _opt(kept, "kept", rows, K)
+    dx = torch.empty((*rows, K), dtype=dtype or dy.dtype, device=dy.device)
+    ws = _layer_scratch(OP_PRODUCT_GRAD_INPUT, fr, N, K, mdy, mw, dy.device)
+    _check(lib.last_product_grad_input(fr, N, K, mdy, mw, mk, _activation(activation), _matrix(dx, "dx"), ws.data_ptr(),
+                                       ws.numel(), _stream()))
+    return dx
+
+
+def last_product_grad_weight(dy, x, activation="none", lengths=None, dtype=torch.float32):
+    """(dw [N, K] of `dtype`, dbias [N] float32): dy^T act(x) and the column sums of dy.  x: of dy's type (activation "none"),
+    or a Kept, whose activation is formed again."""
+    lib = load_library()
+    fr, rows = _frames(dy, lengths, "dy")
+    N, K, device = dy.shape[-1], (x[0] if isinstance(x, Kept) else x).shape[-1], dy.device
+    mdy, mx = _matrix(dy, "dy"), _matrix(x, "x", rows, K)
+    dw = torch.empty((N, K), dtype=dtype, device=device)
+    dbias = torch.empty(N, dtype=torch.float32, device=device)
+    ws = _layer_scratch(OP_PRODUCT_GRAD_WEIGHT, fr, N, K, mdy, mx, device)
+    _check(lib.last_product_grad_weight(fr, N, K, mdy, mx, _activation(activation), _matrix(dw, "dw"), dbias.data_ptr(),
+                                        ws.data_ptr(), ws.numel(), _stream()))
+    return dw, dbias
+
+
+def last_keep(x, dtype=torch.int8, lengths=None):
+    """x in 8 bits: a Kept of torch.int8 or torch.float8_e4m3fn codes."""
+    fr, rows = _frames(x, lengths, "x")
+    mx = _matrix(x, "x")
+    kept = _result(x.shape, dtype, x.device)
+    _check(load_library().last_keep(fr, x.shape[-1], mx, _matrix(kept, "kept"), _stream()))
+    return kept
+
+
+def last_kept_values(kept, activation="none", lengths=None, dtype=torch.bfloat16):
+    """act(kept): what the codes stand for, or the activation formed again from them."""
+    fr, rows = _frames(kept, lengths, "kept")
+    mk = _matrix(kept, "kept")
+    y = torch.empty(kept[0].shape, dtype=dtype, device=kept[0].device)
+    _check(load_library().last_kept_values(fr, y.shape[-1], mk, _activation(activation), _matrix(y, "y"), _stream()))
+    return y
+
+
+def last_kept_grad(dy, kept, activation, lengths=None, dtype=None):
+    """dy * act'(kept), of `dtype` (default: that of dy): the gradient of an activation alone."""
+    fr, rows = _frames(dy, lengths, "dy")
+    H = dy.shape[-1]
+    mdy, mk = _matrix(dy, "dy"), _matrix(kept, "kept", rows, H)
+    dx = torch.empty(dy.shape, dtype=dtype or dy.dtype, device=dy.device)
+    _check(load_library().last_kept_grad(fr, H, mdy, mk, _activation(activation), _matrix(dx, "dx"), _stream()))
+    return dx

@@ -362,6 +362,13 @@ void launch_cluster(const Shape& s, const ClusterPlan& p, const ClusterWs& c, co
 
 hipError_t g_last_hip_error = hipSuccess;     // diagnostics only: what the last failing HIP call said
 
+}  // namespace
+
+namespace last {
+void note_hip_error(hipError_t e) { g_last_hip_error = e; }    // (of the calls in layer_api.hip)
+}
+
+namespace {
 last_status_t hip_status()
 {
     const hipError_t e = hipGetLastError();

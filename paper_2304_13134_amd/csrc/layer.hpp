@@ -1,0 +1,306 @@
+// Helpers of the layer between an encoder's frames and the lattice: element types, activations, values in 8 bits in
+// blocks of 32 columns, and which frames exist.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/last.h"
+#include "common.hpp"
+
+namespace last {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+
+struct bf16_t { uint16_t bits; };
+struct f16_t { _Float16 v; };
+struct i8_t { int8_t v; };
+struct e4m3_t { uint8_t bits; };
+
+constexpr int kBlock = 32;           // columns that share a scale
+
+// rows b T + t of frames; those with t >= len[b] do not exist (lengths below 0 count as 0)
+struct Frames {
+    const int* len;                  // null: all exist
+    int T;
+};
+
+__device__ __forceinline__ bool frame_exists(const Frames& f, int row)
+{
+    if (!f.len) return true;
+    const int b = (int)((unsigned)row / (unsigned)f.T);
+    return row - b * f.T < f.len[b];
+}
+
+__device__ __forceinline__ float bf16_to_float(unsigned bits) { return __uint_as_float(bits << 16); }
+
+// two float32 to bfloat16, to nearest even, NaN stays NaN
+__device__ __forceinline__ unsigned bf16_pair(float lo, float hi)
+{
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    const bf2 r = {(__bf16)lo, (__bf16)hi};
+    return __builtin_bit_cast(unsigned, r);
+}
+
+__device__ __forceinline__ unsigned f16_pair(float lo, float hi)
+{
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    const h2 r = {(_Float16)lo, (_Float16)hi};
+    return __builtin_bit_cast(unsigned, r);
+}
+
+// ---- scales of 8-bit values: byte = exponent + 127, 255 = the block holds a value that is not finite
+
+__device__ __forceinline__ float scale_value(unsigned byte)
+{
+    const unsigned bits = byte == 255u ? 0x7fc00000u : byte == 0u ? 0x00400000u : byte << 23;
+    return __uint_as_float(bits);
+}
+
+// the smallest exponent (from -127) at which the largest magnitude, given as its bits, does not pass the largest code:
+// 127 = 1.984375 2^6, 448 = 1.75 2^8
+template <bool E4M3>
+__device__ __forceinline__ unsigned scale_byte(unsigned top)
+{
+    if (top >= 0x7f800000u) return 255u;
+    const int b = (int)(top >> 23) - (E4M3 ? 8 : 6) + ((top & 0x7fffffu) > (E4M3 ? 0x600000u : 0x7e0000u) ? 1 : 0);
+    return b < 0 ? 0u : (unsigned)b;
+}
+
+// four values times 1 / scale to four codes, to nearest even
+template <bool E4M3>
+__device__ __forceinline__ unsigned encode4(const float* v, unsigned byte)
+{
+    if (byte == 255u) return 0u;
+    const float m = __uint_as_float((254u - byte) << 23);
+    if constexpr (E4M3) {
+        int r = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * m, v[1] * m, 0, false);
+        return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * m, v[3] * m, r, true);
+    } else {
+        unsigned r = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r |= ((unsigned)(int)rintf(v[i] * m) & 255u) << (8 * i);
+        return r;
+    }
+}
+
+template <bool E4M3>
+__device__ __forceinline__ void decode4(unsigned q, float scale, float* v)
+{
+    if constexpr (E4M3) {
+        v[0] = __builtin_amdgcn_cvt_f32_fp8((int)q, 0) * scale;
+        v[1] = __builtin_amdgcn_cvt_f32_fp8((int)q, 1) * scale;
+        v[2] = __builtin_amdgcn_cvt_f32_fp8((int)q, 2) * scale;
+        v[3] = __builtin_amdgcn_cvt_f32_fp8((int)q, 3) * scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(q >> (8 * i)) * scale;
+    }
+}
+
+__device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+__device__ __forceinline__ unsigned umax(unsigned a, unsigned b) { return a > b ? a : b; }
+
+// ---- eight consecutive elements of a row; n of them exist (the others read as 0 and are not written).  `aligned`: every
+// group of eight begins at a multiple of its own size (16 bytes at most)
+
+template <typename E> struct Elt;
+template <> struct Elt<float> {
+    static constexpr int type = LAST_F32, size = 4;
+    static __device__ float get(const void* p, size_t i) { return ((const float*)p)[i]; }
+    static __device__ void put(void* p, size_t i, float v) { ((float*)p)[i] = v; }
+    static __device__ void get8(const void* p, size_t i, float* v)
+    {
+        const f4 a = *(const f4*)((const float*)p + i), b = *(const f4*)((const float*)p + i + 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { v[k] = a[k]; v[4 + k] = b[k]; }
+    }
+    static __device__ void put8(void* p, size_t i, const float* v)
+    {
+        *(f4*)((float*)p + i) = f4{v[0], v[1], v[2], v[3]};
+        *(f4*)((float*)p + i + 4) = f4{v[4], v[5], v[6], v[7]};
+    }
+};
+template <> struct Elt<bf16_t> {
+    static constexpr int type = LAST_BF16, size = 2;
+    static __device__ float get(const void* p, size_t i) { return bf16_to_float(((const uint16_t*)p)[i]); }
+    static __device__ void put(void* p, size_t i, float v) { ((uint16_t*)p)[i] = (uint16_t)bf16_pair(v, 0.f); }
+    static __device__ void get8(const void* p, size_t i, float* v)
+    {
+        const u4 a = *(const u4*)((const uint16_t*)p + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { v[2 * k] = bf16_to_float(a[k] & 0xffffu); v[2 * k + 1] = __uint_as_float(a[k] & 0xffff0000u); }
+    }
+    static __device__ void put8(void* p, size_t i, const float* v)
+    {
+        *(u4*)((uint16_t*)p + i) = u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+    }
+};
+template <> struct Elt<f16_t> {
+    static constexpr int type = LAST_F16, size = 2;
+    static __device__ float get(const void* p, size_t i) { return (float)((const _Float16*)p)[i]; }
+    static __device__ void put(void* p, size_t i, float v) { ((_Float16*)p)[i] = (_Float16)v; }
+    static __device__ void get8(const void* p, size_t i, float* v)
+    {
+        typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+        const h8 a = *(const h8*)((const _Float16*)p + i);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = (float)a[k];
+    }
+    static __device__ void put8(void* p, size_t i, const float* v)
+    {
+        *(u4*)((_Float16*)p + i) = u4{f16_pair(v[0], v[1]), f16_pair(v[2], v[3]), f16_pair(v[4], v[5]), f16_pair(v[6], v[7])};
+    }
+};
+// codes of 8-bit values; the caller brings the scale of their block
+template <bool E4M3> struct EltCodes {
+    static constexpr int type = E4M3 ? LAST_E4M3 : LAST_I8, size = 1;
+    static __device__ void get8(const void* p, size_t i, float* v)
+    {
+        const u2 a = *(const u2*)((const uint8_t*)p + i);
+        decode4<E4M3>(a[0], 1.f, v);
+        decode4<E4M3>(a[1], 1.f, v + 4);
+    }
+    static __device__ float get(const void* p, size_t i)
+    {
+        float v[4];
+        decode4<E4M3>(((const uint8_t*)p)[i], 1.f, v);
+        return v[0];
+    }
+};
+template <> struct Elt<i8_t> : EltCodes<false> {};
+template <> struct Elt<e4m3_t> : EltCodes<true> {};
+
+template <typename E>
+__device__ __forceinline__ void load8(const void* p, size_t i, int n, bool aligned, float* v)
+{
+    if (aligned && n >= 8) {
+        Elt<E>::get8(p, i, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k < n ? Elt<E>::get(p, i + k) : 0.f;
+    }
+}
+
+template <typename E>
+__device__ __forceinline__ void store8(void* p, size_t i, int n, bool aligned, const float* v)
+{
+    if (aligned && n >= 8) {
+        Elt<E>::put8(p, i, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < n) Elt<E>::put(p, i + k, v[k]);
+    }
+}
+
+// the same with the type given at run time, the same for all lanes
+__device__ __forceinline__ void store8_as(int type, void* p, size_t i, int n, bool aligned, const float* v)
+{
+    if (type == LAST_BF16) store8<bf16_t>(p, i, n, aligned, v);
+    else if (type == LAST_F16) store8<f16_t>(p, i, n, aligned, v);
+    else store8<float>(p, i, n, aligned, v);
+}
+
+// eight codes of a row, n of which exist
+__device__ __forceinline__ void store_codes(uint8_t* p, size_t i, int n, bool aligned, unsigned lo, unsigned hi)
+{
+    if (aligned && n >= 8) {
+        *(u2*)(p + i) = u2{lo, hi};
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < n) p[i + k] = (uint8_t)((k < 4 ? lo : hi) >> (8 * (k & 3)));
+    }
+}
+
+__device__ __forceinline__ void load_codes(const uint8_t* p, size_t i, int n, bool aligned, unsigned* lo, unsigned* hi)
+{
+    if (aligned && n >= 8) {
+        const u2 a = *(const u2*)(p + i);
+        *lo = a[0];
+        *hi = a[1];
+    } else {
+        unsigned r[2] = {0u, 0u};
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < n) r[k >> 2] |= (unsigned)p[i + k] << (8 * (k & 3));
+        *lo = r[0];
+        *hi = r[1];
+    }
+}
+
+// ---- a matrix of 8-bit values with its scales
+struct Eight {
+    uint8_t* q;                      // null: there is none
+    uint8_t* scales;
+    long long pitch, scale_pitch;
+    int e4m3;
+    int aligned;                     // groups of eight codes begin at multiples of 8 bytes
+};
+
+// Eight columns c.. of a row, in each of four lanes that hold a block of 32 columns between them; `top`: the largest
+// magnitude of the block.  One of them (first) writes the scale.
+__device__ __forceinline__ void store_eight(const Eight& k, size_t row, int c, int n, bool first, unsigned top, const float* v)
+{
+    const unsigned byte = k.e4m3 ? scale_byte<true>(top) : scale_byte<false>(top);
+    const unsigned lo = k.e4m3 ? encode4<true>(v, byte) : encode4<false>(v, byte);
+    const unsigned hi = k.e4m3 ? encode4<true>(v + 4, byte) : encode4<false>(v + 4, byte);
+    if (n > 0) {
+        store_codes(k.q + row * k.pitch, c, n, k.aligned, lo, hi);
+        if (first) k.scales[row * k.scale_pitch + c / kBlock] = (uint8_t)byte;
+    }
+}
+
+__device__ __forceinline__ unsigned top8(const float* v)
+{
+    unsigned t = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t = umax(t, magnitude_bits(v[k]));
+    return t;
+}
+
+// largest of four neighbouring lanes, which hold a block between them
+__device__ __forceinline__ unsigned quad_max(unsigned t)
+{
+    t = umax(t, (unsigned)__shfl_xor((int)t, 1, kWave));
+    return umax(t, (unsigned)__shfl_xor((int)t, 2, kWave));
+}
+
+// ---- activations and their derivatives, in 32 bits (exp to about 1e-7 of its result for |v| of a few, which a result of
+// 16 bits does not show; tanh and erf are the library's, exact to an ulp or two)
+
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+
+__device__ __forceinline__ float activate(int act, float v)
+{
+    switch (act) {
+    case LAST_ACT_RELU: return v < 0.f ? 0.f : v;
+    case LAST_ACT_SILU: return v * sigmoid(v);
+    case LAST_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+    case LAST_ACT_TANH: return tanhf(v);
+    default: return v;
+    }
+}
+
+__device__ __forceinline__ float slope(int act, float v)
+{
+    switch (act) {
+    case LAST_ACT_RELU: return v > 0.f ? 1.f : v <= 0.f ? 0.f : v;
+    case LAST_ACT_SILU: {
+        const float p = sigmoid(v);
+        return p * (1.f + v * (1.f - p));
+    }
+    case LAST_ACT_GELU:
+        return 0.5f * (1.f + erff(v * 0.70710678118654752f)) + v * 0.39894228040143268f * __expf(-0.5f * v * v);
+    case LAST_ACT_TANH: {
+        const float t = tanhf(v);
+        return 1.f - t * t;
+    }
+    default: return 1.f;
+    }
+}
+
+}  // namespace last

@@ -1,0 +1,244 @@
+// Root-mean-square norm of the sum of a row and a residual, and its gradient.
+//     s = x + residual,  inv = 1 / sqrt(mean_h s^2 + eps),  y = s inv gain
+//     u = gain dy,  dx = inv (u - s inv^2 mean_h(u s)) + ds,  dgain[h] = sum over rows of dy s inv
+// Both read and write every value once and are bound by memory: a row stays in registers between the sum and its use
+// (8 columns a lane in each of CH places), in one wavefront up to 2048 columns, so that no barrier separates them, and in
+// 4 or 16 wavefronts beyond.  Sums are in 32 bits.
+#pragma once
+#include "layer.hpp"
+
+namespace last {
+
+struct NormArgs {
+    Frames frames;
+    int rows, H;
+    const void *x, *res;             // res: null, or of the type of x
+    const float* gain;
+    void *s, *y;                     // each may be null; s of the type of x
+    float* inv;
+    long long px, pr, ps, py;
+    int ytype;
+    bool ax, ar, as_, ay, ag;        // groups of eight begin at multiples of 16 bytes (or their size)
+    float eps;
+    Eight kept;
+};
+
+// sum over the WPR wavefronts of a row; `red`: 2 x WPR floats of LDS, `turn` alternates between their halves so that one
+// barrier a sum is enough
+template <int WPR>
+__device__ __forceinline__ float row_sum(float v, float* red, int turn)
+{
+    v = wave_sum(v);
+    if constexpr (WPR > 1) {
+        red += (turn & 1) * WPR;
+        if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < WPR; ++i) v += red[i];
+    }
+    return v;
+}
+
+template <typename X, int WPR, int CH>
+__global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_kernel(NormArgs a)
+{
+    constexpr int kRows = WPR == 1 ? 4 : 1;                  // rows of a workgroup
+    __shared__ float red[2 * WPR];
+    const int row = (int)blockIdx.x * kRows + (WPR == 1 ? (int)threadIdx.x / kWave : 0);
+    const int lane = WPR == 1 ? (int)threadIdx.x % kWave : (int)threadIdx.x;
+    if (WPR == 1 && row >= a.rows) return;
+    const bool there = frame_exists(a.frames, row);
+    float v[CH][8];
+    float sum = 0.f;
+    if (there) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int h = (c * WPR * kWave + lane) * 8;
+            load8<X>(a.x, (size_t)row * a.px + h, a.H - h, a.ax, v[c]);
+        }
+        if (a.res) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int h = (c * WPR * kWave + lane) * 8;
+                float r[8];
+                load8<X>(a.res, (size_t)row * a.pr + h, a.H - h, a.ar, r);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[c][k] += r[k];
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += v[c][k] * v[c][k];
+    } else {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[c][k] = 0.f;
+    }
+    sum = row_sum<WPR>(sum, red, 0);
+    const float inv = there ? 1.f / sqrtf(sum / (float)a.H + a.eps) : 0.f;
+    if (lane == 0 && a.inv) a.inv[row] = inv;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int h = (c * WPR * kWave + lane) * 8;
+        if (a.s) store8<X>(a.s, (size_t)row * a.ps + h, a.H - h, a.as_, v[c]);
+        float g[8];
+        load8<float>(a.gain, h, a.H - h, a.ag, g);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[c][k] = there ? v[c][k] * inv * g[k] : 0.f;
+        if (a.y) store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, a.ay, v[c]);
+        if (a.kept.q) store_eight(a.kept, row, h, a.H - h, (lane & 3) == 0, quad_max(top8(v[c])), v[c]);
+    }
+}
+
+struct NormGradArgs {
+    Frames frames;
+    int rows, H;
+    const void *dy, *s, *ds;         // ds: null, or of the type of dx
+    const uint8_t* s_scales;         // s in 8 bits only
+    const float *gain, *inv;
+    void* dx;
+    float* part;                     // [workgroups][H] partial sums of dgain, or null
+    long long pdy, ps, pds, pdx, pss;
+    int dxtype;
+    bool ady, as_, ads, adx, ag;
+};
+
+template <typename S>
+__device__ __forceinline__ void load_s(const NormGradArgs& a, int row, int h, float* v)
+{
+    load8<S>(a.s, (size_t)row * a.ps + h, a.H - h, a.as_, v);
+    if constexpr (Elt<S>::size == 1) {
+        const float sc = h < a.H ? scale_value(a.s_scales[(size_t)row * a.pss + h / kBlock]) : 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k < a.H - h ? v[k] * sc : 0.f;
+    }
+}
+
+__device__ __forceinline__ void load_dx_type(int type, const void* p, size_t i, int n, bool aligned, float* v)
+{
+    if (type == LAST_BF16) load8<bf16_t>(p, i, n, aligned, v);
+    else if (type == LAST_F16) load8<f16_t>(p, i, n, aligned, v);
+    else load8<float>(p, i, n, aligned, v);
+}
+
+// Every wavefront (WPR = 1) or workgroup goes over its rows and keeps the sums of its columns of dgain in registers;
+// they meet in LDS and go out as one row of partial sums a workgroup, added in order by column_sum_kernel.
+template <typename DY, typename S, int WPR, int CH>
+__global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel(NormGradArgs a)
+{
+    constexpr int kRows = WPR == 1 ? 4 : 1;
+    __shared__ float red[2 * WPR];
+    __shared__ float cols[WPR == 1 ? 4 * kWave * 8 : 1];
+    const int lane = WPR == 1 ? (int)threadIdx.x % kWave : (int)threadIdx.x;
+    const int wave = WPR == 1 ? (int)threadIdx.x / kWave : 0;
+    float dg[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dg[c][k] = 0.f;
+    int turn = 0;
+    for (int row = (int)blockIdx.x * kRows + wave; row < a.rows; row += (int)gridDim.x * kRows, ++turn) {
+        float u[CH][8], s[CH][8], d[CH][8];
+        if (!frame_exists(a.frames, row)) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[0][k] = 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int h = (c * WPR * kWave + lane) * 8;
+                store8_as(a.dxtype, a.dx, (size_t)row * a.pdx + h, a.H - h, a.adx, u[0]);
+            }
+            if (WPR > 1) __syncthreads();                    // (row_sum's, where `turn` counts)
+            continue;
+        }
+        const float inv = a.inv[row];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int h = (c * WPR * kWave + lane) * 8;
+            load8<DY>(a.dy, (size_t)row * a.pdy + h, a.H - h, a.ady, u[c]);
+            load_s<S>(a, row, h, s[c]);
+        }
+        if (a.ds) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int h = (c * WPR * kWave + lane) * 8;
+                load_dx_type(a.dxtype, a.ds, (size_t)row * a.pds + h, a.H - h, a.ads, d[c]);
+            }
+        }
+        float dot = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int h = (c * WPR * kWave + lane) * 8;
+            float g[8];
+            load8<float>(a.gain, h, a.H - h, a.ag, g);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                dg[c][k] += u[c][k] * s[c][k] * inv;
+                u[c][k] *= g[k];
+                dot += u[c][k] * s[c][k];
+            }
+        }
+        dot = row_sum<WPR>(dot, red, turn);
+        const float m = inv * inv * (dot / (float)a.H);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int h = (c * WPR * kWave + lane) * 8;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[c][k] = inv * (u[c][k] - s[c][k] * m);
+            if (a.ds) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) u[c][k] += d[c][k];
+            }
+            store8_as(a.dxtype, a.dx, (size_t)row * a.pdx + h, a.H - h, a.adx, u[c]);
+        }
+    }
+    if (!a.part) return;
+    float* out = a.part + (size_t)blockIdx.x * a.H;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int h = (c * WPR * kWave + lane) * 8;
+        if constexpr (WPR == 1) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) cols[(wave * 8 + k) * kWave + lane] = dg[c][k];
+            __syncthreads();
+            // wavefront w sums columns 2w, 2w + 1 of every lane's eight
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int k = 2 * wave + j;
+                float t = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) t += cols[(w * 8 + k) * kWave + lane];
+                if (h + k < a.H) out[h + k] = t;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (h + k < a.H) out[h + k] = dg[c][k];
+        }
+    }
+}
+
+// out[h] = sum over n rows of part[n][H], in a fixed order: 32 columns a workgroup, 32 groups of rows
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int n, int H, float* out)
+{
+    __shared__ float red[32][33];
+    const int c = threadIdx.x & 31, g = threadIdx.x >> 5, h = (int)blockIdx.x * 32 + c;
+    float t = 0.f;
+    if (h < H) {
+#pragma unroll 4
+        for (int i = g; i < n; i += 32) t += part[(size_t)i * H + h];
+    }
+    red[g][c] = t;
+    __syncthreads();
+    if (g == 0 && h < H) {
+        t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t += red[i][c];
+        out[h] = t;
+    }
+}
+
+}  // namespace last
