@@ -62,8 +62,7 @@ __global__ __launch_bounds__(256) void kept_values_kernel(KeepArgs a)
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (frame_exists(a.frames, row)) {
         load_eight(a.kept, row, h, a.H - h, v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = activate(a.act, v[k]);
+        activate8(a.act, v);
     }
     store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, a.ay, v);
 }
@@ -78,10 +77,12 @@ __global__ __launch_bounds__(256) void kept_grad_kernel(KeepArgs a)
     if (frame_exists(a.frames, row)) {
         load8<X>(a.x, (size_t)row * a.px + h, a.H - h, a.ax, d);
         load_eight(a.kept, row, h, a.H - h, v);
+        times_slope(a.act, v, d);
+    } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = d[k] * slope(a.act, v[k]);
+        for (int k = 0; k < 8; ++k) d[k] = 0.f;
     }
-    store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, a.ay, v);
+    store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, a.ay, d);
 }
 
 }  // namespace last

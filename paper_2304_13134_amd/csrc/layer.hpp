@@ -303,4 +303,40 @@ __device__ __forceinline__ float slope(int act, float v)
     }
 }
 
+// eight at a time, the choice of the activation outside
+__device__ __forceinline__ void activate8(int act, float* v)
+{
+    if (act == LAST_ACT_NONE) return;
+    if (act == LAST_ACT_RELU) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = activate(LAST_ACT_RELU, v[k]);
+    } else if (act == LAST_ACT_SILU) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = activate(LAST_ACT_SILU, v[k]);
+    } else if (act == LAST_ACT_GELU) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = activate(LAST_ACT_GELU, v[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = activate(LAST_ACT_TANH, v[k]);
+    }
+}
+
+__device__ __forceinline__ void times_slope(int act, const float* h, float* v)
+{
+    if (act == LAST_ACT_RELU) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= slope(LAST_ACT_RELU, h[k]);
+    } else if (act == LAST_ACT_SILU) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= slope(LAST_ACT_SILU, h[k]);
+    } else if (act == LAST_ACT_GELU) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= slope(LAST_ACT_GELU, h[k]);
+    } else if (act == LAST_ACT_TANH) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= slope(LAST_ACT_TANH, h[k]);
+    }
+}
+
 }  // namespace last

@@ -317,6 +317,7 @@ last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, in
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
     a.e.bias = bias;
+    a.e.wide_bias = (uintptr_t)bias % 16 == 0;
     a.e.act = act;
     set_result(a.e, y, res);
     a.e.kept = eight_of(kept);

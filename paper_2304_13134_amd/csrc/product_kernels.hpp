@@ -12,8 +12,7 @@
 //
 // LDS.  A load writes 64 lanes' 16 bytes in a row, so the swizzle that spreads rows over the banks is one of the addresses
 // that are read: along, 16-byte piece c of row r stands at c ^ along_swizzle(r) of its 128 bytes, which gives the 16 rows
-// of an operand 16 different places both where they follow each other and where they are 0-3, 8-11, 16-19, 24-27 (below);
-// across, 32-byte granules of row r stand at g ^ across_swizzle(r), and the transposing read
+// of an operand 16 different places; across, 32-byte granules of row r stand at g ^ across_swizzle(r), and the transposing read
 // (ds_read_b64_tr_b16: 16 lanes read four rows of 16 values and get four values of a column each) brings the reduction
 // index into a lane.  Out-of-range pieces have an offset that the buffer's bounds check turns into zeros, in memory order
 // that is: rows past the end, frames that do not exist, the rest of the reduction.
@@ -28,6 +27,8 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 typedef int i8x __attribute__((ext_vector_type(8)));
 typedef int i4x __attribute__((ext_vector_type(4)));
 
+typedef __attribute__((address_space(3))) void* lds_t;
+
 enum { kAlong = 0, kAcross = 1 };
 constexpr unsigned kNowhere = 0x80000000u;       // beyond every buffer
 constexpr int kStep = 128;                       // bytes of the reduction index at a time (kAlong), 64 rows (kAcross)
@@ -41,7 +42,7 @@ struct Epilogue {
     void* y;                                     // null: 8-bit values `out` instead
     long long py;
     int type;
-    bool wide, wide_res;                         // eight elements at a time are aligned
+    bool wide, wide_res, wide_bias;              // eight elements at a time are aligned
     Eight out;                                   // result in 8 bits
     Eight kept;                                  // forward: written with the sums + bias; of the input: read
     int kept_act;                                // of the input: times act' of what is kept (LAST_ACT_NONE: nothing is)
@@ -65,14 +66,34 @@ struct ProductArgs {
     Epilogue e;
 };
 
-__device__ __forceinline__ int along_swizzle(int r) { return ((r >> 1) & 1) | (((r >> 2) ^ (r >> 4)) & 1) << 1 | ((r >> 3) & 1) << 2; }
+__device__ __forceinline__ int along_swizzle(int r) { return (r >> 1) & 7; }
 __device__ __forceinline__ int across_swizzle(int r) { return (r & 3) | ((r >> 3) & 1) << 2; }
 
-typedef __attribute__((address_space(3))) void* lds_t;
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base)
 {
     return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00020000);
+}
+
+// 64 lanes' 16 (4) bytes at offset `o` of the buffer at `base` to LDS from `to` on.  In assembly, since the compiler makes every
+// later read of LDS wait for its own form of this; whoever reads waits with arrived().
+template <int BYTES>
+__device__ __forceinline__ void to_lds(const void* base, unsigned o, const void* to)
+{
+    const uint64_t p = (uint64_t)base;
+    const u4 b = {(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)p), (unsigned)__builtin_amdgcn_readfirstlane((int)(p >> 32)) & 0xffffu,
+                  0x7fffffffu, 0x00020000u};
+    const unsigned m = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(uintptr_t)(lds_t)to);
+    if constexpr (BYTES == 16)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m), "v"(o), "s"(b) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(m), "v"(o), "s"(b) : "memory");
+}
+
+// what this wavefront sent to LDS and asked from it has come, then the same of the whole workgroup
+__device__ __forceinline__ void arrived()
+{
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // ---- one operand's tile: ROWS rows or columns of the output
@@ -106,7 +127,6 @@ struct Tile {
     // the tile's 128 bytes or 64 rows from `base` on; left: how many of them the reduction still has
     __device__ __forceinline__ void load(const char* base, long long left, unsigned long long mask, char* lds)
     {
-        const __amdgpu_buffer_rsrc_t b = buffer_of(base);
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
@@ -120,7 +140,7 @@ struct Tile {
                 const int r = (j * THREADS + (int)threadIdx.x) / kPieces;
                 if (!(mask >> r & 1)) o = kNowhere;
             }
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_t)(lds + (j * THREADS + wave * kWave) * 16), 16, (int)o, 0, 0, 0);
+            to_lds<16>(base, o, lds + (j * THREADS + wave * kWave) * 16);
         }
     }
 };
@@ -163,109 +183,49 @@ __device__ __forceinline__ u4 across_read(const char* lds, int a0, int a1)
     return u4{lo[0], lo[1], hi[0], hi[1]};
 }
 
-// ---- epilogue of U (8 or 4) neighbouring columns n.. of row m.  All 64 lanes call; columns past Q and rows past P, or
-// that do not exist, are not written or are zeros.
-template <int U>
+// ---- epilogue of eight neighbouring columns n.. of row m; four neighbouring lanes hold a block of 32 columns between them.
+// All lanes call; columns past Q and rows past P, or that do not exist, are not written or are zeros.
 __device__ __forceinline__ void finish(const Epilogue& e, int m, int n, int P, int Q, bool there, float* v)
 {
-    const bool in = m < P;
-    const int left = in ? Q - n : 0;
+    const int left = m < P ? Q - n : 0;
     if (e.kept_act != LAST_ACT_NONE) {
         if (there && left > 0) {
-            const uint8_t* q = e.kept.q + (size_t)m * e.kept.pitch + n;
+            unsigned lo, hi;
+            load_codes(e.kept.q + (size_t)m * e.kept.pitch, n, left, e.kept.aligned, &lo, &hi);
             const float sc = scale_value(e.kept.scales[(size_t)m * e.kept.scale_pitch + n / kBlock]);
-#pragma unroll
-            for (int u = 0; u < U; u += 4) {
-                unsigned c = 0;
-                if (e.kept.aligned && left >= U) {
-                    c = *(const unsigned*)(q + u);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (u + k < left) c |= (unsigned)q[u + k] << (8 * k);
-                }
-                float h[4];
-                if (e.kept.e4m3) decode4<true>(c, sc, h);
-                else decode4<false>(c, sc, h);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[u + k] *= slope(e.kept_act, h[k]);
+            float h[8];
+            if (e.kept.e4m3) {
+                decode4<true>(lo, sc, h);
+                decode4<true>(hi, sc, h + 4);
+            } else {
+                decode4<false>(lo, sc, h);
+                decode4<false>(hi, sc, h + 4);
             }
+            times_slope(e.kept_act, h, v);
         }
     } else if (e.bias) {
+        float b[8];
+        load8<float>(e.bias, n, left, e.wide_bias, b);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < left) v[u] += e.bias[n + u];
+        for (int u = 0; u < 8; ++u) v[u] += b[u];
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < 8; ++u)
         if (!there || u >= left) v[u] = 0.f;
-    if constexpr (U == 8) {
-        if (e.kept_act == LAST_ACT_NONE && e.kept.q) {
-            // lanes l, l + 16, l + 32, l + 48 hold a block between them
-            unsigned t = top8(v);
-            t = umax(t, (unsigned)__shfl_xor((int)t, 16, kWave));
-            t = umax(t, (unsigned)__shfl_xor((int)t, 32, kWave));
-            store_eight(e.kept, m, n, left, (n & (kBlock - 1)) == 0, t, v);
-        }
-    }
-    if (e.act != LAST_ACT_NONE) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = activate(e.act, v[u]);
-    }
+    if (e.kept_act == LAST_ACT_NONE && e.kept.q)
+        store_eight(e.kept, m, n, left, (n & (kBlock - 1)) == 0, quad_max(top8(v)), v);
+    activate8(e.act, v);
     if (e.res && there && left > 0) {
         const size_t at = (size_t)m * e.pres + n;
-        if (U == 8) {
-            float r[8];
-            if (e.type == LAST_BF16) load8<bf16_t>(e.res, at, left, e.wide_res, r);
-            else if (e.type == LAST_F16) load8<f16_t>(e.res, at, left, e.wide_res, r);
-            else load8<float>(e.res, at, left, e.wide_res, r);
+        float r[8];
+        if (e.type == LAST_BF16) load8<bf16_t>(e.res, at, left, e.wide_res, r);
+        else if (e.type == LAST_F16) load8<f16_t>(e.res, at, left, e.wide_res, r);
+        else load8<float>(e.res, at, left, e.wide_res, r);
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] += r[u];
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (u < left)
-                    v[u] += e.type == LAST_BF16 ? Elt<bf16_t>::get(e.res, at + u) : e.type == LAST_F16 ? Elt<f16_t>::get(e.res, at + u) : Elt<float>::get(e.res, at + u);
-        }
+        for (int u = 0; u < 8; ++u) v[u] += r[u];
     }
-    if constexpr (U == 8) {
-        if (e.out.q) {
-            unsigned t = top8(v);
-            t = umax(t, (unsigned)__shfl_xor((int)t, 16, kWave));
-            t = umax(t, (unsigned)__shfl_xor((int)t, 32, kWave));
-            store_eight(e.out, m, n, left, (n & (kBlock - 1)) == 0, t, v);
-        }
-    }
-    if (!e.y || left <= 0) return;
-    const size_t at = (size_t)m * e.py + n;
-    if constexpr (U == 8) {
-        store8_as(e.type, e.y, at, left, e.wide, v);
-    } else if (e.wide && left >= 4) {
-        if (e.type == LAST_BF16) *(u2*)((uint16_t*)e.y + at) = u2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-        else if (e.type == LAST_F16) *(u2*)((_Float16*)e.y + at) = u2{f16_pair(v[0], v[1]), f16_pair(v[2], v[3])};
-        else *(f4*)((float*)e.y + at) = f4{v[0], v[1], v[2], v[3]};
-    } else {
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (u < left) {
-                if (e.type == LAST_BF16) Elt<bf16_t>::put(e.y, at + u, v[u]);
-                else if (e.type == LAST_F16) Elt<f16_t>::put(e.y, at + u, v[u]);
-                else Elt<float>::put(e.y, at + u, v[u]);
-            }
-    }
-}
-
-template <int U>
-__device__ __forceinline__ void store_part(float* row, int n, int Q, const float* v)
-{
-    if ((Q & 3) == 0 && n + U <= Q) {
-#pragma unroll
-        for (int u = 0; u < U; u += 4) *(f4*)(row + n + u) = f4{v[u], v[u + 1], v[u + 2], v[u + 3]};
-    } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (n + u < Q) row[n + u] = v[u];
-    }
+    if (e.out.q) store_eight(e.out, m, n, left, (n & (kBlock - 1)) == 0, quad_max(top8(v)), v);
+    if (e.y && left > 0) store8_as(e.type, e.y, (size_t)m * e.py + n, left, e.wide, v);
 }
 
 // tiles in the order of the workgroups: workgroups i = j (mod 8) share an XCD and its L2, so each XCD gets a stretch of
@@ -280,13 +240,17 @@ __device__ __forceinline__ void tile_of(int id, int n, int tiles_p, int tiles_q,
     *tq = in / h;
 }
 
+// The loop.  While a wavefront multiplies the first half of a step (32 of its 64 rows of the reduction) it reads the second
+// half's operands from LDS, and while it multiplies the second half it reads those of the next step, so that the matrix cores
+// do not wait for LDS; one barrier a step, in the middle, after which the step's own buffer is free and the step after the
+// next is sent for.  The next step has then had a whole step's time to come.  With 8-bit operands one instruction takes
+// 128 values of the reduction, and the halves are those of the rows of P.
 template <typename E, int LP, int LQ, int BP, int BQ, int WP, int WQ>
 __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
 {
     constexpr int kThreads = WP * WQ * kWave;
     constexpr bool kEight = Elt<E>::size == 1;
     constexpr int NP = BP / WP / 16, NQ = BQ / WQ / 16;                   // accumulators of a wavefront
-    constexpr int U = LQ == kAlong && NQ % 2 == 0 ? 8 : 4;
     using TP = Tile<LP, BP, kThreads>;
     using TQ = Tile<LQ, BQ, kThreads>;
     __shared__ __align__(1024) char lds[2][TP::kBytes + TQ::kBytes];
@@ -305,9 +269,10 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
     P.init(p0, a.P, a.pp, LP == kAlong ? &a.frames : nullptr, LP == kAlong ? &any : nullptr);
     Q.init(q0, a.Q, a.pq, nullptr, nullptr);
     const bool work = LP == kAcross || __syncthreads_or(any);
+    const int steps = work ? (int)((k1 - k0 + (LP == kAlong ? kStep : 64) - 1) / (LP == kAlong ? kStep : 64)) : 0;
 
     f4 acc[NP][NQ];
-    f4 accb[NP / WQ];                                                     // row sums of P, shared by the wavefronts that read it
+    f4 accb[(NP + WQ - 1) / WQ];                                          // row sums of P, shared by the wavefronts that read it
 #pragma unroll
     for (int x = 0; x < NP; ++x) {
         accb[x / WQ] = f4{0.f, 0.f, 0.f, 0.f};
@@ -316,132 +281,162 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
     }
     const bool bias_too = LP == kAcross && a.e.part_bias && tq == 0;
 
-    if (work) {
-        const int steps = (int)((k1 - k0 + (LP == kAlong ? kStep : 64) - 1) / (LP == kAlong ? kStep : 64));
-        const char* bp = a.p + (LP == kAlong ? (long long)p0 * a.pp + k0 : (long long)p0 * 2 + k0 * a.pp);
-        const char* bq = a.q + (LQ == kAlong ? (long long)q0 * a.pq + k0 : (long long)q0 * 2 + (LP == kAlong ? k0 / 2 : k0) * a.pq);
+    const char* bp = a.p + (LP == kAlong ? (long long)p0 * a.pp + k0 : (long long)p0 * 2 + k0 * a.pp);
+    const char* bq = a.q + (LQ == kAlong ? (long long)q0 * a.pq + k0 : (long long)q0 * 2 + (LP == kAlong ? k0 / 2 : k0) * a.pq);
 
-        const auto load = [&](int s, int buf) {
-            const long long left = k1 - k0 - (long long)s * (LP == kAlong ? kStep : 64);
-            unsigned long long mask = ~0ull;
-            if constexpr (LP == kAcross) {
-                mask = left < 64 ? (1ull << left) - 1 : ~0ull;
-                if (a.mask) mask &= a.mask[(k0 >> 6) + s];
-            } else if constexpr (LQ == kAcross) {
-                const long long rows = a.q_rows - k0 / 2 - 64ll * s;
-                mask = rows < 64 ? (1ull << rows) - 1 : ~0ull;
-            }
-            P.load(bp + (long long)s * (LP == kAlong ? kStep : 64 * a.pp), left, mask, lds[buf]);
-            Q.load(bq + (long long)s * (LQ == kAlong ? kStep : 64 * a.pq), left, mask, lds[buf] + TP::kBytes);
-            if constexpr (kEight) {
-                // a row's four scales of the step
-                const int wave_first = wave * kWave;
+    const auto send = [&](int s) {
+        const int buf = s & 1;
+        const long long left = k1 - k0 - (long long)s * (LP == kAlong ? kStep : 64);
+        unsigned long long mask = ~0ull;
+        if constexpr (LP == kAcross) {
+            mask = left < 64 ? (1ull << left) - 1 : ~0ull;
+            if (a.mask) mask &= a.mask[(k0 >> 6) + s];
+        } else if constexpr (LQ == kAcross) {
+            const long long rows = a.q_rows - k0 / 2 - 64ll * s;
+            mask = rows < 64 ? (1ull << rows) - 1 : ~0ull;
+        }
+        P.load(bp + (long long)s * (LP == kAlong ? kStep : 64 * a.pp), left, mask, lds[buf]);
+        Q.load(bq + (long long)s * (LQ == kAlong ? kStep : 64 * a.pq), left, mask, lds[buf] + TP::kBytes);
+        if constexpr (kEight) {
+            // a row's four scales of the step
+            const int first = wave * kWave;
 #pragma unroll
-                for (int j = 0; j < (BP + BQ + kThreads - 1) / kThreads; ++j) {
-                    const int r = j * kThreads + (int)threadIdx.x;
-                    if (j * kThreads + wave_first < BP + BQ) {
-                        const bool isp = j * kThreads + wave_first < BP;
-                        const int row = isp ? r : r - BP;
-                        const bool ok = isp ? p0 + row < a.P : q0 + row < a.Q;
-                        const __amdgpu_buffer_rsrc_t b = buffer_of(isp ? a.sp + (long long)p0 * a.psp : a.sq + (long long)q0 * a.psq);
-                        const unsigned o = ok ? (unsigned)(row * (isp ? a.psp : a.psq)) + (unsigned)(k0 / kBlock) + 4u * (unsigned)s : kNowhere;
-                        __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_t)&scales[buf][j * kThreads + wave_first], 4, (int)o, 0, 0, 0);
-                    }
+            for (int j = 0; j < (BP + BQ + kThreads - 1) / kThreads; ++j) {
+                const int r = j * kThreads + (int)threadIdx.x;
+                if (j * kThreads + first < BP + BQ) {
+                    const bool isp = j * kThreads + first < BP;
+                    const int row = isp ? r : r - BP;
+                    const bool ok = isp ? p0 + row < a.P : q0 + row < a.Q;
+                    const unsigned o = ok ? (unsigned)(row * (isp ? a.psp : a.psq)) + (unsigned)(k0 / kBlock) + 4u * (unsigned)s : kNowhere;
+                    to_lds<4>(isp ? a.sp + (long long)p0 * a.psp : a.sq + (long long)q0 * a.psq, o, &scales[buf][j * kThreads + first]);
                 }
             }
-        };
+        }
+    };
+    const auto read_p = [&](int s, int half, int x) {
+        const char* l = lds[s & 1];
+        const int at = wp * (BP / WP) + x * 16, kr = half * 32 + 8 * g + (i16 >> 2);
+        if constexpr (LP == kAlong) return *(const u4*)(l + along_at(at + i16, half * 4 + g));
+        else
+            return across_read(l, kr * (BP * 2) + ((at / 16 ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8,
+                               (kr + 4) * (BP * 2) + ((at / 16 ^ across_swizzle(kr + 4)) << 5) + (i16 & 3) * 8);
+    };
+    const auto read_q = [&](int s, int half, int y) {
+        const char* l = lds[s & 1] + TP::kBytes;
+        const int at = wq * (BQ / WQ) + y * 16, kr = half * 32 + 8 * g + (i16 >> 2);
+        if constexpr (LQ == kAlong) return *(const u4*)(l + along_at(at + i16, half * 4 + g));
+        else
+            return across_read(l, kr * (BQ * 2) + ((at / 16 ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8,
+                               (kr + 4) * (BQ * 2) + ((at / 16 ^ across_swizzle(kr + 4)) << 5) + (i16 & 3) * 8);
+    };
 
-        if (steps > 0) load(0, 0);
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-        for (int s = 0; s < steps; ++s) {
-            const char* l = lds[s & 1];
-            if (s + 1 < steps) load(s + 1, (s + 1) & 1);
-            if constexpr (kEight) {
-                u4 fp[NP][2], fq[NQ][2];
-                int cp[NP], cq[NQ];
-#pragma unroll
-                for (int x = 0; x < NP; ++x) {
-                    const int r = wp * (BP / WP) + x * 16 + i16;
-                    fp[x][0] = *(const u4*)(l + along_at(r, g));
-                    fp[x][1] = *(const u4*)(l + along_at(r, 4 + g));
-                    cp[x] = (int)(scales[s & 1][r] >> (8 * g));
-                }
+    if (steps > 0) {
+        send(0);
+        arrived();
+        if (steps > 1) send(1);
+        if constexpr (kEight) {
+            u4 fp[NP][2], fq[NQ][2];
+            int cp[NP], cq[NQ];
+            for (int s = 0; s < steps; ++s) {
 #pragma unroll
                 for (int y = 0; y < NQ; ++y) {
-                    const int r = wq * (BQ / WQ) + (U == 8 ? 32 * (y >> 1) + 8 * (i16 >> 2) + 4 * (y & 1) + (i16 & 3) : 16 * y + i16);
-                    fq[y][0] = *(const u4*)(l + TP::kBytes + along_at(r, g));
-                    fq[y][1] = *(const u4*)(l + TP::kBytes + along_at(r, 4 + g));
-                    cq[y] = (int)(scales[s & 1][BP + r] >> (8 * g));
+                    fq[y][0] = read_q(s, 0, y);
+                    fq[y][1] = read_q(s, 1, y);
+                    cq[y] = (int)(scales[s & 1][BP + wq * (BQ / WQ) + y * 16 + i16] >> (8 * g));
+                }
+#pragma unroll
+                for (int x = 0; x < NP; ++x) {
+                    fp[x][0] = read_p(s, 0, x);
+                    fp[x][1] = read_p(s, 1, x);
+                    cp[x] = (int)(scales[s & 1][wp * (BP / WP) + x * 16 + i16] >> (8 * g));
                 }
 #pragma unroll
                 for (int x = 0; x < NP; ++x)
 #pragma unroll
                     for (int y = 0; y < NQ; ++y) acc[x][y] = mfma_scaled(fq[y], fp[x], acc[x][y], cq[y], cp[x]);
-            } else {
+                arrived();
+                if (s + 2 < steps) send(s + 2);
+            }
+        } else {
+            u4 fp[2][NP], fq[2][NQ];
+            const auto read = [&](int s, int half) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    u4 fp[NP], fq[NQ];
-                    const int kr = half * 32 + 8 * g + (i16 >> 2);
+                for (int y = 0; y < NQ; ++y) fq[half][y] = read_q(s, half, y);
 #pragma unroll
-                    for (int x = 0; x < NP; ++x) {
-                        const int at = wp * (BP / WP) + x * 16;
-                        if constexpr (LP == kAlong) {
-                            fp[x] = *(const u4*)(l + along_at(at + i16, half * 4 + g));
-                        } else {
-                            fp[x] = across_read(l, kr * (BP * 2) + ((at / 16 ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8,
-                                                (kr + 4) * (BP * 2) + ((at / 16 ^ across_swizzle(kr + 4)) << 5) + (i16 & 3) * 8);
-                        }
-                    }
+                for (int x = 0; x < NP; ++x) fp[half][x] = read_p(s, half, x);
+            };
+            const auto multiply = [&](int half) {
 #pragma unroll
-                    for (int y = 0; y < NQ; ++y) {
-                        const int at = wq * (BQ / WQ);
-                        if constexpr (LQ == kAlong) {
-                            const int r = at + (U == 8 ? 32 * (y >> 1) + 8 * (i16 >> 2) + 4 * (y & 1) + (i16 & 3) : 16 * y + i16);
-                            fq[y] = *(const u4*)(l + TP::kBytes + along_at(r, half * 4 + g));
-                        } else {
-                            const int gr = at / 16 + y;
-                            fq[y] = across_read(l + TP::kBytes, kr * (BQ * 2) + ((gr ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8,
-                                                (kr + 4) * (BQ * 2) + ((gr ^ across_swizzle(kr + 4)) << 5) + (i16 & 3) * 8);
-                        }
-                    }
+                for (int x = 0; x < NP; ++x)
 #pragma unroll
-                    for (int x = 0; x < NP; ++x)
+                    for (int y = 0; y < NQ; ++y) acc[x][y] = Mfma<E>::go(fq[half][y], fp[half][x], acc[x][y]);
+                if constexpr (LP == kAcross) {
+                    if (bias_too) {
+                        const unsigned one = Elt<E>::type == LAST_BF16 ? 0x3f803f80u : 0x3c003c00u;
 #pragma unroll
-                        for (int y = 0; y < NQ; ++y) acc[x][y] = Mfma<E>::go(fq[y], fp[x], acc[x][y]);
-                    if constexpr (LP == kAcross) {
-                        if (bias_too) {
-                            const unsigned one = Elt<E>::type == LAST_BF16 ? 0x3f803f80u : 0x3c003c00u;
-#pragma unroll
-                            for (int x = 0; x < NP; ++x)
-                                if (x % WQ == wq) accb[x / WQ] = Mfma<E>::go(u4{one, one, one, one}, fp[x], accb[x / WQ]);
-                        }
+                        for (int x = 0; x < NP; ++x)
+                            if (x % WQ == wq) accb[x / WQ] = Mfma<E>::go(u4{one, one, one, one}, fp[half][x], accb[x / WQ]);
                     }
                 }
+            };
+            read(0, 0);
+            for (int s = 0; s < steps; ++s) {
+                read(s, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(0);
+                __builtin_amdgcn_sched_barrier(0);
+                arrived();
+                if (s + 2 < steps) send(s + 2);
+                if (s + 1 < steps) read(s + 1, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(1);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
         }
     }
 
-    // lane: row 16 x + i16 of P; column 4 g + i of accumulator y of Q, or, along, 8 g + 4 (y & 1) + i of two
+    // A lane has row 16 x + i16 of P and columns 16 y + 4 g .. of Q.  The epilogue wants eight columns of a row in a lane and
+    // whole lines of rows in a wavefront: 64 rows at a time change places in the wavefront's own part of LDS, whose 16-byte
+    // pieces of a row are swizzled by the row.
+    constexpr int kCols = BQ / WQ, kPieces = kCols / 4, kLanes = kCols / 8, kRows = kWave / kLanes, XS = NP < 4 ? NP : 4;
+    static_assert((size_t)XS * 16 * kCols * 4 * WP * WQ <= sizeof(lds), "room for the epilogue");
+    __syncthreads();
+    char* mine = &lds[0][0] + wave * (XS * 16 * kCols * 4);
+#pragma unroll 1
+    for (int part = 0; part < NP / XS; ++part) {
 #pragma unroll
-    for (int x = 0; x < NP; ++x) {
-        const int m = p0 + wp * (BP / WP) + x * 16 + i16;
-        const bool there = m < a.P && (LP == kAcross || frame_exists(a.frames, m));
+        for (int p = 0; p < NP / XS; ++p)
+            if (p == part) {
 #pragma unroll
-        for (int y = 0; y < NQ; y += U / 4) {
-            const int n = q0 + wq * (BQ / WQ) + y * 16 + g * U;
-            float v[U];
+                for (int x = 0; x < XS; ++x)
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = acc[x][y + u / 4][u & 3];
+                    for (int y = 0; y < NQ; ++y)
+                        *(f4*)(mine + (x * 16 + i16) * (kCols * 4) + (((4 * y + g) ^ (i16 & (kPieces - 1))) << 4)) = acc[p * XS + x][y];
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();                     // (the reads follow the writes in the wavefront's order)
+        const int c = (lane % kLanes) * 8, n = q0 + wq * kCols + c;
+#pragma unroll 1
+        for (int r = lane / kLanes; r < XS * 16; r += kRows) {
+            const int m = p0 + wp * (BP / WP) + part * XS * 16 + r;
+            const f4 lo = *(const f4*)(mine + r * (kCols * 4) + (((c / 4) ^ (r & (kPieces - 1))) << 4));
+            const f4 hi = *(const f4*)(mine + r * (kCols * 4) + (((c / 4 + 1) ^ (r & (kPieces - 1))) << 4));
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             if (a.e.part) {
-                if (m < a.P) store_part<U>(a.e.part + ((size_t)blockIdx.y * a.P + m) * a.Q, n, a.Q, v);
+                if (m < a.P) store8<float>(a.e.part, ((size_t)blockIdx.y * a.P + m) * a.Q + n, a.Q - n, (a.Q & 3) == 0, v);
             } else {
-                finish<U>(a.e, m, n, a.P, a.Q, there, v);
+                finish(a.e, m, n, a.P, a.Q, m < a.P && (LP == kAcross || frame_exists(a.frames, m)), v);
             }
         }
-        if (bias_too && x % WQ == wq && g == 0 && m < a.P) a.e.part_bias[(size_t)blockIdx.y * a.P + m] = accb[x / WQ][0];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    if (bias_too) {
+#pragma unroll
+        for (int x = 0; x < NP; ++x) {
+            const int m = p0 + wp * (BP / WP) + x * 16 + i16;
+            if (x % WQ == wq && g == 0 && m < a.P) a.e.part_bias[(size_t)blockIdx.y * a.P + m] = accb[x / WQ][0];
+        }
     }
 }
 
@@ -455,7 +450,6 @@ template <typename E, int MT, int QF>
 __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
 {
     constexpr bool kEight = Elt<E>::size == 1;
-    constexpr int U = 4 * QF;
     __shared__ f4 red[kFewWaves][MT][QF][kWave];
     const int lane = (int)threadIdx.x % kWave, g = lane >> 4, i16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -465,7 +459,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
     int rq[QF];
 #pragma unroll
     for (int f = 0; f < QF; ++f) {
-        rq[f] = QF == 2 ? 8 * (i16 >> 2) + 4 * f + (i16 & 3) : i16;
+        rq[f] = 16 * f + i16;
         oq[f] = q0 + rq[f] < a.Q ? (unsigned)(rq[f] * a.pq) + 16u * g : kNowhere;
     }
 #pragma unroll
@@ -525,17 +519,21 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
         for (int f = 0; f < QF; ++f) red[wave][t][f][lane] = acc[t][f];
     __syncthreads();
     if (wave >= MT) return;
-    float v[U];
+    // lane: row lane / 4 of the wavefront's 16, columns 8 (lane & 3) .. of the workgroup's 16 QF
+    const int r = lane >> 2, c = lane & 3, m = wave * 16 + r;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < 2 * QF) {
 #pragma unroll
-    for (int f = 0; f < QF; ++f) {
-        f4 t = red[0][wave][f][lane];
+        for (int h = 0; h < 2; ++h) {
+            f4 t = red[0][wave][c >> 1][(2 * (c & 1) + h) * 16 + r];
 #pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) t += red[w][wave][f][lane];
+            for (int w = 1; w < kFewWaves; ++w) t += red[w][wave][c >> 1][(2 * (c & 1) + h) * 16 + r];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[4 * f + i] = t[i];
+            for (int i = 0; i < 4; ++i) v[4 * h + i] = t[i];
+        }
     }
-    const int m = wave * 16 + i16;
-    finish<U>(a.e, m, q0 + g * U, a.P, a.Q, m < a.P && frame_exists(a.frames, m), v);
+    const int P = c < 2 * QF ? a.P : 0;
+    finish(a.e, m, q0 + 8 * c, P, a.Q, m < P && frame_exists(a.frames, m), v);
 }
 
 // ---- shares of a reduction joined, in order, with the epilogue; a wavefront has 16 rows of 32 columns
@@ -544,7 +542,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
     const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
     const int across = (a.Q + 31) / 32;
     const unsigned id = blockIdx.x * 4u + wave;
-    const int m = (int)(id / (unsigned)across) * 16 + (lane & 15), n = (int)(id % (unsigned)across) * 32 + 8 * (lane >> 4);
+    const int m = (int)(id / (unsigned)across) * 16 + (lane >> 2), n = (int)(id % (unsigned)across) * 32 + 8 * (lane & 3);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (m < a.P) {
         for (int s = 0; s < splits; ++s) {
@@ -559,7 +557,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
             a.e.sum_bias[m] = b;
         }
     }
-    finish<8>(a.e, m, n, a.P, a.Q, m < a.P && frame_exists(a.frames, m), v);
+    finish(a.e, m, n, a.P, a.Q, m < a.P && frame_exists(a.frames, m), v);
 }
 
 // ---- rows of `bytes` bytes laid out at multiples of 16 with zeros behind them, 16 bytes a thread
