@@ -176,10 +176,17 @@ void launch_tiles(ProductArgs a, const ProductPlan& p, hipStream_t st)
     a.tiles_p = (a.P + tile - 1) / tile;
     a.tiles_q = (a.Q + tile - 1) / tile;
     const dim3 grid((unsigned)(a.tiles_p * a.tiles_q), (unsigned)p.splits);
-    if (p.variant == 2) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 256, 256, 2, 4>), grid, dim3(512), 0, st, a);
+    const ProductArgs j = a;
+    if (p.splits > 1) {                              // the epilogue comes with the joining
+        a.e.res = nullptr;
+        a.e.kept_act = LAST_ACT_NONE;
+    }
+#ifndef BIGW
+#define BIGW 4
+#endif
+    if (p.variant == 2) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 256, 256, 2, BIGW>), grid, dim3(128 * BIGW), 0, st, a);
     else hipLaunchKernelGGL((product_kernel<E, LP, LQ, 128, 128, 2, 2>), grid, dim3(256), 0, st, a);
     if (p.splits > 1) {
-        ProductArgs j = a;
         const long long waves = (long long)((a.P + 15) / 16) * ((a.Q + 31) / 32);
         hipLaunchKernelGGL(product_join_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, j, p.splits);
     }

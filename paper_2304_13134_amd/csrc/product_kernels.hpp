@@ -90,63 +90,57 @@ __device__ __forceinline__ void to_lds(const void* base, unsigned o, const void*
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(m), "v"(o), "s"(b) : "memory");
 }
 
-// what this wavefront sent to LDS and asked from it has come, then the same of the whole workgroup
+// what this wavefront asked from LDS has come, and what it sent there but for the last LATER loads; then the same of the whole
+// workgroup
+template <int LATER>
 __device__ __forceinline__ void arrived()
 {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
 }
 
 // ---- one operand's tile: ROWS rows or columns of the output
 template <int L, int ROWS, int THREADS>
 struct Tile {
     static constexpr int kBytes = ROWS * kStep;
-    static constexpr int kLoads = kBytes / 16 / THREADS;
+    static constexpr int kLoads = kBytes / 16 / THREADS;                 // of a thread, kApart rows from each other
     static constexpr int kPieces = L == kAlong ? 8 : ROWS / 8;           // 16-byte pieces of a row in LDS
+    static constexpr int kApart = THREADS / kPieces;
     static_assert(kBytes % (16 * THREADS) == 0, "whole loads");
     static_assert(L == kAlong || ROWS >= 128, "eight granules to swizzle");
-    unsigned off[kLoads];
+    static_assert(kApart % 16 == 0, "the same swizzle for all loads of a thread");
+    unsigned off;                                                        // of the first load, from the tile's first byte
+    unsigned valid;                                                      // kAlong: bits of the loads whose row exists
+    int row, piece;                                                      // of the first load
 
     // first: first row or column of the tile; count: how many the matrix has
-    __device__ void init(int first, int count, long long pitch, const Frames* frames, int* any)
+    __device__ void init(int first, int count, long long pitch, const Frames* frames)
     {
+        row = (int)threadIdx.x / kPieces;
+        const int c = (int)threadIdx.x % kPieces;
+        valid = 0;
+        if constexpr (L == kAlong) {
+            piece = c ^ along_swizzle(row);
+            off = (unsigned)(row * pitch) + 16u * (unsigned)piece;
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int i = j * THREADS + (int)threadIdx.x, r = i / kPieces, c = i % kPieces;
-            if constexpr (L == kAlong) {
-                bool ok = first + r < count;
-                if (ok && frames) ok = frame_exists(*frames, first + r);
-                if (any) *any |= ok;
-                off[j] = ok ? (unsigned)(r * pitch) + 16u * (unsigned)(c ^ along_swizzle(r)) : kNowhere;
-            } else {
-                const int g = (c >> 1) ^ across_swizzle(r), col = g * 16 + (c & 1) * 8;
-                off[j] = first + col < count ? (unsigned)(r * pitch) + 2u * (unsigned)col : kNowhere;
+            for (int j = 0; j < kLoads; ++j) {
+                const int r = first + row + j * kApart;
+                if (r < count && (!frames || frame_exists(*frames, r))) valid |= 1u << j;
             }
+        } else {
+            const int col = ((c >> 1) ^ across_swizzle(row)) * 16 + (c & 1) * 8;
+            off = first + col < count ? (unsigned)(row * pitch) + 2u * (unsigned)col : kNowhere;
         }
     }
 
-    // the tile's 128 bytes or 64 rows from `base` on; left: how many of them the reduction still has
-    __device__ __forceinline__ void load(const char* base, long long left, unsigned long long mask, char* lds)
+    // load j of the tile's 128 bytes or 64 rows from `base` on.  left: how many bytes the reduction still has (kAlong),
+    // mask: which rows exist (kAcross)
+    __device__ __forceinline__ void load(int j, const char* base, long long pitch, long long left, unsigned long long mask, char* lds) const
     {
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            unsigned o = off[j];
-            if constexpr (L == kAlong) {
-                if (left < kStep) {
-                    const int i = j * THREADS + (int)threadIdx.x, r = i / kPieces, c = i % kPieces;
-                    if (16 * (c ^ along_swizzle(r)) >= left) o = kNowhere;
-                }
-            } else {
-                const int r = (j * THREADS + (int)threadIdx.x) / kPieces;
-                if (!(mask >> r & 1)) o = kNowhere;
-            }
-            to_lds<16>(base, o, lds + (j * THREADS + wave * kWave) * 16);
-        }
+        char* to = lds + (j * THREADS + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) * kWave) * 16;
+        const bool in = L == kAlong ? (valid >> j & 1) != 0 && 16 * piece < left : (mask >> (row + j * kApart) & 1) != 0;
+        to_lds<16>(base + (long long)(j * kApart) * pitch, in ? off : kNowhere, to);
     }
 };
-
-// LDS byte of a piece of a row (kAlong)
-__device__ __forceinline__ int along_at(int r, int piece) { return r * kStep + ((piece ^ along_swizzle(r)) << 4); }
 
 template <typename E> struct Mfma;
 template <> struct Mfma<bf16_t> {
@@ -162,17 +156,15 @@ template <> struct Mfma<f16_t> {
     }
 };
 
-__device__ __forceinline__ f4 mfma_scaled(const u4* a, const u4* b, f4 c, int sa, int sb)
+__device__ __forceinline__ i8x join8(u4 a, u4 b)
 {
-    i8x x, y;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        x[k] = (int)a[0][k];
-        x[4 + k] = (int)a[1][k];
-        y[k] = (int)b[0][k];
-        y[4 + k] = (int)b[1][k];
-    }
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 0, 0, 0, sa, 0, sb);
+    return i8x{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+// lane: values 16 g .. and 64 + 16 g .. of 128 of its row or column, and the scale of values 32 g ..
+__device__ __forceinline__ f4 mfma_scaled(i8x a, i8x b, f4 c, int sa, int sb)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
 }
 
 __device__ __forceinline__ u4 across_read(const char* lds, int a0, int a1)
@@ -185,47 +177,97 @@ __device__ __forceinline__ u4 across_read(const char* lds, int a0, int a1)
 
 // ---- epilogue of eight neighbouring columns n.. of row m; four neighbouring lanes hold a block of 32 columns between them.
 // All lanes call; columns past Q and rows past P, or that do not exist, are not written or are zeros.
-__device__ __forceinline__ void finish(const Epilogue& e, int m, int n, int P, int Q, bool there, float* v)
+
+// what it reads, sent for ahead of its use: the residual, or the codes and the scale of what was kept
+struct Fetched {
+    u4 a, b;
+    unsigned scale;
+};
+
+template <typename E>
+__device__ __forceinline__ void fetch8(const void* p, size_t i, int n, bool aligned, Fetched* f)
+{
+    if (aligned && n >= 8) {
+        f->a = *(const u4*)((const char*)p + i * Elt<E>::size);
+        if constexpr (Elt<E>::size == 4) f->b = *(const u4*)((const char*)p + i * 4 + 16);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if constexpr (Elt<E>::size == 4) {
+                const unsigned w = k < n ? ((const unsigned*)p)[i + k] : 0u;
+                if (k < 4) f->a[k] = w;
+                else f->b[k - 4] = w;
+            } else {
+                const unsigned w = k < n ? ((const uint16_t*)p)[i + k] : 0u;
+                f->a[k >> 1] = k & 1 ? f->a[k >> 1] | w << 16 : w;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ Fetched fetch(const Epilogue& e, int m, int n, int P, int Q, bool there)
+{
+    Fetched f{};
+    const int left = m < P && there ? Q - n : 0;
+    if (left > 0) {
+        if (e.kept_act != LAST_ACT_NONE) {
+            unsigned lo, hi;
+            load_codes(e.kept.q + (size_t)m * e.kept.pitch, n, left, e.kept.aligned, &lo, &hi);
+            f.a[0] = lo;
+            f.a[1] = hi;
+            f.scale = e.kept.scales[(size_t)m * e.kept.scale_pitch + n / kBlock];
+        } else if (e.res) {
+            const size_t at = (size_t)m * e.pres + n;
+            if (e.type == LAST_F32) fetch8<float>(e.res, at, left, e.wide_res, &f);
+            else fetch8<bf16_t>(e.res, at, left, e.wide_res, &f);
+        }
+    }
+    return f;
+}
+
+__device__ __forceinline__ void finish(const Epilogue& e, int m, int n, int P, int Q, bool there, const float* bias, const Fetched& f, float* v)
 {
     const int left = m < P ? Q - n : 0;
     if (e.kept_act != LAST_ACT_NONE) {
-        if (there && left > 0) {
-            unsigned lo, hi;
-            load_codes(e.kept.q + (size_t)m * e.kept.pitch, n, left, e.kept.aligned, &lo, &hi);
-            const float sc = scale_value(e.kept.scales[(size_t)m * e.kept.scale_pitch + n / kBlock]);
-            float h[8];
-            if (e.kept.e4m3) {
-                decode4<true>(lo, sc, h);
-                decode4<true>(hi, sc, h + 4);
-            } else {
-                decode4<false>(lo, sc, h);
-                decode4<false>(hi, sc, h + 4);
-            }
-            times_slope(e.kept_act, h, v);
+        const float sc = scale_value(f.scale);
+        float h[8];
+        if (e.kept.e4m3) {
+            decode4<true>(f.a[0], sc, h);
+            decode4<true>(f.a[1], sc, h + 4);
+        } else {
+            decode4<false>(f.a[0], sc, h);
+            decode4<false>(f.a[1], sc, h + 4);
         }
-    } else if (e.bias) {
-        float b[8];
-        load8<float>(e.bias, n, left, e.wide_bias, b);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] += b[u];
+        times_slope(e.kept_act, h, v);
     }
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-        if (!there || u >= left) v[u] = 0.f;
+    for (int u = 0; u < 8; ++u) v[u] = there && u < left ? v[u] + bias[u] : 0.f;
     if (e.kept_act == LAST_ACT_NONE && e.kept.q)
         store_eight(e.kept, m, n, left, (n & (kBlock - 1)) == 0, quad_max(top8(v)), v);
     activate8(e.act, v);
-    if (e.res && there && left > 0) {
-        const size_t at = (size_t)m * e.pres + n;
+    if (e.res) {
         float r[8];
-        if (e.type == LAST_BF16) load8<bf16_t>(e.res, at, left, e.wide_res, r);
-        else if (e.type == LAST_F16) load8<f16_t>(e.res, at, left, e.wide_res, r);
-        else load8<float>(e.res, at, left, e.wide_res, r);
+        if (e.type == LAST_F32) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { r[u] = __uint_as_float(f.a[u]); r[4 + u] = __uint_as_float(f.b[u]); }
+        } else if (e.type == LAST_BF16) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { r[2 * u] = bf16_to_float(f.a[u] & 0xffffu); r[2 * u + 1] = __uint_as_float(f.a[u] & 0xffff0000u); }
+        } else {
+            const h8 h = __builtin_bit_cast(h8, f.a);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) r[u] = (float)h[u];
+        }
 #pragma unroll
         for (int u = 0; u < 8; ++u) v[u] += r[u];
     }
     if (e.out.q) store_eight(e.out, m, n, left, (n & (kBlock - 1)) == 0, quad_max(top8(v)), v);
     if (e.y && left > 0) store8_as(e.type, e.y, (size_t)m * e.py + n, left, e.wide, v);
+}
+
+__device__ __forceinline__ void load_bias(const Epilogue& e, int n, int Q, float* b)
+{
+    load8<float>(e.bias, n, e.bias ? Q - n : 0, e.wide_bias, b);
 }
 
 // tiles in the order of the workgroups: workgroups i = j (mod 8) share an XCD and its L2, so each XCD gets a stretch of
@@ -240,11 +282,13 @@ __device__ __forceinline__ void tile_of(int id, int n, int tiles_p, int tiles_q,
     *tq = in / h;
 }
 
-// The loop.  While a wavefront multiplies the first half of a step (32 of its 64 rows of the reduction) it reads the second
-// half's operands from LDS, and while it multiplies the second half it reads those of the next step, so that the matrix cores
-// do not wait for LDS; one barrier a step, in the middle, after which the step's own buffer is free and the step after the
-// next is sent for.  The next step has then had a whole step's time to come.  With 8-bit operands one instruction takes
-// 128 values of the reduction, and the halves are those of the rows of P.
+// The loop.  A step's 128 bytes are multiplied in two phases: the halves of its reduction, or, with 8-bit operands, whose
+// instruction takes 128 values at once, the halves of the rows of P.  A fragment of the next phase is read from LDS into the
+// registers of one that was just used, so that the matrix cores wait for LDS as little as there are few registers for copies.
+// One barrier a step, between the phases: all fragments of the step have then been read, its buffers are free, and the loads
+// that fill them are sent one by one between the matrix instructions of the second phase.  Q has two buffers and a step's time
+// to arrive; P, which comes from farther (each row is read by the few tiles beside it, W by all below), has three and two
+// steps' time: 160 KiB with tiles of 256, of 128 two workgroups' worth.  8-bit operands leave room for two of P, beside their scales.
 template <typename E, int LP, int LQ, int BP, int BQ, int WP, int WQ>
 __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
 {
@@ -253,8 +297,10 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
     constexpr int NP = BP / WP / 16, NQ = BQ / WQ / 16;                   // accumulators of a wavefront
     using TP = Tile<LP, BP, kThreads>;
     using TQ = Tile<LQ, BQ, kThreads>;
-    __shared__ __align__(1024) char lds[2][TP::kBytes + TQ::kBytes];
-    __shared__ unsigned scales[kEight ? 2 : 1][kEight ? BP + BQ : 1];
+    constexpr int kBuffersP = kEight ? 2 : 3, kAhead = kBuffersP;         // P is sent so many steps ahead of its use
+    constexpr unsigned kAtQ = kBuffersP * TP::kBytes, kLds = kAtQ + 2 * TQ::kBytes;
+    __shared__ __align__(1024) char lds[kLds];
+    __shared__ __align__(4) uint8_t scales[kEight ? 2 : 1][kEight ? (BP + BQ) * 4 : 1];
 
     const int lane = (int)threadIdx.x % kWave, g = lane >> 4, i16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wp = wave / WQ, wq = wave % WQ;
@@ -265,10 +311,18 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
 
     TP P;
     TQ Q;
-    int any = 0;
-    P.init(p0, a.P, a.pp, LP == kAlong ? &a.frames : nullptr, LP == kAlong ? &any : nullptr);
-    Q.init(q0, a.Q, a.pq, nullptr, nullptr);
-    const bool work = LP == kAcross || __syncthreads_or(any);
+    P.init(p0, a.P, a.pp, LP == kAlong ? &a.frames : nullptr);
+    Q.init(q0, a.Q, a.pq, nullptr);
+    bool work = true;                                                     // a row of the tile exists
+    if (LP == kAlong && a.frames.len) {
+        unsigned* some = (unsigned*)lds;
+        const unsigned long long b = __ballot(P.valid != 0);
+        if (lane == 0) some[wave] = b != 0;
+        __syncthreads();
+        work = false;
+        for (int w = 0; w < WP * WQ; ++w) work |= __builtin_amdgcn_readfirstlane((int)some[w]) != 0;
+        __syncthreads();
+    }
     const int steps = work ? (int)((k1 - k0 + (LP == kAlong ? kStep : 64) - 1) / (LP == kAlong ? kStep : 64)) : 0;
 
     f4 acc[NP][NQ];
@@ -284,115 +338,185 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
     const char* bp = a.p + (LP == kAlong ? (long long)p0 * a.pp + k0 : (long long)p0 * 2 + k0 * a.pp);
     const char* bq = a.q + (LQ == kAlong ? (long long)q0 * a.pq + k0 : (long long)q0 * 2 + (LP == kAlong ? k0 / 2 : k0) * a.pq);
 
-    const auto send = [&](int s) {
-        const int buf = s & 1;
-        const long long left = k1 - k0 - (long long)s * (LP == kAlong ? kStep : 64);
-        unsigned long long mask = ~0ull;
+    // Loads of step s of P and s of Q; beyond the last step they are sent all the same, from nowhere, so that their number
+    // always tells which have come.
+    const auto left_of = [&](int s) { return s < steps ? k1 - k0 - (long long)s * (LP == kAlong ? kStep : 64) : 0ll; };
+    const auto mask_of = [&](int s) {
         if constexpr (LP == kAcross) {
-            mask = left < 64 ? (1ull << left) - 1 : ~0ull;
-            if (a.mask) mask &= a.mask[(k0 >> 6) + s];
+            const long long left = left_of(s);
+            unsigned long long m = left >= 64 ? ~0ull : (1ull << left) - 1;
+            // (constant memory to the compiler: a scalar load, which is not counted with those that are waited for)
+            typedef const __attribute__((address_space(4))) unsigned long long* constant_t;
+            if (a.mask && s < steps) m &= ((constant_t)(uintptr_t)a.mask)[(k0 >> 6) + s];
+            return m;
         } else if constexpr (LQ == kAcross) {
-            const long long rows = a.q_rows - k0 / 2 - 64ll * s;
-            mask = rows < 64 ? (1ull << rows) - 1 : ~0ull;
-        }
-        P.load(bp + (long long)s * (LP == kAlong ? kStep : 64 * a.pp), left, mask, lds[buf]);
-        Q.load(bq + (long long)s * (LQ == kAlong ? kStep : 64 * a.pq), left, mask, lds[buf] + TP::kBytes);
-        if constexpr (kEight) {
-            // a row's four scales of the step
-            const int first = wave * kWave;
-#pragma unroll
-            for (int j = 0; j < (BP + BQ + kThreads - 1) / kThreads; ++j) {
-                const int r = j * kThreads + (int)threadIdx.x;
-                if (j * kThreads + first < BP + BQ) {
-                    const bool isp = j * kThreads + first < BP;
-                    const int row = isp ? r : r - BP;
-                    const bool ok = isp ? p0 + row < a.P : q0 + row < a.Q;
-                    const unsigned o = ok ? (unsigned)(row * (isp ? a.psp : a.psq)) + (unsigned)(k0 / kBlock) + 4u * (unsigned)s : kNowhere;
-                    to_lds<4>(isp ? a.sp + (long long)p0 * a.psp : a.sq + (long long)q0 * a.psq, o, &scales[buf][j * kThreads + first]);
-                }
-            }
+            const long long rows = s < steps ? a.q_rows - k0 / 2 - 64ll * s : 0;
+            return rows < 64 ? (1ull << rows) - 1 : ~0ull;
+        } else {
+            return ~0ull;
         }
     };
-    const auto read_p = [&](int s, int half, int x) {
-        const char* l = lds[s & 1];
-        const int at = wp * (BP / WP) + x * 16, kr = half * 32 + 8 * g + (i16 >> 2);
-        if constexpr (LP == kAlong) return *(const u4*)(l + along_at(at + i16, half * 4 + g));
-        else
-            return across_read(l, kr * (BP * 2) + ((at / 16 ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8,
-                               (kr + 4) * (BP * 2) + ((at / 16 ^ across_swizzle(kr + 4)) << 5) + (i16 & 3) * 8);
+    const auto send_p = [&](int j, int s, int buf, unsigned long long mask) {
+        P.load(j, bp + (long long)s * (LP == kAlong ? kStep : 64 * a.pp), a.pp, left_of(s), mask, lds + buf * TP::kBytes);
     };
-    const auto read_q = [&](int s, int half, int y) {
-        const char* l = lds[s & 1] + TP::kBytes;
-        const int at = wq * (BQ / WQ) + y * 16, kr = half * 32 + 8 * g + (i16 >> 2);
-        if constexpr (LQ == kAlong) return *(const u4*)(l + along_at(at + i16, half * 4 + g));
-        else
-            return across_read(l, kr * (BQ * 2) + ((at / 16 ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8,
-                               (kr + 4) * (BQ * 2) + ((at / 16 ^ across_swizzle(kr + 4)) << 5) + (i16 & 3) * 8);
+    const auto send_q = [&](int j, int s, unsigned long long mask) {
+        Q.load(j, bq + (long long)s * (LQ == kAlong ? kStep : 64 * a.pq), a.pq, left_of(s), mask, lds + kAtQ + (s & 1) * TQ::kBytes);
+    };
+    constexpr int kScaleLoads = kEight ? (BP + BQ + kThreads - 1) / kThreads : 0;
+    const auto send_scales = [&](int j, int s) {                          // a row's four scales of the step
+        const int r = j * kThreads + (int)threadIdx.x, first = j * kThreads + wave * kWave;
+        const bool isp = first < BP;
+        const int row = isp ? r : r - BP;
+        const bool ok = s < steps && (isp ? p0 + row < a.P : q0 + row < a.Q);
+        const unsigned o = ok ? (unsigned)(row * (isp ? a.psp : a.psq)) + (unsigned)(k0 / kBlock) + 4u * (unsigned)s : kNowhere;
+        to_lds<4>(isp ? a.sp + (long long)p0 * a.psp : a.sq + (long long)q0 * a.psq, o, &scales[s & 1][first * 4]);
+    };
+    static_assert(!kEight || (BP + BQ) % kThreads == 0, "whole loads of scales");
+
+    // LDS byte of a wavefront's first fragment of a step's first half.  Along: fragment x is 16 rows on, half h at piece ^ 4 h.
+    // Across: half h is 32 rows on, the second four rows of a lane four on, and fragment x at granule ^ x (a wavefront's first
+    // column is a multiple of its 16 NP, NQ, powers of two, so the sum is an exclusive or).
+    const int kr = 8 * g + (i16 >> 2), swizzled = (g ^ along_swizzle(i16)) << 4;
+    const unsigned at_p = LP == kAlong ? (wp * (BP / WP) + i16) * kStep + swizzled
+                                       : kr * (BP * 2) + ((wp * NP ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8;
+    const unsigned at_q = kAtQ + (LQ == kAlong ? (wq * (BQ / WQ) + i16) * kStep + swizzled
+                                               : kr * (BQ * 2) + ((wq * NQ ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8);
+    const auto read_p = [&](unsigned at, int half, int x) {
+        if constexpr (LP == kAlong) return *(const u4*)(lds + (at ^ half * 64) + x * 16 * kStep);
+        else return across_read(lds + (at ^ x * 32) + half * 32 * BP * 2, 0, 4 * BP * 2);
+    };
+    const auto read_q = [&](unsigned at, int half, int y) {
+        if constexpr (LQ == kAlong) return *(const u4*)(lds + (at ^ half * 64) + y * 16 * kStep);
+        else return across_read(lds + (at ^ y * 32) + half * 32 * BQ * 2, 0, 4 * BQ * 2);
+    };
+    // an address that the compiler computes here and does not keep for all fragments from step to step
+    const auto here = [&](unsigned at) {
+        asm volatile("" : "+v"(at));
+        return at;
     };
 
     if (steps > 0) {
-        send(0);
-        arrived();
-        if (steps > 1) send(1);
-        if constexpr (kEight) {
-            u4 fp[NP][2], fq[NQ][2];
-            int cp[NP], cq[NQ];
-            for (int s = 0; s < steps; ++s) {
+        unsigned long long mask_q = mask_of(0), mask_p = mask_q;
 #pragma unroll
-                for (int y = 0; y < NQ; ++y) {
-                    fq[y][0] = read_q(s, 0, y);
-                    fq[y][1] = read_q(s, 1, y);
-                    cq[y] = (int)(scales[s & 1][BP + wq * (BQ / WQ) + y * 16 + i16] >> (8 * g));
-                }
+        for (int s = 0; s < kAhead; ++s) {
+            if (s > 0) mask_p = mask_of(s);
 #pragma unroll
-                for (int x = 0; x < NP; ++x) {
-                    fp[x][0] = read_p(s, 0, x);
-                    fp[x][1] = read_p(s, 1, x);
-                    cp[x] = (int)(scales[s & 1][wp * (BP / WP) + x * 16 + i16] >> (8 * g));
-                }
+            for (int j = 0; j < TP::kLoads; ++j) send_p(j, s, s, mask_p);
+            if (s < 2) {
+                mask_q = mask_p;
 #pragma unroll
-                for (int x = 0; x < NP; ++x)
+                for (int j = 0; j < TQ::kLoads; ++j) send_q(j, s, mask_q);
 #pragma unroll
-                    for (int y = 0; y < NQ; ++y) acc[x][y] = mfma_scaled(fq[y], fp[x], acc[x][y], cq[y], cp[x]);
-                arrived();
-                if (s + 2 < steps) send(s + 2);
-            }
-        } else {
-            u4 fp[2][NP], fq[2][NQ];
-            const auto read = [&](int s, int half) {
-#pragma unroll
-                for (int y = 0; y < NQ; ++y) fq[half][y] = read_q(s, half, y);
-#pragma unroll
-                for (int x = 0; x < NP; ++x) fp[half][x] = read_p(s, half, x);
-            };
-            const auto multiply = [&](int half) {
-#pragma unroll
-                for (int x = 0; x < NP; ++x)
-#pragma unroll
-                    for (int y = 0; y < NQ; ++y) acc[x][y] = Mfma<E>::go(fq[half][y], fp[half][x], acc[x][y]);
-                if constexpr (LP == kAcross) {
-                    if (bias_too) {
-                        const unsigned one = Elt<E>::type == LAST_BF16 ? 0x3f803f80u : 0x3c003c00u;
-#pragma unroll
-                        for (int x = 0; x < NP; ++x)
-                            if (x % WQ == wq) accb[x / WQ] = Mfma<E>::go(u4{one, one, one, one}, fp[half][x], accb[x / WQ]);
-                    }
-                }
-            };
-            read(0, 0);
-            for (int s = 0; s < steps; ++s) {
-                read(s, 1);
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(0);
-                __builtin_amdgcn_sched_barrier(0);
-                arrived();
-                if (s + 2 < steps) send(s + 2);
-                if (s + 1 < steps) read(s + 1, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(1);
-                __builtin_amdgcn_sched_barrier(0);
+                for (int j = 0; j < kScaleLoads; ++j) send_scales(j, s);
             }
         }
+        arrived<TP::kLoads * (kAhead - 1) + TQ::kLoads + kScaleLoads>();
+
+        int buf = 0;                                                      // of P, of step s
+        const auto after = [&](int b) { return b + 1 == kBuffersP ? 0 : b + 1; };
+        if constexpr (kEight) {
+            constexpr int H = NP / 2;
+            constexpr int kSends = (TP::kLoads + TQ::kLoads + kScaleLoads + H - 1) / H;
+            i8x fp[NP], fq[NQ];
+            int cp[NP], cq[NQ];
+            const auto take_p = [&](int s, int x) {
+                const unsigned at = here(at_p + (s & 1) * TP::kBytes);
+                fp[x] = join8(read_p(at, 0, x), read_p(at, 1, x));
+                cp[x] = scales[s & 1][(wp * (BP / WP) + x * 16 + i16) * 4 + g];
+            };
+            const auto take_q = [&](int s, int y) {
+                const unsigned at = here(at_q + (s & 1) * TQ::kBytes);
+                fq[y] = join8(read_q(at, 0, y), read_q(at, 1, y));
+                cq[y] = scales[s & 1][(BP + wq * (BQ / WQ) + y * 16 + i16) * 4 + g];
+            };
+#pragma unroll
+            for (int y = 0; y < NQ; ++y) take_q(0, y);
+#pragma unroll
+            for (int x = 0; x < H; ++x) take_p(0, x);
+            for (int s = 0; s < steps; ++s) {
+#pragma unroll
+                for (int x = 0; x < H; ++x) {
+                    take_p(s, H + x);
+#pragma unroll
+                    for (int y = 0; y < NQ; ++y) acc[x][y] = mfma_scaled(fq[y], fp[x], acc[x][y], cq[y], cp[x]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                arrived<0>();
+#pragma unroll
+                for (int x = 0; x < H; ++x) {
+#pragma unroll
+                    for (int j = kSends * x; j < kSends * x + kSends; ++j) {
+                        if (j < TP::kLoads) send_p(j, s + 2, s & 1, ~0ull);
+                        else if (j < TP::kLoads + TQ::kLoads) send_q(j - TP::kLoads, s + 2, ~0ull);
+                        else if (j < TP::kLoads + TQ::kLoads + kScaleLoads) send_scales(j - TP::kLoads - TQ::kLoads, s + 2);
+                    }
+                    take_p(s + 1, x);
+                    if (x + 1 < H) {
+#pragma unroll
+                        for (int y = 0; y < NQ; ++y) acc[H + x][y] = mfma_scaled(fq[y], fp[H + x], acc[H + x][y], cq[y], cp[H + x]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < NQ; ++y) {
+                    acc[NP - 1][y] = mfma_scaled(fq[y], fp[NP - 1], acc[NP - 1][y], cq[y], cp[NP - 1]);
+                    take_q(s + 1, y);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        } else {
+            u4 fp[NP], fq[2][NQ];
+            const unsigned one = Elt<E>::type == LAST_BF16 ? 0x3f803f80u : 0x3c003c00u;
+            const auto multiply = [&](int half, int x) {
+#pragma unroll
+                for (int y = 0; y < NQ; ++y) acc[x][y] = Mfma<E>::go(fq[half][y], fp[x], acc[x][y]);
+                if constexpr (LP == kAcross) {
+                    if (bias_too && x % WQ == wq) accb[x / WQ] = Mfma<E>::go(u4{one, one, one, one}, fp[x], accb[x / WQ]);
+                }
+            };
+            {
+                const unsigned ap = here(at_p), aq = here(at_q);
+#pragma unroll
+                for (int y = 0; y < NQ; ++y) fq[0][y] = read_q(aq, 0, y);
+#pragma unroll
+                for (int x = 0; x < NP; ++x) fp[x] = read_p(ap, 0, x);
+            }
+            mask_q = mask_p;                                              // of step 2
+            for (int s = 0; s < steps; ++s) {
+                {
+                    const unsigned ap = here(at_p + buf * TP::kBytes), aq = here(at_q + (s & 1) * TQ::kBytes);
+#pragma unroll
+                    for (int x = 0; x < NP; ++x) {
+                        multiply(0, x);
+                        fp[x] = read_p(ap, 1, x);
+                        if (x < NQ) fq[1][x] = read_q(aq, 1, x);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                arrived<TP::kLoads>();
+                const int next = after(buf);
+                mask_p = mask_of(s + kAhead);
+                {
+                    const unsigned ap = here(at_p + next * TP::kBytes), aq = here(at_q + (s + 1 & 1) * TQ::kBytes);
+                    constexpr int kSends = (TP::kLoads + TQ::kLoads + NP - 1) / NP;
+#pragma unroll
+                    for (int x = 0; x < NP; ++x) {
+                        multiply(1, x);
+#pragma unroll
+                        for (int j = kSends * x; j < kSends * x + kSends; ++j) {
+                            if (j < TQ::kLoads) send_q(j, s + 2, mask_q);
+                            else if (j < TQ::kLoads + TP::kLoads) send_p(j - TQ::kLoads, s + kAhead, buf, mask_p);
+                        }
+                        fp[x] = read_p(ap, 0, x);
+                        if (x < NQ) fq[0][x] = read_q(aq, 0, x);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                mask_q = mask_p;
+                buf = next;
+            }
+        }
+        arrived<0>();                                                     // the loads from nowhere, before LDS is used again
     }
 
     // A lane has row 16 x + i16 of P and columns 16 y + 4 g .. of Q.  The epilogue wants eight columns of a row in a lane and
@@ -400,8 +524,10 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
     // pieces of a row are swizzled by the row.
     constexpr int kCols = BQ / WQ, kPieces = kCols / 4, kLanes = kCols / 8, kRows = kWave / kLanes, XS = NP < 4 ? NP : 4;
     static_assert((size_t)XS * 16 * kCols * 4 * WP * WQ <= sizeof(lds), "room for the epilogue");
-    __syncthreads();
-    char* mine = &lds[0][0] + wave * (XS * 16 * kCols * 4);
+    char* mine = lds + wave * (XS * 16 * kCols * 4);
+    const int c = (lane % kLanes) * 8, n = q0 + wq * kCols + c;
+    float bias[8];
+    load_bias(a.e, n, a.Q, bias);
 #pragma unroll 1
     for (int part = 0; part < NP / XS; ++part) {
 #pragma unroll
@@ -415,18 +541,25 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();                     // (the reads follow the writes in the wavefront's order)
-        const int c = (lane % kLanes) * 8, n = q0 + wq * kCols + c;
+        const int first = p0 + wp * (BP / WP) + part * XS * 16;
+        const auto exists = [&](int m) { return m < a.P && (LP == kAcross || frame_exists(a.frames, m)); };
+        bool there = exists(first + lane / kLanes);
+        Fetched f = fetch(a.e, first + lane / kLanes, n, a.P, a.Q, there);
 #pragma unroll 1
         for (int r = lane / kLanes; r < XS * 16; r += kRows) {
-            const int m = p0 + wp * (BP / WP) + part * XS * 16 + r;
+            const int m = first + r;
+            const bool there_next = r + kRows < XS * 16 && exists(m + kRows);
+            const Fetched f_next = fetch(a.e, m + kRows, n, a.P, a.Q, there_next);
             const f4 lo = *(const f4*)(mine + r * (kCols * 4) + (((c / 4) ^ (r & (kPieces - 1))) << 4));
             const f4 hi = *(const f4*)(mine + r * (kCols * 4) + (((c / 4 + 1) ^ (r & (kPieces - 1))) << 4));
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             if (a.e.part) {
                 if (m < a.P) store8<float>(a.e.part, ((size_t)blockIdx.y * a.P + m) * a.Q + n, a.Q - n, (a.Q & 3) == 0, v);
             } else {
-                finish(a.e, m, n, a.P, a.Q, m < a.P && (LP == kAcross || frame_exists(a.frames, m)), v);
+                finish(a.e, m, n, a.P, a.Q, there, bias, f, v);
             }
+            f = f_next;
+            there = there_next;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -506,7 +639,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
 #pragma unroll
                 for (int f = 0; f < QF; ++f) {
                     if constexpr (kEight) {
-                        acc[t][f] = mfma_scaled(fq[d][f], fp[d][t], acc[t][f], cq[d][f], cp[d][t]);
+                        acc[t][f] = mfma_scaled(join8(fq[d][f][0], fq[d][f][1]), join8(fp[d][t][0], fp[d][t][1]), acc[t][f], cq[d][f], cp[d][t]);
                     } else {
                         acc[t][f] = Mfma<E>::go(fq[d][f][0], fp[d][t][0], acc[t][f]);
                         acc[t][f] = Mfma<E>::go(fq[d][f][1], fp[d][t][1], acc[t][f]);
@@ -532,8 +665,11 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
             for (int i = 0; i < 4; ++i) v[4 * h + i] = t[i];
         }
     }
-    const int P = c < 2 * QF ? a.P : 0;
-    finish(a.e, m, q0 + 8 * c, P, a.Q, m < P && frame_exists(a.frames, m), v);
+    const int P = c < 2 * QF ? a.P : 0, n = q0 + 8 * c;
+    const bool there = m < P && frame_exists(a.frames, m);
+    float bias[8];
+    load_bias(a.e, n, a.Q, bias);
+    finish(a.e, m, n, P, a.Q, there, bias, fetch(a.e, m, n, P, a.Q, there), v);
 }
 
 // ---- shares of a reduction joined, in order, with the epilogue; a wavefront has 16 rows of 32 columns
@@ -557,7 +693,10 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
             a.e.sum_bias[m] = b;
         }
     }
-    finish(a.e, m, n, a.P, a.Q, m < a.P && frame_exists(a.frames, m), v);
+    const bool there = m < a.P && frame_exists(a.frames, m);
+    float bias[8];
+    load_bias(a.e, n, a.Q, bias);
+    finish(a.e, m, n, a.P, a.Q, there, bias, fetch(a.e, m, n, a.P, a.Q, there), v);
 }
 
 // ---- rows of `bytes` bytes laid out at multiples of 16 with zeros behind them, 16 bytes a thread
