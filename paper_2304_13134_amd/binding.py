@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -118,7 +119,7 @@ def load_library():
     lib.last_set_option.argtypes = [i32, i32]
     lib.last_get_option.restype = i32
     lib.last_get_option.argtypes = [i32]
-    f32, fr, mx = ctypes.c_float, ctypes.POINTER(LastFrames), ctypes.POINTER(LastMatrix)
+    f32, fr, mx = ctypes.c_float, vp, vp      # (the structs of a layer's call are packed, see _matrix)
     for name, arguments in (
             ("last_residual_norm", [fr, i32, mx, mx, vp, f32, mx, mx, mx, vp, vp]),
             ("last_residual_norm_grad", [fr, i32, mx, mx, vp, vp, mx, mx, vp, vp, sz, vp]),
@@ -495,6 +496,11 @@ class Norm(tuple):
     kept = property(lambda self: self[3])
 
 
+# LastMatrix and LastFrames as bytes: a third of the time of a ctypes structure, on calls that take a few microseconds
+_pack_matrix = struct.Struct("@PiqPq").pack
+_pack_frames = struct.Struct("@iiP").pack
+
+
 def _pitch(t, name):
     """Elements from a row of t [R, H] or [B, T, H] to the next: the columns are contiguous, the rows evenly spaced."""
     shape, strides = t.shape, t.stride()
@@ -513,21 +519,23 @@ def _pitch(t, name):
 
 
 def _matrix(t, name, rows=None, columns=None):
-    """LastMatrix of a device tensor or a Kept, whose shape is checked against `rows` (leading sizes) and `columns`."""
+    """The packed LastMatrix of a device tensor or a Kept, whose shape is checked against `rows` (leading sizes) and `columns`."""
     codes, scales = t if isinstance(t, Kept) else (t, None)
-    if not isinstance(codes, torch.Tensor) or not codes.is_cuda or codes.dtype not in _TYPES:
+    type_ = _TYPES.get(codes.dtype) if isinstance(codes, torch.Tensor) else None
+    if type_ is None or not codes.is_cuda:
         raise TypeError("%s must be a device tensor of a supported type" % name)
-    if (codes.dtype in _EIGHT) != (scales is not None):
+    if (type_ >= 3) != (scales is not None):
         raise TypeError("%s: values in 8 bits are a Kept of codes and scales" % name)
     shape = codes.shape
     if (rows is not None and shape[:-1] != rows) or (columns is not None and shape[-1] != columns):
         raise ValueError("%s has shape %s: expected %s" % (name, tuple(shape), (*(rows or ("...",)), columns)))
+    pitch = shape[-1] if len(shape) in (2, 3) and codes.is_contiguous() else _pitch(codes, name)
     if scales is None:
-        return LastMatrix(codes.data_ptr(), _TYPES[codes.dtype], _pitch(codes, name), None, 0)
+        return _pack_matrix(codes.data_ptr(), type_, pitch, 0, 0)
     if not isinstance(scales, torch.Tensor) or not scales.is_cuda or scales.dtype != torch.uint8 \
             or scales.shape != (*shape[:-1], (shape[-1] + 31) // 32):
         raise TypeError("the scales of %s must be device uint8 [..., ceil(columns / 32)]" % name)
-    return LastMatrix(codes.data_ptr(), _TYPES[codes.dtype], _pitch(codes, name), scales.data_ptr(), _pitch(scales, name))
+    return _pack_matrix(codes.data_ptr(), type_, pitch, scales.data_ptr(), _pitch(scales, name))
 
 
 def _opt(t, name, rows, columns):
@@ -544,17 +552,17 @@ def _vector(t, n, name):
 
 
 def _frames(t, lengths, name):
-    """(LastFrames, leading sizes) of a tensor or Kept [R, H] or [B, T, H]; with lengths it is the latter."""
+    """(packed LastFrames, leading sizes, tensor) of a tensor or Kept [R, H] or [B, T, H]; with lengths it is the latter."""
     t = t[0] if isinstance(t, Kept) else t
     if not isinstance(t, torch.Tensor) or t.dim() not in (2, 3):
         raise TypeError("%s must be a device tensor [rows, columns] or [B, T, columns]" % name)
+    rows = t.shape[:-1]
     if lengths is None:
-        rows = t.shape[0] if t.dim() == 2 else t.shape[0] * t.shape[1]
-        return LastFrames(1, rows, None), t.shape[:-1]
+        return _pack_frames(1, rows[0] if len(rows) == 1 else rows[0] * rows[1], 0), rows, t
     _dev_tensor(lengths, torch.int32, "lengths")
-    if t.dim() != 3 or lengths.shape != t.shape[:1]:
+    if len(rows) != 2 or lengths.shape != rows[:1]:
         raise ValueError("with lengths [B], %s must be [B, T, columns]" % name)
-    return LastFrames(t.shape[0], t.shape[1], lengths.data_ptr()), t.shape[:-1]
+    return _pack_frames(rows[0], rows[1], lengths.data_ptr()), rows, t
 
 
 def _activation(name):
@@ -564,14 +572,30 @@ def _activation(name):
 
 
 def _result(shape, dtype, device):
-    return Kept.empty(shape, dtype, device) if dtype in _EIGHT else torch.empty(shape, dtype=dtype, device=device)
+    """(a new tensor or Kept, its packed LastMatrix)"""
+    if dtype in _EIGHT:
+        t = Kept.empty(shape, dtype, device)
+        return t, _matrix(t, "result")
+    if dtype not in _TYPES:
+        raise TypeError("results are float32, bfloat16, float16 or in 8 bits: not %s" % dtype)
+    t = torch.empty(shape, dtype=dtype, device=device)
+    return t, _pack_matrix(t.data_ptr(), _TYPES[dtype], shape[-1], 0, 0)
 
 
-def _layer_scratch(op, frames, N, K, a, b, device):
+def _stream_of(t):
+    """The current stream of the tensor's device."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
+def _layer_scratch(op, frames, N, K, a, b, t, stream):
+    """(address, bytes) of a scratch buffer for a call on tensor t's device and stream"""
     nbytes = load_library().last_layer_workspace_bytes(op, frames, N, K, a, b)
     if nbytes == 0:
         raise LastError(6, "combination not supported")
-    return workspace(nbytes, device)
+    buf = _workspaces.get((t.get_device(), stream))
+    if buf is None or buf.numel() < nbytes:
+        buf = workspace(nbytes, t.device)
+    return buf.data_ptr(), buf.numel()
 
 
 def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=None, keep=None):
@@ -579,16 +603,20 @@ def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=Non
     x), s (None without a residual, where it is x), inv [rows] float32 for the gradient, and, with `keep` torch.int8 or
     torch.float8_e4m3fn, y in 8 bits as a Kept.  With `keep` and no `dtype`, y itself is None.  x: [rows, H], or [B, T, H] with
     lengths [B] of which the frames past the end are zeros in every result."""
-    lib = load_library()
-    fr, rows = _frames(x, lengths, "x")
-    H = x.shape[-1]
+    fr, rows, _ = _frames(x, lengths, "x")
+    shape, device = x.shape, x.device
+    H = shape[-1]
     mx, mr = _matrix(x, "x"), _opt(residual, "residual", rows, H)
-    s = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    y = None if keep is not None and dtype is None else torch.empty(x.shape, dtype=dtype or x.dtype, device=x.device)
-    kept = None if keep is None else _result(x.shape, keep, x.device)
-    inv = torch.empty(rows, dtype=torch.float32, device=x.device)
-    _check(lib.last_residual_norm(fr, H, mx, mr, _vector(gain, H, "gain"), eps, _opt(s, "s", rows, H), _opt(y, "y", rows, H),
-                                  _opt(kept, "keep", rows, H), inv.data_ptr(), _stream()))
+    s = y = kept = ms = my = mk = None
+    if residual is not None:
+        s, ms = _result(shape, x.dtype, device)
+    if keep is None or dtype is not None:
+        y, my = _result(shape, dtype or x.dtype, device)
+    if keep is not None:
+        kept, mk = _result(shape, keep, device)
+    inv = torch.empty(rows, dtype=torch.float32, device=device)
+    _check(load_library().last_residual_norm(fr, H, mx, mr, _vector(gain, H, "gain"), eps, ms, my, mk, inv.data_ptr(),
+                                             _stream_of(x)))
     return Norm(y, s, inv, kept)
 
 
@@ -596,17 +624,18 @@ def last_residual_norm_grad(dy, s, gain, inv, ds=None, lengths=None, dtype=None)
     """(dx, dgain): the gradient of x and of the residual alike, of `dtype` (default: that of ds, or of s, or, s being a
     Kept, of dy), and dgain [H] float32.  s and inv as last_residual_norm returned them, s maybe in 8 bits (a Kept); ds:
     the gradient that reaches s by other ways."""
-    lib = load_library()
-    fr, rows = _frames(dy, lengths, "dy")
+    fr, rows, _ = _frames(dy, lengths, "dy")
     H, device = dy.shape[-1], dy.device
     if dtype is None:
         dtype = ds.dtype if ds is not None else dy.dtype if isinstance(s, Kept) else s.dtype
-    dx = torch.empty(dy.shape, dtype=dtype, device=device)
+    mdy, ms, mds = _matrix(dy, "dy"), _matrix(s, "s", rows, H), _opt(ds, "ds", rows, H)
+    dx, mdx = _result(dy.shape, dtype, device)
     dgain = torch.empty(H, dtype=torch.float32, device=device)
-    m = [_matrix(dy, "dy"), _matrix(s, "s", rows, H), _opt(ds, "ds", rows, H), _matrix(dx, "dx")]
-    ws = _layer_scratch(OP_RESIDUAL_NORM_GRAD, fr, 1, H, None, None, device)
-    _check(lib.last_residual_norm_grad(fr, H, m[0], m[1], _vector(gain, H, "gain"), _vector(inv, fr.B * fr.T, "inv"), m[2], m[3],
-                                       dgain.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
+    stream = _stream_of(dy)
+    ws, nbytes = _layer_scratch(OP_RESIDUAL_NORM_GRAD, fr, 1, H, None, None, dy, stream)
+    _check(load_library().last_residual_norm_grad(fr, H, mdy, ms, _vector(gain, H, "gain"),
+                                                  _vector(inv, dy.numel() // H, "inv"), mds, mdx, dgain.data_ptr(), ws, nbytes,
+                                                  stream))
     return dx, dgain
 
 
@@ -614,74 +643,71 @@ def last_product(x, w, bias=None, activation="none", residual=None, lengths=None
     """(y, kept): y = act(x w^T + bias) + residual, w [N, K], x [rows, K] or [B, T, K]: both bfloat16, float16, or both a Kept
     of float8_e4m3fn.  `dtype` of y: default that of x (bfloat16 for a Kept); torch.int8 or torch.float8_e4m3fn make it a Kept.
     `keep`: such a type to keep what the activation is applied to in (kept, a Kept), or None."""
-    lib = load_library()
-    fr, rows = _frames(x, lengths, "x")
+    fr, rows, t = _frames(x, lengths, "x")
     N, K = (w[0] if isinstance(w, Kept) else w).shape
     mx, mw = _matrix(x, "x", rows, K), _matrix(w, "w", (N,), K)
-    device = x[0].device
-    if dtype is None:
-        dtype = torch.bfloat16 if isinstance(x, Kept) else x.dtype
-    y = _result((*rows, N), dtype, device)
-    kept = None if keep is None else _result((*rows, N), keep, device)
-    ws = _layer_scratch(OP_PRODUCT, fr, N, K, mx, mw, device)
-    _check(lib.last_product(fr, N, K, mx, mw, _vector(bias, N, "bias"), _activation(activation),
-                            _opt(residual, "residual", rows, N), _matrix(y, "y"), _opt(kept, "keep", rows, N),
-                            ws.data_ptr(), ws.numel(), _stream()))
+    shape, device, kept, mk = (*rows, N), t.device, None, None
+    y, my = _result(shape, dtype or (torch.bfloat16 if isinstance(x, Kept) else x.dtype), device)
+    if keep is not None:
+        kept, mk = _result(shape, keep, device)
+    stream = _stream_of(t)
+    ws, nbytes = _layer_scratch(OP_PRODUCT, fr, N, K, mx, mw, t, stream)
+    _check(load_library().last_product(fr, N, K, mx, mw, _vector(bias, N, "bias"), _activation(activation),
+                                       _opt(residual, "residual", rows, N), my, mk, ws, nbytes, stream))
     return y, kept
 
 
 def last_product_grad_input(dy, w, kept=None, activation="none", lengths=None, dtype=None):
     """dx = (dy w) * act'(kept), of `dtype` (default: that of dy): the gradient of a product's input and, with `kept` [.., K],
     through the activation that made this input of what was kept."""
-    lib = load_library()
-    fr, rows = _frames(dy, lengths, "dy")
+    fr, rows, _ = _frames(dy, lengths, "dy")
     N, K = w.shape
     mdy, mw, mk = _matrix(dy, "dy", rows, N), _matrix(w, "w", (N,), K), _opt(kept, "kept", rows, K)
-    dx = torch.empty((*rows, K), dtype=dtype or dy.dtype, device=dy.device)
-    ws = _layer_scratch(OP_PRODUCT_GRAD_INPUT, fr, N, K, mdy, mw, dy.device)
-    _check(lib.last_product_grad_input(fr, N, K, mdy, mw, mk, _activation(activation), _matrix(dx, "dx"), ws.data_ptr(),
-                                       ws.numel(), _stream()))
+    dx, mdx = _result((*rows, K), dtype or dy.dtype, dy.device)
+    stream = _stream_of(dy)
+    ws, nbytes = _layer_scratch(OP_PRODUCT_GRAD_INPUT, fr, N, K, mdy, mw, dy, stream)
+    _check(load_library().last_product_grad_input(fr, N, K, mdy, mw, mk, _activation(activation), mdx, ws, nbytes, stream))
     return dx
 
 
 def last_product_grad_weight(dy, x, activation="none", lengths=None, dtype=torch.float32):
     """(dw [N, K] of `dtype`, dbias [N] float32): dy^T act(x) and the column sums of dy.  x: of dy's type (activation "none"),
     or a Kept, whose activation is formed again."""
-    lib = load_library()
-    fr, rows = _frames(dy, lengths, "dy")
+    fr, rows, _ = _frames(dy, lengths, "dy")
     N, K, device = dy.shape[-1], (x[0] if isinstance(x, Kept) else x).shape[-1], dy.device
     mdy, mx = _matrix(dy, "dy"), _matrix(x, "x", rows, K)
-    dw = torch.empty((N, K), dtype=dtype, device=device)
+    dw, mdw = _result((N, K), dtype, device)
     dbias = torch.empty(N, dtype=torch.float32, device=device)
-    ws = _layer_scratch(OP_PRODUCT_GRAD_WEIGHT, fr, N, K, mdy, mx, device)
-    _check(lib.last_product_grad_weight(fr, N, K, mdy, mx, _activation(activation), _matrix(dw, "dw"), dbias.data_ptr(),
-                                        ws.data_ptr(), ws.numel(), _stream()))
+    stream = _stream_of(dy)
+    ws, nbytes = _layer_scratch(OP_PRODUCT_GRAD_WEIGHT, fr, N, K, mdy, mx, dy, stream)
+    _check(load_library().last_product_grad_weight(fr, N, K, mdy, mx, _activation(activation), mdw, dbias.data_ptr(), ws,
+                                                   nbytes, stream))
     return dw, dbias
 
 
 def last_keep(x, dtype=torch.int8, lengths=None):
     """x in 8 bits: a Kept of torch.int8 or torch.float8_e4m3fn codes."""
-    fr, rows = _frames(x, lengths, "x")
+    fr, _, _ = _frames(x, lengths, "x")
     mx = _matrix(x, "x")
-    kept = _result(x.shape, dtype, x.device)
-    _check(load_library().last_keep(fr, x.shape[-1], mx, _matrix(kept, "kept"), _stream()))
+    kept, mk = _result(x.shape, dtype, x.device)
+    _check(load_library().last_keep(fr, x.shape[-1], mx, mk, _stream_of(x)))
     return kept
 
 
 def last_kept_values(kept, activation="none", lengths=None, dtype=torch.bfloat16):
     """act(kept): what the codes stand for, or the activation formed again from them."""
-    fr, rows = _frames(kept, lengths, "kept")
+    fr, _, t = _frames(kept, lengths, "kept")
     mk = _matrix(kept, "kept")
-    y = torch.empty(kept[0].shape, dtype=dtype, device=kept[0].device)
-    _check(load_library().last_kept_values(fr, y.shape[-1], mk, _activation(activation), _matrix(y, "y"), _stream()))
+    y, my = _result(t.shape, dtype, t.device)
+    _check(load_library().last_kept_values(fr, t.shape[-1], mk, _activation(activation), my, _stream_of(t)))
     return y
 
 
 def last_kept_grad(dy, kept, activation, lengths=None, dtype=None):
     """dy * act'(kept), of `dtype` (default: that of dy): the gradient of an activation alone."""
-    fr, rows = _frames(dy, lengths, "dy")
+    fr, rows, _ = _frames(dy, lengths, "dy")
     H = dy.shape[-1]
     mdy, mk = _matrix(dy, "dy"), _matrix(kept, "kept", rows, H)
-    dx = torch.empty(dy.shape, dtype=dtype or dy.dtype, device=dy.device)
-    _check(load_library().last_kept_grad(fr, H, mdy, mk, _activation(activation), _matrix(dx, "dx"), _stream()))
+    dx, mdx = _result(dy.shape, dtype or dy.dtype, dy.device)
+    _check(load_library().last_kept_grad(fr, H, mdy, mk, _activation(activation), mdx, _stream_of(dy)))
     return dx

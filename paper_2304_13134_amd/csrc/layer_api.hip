@@ -138,7 +138,7 @@ void launch_norm_grad_on(int s, const NormGradArgs& a, int groups, hipStream_t s
 // ---------------------------------------------------------------- products
 
 struct ProductPlan {
-    int variant;                     // 0: few rows, 1: tiles of 128, 2: tiles of 256
+    int variant;                     // 0: few rows, 1: tiles of 64, 2: of 128, 3: of 256
     int splits;
     long long share;                 // of the reduction, in bytes (kAlong) or rows
 };
@@ -149,15 +149,15 @@ ProductPlan plan_product(bool forward, long long P, long long Q, long long steps
     ProductPlan best{0, 1, 0};
     if (forward && P <= 64) return best;
     double least = 1e30;
-    for (int variant = 1; variant <= 2; ++variant) {
-        const long long tile = variant == 2 ? 256 : 128;
+    for (int variant = 2; variant <= 3; ++variant) {
+        const long long tile = variant == 3 ? 256 : 128;
         const long long tiles = ((P + tile - 1) / tile) * ((Q + tile - 1) / tile);
         for (int splits = 1; splits <= 64; splits *= 2) {
             const long long part = (steps + splits - 1) / splits;
             if (splits > 1 && (part < 8 || (steps + part - 1) / part != splits)) continue;
             const long long blocks = tiles * splits;
             double us;
-            if (variant == 2) us = (double)((blocks + 255) / 256) * (part * 1.1 + 6);
+            if (variant == 3) us = (double)((blocks + 255) / 256) * (part * 1.1 + 6);
             else us = (double)((blocks + 511) / 512) * (part * (blocks <= 256 ? 0.4 : 0.7) + 4);
             if (splits > 1) us += 4 + (double)splits * P * Q * 8 / 4e6;
             if (us < least) {
@@ -172,20 +172,21 @@ ProductPlan plan_product(bool forward, long long P, long long Q, long long steps
 template <typename E, int LP, int LQ>
 void launch_tiles(ProductArgs a, const ProductPlan& p, hipStream_t st)
 {
-    const int tile = p.variant == 2 ? 256 : 128;
+    const int tile = 32 << p.variant;
     a.tiles_p = (a.P + tile - 1) / tile;
     a.tiles_q = (a.Q + tile - 1) / tile;
     const dim3 grid((unsigned)(a.tiles_p * a.tiles_q), (unsigned)p.splits);
     const ProductArgs j = a;
     if (p.splits > 1) {                              // the epilogue comes with the joining
-        a.e.res = nullptr;
-        a.e.kept_act = LAST_ACT_NONE;
+        Epilogue none{};
+        none.part = a.e.part;
+        none.part_bias = a.e.part_bias;
+        a.e = none;
     }
-#ifndef BIGW
-#define BIGW 4
-#endif
-    if (p.variant == 2) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 256, 256, 2, BIGW>), grid, dim3(128 * BIGW), 0, st, a);
-    else hipLaunchKernelGGL((product_kernel<E, LP, LQ, 128, 128, 2, 2>), grid, dim3(256), 0, st, a);
+    constexpr bool kEight = Elt<E>::size == 1;
+    if (p.variant == 3) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 256, 256, 2, 4, kEight ? 2 : 3, 2>), grid, dim3(512), 0, st, a);
+    else if (p.variant == 2) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 128, 128, 2, 2, kEight ? 2 : 3, 2>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((product_kernel<E, LP, LQ, 64, 64, 2, 2, 4, 4>), grid, dim3(256), 0, st, a);
     if (p.splits > 1) {
         const long long waves = (long long)((a.P + 15) / 16) * ((a.Q + 31) / 32);
         hipLaunchKernelGGL(product_join_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, j, p.splits);

@@ -67,7 +67,11 @@ struct ProductArgs {
 };
 
 __device__ __forceinline__ int along_swizzle(int r) { return (r >> 1) & 7; }
-__device__ __forceinline__ int across_swizzle(int r) { return (r & 3) | ((r >> 3) & 1) << 2; }
+template <int ROWS>
+__device__ __forceinline__ int across_swizzle(int r)         // (rows of 64 columns have four granules only)
+{
+    return ((r & 3) | ((r >> 3) & 1) << 2) & (ROWS / 16 - 1);
+}
 
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base)
@@ -75,19 +79,24 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base)
     return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00020000);
 }
 
-// 64 lanes' 16 (4) bytes at offset `o` of the buffer at `base` to LDS from `to` on.  In assembly, since the compiler makes every
-// later read of LDS wait for its own form of this; whoever reads waits with arrived().
-template <int BYTES>
-__device__ __forceinline__ void to_lds(const void* base, unsigned o, const void* to)
+// a buffer's descriptor for the assembly below; base + offsets stay below 2^31, kNowhere is out of range whatever is added
+__device__ __forceinline__ u4 descriptor(const void* base)
 {
     const uint64_t p = (uint64_t)base;
-    const u4 b = {(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)p), (unsigned)__builtin_amdgcn_readfirstlane((int)(p >> 32)) & 0xffffu,
-                  0x7fffffffu, 0x00020000u};
-    const unsigned m = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(uintptr_t)(lds_t)to);
+    return u4{(unsigned)p, (unsigned)(p >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+}
+
+__device__ __forceinline__ unsigned lds_byte(const void* p) { return (unsigned)(uintptr_t)(lds_t)p; }
+
+// 64 lanes' 16 (4) bytes at offset o + more of the buffer to LDS from byte `to` on.  In assembly, since the compiler makes every
+// later read of LDS wait for its own form of this; whoever reads waits with arrived().
+template <int BYTES>
+__device__ __forceinline__ void to_lds(u4 b, unsigned o, unsigned more, unsigned to)
+{
     if constexpr (BYTES == 16)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m), "v"(o), "s"(b) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(o), "s"(b), "s"(more) : "memory");
     else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(m), "v"(o), "s"(b) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(o), "s"(b), "s"(more) : "memory");
 }
 
 // what this wavefront asked from LDS has come, and what it sent there but for the last LATER loads; then the same of the whole
@@ -106,10 +115,12 @@ struct Tile {
     static constexpr int kPieces = L == kAlong ? 8 : ROWS / 8;           // 16-byte pieces of a row in LDS
     static constexpr int kApart = THREADS / kPieces;
     static_assert(kBytes % (16 * THREADS) == 0, "whole loads");
-    static_assert(L == kAlong || ROWS >= 128, "eight granules to swizzle");
+    static_assert(L == kAlong || ROWS >= 64, "granules to swizzle");
     static_assert(kApart % 16 == 0, "the same swizzle for all loads of a thread");
     unsigned off;                                                        // of the first load, from the tile's first byte
     unsigned valid;                                                      // kAlong: bits of the loads whose row exists
+    unsigned apart;                                                      // bytes from a load to the next
+    unsigned wave_at;                                                    // of the wavefront's part of a load in LDS
     int row, piece;                                                      // of the first load
 
     // first: first row or column of the tile; count: how many the matrix has
@@ -118,6 +129,8 @@ struct Tile {
         row = (int)threadIdx.x / kPieces;
         const int c = (int)threadIdx.x % kPieces;
         valid = 0;
+        apart = (unsigned)(kApart * pitch);
+        wave_at = (unsigned)__builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) * kWave * 16;
         if constexpr (L == kAlong) {
             piece = c ^ along_swizzle(row);
             off = (unsigned)(row * pitch) + 16u * (unsigned)piece;
@@ -127,18 +140,30 @@ struct Tile {
                 if (r < count && (!frames || frame_exists(*frames, r))) valid |= 1u << j;
             }
         } else {
-            const int col = ((c >> 1) ^ across_swizzle(row)) * 16 + (c & 1) * 8;
+            const int col = ((c >> 1) ^ across_swizzle<ROWS>(row)) * 16 + (c & 1) * 8;
             off = first + col < count ? (unsigned)(row * pitch) + 2u * (unsigned)col : kNowhere;
         }
     }
 
-    // load j of the tile's 128 bytes or 64 rows from `base` on.  left: how many bytes the reduction still has (kAlong),
-    // mask: which rows exist (kAcross)
-    __device__ __forceinline__ void load(int j, const char* base, long long pitch, long long left, unsigned long long mask, char* lds) const
+    // bits of a step's loads that read what exists.  left: how many bytes the reduction still has (kAlong), mask: which rows
+    // exist (kAcross)
+    __device__ __forceinline__ unsigned bits(long long left, unsigned long long mask) const
     {
-        char* to = lds + (j * THREADS + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) * kWave) * 16;
-        const bool in = L == kAlong ? (valid >> j & 1) != 0 && 16 * piece < left : (mask >> (row + j * kApart) & 1) != 0;
-        to_lds<16>(base + (long long)(j * kApart) * pitch, in ? off : kNowhere, to);
+        if constexpr (L == kAlong) {
+            return left >= kStep || 16 * piece < left ? valid : 0u;
+        } else {
+            if (mask == ~0ull) return (1u << kLoads) - 1;
+            unsigned b = 0;
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) b |= (unsigned)(mask >> (row + j * kApart) & 1) << j;
+            return b;
+        }
+    }
+
+    // load j of the tile's 128 bytes or 64 rows from the buffer's base on, to LDS byte `to`
+    __device__ __forceinline__ void load(int j, u4 buffer, unsigned bits, unsigned to) const
+    {
+        to_lds<16>(buffer, bits >> j & 1 ? off : kNowhere, j * apart, to + wave_at + j * THREADS * 16);
     }
 };
 
@@ -270,6 +295,117 @@ __device__ __forceinline__ void load_bias(const Epilogue& e, int n, int Q, float
     load8<float>(e.bias, n, e.bias ? Q - n : 0, e.wide_bias, b);
 }
 
+// Rows of results that are all inside and aligned, the common case, in a loop without a branch around a load or a store, so that
+// no store is waited for (they count with the loads, in order): an extra load is two rows ahead of its use.
+enum { kRowsPlain = 0, kRowsResidual = 1, kRowsSlope = 2, kRowsKeep = 3, kRowsWide = 4, kRowsEight = 5, kRowsAny = 6 };
+
+__device__ __forceinline__ int rows_kind(const Epilogue& e)
+{
+    if (e.out.q) return !e.res && !e.kept.q && e.out.aligned ? kRowsEight : kRowsAny;
+    if (!e.wide) return kRowsAny;
+    if (e.type == LAST_F32) return !e.res && !e.kept.q ? kRowsWide : kRowsAny;
+    if (e.kept_act != LAST_ACT_NONE) return e.kept.aligned ? kRowsSlope : kRowsAny;
+    if (e.res) return e.wide_res && !e.kept.q ? kRowsResidual : kRowsAny;
+    if (e.kept.q) return e.kept.aligned ? kRowsKeep : kRowsAny;
+    return kRowsPlain;
+}
+
+__device__ __forceinline__ void unpack8(int type, u4 w, float* r)
+{
+    if (type == LAST_BF16) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) { r[2 * u] = bf16_to_float(w[u] & 0xffffu); r[2 * u + 1] = __uint_as_float(w[u] & 0xffff0000u); }
+    } else {
+        const h8 h = __builtin_bit_cast(h8, w);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) r[u] = (float)h[u];
+    }
+}
+
+__device__ __forceinline__ u4 pack8(int type, const float* v)
+{
+    if (type == LAST_BF16) return u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+    return u4{f16_pair(v[0], v[1]), f16_pair(v[2], v[3]), f16_pair(v[4], v[5]), f16_pair(v[6], v[7])};
+}
+
+__device__ __forceinline__ unsigned encode_block(bool e4m3, const float* v, unsigned* lo, unsigned* hi)
+{
+    const unsigned top = quad_max(top8(v));
+    const unsigned byte = e4m3 ? scale_byte<true>(top) : scale_byte<false>(top);
+    *lo = e4m3 ? encode4<true>(v, byte) : encode4<false>(v, byte);
+    *hi = e4m3 ? encode4<true>(v + 4, byte) : encode4<false>(v + 4, byte);
+    return byte;
+}
+
+// m: this lane's first row, every `step`-th of which it has, `count` in all; n: its columns.  get(i, v): the sums of its i-th row.
+template <int KIND, typename Get>
+__device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, int step, int count, const float* bias, Get get)
+{
+    const auto at = [&](int i) { return m + (size_t)(i < count ? i : count - 1) * step; };
+    struct Extra {
+        u4 w;
+        unsigned scale;
+    };
+    const auto extra = [&](int i) {
+        Extra x{};
+        if constexpr (KIND == kRowsResidual) x.w = *(const u4*)((const uint16_t*)e.res + at(i) * e.pres + n);
+        if constexpr (KIND == kRowsSlope) {
+            const u2 q = *(const u2*)(e.kept.q + at(i) * e.kept.pitch + n);
+            x.w[0] = q[0];
+            x.w[1] = q[1];
+            x.scale = e.kept.scales[at(i) * e.kept.scale_pitch + n / kBlock];
+        }
+        return x;
+    };
+    Extra x0 = extra(0), x1 = extra(1);
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+        const Extra x = x0;
+        x0 = x1;
+        x1 = extra(i + 2);
+        const size_t row = m + (size_t)i * step;
+        float v[8];
+        get(i, v);
+        if constexpr (KIND == kRowsSlope) {
+            float h[8];
+            const float sc = scale_value(x.scale);
+            if (e.kept.e4m3) {
+                decode4<true>(x.w[0], sc, h);
+                decode4<true>(x.w[1], sc, h + 4);
+            } else {
+                decode4<false>(x.w[0], sc, h);
+                decode4<false>(x.w[1], sc, h + 4);
+            }
+            times_slope(e.kept_act, h, v);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] += bias[u];
+        if constexpr (KIND == kRowsKeep) {
+            unsigned lo, hi;
+            const unsigned byte = encode_block(e.kept.e4m3, v, &lo, &hi);
+            *(u2*)(e.kept.q + row * e.kept.pitch + n) = u2{lo, hi};
+            e.kept.scales[row * e.kept.scale_pitch + n / kBlock] = (uint8_t)byte;    // (all four lanes of the block, the same)
+        }
+        activate8(e.act, v);
+        if constexpr (KIND == kRowsResidual) {
+            float r[8];
+            unpack8(e.type, x.w, r);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] += r[u];
+        }
+        if constexpr (KIND == kRowsEight) {
+            unsigned lo, hi;
+            const unsigned byte = encode_block(e.out.e4m3, v, &lo, &hi);
+            *(u2*)(e.out.q + row * e.out.pitch + n) = u2{lo, hi};
+            e.out.scales[row * e.out.scale_pitch + n / kBlock] = (uint8_t)byte;
+        } else if constexpr (KIND == kRowsWide) {
+            Elt<float>::put8(e.y, row * e.py + n, v);
+        } else {
+            *(u4*)((uint16_t*)e.y + row * e.py + n) = pack8(e.type, v);
+        }
+    }
+}
+
 // tiles in the order of the workgroups: workgroups i = j (mod 8) share an XCD and its L2, so each XCD gets a stretch of
 // the tiles; within it, columns of eight tiles
 __device__ __forceinline__ void tile_of(int id, int n, int tiles_p, int tiles_q, int* tp, int* tq)
@@ -286,21 +422,21 @@ __device__ __forceinline__ void tile_of(int id, int n, int tiles_p, int tiles_q,
 // instruction takes 128 values at once, the halves of the rows of P.  A fragment of the next phase is read from LDS into the
 // registers of one that was just used, so that the matrix cores wait for LDS as little as there are few registers for copies.
 // One barrier a step, between the phases: all fragments of the step have then been read, its buffers are free, and the loads
-// that fill them are sent one by one between the matrix instructions of the second phase.  Q has two buffers and a step's time
-// to arrive; P, which comes from farther (each row is read by the few tiles beside it, W by all below), has three and two
-// steps' time: 160 KiB with tiles of 256, of 128 two workgroups' worth.  8-bit operands leave room for two of P, beside their scales.
-template <typename E, int LP, int LQ, int BP, int BQ, int WP, int WQ>
-__global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
+// that fill them are sent one by one between the matrix instructions of the second phase, SP steps of P and SQ of Q ahead of
+// their use.
+template <typename E, int LP, int LQ, int BP, int BQ, int WP, int WQ, int SP, int SQ>
+__global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs a)
 {
     constexpr int kThreads = WP * WQ * kWave;
     constexpr bool kEight = Elt<E>::size == 1;
     constexpr int NP = BP / WP / 16, NQ = BQ / WQ / 16;                   // accumulators of a wavefront
     using TP = Tile<LP, BP, kThreads>;
     using TQ = Tile<LQ, BQ, kThreads>;
-    constexpr int kBuffersP = kEight ? 2 : 3, kAhead = kBuffersP;         // P is sent so many steps ahead of its use
-    constexpr unsigned kAtQ = kBuffersP * TP::kBytes, kLds = kAtQ + 2 * TQ::kBytes;
+    constexpr unsigned kAtQ = SP * TP::kBytes, kLds = kAtQ + SQ * TQ::kBytes;
+    constexpr int kScaleRows = (BP + BQ + kThreads - 1) / kThreads * kThreads, kScaleLoads = kEight ? kScaleRows / kThreads : 0;
+    static_assert(SQ >= 2 && (SP == SQ || (SP == SQ + 1 && !kEight)), "the order of the loads");
     __shared__ __align__(1024) char lds[kLds];
-    __shared__ __align__(4) uint8_t scales[kEight ? 2 : 1][kEight ? (BP + BQ) * 4 : 1];
+    __shared__ __align__(4) uint8_t scales[kEight ? SQ : 1][kEight ? kScaleRows * 4 : 1];
 
     const int lane = (int)threadIdx.x % kWave, g = lane >> 4, i16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wp = wave / WQ, wq = wave % WQ;
@@ -326,10 +462,12 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
     const int steps = work ? (int)((k1 - k0 + (LP == kAlong ? kStep : 64) - 1) / (LP == kAlong ? kStep : 64)) : 0;
 
     f4 acc[NP][NQ];
-    f4 accb[(NP + WQ - 1) / WQ];                                          // row sums of P, shared by the wavefronts that read it
+    constexpr int NB = NP / WQ;                                           // row sums of P: the WQ wavefronts of the same rows share them
+    f4 accb[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) accb[j] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < NP; ++x) {
-        accb[x / WQ] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int y = 0; y < NQ; ++y) acc[x][y] = f4{0.f, 0.f, 0.f, 0.f};
     }
@@ -356,31 +494,34 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
             return ~0ull;
         }
     };
-    const auto send_p = [&](int j, int s, int buf, unsigned long long mask) {
-        P.load(j, bp + (long long)s * (LP == kAlong ? kStep : 64 * a.pp), a.pp, left_of(s), mask, lds + buf * TP::kBytes);
+    struct Sent {                                                         // a step's loads of an operand
+        u4 buffer;
+        unsigned bits, to;
     };
-    const auto send_q = [&](int j, int s, unsigned long long mask) {
-        Q.load(j, bq + (long long)s * (LQ == kAlong ? kStep : 64 * a.pq), a.pq, left_of(s), mask, lds + kAtQ + (s & 1) * TQ::kBytes);
+    const unsigned lds_at = lds_byte(lds);
+    const auto sent_p = [&](int s, int buf, unsigned long long mask) {
+        return Sent{descriptor(bp + (long long)s * (LP == kAlong ? kStep : 64 * a.pp)), P.bits(left_of(s), mask), lds_at + buf * TP::kBytes};
     };
-    constexpr int kScaleLoads = kEight ? (BP + BQ + kThreads - 1) / kThreads : 0;
-    const auto send_scales = [&](int j, int s) {                          // a row's four scales of the step
+    const auto sent_q = [&](int s, int buf, unsigned long long mask) {
+        return Sent{descriptor(bq + (long long)s * (LQ == kAlong ? kStep : 64 * a.pq)), Q.bits(left_of(s), mask), lds_at + kAtQ + buf * TQ::kBytes};
+    };
+    const auto send_scales = [&](int j, int s, int buf) {                 // a row's four scales of the step
         const int r = j * kThreads + (int)threadIdx.x, first = j * kThreads + wave * kWave;
         const bool isp = first < BP;
         const int row = isp ? r : r - BP;
-        const bool ok = s < steps && (isp ? p0 + row < a.P : q0 + row < a.Q);
+        const bool ok = s < steps && (isp ? p0 + row < a.P : row < BQ && q0 + row < a.Q);
         const unsigned o = ok ? (unsigned)(row * (isp ? a.psp : a.psq)) + (unsigned)(k0 / kBlock) + 4u * (unsigned)s : kNowhere;
-        to_lds<4>(isp ? a.sp + (long long)p0 * a.psp : a.sq + (long long)q0 * a.psq, o, &scales[s & 1][first * 4]);
+        to_lds<4>(descriptor(isp ? a.sp + (long long)p0 * a.psp : a.sq + (long long)q0 * a.psq), o, 0, lds_byte(&scales[buf][first * 4]));
     };
-    static_assert(!kEight || (BP + BQ) % kThreads == 0, "whole loads of scales");
 
     // LDS byte of a wavefront's first fragment of a step's first half.  Along: fragment x is 16 rows on, half h at piece ^ 4 h.
     // Across: half h is 32 rows on, the second four rows of a lane four on, and fragment x at granule ^ x (a wavefront's first
     // column is a multiple of its 16 NP, NQ, powers of two, so the sum is an exclusive or).
     const int kr = 8 * g + (i16 >> 2), swizzled = (g ^ along_swizzle(i16)) << 4;
     const unsigned at_p = LP == kAlong ? (wp * (BP / WP) + i16) * kStep + swizzled
-                                       : kr * (BP * 2) + ((wp * NP ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8;
+                                       : kr * (BP * 2) + ((wp * NP ^ across_swizzle<BP>(kr)) << 5) + (i16 & 3) * 8;
     const unsigned at_q = kAtQ + (LQ == kAlong ? (wq * (BQ / WQ) + i16) * kStep + swizzled
-                                               : kr * (BQ * 2) + ((wq * NQ ^ across_swizzle(kr)) << 5) + (i16 & 3) * 8);
+                                               : kr * (BQ * 2) + ((wq * NQ ^ across_swizzle<BQ>(kr)) << 5) + (i16 & 3) * 8);
     const auto read_p = [&](unsigned at, int half, int x) {
         if constexpr (LP == kAlong) return *(const u4*)(lds + (at ^ half * 64) + x * 16 * kStep);
         else return across_read(lds + (at ^ x * 32) + half * 32 * BP * 2, 0, 4 * BP * 2);
@@ -396,38 +537,41 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
     };
 
     if (steps > 0) {
-        unsigned long long mask_q = mask_of(0), mask_p = mask_q;
+        unsigned long long mask = ~0ull, mask_last = ~0ull;
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s) {
-            if (s > 0) mask_p = mask_of(s);
+        for (int s = 0; s < SP; ++s) {
+            mask_last = mask;
+            mask = mask_of(s);
+            const Sent p = sent_p(s, s, mask);
 #pragma unroll
-            for (int j = 0; j < TP::kLoads; ++j) send_p(j, s, s, mask_p);
-            if (s < 2) {
-                mask_q = mask_p;
+            for (int j = 0; j < TP::kLoads; ++j) P.load(j, p.buffer, p.bits, p.to);
+            if (s < SQ) {
+                const Sent q = sent_q(s, s, mask);
 #pragma unroll
-                for (int j = 0; j < TQ::kLoads; ++j) send_q(j, s, mask_q);
+                for (int j = 0; j < TQ::kLoads; ++j) Q.load(j, q.buffer, q.bits, q.to);
 #pragma unroll
-                for (int j = 0; j < kScaleLoads; ++j) send_scales(j, s);
+                for (int j = 0; j < kScaleLoads; ++j) send_scales(j, s, s);
             }
         }
-        arrived<TP::kLoads * (kAhead - 1) + TQ::kLoads + kScaleLoads>();
+        arrived<TP::kLoads * (SP - 1) + (TQ::kLoads + kScaleLoads) * (SQ - 1)>();
 
-        int buf = 0;                                                      // of P, of step s
-        const auto after = [&](int b) { return b + 1 == kBuffersP ? 0 : b + 1; };
+        // of those sent, a step's Q before its P, what may still be on its way when the next step's fragments are read
+        constexpr int kLater = (SQ - 2) * (TP::kLoads + TQ::kLoads + kScaleLoads) + (SP > SQ ? TP::kLoads : 0);
+        int buf_p = 0, buf_q = 0;                                         // of step s
+        const auto after = [&](int b, int n) { return b + 1 == n ? 0 : b + 1; };
         if constexpr (kEight) {
-            constexpr int H = NP / 2;
-            constexpr int kSends = (TP::kLoads + TQ::kLoads + kScaleLoads + H - 1) / H;
+            constexpr int H = NP / 2, kSends = (TP::kLoads + TQ::kLoads + kScaleLoads + H - 1) / H;
             i8x fp[NP], fq[NQ];
             int cp[NP], cq[NQ];
-            const auto take_p = [&](int s, int x) {
-                const unsigned at = here(at_p + (s & 1) * TP::kBytes);
+            const auto take_p = [&](int buf, int x) {
+                const unsigned at = here(at_p + buf * TP::kBytes);
                 fp[x] = join8(read_p(at, 0, x), read_p(at, 1, x));
-                cp[x] = scales[s & 1][(wp * (BP / WP) + x * 16 + i16) * 4 + g];
+                cp[x] = scales[buf][(wp * (BP / WP) + x * 16 + i16) * 4 + g];
             };
-            const auto take_q = [&](int s, int y) {
-                const unsigned at = here(at_q + (s & 1) * TQ::kBytes);
+            const auto take_q = [&](int buf, int y) {
+                const unsigned at = here(at_q + buf * TQ::kBytes);
                 fq[y] = join8(read_q(at, 0, y), read_q(at, 1, y));
-                cq[y] = scales[s & 1][(BP + wq * (BQ / WQ) + y * 16 + i16) * 4 + g];
+                cq[y] = scales[buf][(BP + wq * (BQ / WQ) + y * 16 + i16) * 4 + g];
             };
 #pragma unroll
             for (int y = 0; y < NQ; ++y) take_q(0, y);
@@ -436,21 +580,23 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
             for (int s = 0; s < steps; ++s) {
 #pragma unroll
                 for (int x = 0; x < H; ++x) {
-                    take_p(s, H + x);
+                    take_p(buf_q, H + x);
 #pragma unroll
                     for (int y = 0; y < NQ; ++y) acc[x][y] = mfma_scaled(fq[y], fp[x], acc[x][y], cq[y], cp[x]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                arrived<0>();
+                arrived<kLater>();
+                const int next = after(buf_q, SQ);
+                const Sent p = sent_p(s + SP, buf_q, ~0ull), q = sent_q(s + SQ, buf_q, ~0ull);
 #pragma unroll
                 for (int x = 0; x < H; ++x) {
 #pragma unroll
                     for (int j = kSends * x; j < kSends * x + kSends; ++j) {
-                        if (j < TP::kLoads) send_p(j, s + 2, s & 1, ~0ull);
-                        else if (j < TP::kLoads + TQ::kLoads) send_q(j - TP::kLoads, s + 2, ~0ull);
-                        else if (j < TP::kLoads + TQ::kLoads + kScaleLoads) send_scales(j - TP::kLoads - TQ::kLoads, s + 2);
+                        if (j < TP::kLoads) P.load(j, p.buffer, p.bits, p.to);
+                        else if (j < TP::kLoads + TQ::kLoads) Q.load(j - TP::kLoads, q.buffer, q.bits, q.to);
+                        else if (j < TP::kLoads + TQ::kLoads + kScaleLoads) send_scales(j - TP::kLoads - TQ::kLoads, s + SQ, buf_q);
                     }
-                    take_p(s + 1, x);
+                    take_p(next, x);
                     if (x + 1 < H) {
 #pragma unroll
                         for (int y = 0; y < NQ; ++y) acc[H + x][y] = mfma_scaled(fq[y], fp[H + x], acc[H + x][y], cq[y], cp[H + x]);
@@ -460,9 +606,10 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
 #pragma unroll
                 for (int y = 0; y < NQ; ++y) {
                     acc[NP - 1][y] = mfma_scaled(fq[y], fp[NP - 1], acc[NP - 1][y], cq[y], cp[NP - 1]);
-                    take_q(s + 1, y);
+                    take_q(next, y);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                buf_q = next;
             }
         } else {
             u4 fp[NP], fq[2][NQ];
@@ -471,9 +618,10 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
 #pragma unroll
                 for (int y = 0; y < NQ; ++y) acc[x][y] = Mfma<E>::go(fq[half][y], fp[x], acc[x][y]);
                 if constexpr (LP == kAcross) {
-                    if (bias_too && x % WQ == wq) accb[x / WQ] = Mfma<E>::go(u4{one, one, one, one}, fp[x], accb[x / WQ]);
+                    if (bias_too && x / NB == wq) accb[x % NB] = Mfma<E>::go(u4{one, one, one, one}, fp[x], accb[x % NB]);
                 }
             };
+            static_assert(NQ <= NP, "a fragment of Q read beside each of P");
             {
                 const unsigned ap = here(at_p), aq = here(at_q);
 #pragma unroll
@@ -481,10 +629,9 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
 #pragma unroll
                 for (int x = 0; x < NP; ++x) fp[x] = read_p(ap, 0, x);
             }
-            mask_q = mask_p;                                              // of step 2
             for (int s = 0; s < steps; ++s) {
                 {
-                    const unsigned ap = here(at_p + buf * TP::kBytes), aq = here(at_q + (s & 1) * TQ::kBytes);
+                    const unsigned ap = here(at_p + buf_p * TP::kBytes), aq = here(at_q + buf_q * TQ::kBytes);
 #pragma unroll
                     for (int x = 0; x < NP; ++x) {
                         multiply(0, x);
@@ -493,27 +640,30 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
-                arrived<TP::kLoads>();
-                const int next = after(buf);
-                mask_p = mask_of(s + kAhead);
+                arrived<kLater>();
+                const int next_p = after(buf_p, SP), next_q = after(buf_q, SQ);
+                mask_last = mask;
+                mask = mask_of(s + SP);
+                const unsigned long long mask_q = SP > SQ ? mask_last : mask;
                 {
-                    const unsigned ap = here(at_p + next * TP::kBytes), aq = here(at_q + (s + 1 & 1) * TQ::kBytes);
+                    const unsigned ap = here(at_p + next_p * TP::kBytes), aq = here(at_q + next_q * TQ::kBytes);
                     constexpr int kSends = (TP::kLoads + TQ::kLoads + NP - 1) / NP;
+                    const Sent q = sent_q(s + SQ, buf_q, mask_q), p = sent_p(s + SP, buf_p, mask);
 #pragma unroll
                     for (int x = 0; x < NP; ++x) {
                         multiply(1, x);
 #pragma unroll
                         for (int j = kSends * x; j < kSends * x + kSends; ++j) {
-                            if (j < TQ::kLoads) send_q(j, s + 2, mask_q);
-                            else if (j < TQ::kLoads + TP::kLoads) send_p(j - TQ::kLoads, s + kAhead, buf, mask_p);
+                            if (j < TQ::kLoads) Q.load(j, q.buffer, q.bits, q.to);
+                            else if (j < TQ::kLoads + TP::kLoads) P.load(j - TQ::kLoads, p.buffer, p.bits, p.to);
                         }
                         fp[x] = read_p(ap, 0, x);
                         if (x < NQ) fq[0][x] = read_q(aq, 0, x);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
-                mask_q = mask_p;
-                buf = next;
+                buf_p = next_p;
+                buf_q = next_q;
             }
         }
         arrived<0>();                                                     // the loads from nowhere, before LDS is used again
@@ -526,8 +676,16 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
     static_assert((size_t)XS * 16 * kCols * 4 * WP * WQ <= sizeof(lds), "room for the epilogue");
     char* mine = lds + wave * (XS * 16 * kCols * 4);
     const int c = (lane % kLanes) * 8, n = q0 + wq * kCols + c;
+    Epilogue e = a.e;
+    if (e.part) {                                                         // sums of a share go out as they are
+        e.y = e.part + (size_t)blockIdx.y * a.P * a.Q;
+        e.py = a.Q;
+        e.type = LAST_F32;
+        e.wide = (a.Q & 3) == 0;
+    }
+    const int kind = rows_kind(e);
     float bias[8];
-    load_bias(a.e, n, a.Q, bias);
+    load_bias(e, n, a.Q, bias);
 #pragma unroll 1
     for (int part = 0; part < NP / XS; ++part) {
 #pragma unroll
@@ -542,47 +700,68 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product_kernel(ProductArgs a)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();                     // (the reads follow the writes in the wavefront's order)
         const int first = p0 + wp * (BP / WP) + part * XS * 16;
-        const auto exists = [&](int m) { return m < a.P && (LP == kAcross || frame_exists(a.frames, m)); };
-        bool there = exists(first + lane / kLanes);
-        Fetched f = fetch(a.e, first + lane / kLanes, n, a.P, a.Q, there);
-#pragma unroll 1
-        for (int r = lane / kLanes; r < XS * 16; r += kRows) {
-            const int m = first + r;
-            const bool there_next = r + kRows < XS * 16 && exists(m + kRows);
-            const Fetched f_next = fetch(a.e, m + kRows, n, a.P, a.Q, there_next);
+        const auto get = [&](int r, float* v) {
             const f4 lo = *(const f4*)(mine + r * (kCols * 4) + (((c / 4) ^ (r & (kPieces - 1))) << 4));
             const f4 hi = *(const f4*)(mine + r * (kCols * 4) + (((c / 4 + 1) ^ (r & (kPieces - 1))) << 4));
-            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            if (a.e.part) {
-                if (m < a.P) store8<float>(a.e.part, ((size_t)blockIdx.y * a.P + m) * a.Q + n, a.Q - n, (a.Q & 3) == 0, v);
-            } else {
-                finish(a.e, m, n, a.P, a.Q, there, bias, f, v);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { v[u] = lo[u]; v[4 + u] = hi[u]; }
+        };
+        const auto get_mine = [&](int i, float* v) { get(lane / kLanes + i * kRows, v); };
+        // bits of the rows that exist
+        const int mine_row = first + lane % (XS * 16);
+        const unsigned long long rows = __ballot(mine_row < a.P && (LP == kAcross || frame_exists(a.frames, mine_row)));
+        const bool inside = rows == ~0ull && q0 + (wq + 1) * kCols <= a.Q;
+        const size_t m0 = (size_t)first + lane / kLanes;
+        constexpr int kCount = XS * 16 / kRows;
+        if (!inside || kind == kRowsAny) {
+            bool there = rows >> (lane / kLanes) & 1;
+            Fetched f = fetch(e, (int)m0, n, a.P, a.Q, there);
+#pragma unroll 1
+            for (int r = lane / kLanes; r < XS * 16; r += kRows) {
+                const int m = first + r;
+                const bool there_next = r + kRows < XS * 16 && (rows >> (r + kRows) & 1) != 0;
+                const Fetched f_next = fetch(e, m + kRows, n, a.P, a.Q, there_next);
+                float v[8];
+                get(r, v);
+                finish(e, m, n, a.P, a.Q, there, bias, f, v);
+                f = f_next;
+                there = there_next;
             }
-            f = f_next;
-            there = there_next;
+        } else if (kind == kRowsPlain) {
+            fast_rows<kRowsPlain>(e, m0, n, kRows, kCount, bias, get_mine);
+        } else if (kind == kRowsResidual) {
+            fast_rows<kRowsResidual>(e, m0, n, kRows, kCount, bias, get_mine);
+        } else if (kind == kRowsSlope) {
+            fast_rows<kRowsSlope>(e, m0, n, kRows, kCount, bias, get_mine);
+        } else if (kind == kRowsKeep) {
+            fast_rows<kRowsKeep>(e, m0, n, kRows, kCount, bias, get_mine);
+        } else if (kind == kRowsEight) {
+            fast_rows<kRowsEight>(e, m0, n, kRows, kCount, bias, get_mine);
+        } else {
+            fast_rows<kRowsWide>(e, m0, n, kRows, kCount, bias, get_mine);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
-    if (bias_too) {
+    if (bias_too && g == 0) {
 #pragma unroll
-        for (int x = 0; x < NP; ++x) {
-            const int m = p0 + wp * (BP / WP) + x * 16 + i16;
-            if (x % WQ == wq && g == 0 && m < a.P) a.e.part_bias[(size_t)blockIdx.y * a.P + m] = accb[x / WQ][0];
+        for (int j = 0; j < NB; ++j) {
+            const int m = p0 + wp * (BP / WP) + (wq * NB + j) * 16 + i16;
+            if (m < a.P) a.e.part_bias[(size_t)blockIdx.y * a.P + m] = accb[j][0];
         }
     }
 }
 
 // ---- few rows: y = act(x w^T + bias) + residual for at most 16 MT rows, bound by the bytes of w, which go from memory to
-// registers once.  A workgroup takes 16 QF columns, its wavefronts every kFewWaves-th 128 bytes of the rows, four such
+// registers once.  A workgroup takes 16 QF columns, its wavefronts every kFewWaves-th 128 bytes of the rows, four (two) such
 // steps' loads under way at a time; their sums meet in LDS.
 constexpr int kFewWaves = 8;
-constexpr int kFewDeep = 4;
 
 template <typename E, int MT, int QF>
 __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
 {
     constexpr bool kEight = Elt<E>::size == 1;
+    constexpr int kDeep = kEight && MT * QF >= 8 ? 2 : 4;                 // (steps under way: as many as there are registers for)
     __shared__ f4 red[kFewWaves][MT][QF][kWave];
     const int lane = (int)threadIdx.x % kWave, g = lane >> 4, i16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -606,11 +785,11 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
 #pragma unroll
         for (int f = 0; f < QF; ++f) acc[t][f] = f4{0.f, 0.f, 0.f, 0.f};
     const int bytes = (int)a.K, steps = (bytes + kStep - 1) / kStep;
-    for (int s0 = wave; s0 < steps; s0 += kFewWaves * kFewDeep) {
-        u4 fq[kFewDeep][QF][2], fp[kFewDeep][MT][2];
-        int cq[kFewDeep][QF], cp[kFewDeep][MT];
+    for (int s0 = wave; s0 < steps; s0 += kFewWaves * kDeep) {
+        u4 fq[kDeep][QF][2], fp[kDeep][MT][2];
+        int cq[kDeep][QF], cp[kDeep][MT];
 #pragma unroll
-        for (int d = 0; d < kFewDeep; ++d) {
+        for (int d = 0; d < kDeep; ++d) {
             const int k = (s0 + d * kFewWaves) * kStep;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -633,7 +812,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
             }
         }
 #pragma unroll
-        for (int d = 0; d < kFewDeep; ++d)
+        for (int d = 0; d < kDeep; ++d)
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
