@@ -143,23 +143,33 @@ struct ProductPlan {
     long long share;                 // of the reduction, in bytes (kAlong) or rows
 };
 
-// `steps`: of 128 bytes or 64 rows of the reduction
-ProductPlan plan_product(bool forward, long long P, long long Q, long long steps)
+// Tiles and shares of a reduction of `steps` steps (128 bytes, or 64 rows).  Up to 64 rows of a forward product go to the
+// kernel that reads w once and keeps nothing in LDS; beyond, the cheapest of what these would take, from measurements on
+// MI355X: a workgroup with a compute unit to itself takes 1.2, 0.5 and 0.2 us a step with tiles of 256, 128 and 64, two
+// that share one 0.95 and 0.4 us a step (tiles of 128 and 64), and 9, 5 and 3.5 us beside its steps; across the rows of
+// both operands a step takes 1.15 to 1.9 times as long (transposing reads).  Tiles of 256 win from a full chip on (16384 x 1024 on
+// 4096: 107 us, with tiles of 128 122), tiles of 64 up to about half a million results (512 x 1024 on 4096: 20 us, 37 and 80).  Shares are
+// written and read in 32 bits at about 5 TB/s and cost a launch: 16384 x 1024 x 4096 rows of weight gradient in 4 shares
+// 161 us, in one 357 us.
+ProductPlan plan_product(bool forward, bool across, long long P, long long Q, long long steps)
 {
-    ProductPlan best{0, 1, 0};
+    ProductPlan best{0, 1, steps};
     if (forward && P <= 64) return best;
+    static const double alone[4] = {0, 0.2, 0.5, 1.2}, shared[4] = {0, 0.4, 0.95, 1.2}, beside[4] = {0, 3.5, 5, 9};
+    static const double by_rows[4] = {0, 1.9, 1.4, 1.15};
     double least = 1e30;
-    for (int variant = 2; variant <= 3; ++variant) {
-        const long long tile = variant == 3 ? 256 : 128;
+    for (int variant = 1; variant <= 3; ++variant) {
+        const long long tile = 32 << variant;
         const long long tiles = ((P + tile - 1) / tile) * ((Q + tile - 1) / tile);
         for (int splits = 1; splits <= 64; splits *= 2) {
-            const long long part = (steps + splits - 1) / splits;
-            if (splits > 1 && (part < 8 || (steps + part - 1) / part != splits)) continue;
-            const long long blocks = tiles * splits;
-            double us;
-            if (variant == 3) us = (double)((blocks + 255) / 256) * (part * 1.1 + 6);
-            else us = (double)((blocks + 511) / 512) * (part * (blocks <= 256 ? 0.4 : 0.7) + 4);
-            if (splits > 1) us += 4 + (double)splits * P * Q * 8 / 4e6;
+            const long long part = std::max(1ll, (steps + splits - 1) / splits);
+            if (splits > 1 && (part < 4 || (steps + part - 1) / part != splits)) continue;
+            const long long blocks = tiles * splits, at_once = variant == 3 ? 256 : 512;
+            const long long rounds = (blocks + at_once - 1) / at_once, last = blocks - (rounds - 1) * at_once;
+            const double factor = across ? by_rows[variant] : 1.0;
+            double us = (rounds - 1) * (part * shared[variant] * factor + beside[variant]);
+            us += part * (last <= 256 ? alone[variant] : shared[variant]) * factor + beside[variant];
+            if (splits > 1) us += 4 + (double)splits * P * Q * 8 / 5e6;
             if (us < least) {
                 least = us;
                 best = ProductPlan{variant, splits, part};
@@ -321,7 +331,7 @@ last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, in
     a.Q = N;
     a.K = bytes;
     a.frames = frames_of(f);
-    const ProductPlan plan = plan_product(true, rows, N, (bytes + kStep - 1) / kStep);
+    const ProductPlan plan = plan_product(true, false, rows, N, (bytes + kStep - 1) / kStep);
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
     a.e.bias = bias;
@@ -356,7 +366,7 @@ last_status_t run_grad_input(Carver& cv, const last_frames_t* f, long long rows,
     a.K = bytes;
     a.q_rows = N;
     a.frames = frames_of(f);
-    const ProductPlan plan = plan_product(false, rows, K, (bytes + kStep - 1) / kStep);
+    const ProductPlan plan = plan_product(false, false, rows, K, (bytes + kStep - 1) / kStep);
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
     set_result(a.e, dx, nullptr);
@@ -393,7 +403,7 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
     a.P = N;
     a.Q = K;
     a.K = rows;
-    const ProductPlan plan = plan_product(false, N, K, (rows + 63) / 64);
+    const ProductPlan plan = plan_product(false, true, N, K, (rows + 63) / 64);
     set_plan(cv, a, plan, 64, dbias);
     unsigned long long* mask = f->lengths ? (unsigned long long*)cv.take((size_t)((rows + 63) / 64 * 8)) : nullptr;
     if (!cv.base) return LAST_OK;
