@@ -16,7 +16,6 @@ struct KeepArgs {
     void* y;                         // values, grad: results
     long long px, py;
     int act, ytype;
-    bool ax, ay;
     Eight kept;
 };
 
@@ -35,7 +34,7 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a)
     int row, h;
     const bool in = keep_place(a, &row, &h);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (in && h < a.H && frame_exists(a.frames, row)) load8<X>(a.x, (size_t)row * a.px + h, a.H - h, a.ax, v);
+    if (in && h < a.H && frame_exists(a.frames, row)) load8<X>(a.x, (size_t)row * a.px + h, a.H - h, v);
     const unsigned top = quad_max(top8(v));
     if (in) store_eight(a.kept, row, h, a.H - h, (h & (kBlock - 1)) == 0, top, v);
 }
@@ -43,7 +42,7 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a)
 __device__ __forceinline__ void load_eight(const Eight& k, size_t row, int h, int n, float* v)
 {
     unsigned lo, hi;
-    load_codes(k.q + row * k.pitch, h, n, k.aligned, &lo, &hi);
+    load_codes(k.q + row * k.pitch, h, n, &lo, &hi);
     const float sc = scale_value(k.scales[row * k.scale_pitch + h / kBlock]);
     if (k.e4m3) {
         decode4<true>(lo, sc, v);
@@ -64,7 +63,7 @@ __global__ __launch_bounds__(256) void kept_values_kernel(KeepArgs a)
         load_eight(a.kept, row, h, a.H - h, v);
         activate8(a.act, v);
     }
-    store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, a.ay, v);
+    store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, v);
 }
 
 // y = dy act'(kept)
@@ -75,14 +74,14 @@ __global__ __launch_bounds__(256) void kept_grad_kernel(KeepArgs a)
     if (!keep_place(a, &row, &h) || h >= a.H) return;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, d[8];
     if (frame_exists(a.frames, row)) {
-        load8<X>(a.x, (size_t)row * a.px + h, a.H - h, a.ax, d);
+        load8<X>(a.x, (size_t)row * a.px + h, a.H - h, d);
         load_eight(a.kept, row, h, a.H - h, v);
         times_slope(a.act, v, d);
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) d[k] = 0.f;
     }
-    store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, a.ay, d);
+    store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, d);
 }
 
 }  // namespace last

@@ -12,6 +12,15 @@ namespace last {
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 typedef unsigned u2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+
+// Rows begin wherever an element may, e.g. those of 257 columns: memory takes vectors at any address, and what is aligned is
+// no slower for it (one instruction either way).
+typedef f4 f4_any __attribute__((aligned(4)));
+typedef u4 u4_any __attribute__((aligned(2)));
+typedef h8 h8_any __attribute__((aligned(2)));
+typedef u2 u2_any __attribute__((aligned(1)));
+typedef u4 u4_byte __attribute__((aligned(1)));
 
 struct bf16_t { uint16_t bits; };
 struct f16_t { _Float16 v; };
@@ -103,8 +112,7 @@ __device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_
 
 __device__ __forceinline__ unsigned umax(unsigned a, unsigned b) { return a > b ? a : b; }
 
-// ---- eight consecutive elements of a row; n of them exist (the others read as 0 and are not written).  `aligned`: every
-// group of eight begins at a multiple of its own size (16 bytes at most)
+// ---- eight consecutive elements of a row; n of them exist (the others read as 0 and are not written)
 
 template <typename E> struct Elt;
 template <> struct Elt<float> {
@@ -113,14 +121,14 @@ template <> struct Elt<float> {
     static __device__ void put(void* p, size_t i, float v) { ((float*)p)[i] = v; }
     static __device__ void get8(const void* p, size_t i, float* v)
     {
-        const f4 a = *(const f4*)((const float*)p + i), b = *(const f4*)((const float*)p + i + 4);
+        const f4 a = *(const f4_any*)((const float*)p + i), b = *(const f4_any*)((const float*)p + i + 4);
 #pragma unroll
         for (int k = 0; k < 4; ++k) { v[k] = a[k]; v[4 + k] = b[k]; }
     }
     static __device__ void put8(void* p, size_t i, const float* v)
     {
-        *(f4*)((float*)p + i) = f4{v[0], v[1], v[2], v[3]};
-        *(f4*)((float*)p + i + 4) = f4{v[4], v[5], v[6], v[7]};
+        *(f4_any*)((float*)p + i) = f4{v[0], v[1], v[2], v[3]};
+        *(f4_any*)((float*)p + i + 4) = f4{v[4], v[5], v[6], v[7]};
     }
 };
 template <> struct Elt<bf16_t> {
@@ -129,13 +137,13 @@ template <> struct Elt<bf16_t> {
     static __device__ void put(void* p, size_t i, float v) { ((uint16_t*)p)[i] = (uint16_t)bf16_pair(v, 0.f); }
     static __device__ void get8(const void* p, size_t i, float* v)
     {
-        const u4 a = *(const u4*)((const uint16_t*)p + i);
+        const u4 a = *(const u4_any*)((const uint16_t*)p + i);
 #pragma unroll
         for (int k = 0; k < 4; ++k) { v[2 * k] = bf16_to_float(a[k] & 0xffffu); v[2 * k + 1] = __uint_as_float(a[k] & 0xffff0000u); }
     }
     static __device__ void put8(void* p, size_t i, const float* v)
     {
-        *(u4*)((uint16_t*)p + i) = u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+        *(u4_any*)((uint16_t*)p + i) = u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
     }
 };
 template <> struct Elt<f16_t> {
@@ -144,14 +152,13 @@ template <> struct Elt<f16_t> {
     static __device__ void put(void* p, size_t i, float v) { ((_Float16*)p)[i] = (_Float16)v; }
     static __device__ void get8(const void* p, size_t i, float* v)
     {
-        typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-        const h8 a = *(const h8*)((const _Float16*)p + i);
+        const h8 a = *(const h8_any*)((const _Float16*)p + i);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = (float)a[k];
     }
     static __device__ void put8(void* p, size_t i, const float* v)
     {
-        *(u4*)((_Float16*)p + i) = u4{f16_pair(v[0], v[1]), f16_pair(v[2], v[3]), f16_pair(v[4], v[5]), f16_pair(v[6], v[7])};
+        *(u4_any*)((_Float16*)p + i) = u4{f16_pair(v[0], v[1]), f16_pair(v[2], v[3]), f16_pair(v[4], v[5]), f16_pair(v[6], v[7])};
     }
 };
 // codes of 8-bit values; the caller brings the scale of their block
@@ -159,7 +166,7 @@ template <bool E4M3> struct EltCodes {
     static constexpr int type = E4M3 ? LAST_E4M3 : LAST_I8, size = 1;
     static __device__ void get8(const void* p, size_t i, float* v)
     {
-        const u2 a = *(const u2*)((const uint8_t*)p + i);
+        const u2 a = *(const u2_any*)((const uint8_t*)p + i);
         decode4<E4M3>(a[0], 1.f, v);
         decode4<E4M3>(a[1], 1.f, v + 4);
     }
@@ -174,9 +181,9 @@ template <> struct Elt<i8_t> : EltCodes<false> {};
 template <> struct Elt<e4m3_t> : EltCodes<true> {};
 
 template <typename E>
-__device__ __forceinline__ void load8(const void* p, size_t i, int n, bool aligned, float* v)
+__device__ __forceinline__ void load8(const void* p, size_t i, int n, float* v)
 {
-    if (aligned && n >= 8) {
+    if (n >= 8) {
         Elt<E>::get8(p, i, v);
     } else {
 #pragma unroll
@@ -185,9 +192,9 @@ __device__ __forceinline__ void load8(const void* p, size_t i, int n, bool align
 }
 
 template <typename E>
-__device__ __forceinline__ void store8(void* p, size_t i, int n, bool aligned, const float* v)
+__device__ __forceinline__ void store8(void* p, size_t i, int n, const float* v)
 {
-    if (aligned && n >= 8) {
+    if (n >= 8) {
         Elt<E>::put8(p, i, v);
     } else {
 #pragma unroll
@@ -197,18 +204,18 @@ __device__ __forceinline__ void store8(void* p, size_t i, int n, bool aligned, c
 }
 
 // the same with the type given at run time, the same for all lanes
-__device__ __forceinline__ void store8_as(int type, void* p, size_t i, int n, bool aligned, const float* v)
+__device__ __forceinline__ void store8_as(int type, void* p, size_t i, int n, const float* v)
 {
-    if (type == LAST_BF16) store8<bf16_t>(p, i, n, aligned, v);
-    else if (type == LAST_F16) store8<f16_t>(p, i, n, aligned, v);
-    else store8<float>(p, i, n, aligned, v);
+    if (type == LAST_BF16) store8<bf16_t>(p, i, n, v);
+    else if (type == LAST_F16) store8<f16_t>(p, i, n, v);
+    else store8<float>(p, i, n, v);
 }
 
 // eight codes of a row, n of which exist
-__device__ __forceinline__ void store_codes(uint8_t* p, size_t i, int n, bool aligned, unsigned lo, unsigned hi)
+__device__ __forceinline__ void store_codes(uint8_t* p, size_t i, int n, unsigned lo, unsigned hi)
 {
-    if (aligned && n >= 8) {
-        *(u2*)(p + i) = u2{lo, hi};
+    if (n >= 8) {
+        *(u2_any*)(p + i) = u2{lo, hi};
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
@@ -216,10 +223,10 @@ __device__ __forceinline__ void store_codes(uint8_t* p, size_t i, int n, bool al
     }
 }
 
-__device__ __forceinline__ void load_codes(const uint8_t* p, size_t i, int n, bool aligned, unsigned* lo, unsigned* hi)
+__device__ __forceinline__ void load_codes(const uint8_t* p, size_t i, int n, unsigned* lo, unsigned* hi)
 {
-    if (aligned && n >= 8) {
-        const u2 a = *(const u2*)(p + i);
+    if (n >= 8) {
+        const u2 a = *(const u2_any*)(p + i);
         *lo = a[0];
         *hi = a[1];
     } else {
@@ -238,7 +245,6 @@ struct Eight {
     uint8_t* scales;
     long long pitch, scale_pitch;
     int e4m3;
-    int aligned;                     // groups of eight codes begin at multiples of 8 bytes
 };
 
 // Eight columns c.. of a row, in each of four lanes that hold a block of 32 columns between them; `top`: the largest
@@ -249,7 +255,7 @@ __device__ __forceinline__ void store_eight(const Eight& k, size_t row, int c, i
     const unsigned lo = k.e4m3 ? encode4<true>(v, byte) : encode4<false>(v, byte);
     const unsigned hi = k.e4m3 ? encode4<true>(v + 4, byte) : encode4<false>(v + 4, byte);
     if (n > 0) {
-        store_codes(k.q + row * k.pitch, c, n, k.aligned, lo, hi);
+        store_codes(k.q + row * k.pitch, c, n, lo, hi);
         if (first) k.scales[row * k.scale_pitch + c / kBlock] = (uint8_t)byte;
     }
 }

@@ -64,13 +64,6 @@ last_status_t check_matrix(const last_matrix_t* m, long long columns, bool types
         if (rc_ != LAST_OK) return rc_;                 \
     } while (0)
 
-// groups of eight elements begin at multiples of 16 bytes, or of their size
-bool wide(const last_matrix_t* m)
-{
-    const long long unit = std::min(16, 8 * size_of(m->type));
-    return (uintptr_t)m->data % unit == 0 && m->pitch * size_of(m->type) % unit == 0;
-}
-
 Frames frames_of(const last_frames_t* f) { return Frames{f->lengths, f->T}; }
 
 Eight eight_of(const last_matrix_t* m)
@@ -82,7 +75,6 @@ Eight eight_of(const last_matrix_t* m)
     e.pitch = m->pitch;
     e.scale_pitch = m->scale_pitch;
     e.e4m3 = m->type == LAST_E4M3;
-    e.aligned = wide(m);
     return e;
 }
 
@@ -257,29 +249,47 @@ struct Carver {
     }
 };
 
-void launch_repack(const void* in, long long pitch, long long bytes, char* out, long long out_pitch, long long rows, hipStream_t st)
-{
-    const long long pieces = rows * (out_pitch / 16);
-    if (pieces == 0) return;
-    hipLaunchKernelGGL(repack_kernel, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, st, (const uint8_t*)in, pitch, (int)bytes,
-                       (uint8_t*)out, (int)out_pitch, pieces);
-}
+// What has to be laid out before a product, collected and launched at once.
+struct Preparation {
+    PrepareArgs a{};
+    int n = 0;
+    unsigned mask_groups = 0;
+    void rows(const void* in, long long pitch, long long bytes, char* out, long long out_pitch, long long count)
+    {
+        if (count == 0) return;
+        auto& r = a.rows[n++];
+        r = PrepareArgs::Rows{(const uint8_t*)in, (uint8_t*)out, pitch, out_pitch, count, (int)bytes,
+                              (unsigned)((count * (out_pitch / 16) + 255) / 256)};
+        a.groups += r.groups;
+    }
+    void mask(const last_frames_t* f, long long count, unsigned long long* out)
+    {
+        a.frames = frames_of(f);
+        a.frame_rows = (int)count;
+        a.mask = out;
+        mask_groups = (unsigned)((count + 255) / 256);
+    }
+    void launch(hipStream_t st) const
+    {
+        if (a.groups + mask_groups) hipLaunchKernelGGL(prepare_kernel, dim3(a.groups + mask_groups), dim3(256), 0, st, a);
+    }
+};
 
-// With a workspace that only measures (cv.base null) nothing is launched.
-Operand lay_out(Carver& cv, const last_matrix_t* m, long long rows, long long columns, hipStream_t st)
+// With a workspace that only measures (cv.base null) nothing is prepared.
+Operand lay_out(Carver& cv, Preparation& pre, const last_matrix_t* m, long long rows, long long columns)
 {
     const long long es = size_of(m->type);
     Operand o{(const char*)m->data, m->pitch * es, m->scales, m->scale_pitch};
     if (!direct(m, columns)) {
         o.pitch = packed_pitch(columns, m->type);
         char* at = cv.take((size_t)(rows * o.pitch));
-        if (at) launch_repack(m->data, m->pitch * es, columns * es, at, o.pitch, rows, st);
+        if (at) pre.rows(m->data, m->pitch * es, columns * es, at, o.pitch, rows);
         o.data = at;
     }
     if (eight(m->type) && !direct_scales(m, columns)) {
         o.scale_pitch = packed_scale_pitch(columns);
         char* at = cv.take((size_t)(rows * o.scale_pitch));
-        if (at) launch_repack(m->scales, m->scale_pitch, (columns + kBlock - 1) / kBlock, at, o.scale_pitch, rows, st);
+        if (at) pre.rows(m->scales, m->scale_pitch, (columns + kBlock - 1) / kBlock, at, o.scale_pitch, rows);
         o.scales = (const uint8_t*)at;
     }
     return o;
@@ -303,12 +313,10 @@ void set_result(Epilogue& e, const last_matrix_t* y, const last_matrix_t* res)
         e.y = y->data;
         e.py = y->pitch;
         e.type = y->type;
-        e.wide = wide(y);
     }
     if (res) {
         e.res = res->data;
         e.pres = res->pitch;
-        e.wide_res = wide(res);
     }
 }
 
@@ -318,7 +326,8 @@ last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, in
 {
     ProductArgs a{};
     const long long bytes = packed_pitch(K, x->type);
-    const Operand p = lay_out(cv, x, rows, K, st), q = lay_out(cv, w, N, K, st);
+    Preparation pre;
+    const Operand p = lay_out(cv, pre, x, rows, K), q = lay_out(cv, pre, w, N, K);
     a.p = p.data;
     a.q = q.data;
     a.pp = p.pitch;
@@ -334,8 +343,8 @@ last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, in
     const ProductPlan plan = plan_product(true, false, rows, N, (bytes + kStep - 1) / kStep);
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
+    pre.launch(st);
     a.e.bias = bias;
-    a.e.wide_bias = (uintptr_t)bias % 16 == 0;
     a.e.act = act;
     set_result(a.e, y, res);
     a.e.kept = eight_of(kept);
@@ -356,7 +365,8 @@ last_status_t run_grad_input(Carver& cv, const last_frames_t* f, long long rows,
 {
     ProductArgs a{};
     const long long bytes = packed_pitch(N, dy->type);
-    const Operand p = lay_out(cv, dy, rows, N, st), q = lay_out(cv, w, N, K, st);
+    Preparation pre;
+    const Operand p = lay_out(cv, pre, dy, rows, N), q = lay_out(cv, pre, w, N, K);
     a.p = p.data;
     a.q = q.data;
     a.pp = p.pitch;
@@ -369,6 +379,7 @@ last_status_t run_grad_input(Carver& cv, const last_frames_t* f, long long rows,
     const ProductPlan plan = plan_product(false, false, rows, K, (bytes + kStep - 1) / kStep);
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
+    pre.launch(st);
     set_result(a.e, dx, nullptr);
     a.e.kept_act = act;
     if (act != LAST_ACT_NONE) a.e.kept = eight_of(kept);
@@ -383,7 +394,8 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
                               int act, const last_matrix_t* dw, float* dbias, hipStream_t st)
 {
     ProductArgs a{};
-    const Operand p = lay_out(cv, dy, rows, N, st);
+    Preparation pre;
+    const Operand p = lay_out(cv, pre, dy, rows, N);
     Operand q;
     if (eight(x->type)) {
         // the activation formed again, once, instead of by every tile that reads it
@@ -394,7 +406,7 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
         if (cv.base && rows > 0) LAST_TRY(run_kept_values(f, rows, K, x, act, &v, st));
         q = Operand{(const char*)v.data, v.pitch * 2, nullptr, 0};
     } else {
-        q = lay_out(cv, x, rows, K, st);
+        q = lay_out(cv, pre, x, rows, K);
     }
     a.p = p.data;
     a.q = q.data;
@@ -407,8 +419,8 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
     set_plan(cv, a, plan, 64, dbias);
     unsigned long long* mask = f->lengths ? (unsigned long long*)cv.take((size_t)((rows + 63) / 64 * 8)) : nullptr;
     if (!cv.base) return LAST_OK;
-    if (mask && rows > 0)
-        hipLaunchKernelGGL(frame_mask_kernel, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, st, frames_of(f), (int)rows, mask);
+    if (mask) pre.mask(f, rows, mask);
+    pre.launch(st);
     a.mask = mask;
     set_result(a.e, dw, nullptr);
     if (dy->type == LAST_BF16) launch_tiles<bf16_t, kAcross, kAcross>(a, plan, st);
@@ -445,7 +457,6 @@ last_status_t run_kept_values(const last_frames_t* f, long long rows, int H, con
     a.H = H;
     a.y = y->data;
     a.py = y->pitch;
-    a.ay = wide(y);
     a.act = act;
     a.ytype = y->type;
     a.kept = eight_of(kept);
@@ -499,13 +510,11 @@ last_status_t last_residual_norm(const last_frames_t* frames, int32_t H, const l
     a.H = H;
     a.x = x->data;
     a.px = x->pitch;
-    a.ax = wide(x);
-    if (residual) { a.res = residual->data; a.pr = residual->pitch; a.ar = wide(residual); }
-    if (s) { a.s = s->data; a.ps = s->pitch; a.as_ = wide(s); }
-    if (y) { a.y = y->data; a.py = y->pitch; a.ay = wide(y); a.ytype = y->type; }
+    if (residual) { a.res = residual->data; a.pr = residual->pitch; }
+    if (s) { a.s = s->data; a.ps = s->pitch; }
+    if (y) { a.y = y->data; a.py = y->pitch; a.ytype = y->type; }
     a.kept = eight_of(kept);
     a.gain = gain;
-    a.ag = (uintptr_t)gain % 16 == 0;
     a.inv = inv;
     a.eps = eps;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -535,19 +544,15 @@ last_status_t last_residual_norm_grad(const last_frames_t* frames, int32_t H, co
     a.H = H;
     a.dy = dy->data;
     a.pdy = dy->pitch;
-    a.ady = wide(dy);
     a.s = s->data;
     a.ps = s->pitch;
-    a.as_ = wide(s);
     a.s_scales = s->scales;
     a.pss = s->scale_pitch;
-    if (ds) { a.ds = ds->data; a.pds = ds->pitch; a.ads = wide(ds); }
+    if (ds) { a.ds = ds->data; a.pds = ds->pitch; }
     a.dx = dx->data;
     a.pdx = dx->pitch;
-    a.adx = wide(dx);
     a.dxtype = dx->type;
     a.gain = gain;
-    a.ag = (uintptr_t)gain % 16 == 0;
     a.inv = inv;
     a.part = dgain ? (float*)ws : nullptr;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -629,7 +634,6 @@ last_status_t last_keep(const last_frames_t* frames, int32_t H, const last_matri
     a.H = H;
     a.x = x->data;
     a.px = x->pitch;
-    a.ax = wide(x);
     a.kept = eight_of(kept);
     hipStream_t st = (hipStream_t)hip_stream;
     const int type = x->type;
@@ -669,10 +673,8 @@ last_status_t last_kept_grad(const last_frames_t* frames, int32_t H, const last_
     a.H = H;
     a.x = dy->data;
     a.px = dy->pitch;
-    a.ax = wide(dy);
     a.y = dx->data;
     a.py = dx->pitch;
-    a.ay = wide(dx);
     a.act = act;
     a.ytype = dx->type;
     a.kept = eight_of(kept);

@@ -18,7 +18,6 @@ struct NormArgs {
     float* inv;
     long long px, pr, ps, py;
     int ytype;
-    bool ax, ar, as_, ay, ag;        // groups of eight begin at multiples of 16 bytes (or their size)
     float eps;
     Eight kept;
 };
@@ -55,14 +54,14 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_kernel(Norm
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int h = (c * WPR * kWave + lane) * 8;
-            load8<X>(a.x, (size_t)row * a.px + h, a.H - h, a.ax, v[c]);
+            load8<X>(a.x, (size_t)row * a.px + h, a.H - h, v[c]);
         }
         if (a.res) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int h = (c * WPR * kWave + lane) * 8;
                 float r[8];
-                load8<X>(a.res, (size_t)row * a.pr + h, a.H - h, a.ar, r);
+                load8<X>(a.res, (size_t)row * a.pr + h, a.H - h, r);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[c][k] += r[k];
             }
@@ -83,12 +82,12 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_kernel(Norm
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int h = (c * WPR * kWave + lane) * 8;
-        if (a.s) store8<X>(a.s, (size_t)row * a.ps + h, a.H - h, a.as_, v[c]);
+        if (a.s) store8<X>(a.s, (size_t)row * a.ps + h, a.H - h, v[c]);
         float g[8];
-        load8<float>(a.gain, h, a.H - h, a.ag, g);
+        load8<float>(a.gain, h, a.H - h, g);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[c][k] = there ? v[c][k] * inv * g[k] : 0.f;
-        if (a.y) store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, a.ay, v[c]);
+        if (a.y) store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, v[c]);
         if (a.kept.q) store_eight(a.kept, row, h, a.H - h, (lane & 3) == 0, quad_max(top8(v[c])), v[c]);
     }
 }
@@ -103,13 +102,12 @@ struct NormGradArgs {
     float* part;                     // [workgroups][H] partial sums of dgain, or null
     long long pdy, ps, pds, pdx, pss;
     int dxtype;
-    bool ady, as_, ads, adx, ag;
 };
 
 template <typename S>
 __device__ __forceinline__ void load_s(const NormGradArgs& a, int row, int h, float* v)
 {
-    load8<S>(a.s, (size_t)row * a.ps + h, a.H - h, a.as_, v);
+    load8<S>(a.s, (size_t)row * a.ps + h, a.H - h, v);
     if constexpr (Elt<S>::size == 1) {
         const float sc = h < a.H ? scale_value(a.s_scales[(size_t)row * a.pss + h / kBlock]) : 0.f;
 #pragma unroll
@@ -117,11 +115,11 @@ __device__ __forceinline__ void load_s(const NormGradArgs& a, int row, int h, fl
     }
 }
 
-__device__ __forceinline__ void load_dx_type(int type, const void* p, size_t i, int n, bool aligned, float* v)
+__device__ __forceinline__ void load_dx_type(int type, const void* p, size_t i, int n, float* v)
 {
-    if (type == LAST_BF16) load8<bf16_t>(p, i, n, aligned, v);
-    else if (type == LAST_F16) load8<f16_t>(p, i, n, aligned, v);
-    else load8<float>(p, i, n, aligned, v);
+    if (type == LAST_BF16) load8<bf16_t>(p, i, n, v);
+    else if (type == LAST_F16) load8<f16_t>(p, i, n, v);
+    else load8<float>(p, i, n, v);
 }
 
 // Every wavefront (WPR = 1) or workgroup goes over its rows and keeps the sums of its columns of dgain in registers;
@@ -148,7 +146,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int h = (c * WPR * kWave + lane) * 8;
-                store8_as(a.dxtype, a.dx, (size_t)row * a.pdx + h, a.H - h, a.adx, u[0]);
+                store8_as(a.dxtype, a.dx, (size_t)row * a.pdx + h, a.H - h, u[0]);
             }
             if (WPR > 1) __syncthreads();                    // (row_sum's, where `turn` counts)
             continue;
@@ -157,14 +155,14 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int h = (c * WPR * kWave + lane) * 8;
-            load8<DY>(a.dy, (size_t)row * a.pdy + h, a.H - h, a.ady, u[c]);
+            load8<DY>(a.dy, (size_t)row * a.pdy + h, a.H - h, u[c]);
             load_s<S>(a, row, h, s[c]);
         }
         if (a.ds) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int h = (c * WPR * kWave + lane) * 8;
-                load_dx_type(a.dxtype, a.ds, (size_t)row * a.pds + h, a.H - h, a.ads, d[c]);
+                load_dx_type(a.dxtype, a.ds, (size_t)row * a.pds + h, a.H - h, d[c]);
             }
         }
         float dot = 0.f;
@@ -172,7 +170,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel
         for (int c = 0; c < CH; ++c) {
             const int h = (c * WPR * kWave + lane) * 8;
             float g[8];
-            load8<float>(a.gain, h, a.H - h, a.ag, g);
+            load8<float>(a.gain, h, a.H - h, g);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 dg[c][k] += u[c][k] * s[c][k] * inv;
@@ -191,7 +189,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel
 #pragma unroll
                 for (int k = 0; k < 8; ++k) u[c][k] += d[c][k];
             }
-            store8_as(a.dxtype, a.dx, (size_t)row * a.pdx + h, a.H - h, a.adx, u[c]);
+            store8_as(a.dxtype, a.dx, (size_t)row * a.pdx + h, a.H - h, u[c]);
         }
     }
     if (!a.part) return;

@@ -22,7 +22,6 @@
 namespace last {
 
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef int i8x __attribute__((ext_vector_type(8)));
 typedef int i4x __attribute__((ext_vector_type(4)));
@@ -42,7 +41,6 @@ struct Epilogue {
     void* y;                                     // null: 8-bit values `out` instead
     long long py;
     int type;
-    bool wide, wide_res, wide_bias;              // eight elements at a time are aligned
     Eight out;                                   // result in 8 bits
     Eight kept;                                  // forward: written with the sums + bias; of the input: read
     int kept_act;                                // of the input: times act' of what is kept (LAST_ACT_NONE: nothing is)
@@ -210,11 +208,11 @@ struct Fetched {
 };
 
 template <typename E>
-__device__ __forceinline__ void fetch8(const void* p, size_t i, int n, bool aligned, Fetched* f)
+__device__ __forceinline__ void fetch8(const void* p, size_t i, int n, Fetched* f)
 {
-    if (aligned && n >= 8) {
-        f->a = *(const u4*)((const char*)p + i * Elt<E>::size);
-        if constexpr (Elt<E>::size == 4) f->b = *(const u4*)((const char*)p + i * 4 + 16);
+    if (n >= 8) {
+        f->a = *(const u4_any*)((const char*)p + i * Elt<E>::size);
+        if constexpr (Elt<E>::size == 4) f->b = *(const u4_any*)((const char*)p + i * 4 + 16);
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -237,14 +235,14 @@ __device__ __forceinline__ Fetched fetch(const Epilogue& e, int m, int n, int P,
     if (left > 0) {
         if (e.kept_act != LAST_ACT_NONE) {
             unsigned lo, hi;
-            load_codes(e.kept.q + (size_t)m * e.kept.pitch, n, left, e.kept.aligned, &lo, &hi);
+            load_codes(e.kept.q + (size_t)m * e.kept.pitch, n, left, &lo, &hi);
             f.a[0] = lo;
             f.a[1] = hi;
             f.scale = e.kept.scales[(size_t)m * e.kept.scale_pitch + n / kBlock];
         } else if (e.res) {
             const size_t at = (size_t)m * e.pres + n;
-            if (e.type == LAST_F32) fetch8<float>(e.res, at, left, e.wide_res, &f);
-            else fetch8<bf16_t>(e.res, at, left, e.wide_res, &f);
+            if (e.type == LAST_F32) fetch8<float>(e.res, at, left, &f);
+            else fetch8<bf16_t>(e.res, at, left, &f);
         }
     }
     return f;
@@ -287,27 +285,25 @@ __device__ __forceinline__ void finish(const Epilogue& e, int m, int n, int P, i
         for (int u = 0; u < 8; ++u) v[u] += r[u];
     }
     if (e.out.q) store_eight(e.out, m, n, left, (n & (kBlock - 1)) == 0, quad_max(top8(v)), v);
-    if (e.y && left > 0) store8_as(e.type, e.y, (size_t)m * e.py + n, left, e.wide, v);
+    if (e.y && left > 0) store8_as(e.type, e.y, (size_t)m * e.py + n, left, v);
 }
 
 __device__ __forceinline__ void load_bias(const Epilogue& e, int n, int Q, float* b)
 {
-    load8<float>(e.bias, n, e.bias ? Q - n : 0, e.wide_bias, b);
+    load8<float>(e.bias, n, e.bias ? Q - n : 0, b);
 }
 
-// Rows of results that are all inside and aligned, the common case, in a loop without a branch around a load or a store, so that
+// Eight columns that are all inside of rows that all exist, the common case, in a loop without a branch around a load or a store, so that
 // no store is waited for (they count with the loads, in order): an extra load is two rows ahead of its use.
 enum { kRowsPlain = 0, kRowsResidual = 1, kRowsSlope = 2, kRowsKeep = 3, kRowsWide = 4, kRowsEight = 5, kRowsAny = 6 };
 
 __device__ __forceinline__ int rows_kind(const Epilogue& e)
 {
-    if (e.out.q) return !e.res && !e.kept.q && e.out.aligned ? kRowsEight : kRowsAny;
-    if (!e.wide) return kRowsAny;
+    if (e.out.q) return !e.res && !e.kept.q ? kRowsEight : kRowsAny;
     if (e.type == LAST_F32) return !e.res && !e.kept.q ? kRowsWide : kRowsAny;
-    if (e.kept_act != LAST_ACT_NONE) return e.kept.aligned ? kRowsSlope : kRowsAny;
-    if (e.res) return e.wide_res && !e.kept.q ? kRowsResidual : kRowsAny;
-    if (e.kept.q) return e.kept.aligned ? kRowsKeep : kRowsAny;
-    return kRowsPlain;
+    if (e.kept_act != LAST_ACT_NONE) return kRowsSlope;
+    if (e.res) return !e.kept.q ? kRowsResidual : kRowsAny;
+    return e.kept.q ? kRowsKeep : kRowsPlain;
 }
 
 __device__ __forceinline__ void unpack8(int type, u4 w, float* r)
@@ -348,9 +344,9 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
     };
     const auto extra = [&](int i) {
         Extra x{};
-        if constexpr (KIND == kRowsResidual) x.w = *(const u4*)((const uint16_t*)e.res + at(i) * e.pres + n);
+        if constexpr (KIND == kRowsResidual) x.w = *(const u4_any*)((const uint16_t*)e.res + at(i) * e.pres + n);
         if constexpr (KIND == kRowsSlope) {
-            const u2 q = *(const u2*)(e.kept.q + at(i) * e.kept.pitch + n);
+            const u2 q = *(const u2_any*)(e.kept.q + at(i) * e.kept.pitch + n);
             x.w[0] = q[0];
             x.w[1] = q[1];
             x.scale = e.kept.scales[at(i) * e.kept.scale_pitch + n / kBlock];
@@ -383,7 +379,7 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
         if constexpr (KIND == kRowsKeep) {
             unsigned lo, hi;
             const unsigned byte = encode_block(e.kept.e4m3, v, &lo, &hi);
-            *(u2*)(e.kept.q + row * e.kept.pitch + n) = u2{lo, hi};
+            *(u2_any*)(e.kept.q + row * e.kept.pitch + n) = u2{lo, hi};
             e.kept.scales[row * e.kept.scale_pitch + n / kBlock] = (uint8_t)byte;    // (all four lanes of the block, the same)
         }
         activate8(e.act, v);
@@ -396,12 +392,12 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
         if constexpr (KIND == kRowsEight) {
             unsigned lo, hi;
             const unsigned byte = encode_block(e.out.e4m3, v, &lo, &hi);
-            *(u2*)(e.out.q + row * e.out.pitch + n) = u2{lo, hi};
+            *(u2_any*)(e.out.q + row * e.out.pitch + n) = u2{lo, hi};
             e.out.scales[row * e.out.scale_pitch + n / kBlock] = (uint8_t)byte;
         } else if constexpr (KIND == kRowsWide) {
             Elt<float>::put8(e.y, row * e.py + n, v);
         } else {
-            *(u4*)((uint16_t*)e.y + row * e.py + n) = pack8(e.type, v);
+            *(u4_any*)((uint16_t*)e.y + row * e.py + n) = pack8(e.type, v);
         }
     }
 }
@@ -681,7 +677,6 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
         e.y = e.part + (size_t)blockIdx.y * a.P * a.Q;
         e.py = a.Q;
         e.type = LAST_F32;
-        e.wide = (a.Q & 3) == 0;
     }
     const int kind = rows_kind(e);
     float bias[8];
@@ -710,10 +705,18 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
         // bits of the rows that exist
         const int mine_row = first + lane % (XS * 16);
         const unsigned long long rows = __ballot(mine_row < a.P && (LP == kAcross || frame_exists(a.frames, mine_row)));
-        const bool inside = rows == ~0ull && q0 + (wq + 1) * kCols <= a.Q;
         const size_t m0 = (size_t)first + lane / kLanes;
         constexpr int kCount = XS * 16 / kRows;
-        if (!inside || kind == kRowsAny) {
+        // blocks in 8 bits need all their lanes, else a lane goes by its own columns
+        const int last = kind == kRowsKeep || kind == kRowsEight ? q0 + (wq + 1) * kCols : n + 8;
+        if (rows == ~0ull && last <= a.Q && kind != kRowsAny) {
+            if (kind == kRowsPlain) fast_rows<kRowsPlain>(e, m0, n, kRows, kCount, bias, get_mine);
+            else if (kind == kRowsResidual) fast_rows<kRowsResidual>(e, m0, n, kRows, kCount, bias, get_mine);
+            else if (kind == kRowsSlope) fast_rows<kRowsSlope>(e, m0, n, kRows, kCount, bias, get_mine);
+            else if (kind == kRowsKeep) fast_rows<kRowsKeep>(e, m0, n, kRows, kCount, bias, get_mine);
+            else if (kind == kRowsEight) fast_rows<kRowsEight>(e, m0, n, kRows, kCount, bias, get_mine);
+            else fast_rows<kRowsWide>(e, m0, n, kRows, kCount, bias, get_mine);
+        } else if (n - c < a.Q) {                            // (some column of the wavefront)
             bool there = rows >> (lane / kLanes) & 1;
             Fetched f = fetch(e, (int)m0, n, a.P, a.Q, there);
 #pragma unroll 1
@@ -727,18 +730,6 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
                 f = f_next;
                 there = there_next;
             }
-        } else if (kind == kRowsPlain) {
-            fast_rows<kRowsPlain>(e, m0, n, kRows, kCount, bias, get_mine);
-        } else if (kind == kRowsResidual) {
-            fast_rows<kRowsResidual>(e, m0, n, kRows, kCount, bias, get_mine);
-        } else if (kind == kRowsSlope) {
-            fast_rows<kRowsSlope>(e, m0, n, kRows, kCount, bias, get_mine);
-        } else if (kind == kRowsKeep) {
-            fast_rows<kRowsKeep>(e, m0, n, kRows, kCount, bias, get_mine);
-        } else if (kind == kRowsEight) {
-            fast_rows<kRowsEight>(e, m0, n, kRows, kCount, bias, get_mine);
-        } else {
-            fast_rows<kRowsWide>(e, m0, n, kRows, kCount, bias, get_mine);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -862,7 +853,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
     if (m < a.P) {
         for (int s = 0; s < splits; ++s) {
             float t[8];
-            load8<float>(a.e.part + ((size_t)s * a.P + m) * a.Q, n, a.Q - n, (a.Q & 3) == 0, t);
+            load8<float>(a.e.part + ((size_t)s * a.P + m) * a.Q, n, a.Q - n, t);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] += t[k];
         }
@@ -878,34 +869,49 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
     finish(a.e, m, n, a.P, a.Q, there, bias, fetch(a.e, m, n, a.P, a.Q, there), v);
 }
 
-// ---- rows of `bytes` bytes laid out at multiples of 16 with zeros behind them, 16 bytes a thread
-__global__ __launch_bounds__(256) void repack_kernel(const uint8_t* in, long long pitch, int bytes, uint8_t* out, int out_pitch, long long pieces)
+// ---- before a product, in one launch: rows of operands laid out at multiples of 16 bytes with zeros behind them, 16 bytes a
+// thread, and which rows exist, a bit each
+struct PrepareArgs {
+    struct Rows {
+        const uint8_t* in;
+        uint8_t* out;
+        long long pitch, out_pitch, count;       // bytes from a row to the next, rows
+        int bytes;                               // of a row
+        unsigned groups;                         // workgroups that do it
+    } rows[4];
+    unsigned groups;                             // of all four
+    Frames frames;
+    int frame_rows;
+    unsigned long long* mask;
+};
+
+__global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a)
 {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= pieces) return;
-    const int per = out_pitch / 16;
-    const long long row = i / per;
+    unsigned group = blockIdx.x;
+    if (group >= a.groups) {
+        const int row = (int)((group - a.groups) * 256 + threadIdx.x);
+        const unsigned long long m = __ballot(row < a.frame_rows && frame_exists(a.frames, row));
+        if ((threadIdx.x & (kWave - 1)) == 0 && row < a.frame_rows) a.mask[row >> 6] = m;
+        return;
+    }
+    int k = 0;
+    while (group >= a.rows[k].groups) group -= a.rows[k++].groups;
+    const auto& r = a.rows[k];
+    const unsigned per = (unsigned)(r.out_pitch / 16);
+    const unsigned long long i = (unsigned long long)group * 256 + threadIdx.x;
+    const unsigned long long row = i >> 32 ? i / per : (unsigned)i / per;
     const int at = (int)(i - row * per) * 16;
-    const uint8_t* p = in + row * pitch + at;
-    unsigned w[4] = {0u, 0u, 0u, 0u};
-    if (((uintptr_t)in & 1) == 0 && (pitch & 1) == 0 && (bytes & 1) == 0) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (at + 2 * k < bytes) w[k >> 1] |= (unsigned)*(const uint16_t*)(p + 2 * k) << (16 * (k & 1));
+    if (row >= (unsigned long long)r.count) return;
+    const uint8_t* p = r.in + row * r.pitch + at;
+    u4 w = {0u, 0u, 0u, 0u};
+    if (at + 16 <= r.bytes) {
+        w = *(const u4_byte*)p;
     } else {
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
-            if (at + k < bytes) w[k >> 2] |= (unsigned)p[k] << (8 * (k & 3));
+        for (int j = 0; j < 16; ++j)
+            if (at + j < r.bytes) w[j >> 2] |= (unsigned)p[j] << (8 * (j & 3));
     }
-    *(u4*)(out + row * out_pitch + at) = u4{w[0], w[1], w[2], w[3]};
-}
-
-// ---- which rows exist, a bit each
-__global__ __launch_bounds__(256) void frame_mask_kernel(Frames f, int rows, unsigned long long* mask)
-{
-    const int row = (int)(blockIdx.x * 256 + threadIdx.x);
-    const unsigned long long m = __ballot(row < rows && frame_exists(f, row));
-    if ((threadIdx.x & (kWave - 1)) == 0 && row < rows) mask[row >> 6] = m;
+    *(u4*)(r.out + row * r.out_pitch + at) = w;
 }
 
 }  // namespace last
