@@ -19,69 +19,110 @@ struct KeepArgs {
     Eight kept;
 };
 
-__device__ __forceinline__ bool keep_place(const KeepArgs& a, int* row, int* h)
+// Eight columns in each of kKeepDeep places, the loads of all under way before the first is worked on.
+constexpr int kKeepDeep = 4;
+
+struct KeepPlace {
+    int row, h;
+    bool in;                         // of the matrix's rows
+    int n;                           // columns to read: 0 past the end, or where no frame is
+};
+
+__device__ __forceinline__ KeepPlace keep_place(const KeepArgs& a, int d)
 {
-    const unsigned i = blockIdx.x * 256u + threadIdx.x;
+    const unsigned i = (blockIdx.x * kKeepDeep + d) * 256u + threadIdx.x;
     const unsigned r = i / (unsigned)a.groups;
-    *row = a.row0 + (int)r;
-    *h = (int)(i - r * a.groups) * 8;
-    return r < (unsigned)a.rows;
+    KeepPlace p;
+    p.row = a.row0 + (int)r;
+    p.h = (int)(i - r * a.groups) * 8;
+    p.in = r < (unsigned)a.rows;
+    p.n = p.in && frame_exists(a.frames, p.row) ? a.H - p.h : 0;
+    return p;
 }
 
 template <typename X>
 __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a)
 {
-    int row, h;
-    const bool in = keep_place(a, &row, &h);
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (in && h < a.H && frame_exists(a.frames, row)) load8<X>(a.x, (size_t)row * a.px + h, a.H - h, v);
-    const unsigned top = quad_max(top8(v));
-    if (in) store_eight(a.kept, row, h, a.H - h, (h & (kBlock - 1)) == 0, top, v);
+    KeepPlace p[kKeepDeep];
+    Raw<X> x[kKeepDeep];
+#pragma unroll
+    for (int d = 0; d < kKeepDeep; ++d) p[d] = keep_place(a, d);
+#pragma unroll
+    for (int d = 0; d < kKeepDeep; ++d) x[d] = raw8<X>(a.x, (size_t)p[d].row * a.px + p[d].h, p[d].n);
+#pragma unroll
+    for (int d = 0; d < kKeepDeep; ++d) {
+        float v[8];
+        unpack<X>(x[d], v);
+        const unsigned top = quad_max(top8(v));
+        if (p[d].in) store_eight(a.kept, p[d].row, p[d].h, a.H - p[d].h, (p[d].h & (kBlock - 1)) == 0, top, v);
+    }
 }
 
-__device__ __forceinline__ void load_eight(const Eight& k, size_t row, int h, int n, float* v)
+struct RawEight {
+    Raw<i8_t> q;
+    unsigned scale;
+};
+
+__device__ __forceinline__ RawEight raw_eight(const Eight& k, const KeepPlace& p)
 {
-    unsigned lo, hi;
-    load_codes(k.q + row * k.pitch, h, n, &lo, &hi);
-    const float sc = scale_value(k.scales[row * k.scale_pitch + h / kBlock]);
-    if (k.e4m3) {
-        decode4<true>(lo, sc, v);
-        decode4<true>(hi, sc, v + 4);
+    RawEight r{};
+    r.q = raw8<i8_t>(k.q, (size_t)p.row * k.pitch + p.h, p.n);
+    if (p.n > 0) r.scale = k.scales[(size_t)p.row * k.scale_pitch + p.h / kBlock];
+    return r;
+}
+
+__device__ __forceinline__ void unpack_eight(bool e4m3, const RawEight& r, float* v)
+{
+    const float sc = scale_value(r.scale);
+    if (e4m3) {
+        decode4<true>(r.q.a[0], sc, v);
+        decode4<true>(r.q.a[1], sc, v + 4);
     } else {
-        decode4<false>(lo, sc, v);
-        decode4<false>(hi, sc, v + 4);
+        decode4<false>(r.q.a[0], sc, v);
+        decode4<false>(r.q.a[1], sc, v + 4);
     }
 }
 
 // y = act(kept)
 __global__ __launch_bounds__(256) void kept_values_kernel(KeepArgs a)
 {
-    int row, h;
-    if (!keep_place(a, &row, &h) || h >= a.H) return;
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (frame_exists(a.frames, row)) {
-        load_eight(a.kept, row, h, a.H - h, v);
+    KeepPlace p[kKeepDeep];
+    RawEight x[kKeepDeep];
+#pragma unroll
+    for (int d = 0; d < kKeepDeep; ++d) p[d] = keep_place(a, d);
+#pragma unroll
+    for (int d = 0; d < kKeepDeep; ++d) x[d] = raw_eight(a.kept, p[d]);
+#pragma unroll
+    for (int d = 0; d < kKeepDeep; ++d) {
+        float v[8];
+        unpack_eight(a.kept.e4m3, x[d], v);                  // (act(0) = 0 for each)
         activate8(a.act, v);
+        store8_as(a.ytype, a.y, (size_t)p[d].row * a.py + p[d].h, p[d].in ? a.H - p[d].h : 0, v);
     }
-    store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, v);
 }
 
 // y = dy act'(kept)
 template <typename X>
 __global__ __launch_bounds__(256) void kept_grad_kernel(KeepArgs a)
 {
-    int row, h;
-    if (!keep_place(a, &row, &h) || h >= a.H) return;
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, d[8];
-    if (frame_exists(a.frames, row)) {
-        load8<X>(a.x, (size_t)row * a.px + h, a.H - h, d);
-        load_eight(a.kept, row, h, a.H - h, v);
-        times_slope(a.act, v, d);
-    } else {
+    KeepPlace p[kKeepDeep];
+    RawEight x[kKeepDeep];
+    Raw<X> dy[kKeepDeep];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) d[k] = 0.f;
+    for (int d = 0; d < kKeepDeep; ++d) p[d] = keep_place(a, d);
+#pragma unroll
+    for (int d = 0; d < kKeepDeep; ++d) {
+        x[d] = raw_eight(a.kept, p[d]);
+        dy[d] = raw8<X>(a.x, (size_t)p[d].row * a.px + p[d].h, p[d].n);
     }
-    store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, d);
+#pragma unroll
+    for (int d = 0; d < kKeepDeep; ++d) {
+        float h[8], v[8];
+        unpack_eight(a.kept.e4m3, x[d], h);
+        unpack<X>(dy[d], v);
+        times_slope(a.act, h, v);
+        store8_as(a.ytype, a.y, (size_t)p[d].row * a.py + p[d].h, p[d].in ? a.H - p[d].h : 0, v);
+    }
 }
 
 }  // namespace last

@@ -117,14 +117,7 @@ __device__ __forceinline__ unsigned umax(unsigned a, unsigned b) { return a > b 
 template <typename E> struct Elt;
 template <> struct Elt<float> {
     static constexpr int type = LAST_F32, size = 4;
-    static __device__ float get(const void* p, size_t i) { return ((const float*)p)[i]; }
     static __device__ void put(void* p, size_t i, float v) { ((float*)p)[i] = v; }
-    static __device__ void get8(const void* p, size_t i, float* v)
-    {
-        const f4 a = *(const f4_any*)((const float*)p + i), b = *(const f4_any*)((const float*)p + i + 4);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { v[k] = a[k]; v[4 + k] = b[k]; }
-    }
     static __device__ void put8(void* p, size_t i, const float* v)
     {
         *(f4_any*)((float*)p + i) = f4{v[0], v[1], v[2], v[3]};
@@ -133,14 +126,7 @@ template <> struct Elt<float> {
 };
 template <> struct Elt<bf16_t> {
     static constexpr int type = LAST_BF16, size = 2;
-    static __device__ float get(const void* p, size_t i) { return bf16_to_float(((const uint16_t*)p)[i]); }
     static __device__ void put(void* p, size_t i, float v) { ((uint16_t*)p)[i] = (uint16_t)bf16_pair(v, 0.f); }
-    static __device__ void get8(const void* p, size_t i, float* v)
-    {
-        const u4 a = *(const u4_any*)((const uint16_t*)p + i);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { v[2 * k] = bf16_to_float(a[k] & 0xffffu); v[2 * k + 1] = __uint_as_float(a[k] & 0xffff0000u); }
-    }
     static __device__ void put8(void* p, size_t i, const float* v)
     {
         *(u4_any*)((uint16_t*)p + i) = u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
@@ -148,14 +134,7 @@ template <> struct Elt<bf16_t> {
 };
 template <> struct Elt<f16_t> {
     static constexpr int type = LAST_F16, size = 2;
-    static __device__ float get(const void* p, size_t i) { return (float)((const _Float16*)p)[i]; }
     static __device__ void put(void* p, size_t i, float v) { ((_Float16*)p)[i] = (_Float16)v; }
-    static __device__ void get8(const void* p, size_t i, float* v)
-    {
-        const h8 a = *(const h8_any*)((const _Float16*)p + i);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = (float)a[k];
-    }
     static __device__ void put8(void* p, size_t i, const float* v)
     {
         *(u4_any*)((_Float16*)p + i) = u4{f16_pair(v[0], v[1]), f16_pair(v[2], v[3]), f16_pair(v[4], v[5]), f16_pair(v[6], v[7])};
@@ -164,32 +143,75 @@ template <> struct Elt<f16_t> {
 // codes of 8-bit values; the caller brings the scale of their block
 template <bool E4M3> struct EltCodes {
     static constexpr int type = E4M3 ? LAST_E4M3 : LAST_I8, size = 1;
-    static __device__ void get8(const void* p, size_t i, float* v)
-    {
-        const u2 a = *(const u2_any*)((const uint8_t*)p + i);
-        decode4<E4M3>(a[0], 1.f, v);
-        decode4<E4M3>(a[1], 1.f, v + 4);
-    }
-    static __device__ float get(const void* p, size_t i)
-    {
-        float v[4];
-        decode4<E4M3>(((const uint8_t*)p)[i], 1.f, v);
-        return v[0];
-    }
 };
 template <> struct Elt<i8_t> : EltCodes<false> {};
 template <> struct Elt<e4m3_t> : EltCodes<true> {};
 
+// as they stand in memory: to be sent for ahead of their use
+template <typename E> struct Raw {
+    u4 a;
+};
+template <> struct Raw<float> {
+    u4 a, b;
+};
+template <> struct Raw<i8_t> {
+    u2 a;
+};
+template <> struct Raw<e4m3_t> {
+    u2 a;
+};
+
 template <typename E>
-__device__ __forceinline__ void load8(const void* p, size_t i, int n, float* v)
+__device__ __forceinline__ Raw<E> raw8(const void* p, size_t i, int n)
 {
+    Raw<E> r{};
     if (n >= 8) {
-        Elt<E>::get8(p, i, v);
+        if constexpr (Elt<E>::size == 1) {
+            r.a = *(const u2_any*)((const uint8_t*)p + i);
+        } else {
+            r.a = *(const u4_any*)((const char*)p + i * Elt<E>::size);
+            if constexpr (Elt<E>::size == 4) r.b = *(const u4_any*)((const char*)p + i * 4 + 16);
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = k < n ? Elt<E>::get(p, i + k) : 0.f;
+        for (int k = 0; k < 7; ++k) {
+            if (k >= n) continue;
+            if constexpr (Elt<E>::size == 4) {
+                const unsigned w = ((const unsigned*)p)[i + k];
+                if (k < 4) r.a[k] = w;
+                else r.b[k & 3] = w;
+            } else if constexpr (Elt<E>::size == 2) {
+                r.a[k >> 1] |= (unsigned)((const uint16_t*)p)[i + k] << (16 * (k & 1));
+            } else {
+                r.a[k >> 2] |= (unsigned)((const uint8_t*)p)[i + k] << (8 * (k & 3));
+            }
+        }
+    }
+    return r;
+}
+
+// (8-bit values: codes, the caller brings the scale of their block)
+template <typename E>
+__device__ __forceinline__ void unpack(const Raw<E>& r, float* v)
+{
+    if constexpr (Elt<E>::type == LAST_F32) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { v[k] = __uint_as_float(r.a[k]); v[4 + k] = __uint_as_float(r.b[k]); }
+    } else if constexpr (Elt<E>::type == LAST_BF16) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { v[2 * k] = bf16_to_float(r.a[k] & 0xffffu); v[2 * k + 1] = __uint_as_float(r.a[k] & 0xffff0000u); }
+    } else if constexpr (Elt<E>::type == LAST_F16) {
+        const h8 h = __builtin_bit_cast(h8, r.a);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = (float)h[k];
+    } else {
+        decode4<Elt<E>::type == LAST_E4M3>(r.a[0], 1.f, v);
+        decode4<Elt<E>::type == LAST_E4M3>(r.a[1], 1.f, v + 4);
     }
 }
+
+template <typename E>
+__device__ __forceinline__ void load8(const void* p, size_t i, int n, float* v) { unpack<E>(raw8<E>(p, i, n), v); }
 
 template <typename E>
 __device__ __forceinline__ void store8(void* p, size_t i, int n, const float* v)

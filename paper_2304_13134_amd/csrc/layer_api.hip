@@ -94,19 +94,29 @@ void launch_norm(const NormArgs& a, hipStream_t st)
     else hipLaunchKernelGGL((norm_kernel<X, 16, 2>), dim3(a.rows), dim3(1024), 0, st, a);
 }
 
-// workgroups of the gradient: each leaves a row of partial sums of dgain
-constexpr int kNormGradGroups = 768;
-int norm_grad_groups(long long rows, int H) { return (int)std::min<long long>(H <= 2048 ? (rows + 3) / 4 : rows, kNormGradGroups); }
+// Workgroups of the gradient: as many as are resident, since each leaves a row of partial sums of dgain.
+int norm_grad_groups(long long rows, int H)
+{
+    if (H <= 1024) return (int)std::min<long long>((rows + 3) / 4, 1024);
+    return (int)std::min<long long>(rows, H <= 4096 ? 1024 : 512);
+}
+
+template <typename DY, typename S, bool DS>
+void launch_norm_grad(const NormGradArgs& a, int groups, hipStream_t st)
+{
+    if (a.H <= 512) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 1, 1, DS>), dim3(groups), dim3(256), 0, st, a);
+    else if (a.H <= 1024) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 1, 2, DS>), dim3(groups), dim3(256), 0, st, a);
+    else if (a.H <= 2048) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 4, 1, DS>), dim3(groups), dim3(256), 0, st, a);
+    else if (a.H <= 4096) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 4, 2, DS>), dim3(groups), dim3(256), 0, st, a);
+    else if (a.H <= 8192) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 16, 1, DS>), dim3(groups), dim3(1024), 0, st, a);
+    else hipLaunchKernelGGL((norm_grad_kernel<DY, S, 16, 2, DS>), dim3(groups), dim3(1024), 0, st, a);
+}
 
 template <typename DY, typename S>
 void launch_norm_grad(const NormGradArgs& a, int groups, hipStream_t st)
 {
-    if (a.H <= 512) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 1, 1>), dim3(groups), dim3(256), 0, st, a);
-    else if (a.H <= 1024) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 1, 2>), dim3(groups), dim3(256), 0, st, a);
-    else if (a.H <= 2048) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 1, 4>), dim3(groups), dim3(256), 0, st, a);
-    else if (a.H <= 4096) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 4, 2>), dim3(groups), dim3(256), 0, st, a);
-    else if (a.H <= 8192) hipLaunchKernelGGL((norm_grad_kernel<DY, S, 16, 1>), dim3(groups), dim3(1024), 0, st, a);
-    else hipLaunchKernelGGL((norm_grad_kernel<DY, S, 16, 2>), dim3(groups), dim3(1024), 0, st, a);
+    if (a.ds) launch_norm_grad<DY, S, true>(a, groups, st);
+    else launch_norm_grad<DY, S, false>(a, groups, st);
 }
 
 // dy and s of one plain type, dy in 32 bits beside s in 16, or s in 8 bits
@@ -436,16 +446,16 @@ last_status_t check_ws(void* ws, size_t have, size_t need)
     return LAST_OK;
 }
 
-// rows of the element-wise calls in launches of at most 2^30 threads
+// rows of the element-wise calls in launches of at most 2^29 places
 template <typename Launch>
 last_status_t in_pieces(KeepArgs a, long long rows, Launch launch)
 {
     a.groups = (a.H + kBlock - 1) / kBlock * 4;
-    const long long most = std::max(1ll, (1ll << 30) / a.groups);
+    const long long most = std::max(1ll, (1ll << 29) / a.groups);
     for (long long r = 0; r < rows; r += most) {
         a.row0 = (int)r;
         a.rows = (int)std::min(most, rows - r);
-        launch(a, dim3((unsigned)(((long long)a.rows * a.groups + 255) / 256)));
+        launch(a, dim3((unsigned)(((long long)a.rows * a.groups + 256 * kKeepDeep - 1) / (256 * kKeepDeep))));
     }
     return hip_done();
 }

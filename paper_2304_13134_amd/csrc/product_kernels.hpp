@@ -210,27 +210,6 @@ struct Fetched {
     unsigned scale;
 };
 
-template <typename E>
-__device__ __forceinline__ void fetch8(const void* p, size_t i, int n, Fetched* f)
-{
-    if (n >= 8) {
-        f->a = *(const u4_any*)((const char*)p + i * Elt<E>::size);
-        if constexpr (Elt<E>::size == 4) f->b = *(const u4_any*)((const char*)p + i * 4 + 16);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if constexpr (Elt<E>::size == 4) {
-                const unsigned w = k < n ? ((const unsigned*)p)[i + k] : 0u;
-                if (k < 4) f->a[k] = w;
-                else f->b[k - 4] = w;
-            } else {
-                const unsigned w = k < n ? ((const uint16_t*)p)[i + k] : 0u;
-                f->a[k >> 1] = k & 1 ? f->a[k >> 1] | w << 16 : w;
-            }
-        }
-    }
-}
-
 __device__ __forceinline__ Fetched fetch(const Epilogue& e, int m, int n, int P, int Q, bool there)
 {
     Fetched f{};
@@ -244,8 +223,13 @@ __device__ __forceinline__ Fetched fetch(const Epilogue& e, int m, int n, int P,
             f.scale = e.kept.scales[(size_t)m * e.kept.scale_pitch + n / kBlock];
         } else if (e.res) {
             const size_t at = (size_t)m * e.pres + n;
-            if (e.type == LAST_F32) fetch8<float>(e.res, at, left, &f);
-            else fetch8<bf16_t>(e.res, at, left, &f);
+            if (e.type == LAST_F32) {
+                const Raw<float> r = raw8<float>(e.res, at, left);
+                f.a = r.a;
+                f.b = r.b;
+            } else {
+                f.a = raw8<bf16_t>(e.res, at, left).a;
+            }
         }
     }
     return f;
@@ -273,17 +257,9 @@ __device__ __forceinline__ void finish(const Epilogue& e, int m, int n, int P, i
     activate8(e.act, v);
     if (e.res) {
         float r[8];
-        if (e.type == LAST_F32) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) { r[u] = __uint_as_float(f.a[u]); r[4 + u] = __uint_as_float(f.b[u]); }
-        } else if (e.type == LAST_BF16) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) { r[2 * u] = bf16_to_float(f.a[u] & 0xffffu); r[2 * u + 1] = __uint_as_float(f.a[u] & 0xffff0000u); }
-        } else {
-            const h8 h = __builtin_bit_cast(h8, f.a);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) r[u] = (float)h[u];
-        }
+        if (e.type == LAST_F32) unpack<float>(Raw<float>{f.a, f.b}, r);
+        else if (e.type == LAST_BF16) unpack<bf16_t>(Raw<bf16_t>{f.a}, r);
+        else unpack<f16_t>(Raw<f16_t>{f.a}, r);
 #pragma unroll
         for (int u = 0; u < 8; ++u) v[u] += r[u];
     }
@@ -307,18 +283,6 @@ __device__ __forceinline__ int rows_kind(const Epilogue& e)
     if (e.kept_act != LAST_ACT_NONE) return kRowsSlope;
     if (e.res) return !e.kept.q ? kRowsResidual : kRowsAny;
     return e.kept.q ? kRowsKeep : kRowsPlain;
-}
-
-__device__ __forceinline__ void unpack8(int type, u4 w, float* r)
-{
-    if (type == LAST_BF16) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) { r[2 * u] = bf16_to_float(w[u] & 0xffffu); r[2 * u + 1] = __uint_as_float(w[u] & 0xffff0000u); }
-    } else {
-        const h8 h = __builtin_bit_cast(h8, w);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) r[u] = (float)h[u];
-    }
 }
 
 __device__ __forceinline__ u4 pack8(int type, const float* v)
@@ -388,7 +352,8 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
         activate8(e.act, v);
         if constexpr (KIND == kRowsResidual) {
             float r[8];
-            unpack8(e.type, x.w, r);
+            if (e.type == LAST_BF16) unpack<bf16_t>(Raw<bf16_t>{x.w}, r);
+            else unpack<f16_t>(Raw<f16_t>{x.w}, r);
 #pragma unroll
             for (int u = 0; u < 8; ++u) v[u] += r[u];
         }
