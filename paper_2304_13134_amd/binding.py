@@ -478,11 +478,6 @@ class Kept(tuple):
     codes = property(lambda self: self[0])
     scales = property(lambda self: self[1])
 
-    @classmethod
-    def empty(cls, shape, dtype, device):
-        return cls(torch.empty(shape, dtype=dtype, device=device),
-                   torch.empty((*shape[:-1], (shape[-1] + 31) // 32), dtype=torch.uint8, device=device))
-
 
 class Norm(tuple):
     """(y, s, inv, kept) of last_residual_norm; what was not asked for is None."""
@@ -535,7 +530,8 @@ def _matrix(t, name, rows=None, columns=None):
     if not isinstance(scales, torch.Tensor) or not scales.is_cuda or scales.dtype != torch.uint8 \
             or scales.shape != (*shape[:-1], (shape[-1] + 31) // 32):
         raise TypeError("the scales of %s must be device uint8 [..., ceil(columns / 32)]" % name)
-    return _pack_matrix(codes.data_ptr(), type_, pitch, scales.data_ptr(), _pitch(scales, name))
+    scale_pitch = scales.shape[-1] if scales.is_contiguous() else _pitch(scales, name)
+    return _pack_matrix(codes.data_ptr(), type_, pitch, scales.data_ptr(), scale_pitch)
 
 
 def _opt(t, name, rows, columns):
@@ -571,15 +567,20 @@ def _activation(name):
     return ACTIVATIONS[name]
 
 
-def _result(shape, dtype, device):
-    """(a new tensor or Kept, its packed LastMatrix)"""
-    if dtype in _EIGHT:
-        t = Kept.empty(shape, dtype, device)
-        return t, _matrix(t, "result")
-    if dtype not in _TYPES:
+def _result(shape, dtype, device, like=None):
+    """(a new tensor or Kept, its packed LastMatrix); like: a tensor of that shape (its copy is the faster to make)"""
+    type_ = _TYPES.get(dtype)
+    if type_ is None:
         raise TypeError("results are float32, bfloat16, float16 or in 8 bits: not %s" % dtype)
-    t = torch.empty(shape, dtype=dtype, device=device)
-    return t, _pack_matrix(t.data_ptr(), _TYPES[dtype], shape[-1], 0, 0)
+    if like is not None and like.is_contiguous():
+        t = torch.empty_like(like, dtype=dtype)
+    else:
+        t = torch.empty(tuple(shape), dtype=dtype, device=device)
+    if type_ < 3:
+        return t, _pack_matrix(t.data_ptr(), type_, shape[-1], 0, 0)
+    blocks = (shape[-1] + 31) // 32
+    scales = torch.empty((*shape[:-1], blocks), dtype=torch.uint8, device=device)
+    return Kept(t, scales), _pack_matrix(t.data_ptr(), type_, shape[-1], scales.data_ptr(), blocks)
 
 
 def _stream_of(t):
@@ -609,12 +610,12 @@ def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=Non
     mx, mr = _matrix(x, "x"), _opt(residual, "residual", rows, H)
     s = y = kept = ms = my = mk = None
     if residual is not None:
-        s, ms = _result(shape, x.dtype, device)
+        s, ms = _result(shape, x.dtype, device, x)
     if keep is None or dtype is not None:
-        y, my = _result(shape, dtype or x.dtype, device)
+        y, my = _result(shape, dtype or x.dtype, device, x)
     if keep is not None:
-        kept, mk = _result(shape, keep, device)
-    inv = torch.empty(rows, dtype=torch.float32, device=device)
+        kept, mk = _result(shape, keep, device, x)
+    inv = torch.empty(tuple(rows), dtype=torch.float32, device=device)
     _check(load_library().last_residual_norm(fr, H, mx, mr, _vector(gain, H, "gain"), eps, ms, my, mk, inv.data_ptr(),
                                              _stream_of(x)))
     return Norm(y, s, inv, kept)
@@ -629,7 +630,7 @@ def last_residual_norm_grad(dy, s, gain, inv, ds=None, lengths=None, dtype=None)
     if dtype is None:
         dtype = ds.dtype if ds is not None else dy.dtype if isinstance(s, Kept) else s.dtype
     mdy, ms, mds = _matrix(dy, "dy"), _matrix(s, "s", rows, H), _opt(ds, "ds", rows, H)
-    dx, mdx = _result(dy.shape, dtype, device)
+    dx, mdx = _result(dy.shape, dtype, device, dy)
     dgain = torch.empty(H, dtype=torch.float32, device=device)
     stream = _stream_of(dy)
     ws, nbytes = _layer_scratch(OP_RESIDUAL_NORM_GRAD, fr, 1, H, None, None, dy, stream)
@@ -689,7 +690,7 @@ def last_keep(x, dtype=torch.int8, lengths=None):
     """x in 8 bits: a Kept of torch.int8 or torch.float8_e4m3fn codes."""
     fr, _, _ = _frames(x, lengths, "x")
     mx = _matrix(x, "x")
-    kept, mk = _result(x.shape, dtype, x.device)
+    kept, mk = _result(x.shape, dtype, x.device, x)
     _check(load_library().last_keep(fr, x.shape[-1], mx, mk, _stream_of(x)))
     return kept
 
@@ -698,7 +699,7 @@ def last_kept_values(kept, activation="none", lengths=None, dtype=torch.bfloat16
     """act(kept): what the codes stand for, or the activation formed again from them."""
     fr, _, t = _frames(kept, lengths, "kept")
     mk = _matrix(kept, "kept")
-    y, my = _result(t.shape, dtype, t.device)
+    y, my = _result(t.shape, dtype, t.device, t)
     _check(load_library().last_kept_values(fr, t.shape[-1], mk, _activation(activation), my, _stream_of(t)))
     return y
 
@@ -708,6 +709,6 @@ def last_kept_grad(dy, kept, activation, lengths=None, dtype=None):
     fr, rows, _ = _frames(dy, lengths, "dy")
     H = dy.shape[-1]
     mdy, mk = _matrix(dy, "dy"), _matrix(kept, "kept", rows, H)
-    dx, mdx = _result(dy.shape, dtype or dy.dtype, dy.device)
+    dx, mdx = _result(dy.shape, dtype or dy.dtype, dy.device, dy)
     _check(load_library().last_kept_grad(fr, H, mdy, mk, _activation(activation), mdx, _stream_of(dy)))
     return dx
