@@ -494,6 +494,7 @@ class Norm(tuple):
 # LastMatrix and LastFrames as bytes: a third of the time of a ctypes structure, on calls that take a few microseconds
 _pack_matrix = struct.Struct("@PiqPq").pack
 _pack_frames = struct.Struct("@iiP").pack
+_NO_ROWS = 256      # the address of a tensor without rows, which torch gives none and the library does not touch
 
 
 def _pitch(t, name):
@@ -526,12 +527,12 @@ def _matrix(t, name, rows=None, columns=None):
         raise ValueError("%s has shape %s: expected %s" % (name, tuple(shape), (*(rows or ("...",)), columns)))
     pitch = shape[-1] if len(shape) in (2, 3) and codes.is_contiguous() else _pitch(codes, name)
     if scales is None:
-        return _pack_matrix(codes.data_ptr(), type_, pitch, 0, 0)
+        return _pack_matrix(codes.data_ptr() or _NO_ROWS, type_, pitch, 0, 0)
     if not isinstance(scales, torch.Tensor) or not scales.is_cuda or scales.dtype != torch.uint8 \
             or scales.shape != (*shape[:-1], (shape[-1] + 31) // 32):
         raise TypeError("the scales of %s must be device uint8 [..., ceil(columns / 32)]" % name)
     scale_pitch = scales.shape[-1] if scales.is_contiguous() else _pitch(scales, name)
-    return _pack_matrix(codes.data_ptr(), type_, pitch, scales.data_ptr(), scale_pitch)
+    return _pack_matrix(codes.data_ptr() or _NO_ROWS, type_, pitch, scales.data_ptr() or _NO_ROWS, scale_pitch)
 
 
 def _opt(t, name, rows, columns):
@@ -577,10 +578,10 @@ def _result(shape, dtype, device, like=None):
     else:
         t = torch.empty(tuple(shape), dtype=dtype, device=device)
     if type_ < 3:
-        return t, _pack_matrix(t.data_ptr(), type_, shape[-1], 0, 0)
+        return t, _pack_matrix(t.data_ptr() or _NO_ROWS, type_, shape[-1], 0, 0)
     blocks = (shape[-1] + 31) // 32
     scales = torch.empty((*shape[:-1], blocks), dtype=torch.uint8, device=device)
-    return Kept(t, scales), _pack_matrix(t.data_ptr(), type_, shape[-1], scales.data_ptr(), blocks)
+    return Kept(t, scales), _pack_matrix(t.data_ptr() or _NO_ROWS, type_, shape[-1], scales.data_ptr() or _NO_ROWS, blocks)
 
 
 def _stream_of(t):
@@ -616,7 +617,7 @@ def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=Non
     if keep is not None:
         kept, mk = _result(shape, keep, device, x)
     inv = torch.empty(tuple(rows), dtype=torch.float32, device=device)
-    _check(load_library().last_residual_norm(fr, H, mx, mr, _vector(gain, H, "gain"), eps, ms, my, mk, inv.data_ptr(),
+    _check(load_library().last_residual_norm(fr, H, mx, mr, _vector(gain, H, "gain"), eps, ms, my, mk, inv.data_ptr() or _NO_ROWS,
                                              _stream_of(x)))
     return Norm(y, s, inv, kept)
 
@@ -635,7 +636,7 @@ def last_residual_norm_grad(dy, s, gain, inv, ds=None, lengths=None, dtype=None)
     stream = _stream_of(dy)
     ws, nbytes = _layer_scratch(OP_RESIDUAL_NORM_GRAD, fr, 1, H, None, None, dy, stream)
     _check(load_library().last_residual_norm_grad(fr, H, mdy, ms, _vector(gain, H, "gain"),
-                                                  _vector(inv, dy.numel() // H, "inv"), mds, mdx, dgain.data_ptr(), ws, nbytes,
+                                                  _vector(inv, dy.numel() // H, "inv") or _NO_ROWS, mds, mdx, dgain.data_ptr(), ws, nbytes,
                                                   stream))
     return dx, dgain
 

@@ -82,16 +82,23 @@ bool bad_activation(int act) { return act < LAST_ACT_NONE || act > LAST_ACT_TANH
 
 // ---------------------------------------------------------------- norm
 
-template <typename X>
+template <typename X, bool KEEP>
 void launch_norm(const NormArgs& a, hipStream_t st)
 {
     const int four = (a.rows + 3) / 4;
-    if (a.H <= 512) hipLaunchKernelGGL((norm_kernel<X, 1, 1>), dim3(four), dim3(256), 0, st, a);
-    else if (a.H <= 1024) hipLaunchKernelGGL((norm_kernel<X, 1, 2>), dim3(four), dim3(256), 0, st, a);
-    else if (a.H <= 2048) hipLaunchKernelGGL((norm_kernel<X, 1, 4>), dim3(four), dim3(256), 0, st, a);
-    else if (a.H <= 4096) hipLaunchKernelGGL((norm_kernel<X, 4, 2>), dim3(a.rows), dim3(256), 0, st, a);
-    else if (a.H <= 8192) hipLaunchKernelGGL((norm_kernel<X, 4, 4>), dim3(a.rows), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((norm_kernel<X, 16, 2>), dim3(a.rows), dim3(1024), 0, st, a);
+    if (a.H <= 512) hipLaunchKernelGGL((norm_kernel<X, 1, 1, KEEP>), dim3(four), dim3(256), 0, st, a);
+    else if (a.H <= 1024) hipLaunchKernelGGL((norm_kernel<X, 1, 2, KEEP>), dim3(four), dim3(256), 0, st, a);
+    else if (a.H <= 2048) hipLaunchKernelGGL((norm_kernel<X, 1, 4, KEEP>), dim3(four), dim3(256), 0, st, a);
+    else if (a.H <= 4096) hipLaunchKernelGGL((norm_kernel<X, 4, 2, KEEP>), dim3(a.rows), dim3(256), 0, st, a);
+    else if (a.H <= 8192) hipLaunchKernelGGL((norm_kernel<X, 4, 4, KEEP>), dim3(a.rows), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((norm_kernel<X, 16, 2, KEEP>), dim3(a.rows), dim3(1024), 0, st, a);
+}
+
+template <typename X>
+void launch_norm(const NormArgs& a, hipStream_t st)
+{
+    if (a.kept.q) launch_norm<X, true>(a, st);
+    else launch_norm<X, false>(a, st);
 }
 
 // Workgroups of the gradient: as many as are resident, since each leaves a row of partial sums of dgain.
@@ -438,7 +445,11 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
     return hip_done();
 }
 
-bool bad_sizes(int N, int K) { return N < 1 || K < 1 || N > kMaxColumns || K > kMaxColumns; }
+// (the last: so that tiles are counted in 32 bits)
+bool bad_sizes(long long rows, int N, int K)
+{
+    return N < 1 || K < 1 || N > kMaxColumns || K > kMaxColumns || rows * std::max(N, K) > 1ll << 42;
+}
 
 last_status_t check_ws(void* ws, size_t have, size_t need)
 {
@@ -482,7 +493,7 @@ extern "C" {
 size_t last_layer_workspace_bytes(int32_t op, const last_frames_t* frames, int32_t N, int32_t K, const last_matrix_t* a, const last_matrix_t* b)
 {
     long long rows;
-    if (check_frames(frames, &rows) != LAST_OK || bad_sizes(N, K)) return 0;
+    if (check_frames(frames, &rows) != LAST_OK || bad_sizes(rows, N, K)) return 0;
     if (op == LAST_OP_RESIDUAL_NORM_GRAD) return K > kMaxNormColumns ? 0 : align_up(std::max<size_t>(1, part_bytes(rows, K)));
     if (op != LAST_OP_PRODUCT && op != LAST_OP_PRODUCT_GRAD_INPUT && op != LAST_OP_PRODUCT_GRAD_WEIGHT) return 0;
     if (!a || !b) return 0;
@@ -584,7 +595,7 @@ last_status_t last_product(const last_frames_t* frames, int32_t N, int32_t K, co
     long long rows;
     LAST_TRY(check_frames(frames, &rows));
     if (!x || !w || !y) return LAST_ERR_NULL;
-    if (bad_sizes(N, K)) return LAST_ERR_SHAPE;
+    if (bad_sizes(rows, N, K)) return LAST_ERR_SHAPE;
     if (bad_activation(act)) return LAST_ERR_UNSUPPORTED;
     LAST_TRY(check_matrix(x, K, half_width(x->type) || x->type == LAST_E4M3));
     LAST_TRY(check_matrix(w, K, w->type == x->type));
@@ -603,7 +614,7 @@ last_status_t last_product_grad_input(const last_frames_t* frames, int32_t N, in
     long long rows;
     LAST_TRY(check_frames(frames, &rows));
     if (!dy || !w || !dx || (act != LAST_ACT_NONE && !kept)) return LAST_ERR_NULL;
-    if (bad_sizes(N, K)) return LAST_ERR_SHAPE;
+    if (bad_sizes(rows, N, K)) return LAST_ERR_SHAPE;
     if (bad_activation(act)) return LAST_ERR_UNSUPPORTED;
     LAST_TRY(check_matrix(dy, N, half_width(dy->type)));
     LAST_TRY(check_matrix(w, K, w->type == dy->type));
@@ -621,7 +632,7 @@ last_status_t last_product_grad_weight(const last_frames_t* frames, int32_t N, i
     long long rows;
     LAST_TRY(check_frames(frames, &rows));
     if (!dy || !x || !dw) return LAST_ERR_NULL;
-    if (bad_sizes(N, K)) return LAST_ERR_SHAPE;
+    if (bad_sizes(rows, N, K)) return LAST_ERR_SHAPE;
     if (bad_activation(act)) return LAST_ERR_UNSUPPORTED;
     LAST_TRY(check_matrix(dy, N, half_width(dy->type)));
     LAST_TRY(check_matrix(x, K, eight(x->type) || (x->type == dy->type && act == LAST_ACT_NONE)));

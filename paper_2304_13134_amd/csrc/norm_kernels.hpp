@@ -3,9 +3,11 @@
 //     u = gain dy,  dx = inv (u - s inv^2 mean_h(u s)) + ds,  dgain[h] = sum over rows of dy s inv
 // Both read and write every value once and are bound by memory: a row stays in registers between the sum and its use
 // (8 columns a lane in each of CH places), in one wavefront up to 2048 columns, so that no barrier separates them, and in
-// 4 or 16 wavefronts beyond.  Sums are in 32 bits.
+// 4 or 16 wavefronts beyond.
 #pragma once
 #include "layer.hpp"
+
+#include <type_traits>
 
 namespace last {
 
@@ -22,34 +24,53 @@ struct NormArgs {
     Eight kept;
 };
 
-// sum over the WPR wavefronts of a row; `red`: 2 x WPR floats of LDS, `turn` alternates between their halves so that one
+// sum over the WPR wavefronts of a row; `red`: 2 x WPR places of LDS, `turn` alternates between their halves so that one
 // barrier a sum is enough
-template <int WPR>
-__device__ __forceinline__ float row_sum(float v, float* red, int turn)
+template <int WPR, typename F>
+__device__ __forceinline__ F row_sum(F v, F* red, int turn)
 {
-    v = wave_sum(v);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
     if constexpr (WPR > 1) {
         red += (turn & 1) * WPR;
         if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = v;
         __syncthreads();
-        v = 0.f;
+        v = 0;
 #pragma unroll
         for (int i = 0; i < WPR; ++i) v += red[i];
     }
     return v;
 }
 
-template <typename X, int WPR, int CH>
+// to 32 bits, inexact values to the neighbour whose last bit is 1: rounding that again, to fewer bits, is rounding once
+__device__ __forceinline__ float to_odd(double v)
+{
+    const float f = __double2float_rz(v);
+    return (double)f == v || !(fabsf(f) < __builtin_huge_valf()) ? f : __uint_as_float(__float_as_uint(f) | 1u);
+}
+
+// KEEP: with the result in 8 bits.  Its codes are those of the exact row: where 32 bits are enough for a result that is
+// rounded by 2^-8 of itself, a code moves by 2^-4 where a sum in another order falls on the other side of a half, so these rows
+// are formed in 64 bits (the sum of x and residual as its rounded value and the rest), a few operations a value beside its bytes.
+template <typename X, int WPR, int CH, bool KEEP>
 __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_kernel(NormArgs a)
 {
     constexpr int kRows = WPR == 1 ? 4 : 1;                  // rows of a workgroup
-    __shared__ float red[2 * WPR];
+    using F = std::conditional_t<KEEP, double, float>;
+    __shared__ F red[2 * WPR];
     const int row = (int)blockIdx.x * kRows + (WPR == 1 ? (int)threadIdx.x / kWave : 0);
     const int lane = WPR == 1 ? (int)threadIdx.x % kWave : (int)threadIdx.x;
     if (WPR == 1 && row >= a.rows) return;
     const bool there = frame_exists(a.frames, row);
-    float v[CH][8];
-    float sum = 0.f;
+    float v[CH][8], rest[KEEP ? CH : 1][8];
+    F sum = 0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            v[c][k] = 0.f;
+            if constexpr (KEEP) rest[c][k] = 0.f;
+        }
     if (there) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -63,32 +84,47 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_kernel(Norm
                 float r[8];
                 load8<X>(a.res, (size_t)row * a.pr + h, a.H - h, r);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[c][k] += r[k];
+                for (int k = 0; k < 8; ++k) {
+                    const float x = v[c][k], s = x + r[k];
+                    if constexpr (KEEP) {
+                        const float t = s - x;
+                        rest[c][k] = (x - (s - t)) + (r[k] - t);
+                    }
+                    v[c][k] = s;
+                }
             }
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum += v[c][k] * v[c][k];
-    } else {
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[c][k] = 0.f;
+            for (int k = 0; k < 8; ++k) {
+                F s = v[c][k];
+                if constexpr (KEEP) s += (double)rest[c][k];
+                sum += s * s;
+            }
     }
     sum = row_sum<WPR>(sum, red, 0);
-    const float inv = there ? 1.f / sqrtf(sum / (float)a.H + a.eps) : 0.f;
-    if (lane == 0 && a.inv) a.inv[row] = inv;
+    F inv = 0;
+    if (there) {
+        if constexpr (KEEP) inv = 1.0 / sqrt(sum / a.H + (double)a.eps);
+        else inv = 1.f / sqrtf(sum / (float)a.H + a.eps);
+    }
+    if (lane == 0 && a.inv) a.inv[row] = (float)inv;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int h = (c * WPR * kWave + lane) * 8;
         if (a.s) store8<X>(a.s, (size_t)row * a.ps + h, a.H - h, v[c]);
         float g[8];
         load8<float>(a.gain, h, a.H - h, g);
+        if constexpr (KEEP) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[c][k] = there ? v[c][k] * inv * g[k] : 0.f;
+            for (int k = 0; k < 8; ++k) v[c][k] = there ? to_odd(((double)v[c][k] + (double)rest[c][k]) * inv * (double)g[k]) : 0.f;
+            store_eight(a.kept, row, h, a.H - h, (lane & 3) == 0, quad_max(top8(v[c])), v[c]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[c][k] = there ? v[c][k] * inv * g[k] : 0.f;
+        }
         if (a.y) store8_as(a.ytype, a.y, (size_t)row * a.py + h, a.H - h, v[c]);
-        if (a.kept.q) store_eight(a.kept, row, h, a.H - h, (lane & 3) == 0, quad_max(top8(v[c])), v[c]);
     }
 }
 

@@ -87,7 +87,8 @@ __device__ __forceinline__ u4 descriptor(const void* base)
 __device__ __forceinline__ unsigned lds_byte(const void* p) { return (unsigned)(uintptr_t)(lds_t)p; }
 
 // 64 lanes' 16 (4) bytes at offset o + more of the buffer to LDS from byte `to` on.  In assembly, since the compiler makes every
-// later read of LDS wait for its own form of this; whoever reads waits with arrived().
+// later read of LDS wait for its own form of this; whoever reads waits with arrived().  (m0 is a register that the compiler
+// keeps nothing in: it sets it right before an instruction that reads it.)
 template <int BYTES>
 __device__ __forceinline__ void to_lds(u4 b, unsigned o, unsigned more, unsigned to)
 {
@@ -321,6 +322,8 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
         return x;
     };
     Extra x0 = extra(0), x1 = extra(1);
+    float ahead[8];
+    get(0, ahead);
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
         const Extra x = x0;
@@ -328,7 +331,9 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
         x1 = extra(i + 2);
         const size_t row = m + (size_t)i * step;
         float v[8];
-        get(i, v);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = ahead[u];
+        get(i + 1 < count ? i + 1 : i, ahead);
         if constexpr (KIND == kRowsSlope) {
             float h[8];
             const float sc = scale_value(x.scale);
@@ -576,43 +581,51 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
                 buf_q = next;
             }
         } else {
-            u4 fp[NP], fq[2][NQ];
+            // Of P's fragments the last kTwice have two places, so that the next phase's can be read while they are used, and the last
+            // read of a phase has the products of as many rows to come.
+            constexpr int kTwice = NP >= 8 ? 2 : 1, kOwn = NP - kTwice;
+            u4 fp[kOwn], fe[2][kTwice], fq[2][NQ];
             const unsigned one = Elt<E>::type == LAST_BF16 ? 0x3f803f80u : 0x3c003c00u;
             const auto multiply = [&](int half, int x) {
+                const u4 f = x < kOwn ? fp[x < kOwn ? x : 0] : fe[half][x < kOwn ? 0 : x - kOwn];
 #pragma unroll
-                for (int y = 0; y < NQ; ++y) acc[x][y] = Mfma<E>::go(fq[half][y], fp[x], acc[x][y]);
+                for (int y = 0; y < NQ; ++y) acc[x][y] = Mfma<E>::go(fq[half][y], f, acc[x][y]);
                 if constexpr (LP == kAcross) {
-                    if (bias_too && x / NB == wq) accb[x % NB] = Mfma<E>::go(u4{one, one, one, one}, fp[x], accb[x % NB]);
+                    if (bias_too && x / NB == wq) accb[x % NB] = Mfma<E>::go(u4{one, one, one, one}, f, accb[x % NB]);
                 }
             };
-            static_assert(NQ <= NP, "a fragment of Q read beside each of P");
+            // what is read for the phase of `half` beside the products of row x of the phase before
+            const auto read = [&](unsigned ap, unsigned aq, int half, int x) {
+#pragma unroll
+                for (int y = 2 * x; y < 2 * x + 2; ++y)
+                    if (y < NQ) fq[half][y] = read_q(aq, half, y);
+                if (x < kTwice) fe[half][x] = read_p(ap, half, kOwn + x);
+                if (x < kOwn) fp[x] = read_p(ap, half, x);
+            };
+            static_assert(2 * NP >= NQ && kOwn >= kTwice, "all fragments are read");
             {
                 const unsigned ap = here(at_p), aq = here(at_q);
 #pragma unroll
-                for (int y = 0; y < NQ; ++y) fq[0][y] = read_q(aq, 0, y);
-#pragma unroll
-                for (int x = 0; x < NP; ++x) fp[x] = read_p(ap, 0, x);
+                for (int x = 0; x < NP; ++x) read(ap, aq, 0, x);
             }
             for (int s = 0; s < steps; ++s) {
+                const int next_p = after(buf_p, SP), next_q = after(buf_q, SQ);
+                mask_last = mask;
+                mask = mask_of(s + SP);
+                const Sent q = sent_q(s + SQ, buf_q, SP > SQ ? mask_last : mask), p = sent_p(s + SP, buf_p, mask);
                 {
                     const unsigned ap = here(at_p + buf_p * TP::kBytes), aq = here(at_q + buf_q * TQ::kBytes);
 #pragma unroll
                     for (int x = 0; x < NP; ++x) {
                         multiply(0, x);
-                        fp[x] = read_p(ap, 1, x);
-                        if (x < NQ) fq[1][x] = read_q(aq, 1, x);
+                        read(ap, aq, 1, x);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
                 arrived<kLater>();
-                const int next_p = after(buf_p, SP), next_q = after(buf_q, SQ);
-                mask_last = mask;
-                mask = mask_of(s + SP);
-                const unsigned long long mask_q = SP > SQ ? mask_last : mask;
                 {
                     const unsigned ap = here(at_p + next_p * TP::kBytes), aq = here(at_q + next_q * TQ::kBytes);
                     constexpr int kSends = (TP::kLoads + TQ::kLoads + NP - 1) / NP;
-                    const Sent q = sent_q(s + SQ, buf_q, mask_q), p = sent_p(s + SP, buf_p, mask);
 #pragma unroll
                     for (int x = 0; x < NP; ++x) {
                         multiply(1, x);
@@ -621,8 +634,7 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
                             if (j < TQ::kLoads) Q.load(j, q.buffer, q.bits, q.to);
                             else if (j < TQ::kLoads + TP::kLoads) P.load(j - TQ::kLoads, p.buffer, p.bits, p.to);
                         }
-                        fp[x] = read_p(ap, 0, x);
-                        if (x < NQ) fq[0][x] = read_q(aq, 0, x);
+                        read(ap, aq, 0, x);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }

@@ -154,6 +154,8 @@ def test_norm(B, T, H, pitch, type_, out, residual, kind):
         assert got.s is None
     if kind:
         assert_kept(got.kept, y, np.abs(y) * rel, kind, "kept")
+        want, scales = encode(y, kind)                             # the codes of the exact row, wherever its sum is rounded
+        assert np.array_equal(decode(got.kept), want) and np.array_equal(got.kept[1].cpu().numpy(), scales)
         only = lb.last_residual_norm(x, gain, residual=r, lengths=dev_lengths(n), eps=eps, keep=EIGHT[kind])
         assert only.y is None and torch.equal(only.kept[0].view(torch.uint8), got.kept[0].view(torch.uint8)) and torch.equal(only.kept[1], got.kept[1])
 
@@ -367,6 +369,27 @@ def test_product_weight_gradient(B, T, N, K, type_, out, kind, name, lens):
     dw, db = lb.last_product_grad_weight(dy, x, activation=name, lengths=dev_lengths(n), dtype=TYPES[out])
     assert_within(dw, want, err + rounding(want, out), "dw")
     assert_within(db, g.sum(0), (R + 4) * U32 * np.abs(g).sum(0), "dbias")
+
+
+def test_no_frames_at_all():
+    """B items of no frames: nothing to write but the sums over frames, which are zeros."""
+    announce("no frames at all")
+    x, dy = torch.empty(3, 0, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 0, 40, dtype=torch.bfloat16, device="cuda")
+    w, gain = torch.ones(40, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(64, device="cuda")
+    n = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for lengths in (None, n):
+        fw = lb.last_residual_norm(x, gain, residual=x, lengths=lengths, keep=torch.int8, dtype=torch.bfloat16)
+        assert fw.y.shape == x.shape and fw.s.shape == x.shape and fw.inv.shape == (3, 0) and fw.kept[1].shape == (3, 0, 2)
+        y, kept = lb.last_product(x, w, lengths=lengths, keep=torch.float8_e4m3fn)
+        assert y.shape == (3, 0, 40) and kept[0].shape == (3, 0, 40)
+        assert lb.last_product_grad_input(dy, w, lengths=lengths).shape == x.shape
+        dw, db = lb.last_product_grad_weight(dy, x, lengths=lengths)
+        assert not dw.any() and not db.any() and dw.shape == w.shape
+        dw, db = lb.last_product_grad_weight(dy, fw.kept, "silu", lengths=lengths)
+        assert not dw.any() and not db.any()
+        dx, dgain = lb.last_residual_norm_grad(x, x, gain, fw.inv, lengths=lengths)
+        assert dx.shape == x.shape and not dgain.any()
+        assert lb.last_kept_values(lb.last_keep(x, lengths=lengths), "gelu").shape == x.shape
 
 
 def test_results_do_not_depend_on_timing():
