@@ -589,15 +589,20 @@ def _stream_of(t):
     return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
-def _layer_scratch(op, frames, N, K, a, b, t, stream):
-    """(address, bytes) of a scratch buffer for a call on tensor t's device and stream"""
+def _with_scratch(call, op, frames, N, K, a, b, t):
+    """call(workspace address, bytes, stream) for tensor t's device and stream.  The buffer that is there is tried first: the
+    library refuses one that is too small before it enqueues anything."""
+    stream = _stream_of(t)
+    buf = _workspaces.get((t.get_device(), stream))
+    if buf is not None:
+        code = call(buf.data_ptr(), buf.numel(), stream)
+        if code != 5:
+            return _check(code)
     nbytes = load_library().last_layer_workspace_bytes(op, frames, N, K, a, b)
     if nbytes == 0:
-        raise LastError(6, "combination not supported")
-    buf = _workspaces.get((t.get_device(), stream))
-    if buf is None or buf.numel() < nbytes:
-        buf = workspace(nbytes, t.device)
-    return buf.data_ptr(), buf.numel()
+        nbytes = 256                                  # (the call says what is wrong)
+    buf = workspace(nbytes, t.device)
+    _check(call(buf.data_ptr(), buf.numel(), stream))
 
 
 def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=None, keep=None):
@@ -633,11 +638,10 @@ def last_residual_norm_grad(dy, s, gain, inv, ds=None, lengths=None, dtype=None)
     mdy, ms, mds = _matrix(dy, "dy"), _matrix(s, "s", rows, H), _opt(ds, "ds", rows, H)
     dx, mdx = _result(dy.shape, dtype, device, dy)
     dgain = torch.empty(H, dtype=torch.float32, device=device)
-    stream = _stream_of(dy)
-    ws, nbytes = _layer_scratch(OP_RESIDUAL_NORM_GRAD, fr, 1, H, None, None, dy, stream)
-    _check(load_library().last_residual_norm_grad(fr, H, mdy, ms, _vector(gain, H, "gain"),
-                                                  _vector(inv, dy.numel() // H, "inv") or _NO_ROWS, mds, mdx, dgain.data_ptr(), ws, nbytes,
-                                                  stream))
+    call = load_library().last_residual_norm_grad
+    g, i = _vector(gain, H, "gain"), _vector(inv, dy.numel() // H, "inv") or _NO_ROWS
+    _with_scratch(lambda ws, n, stream: call(fr, H, mdy, ms, g, i, mds, mdx, dgain.data_ptr(), ws, n, stream),
+                  OP_RESIDUAL_NORM_GRAD, fr, 1, H, None, None, dy)
     return dx, dgain
 
 
@@ -652,10 +656,8 @@ def last_product(x, w, bias=None, activation="none", residual=None, lengths=None
     y, my = _result(shape, dtype or (torch.bfloat16 if isinstance(x, Kept) else x.dtype), device)
     if keep is not None:
         kept, mk = _result(shape, keep, device)
-    stream = _stream_of(t)
-    ws, nbytes = _layer_scratch(OP_PRODUCT, fr, N, K, mx, mw, t, stream)
-    _check(load_library().last_product(fr, N, K, mx, mw, _vector(bias, N, "bias"), _activation(activation),
-                                       _opt(residual, "residual", rows, N), my, mk, ws, nbytes, stream))
+    call, b, act, mr = load_library().last_product, _vector(bias, N, "bias"), _activation(activation), _opt(residual, "residual", rows, N)
+    _with_scratch(lambda ws, n, stream: call(fr, N, K, mx, mw, b, act, mr, my, mk, ws, n, stream), OP_PRODUCT, fr, N, K, mx, mw, t)
     return y, kept
 
 
@@ -666,9 +668,8 @@ def last_product_grad_input(dy, w, kept=None, activation="none", lengths=None, d
     N, K = w.shape
     mdy, mw, mk = _matrix(dy, "dy", rows, N), _matrix(w, "w", (N,), K), _opt(kept, "kept", rows, K)
     dx, mdx = _result((*rows, K), dtype or dy.dtype, dy.device)
-    stream = _stream_of(dy)
-    ws, nbytes = _layer_scratch(OP_PRODUCT_GRAD_INPUT, fr, N, K, mdy, mw, dy, stream)
-    _check(load_library().last_product_grad_input(fr, N, K, mdy, mw, mk, _activation(activation), mdx, ws, nbytes, stream))
+    call, act = load_library().last_product_grad_input, _activation(activation)
+    _with_scratch(lambda ws, n, stream: call(fr, N, K, mdy, mw, mk, act, mdx, ws, n, stream), OP_PRODUCT_GRAD_INPUT, fr, N, K, mdy, mw, dy)
     return dx
 
 
@@ -680,10 +681,9 @@ def last_product_grad_weight(dy, x, activation="none", lengths=None, dtype=torch
     mdy, mx = _matrix(dy, "dy"), _matrix(x, "x", rows, K)
     dw, mdw = _result((N, K), dtype, device)
     dbias = torch.empty(N, dtype=torch.float32, device=device)
-    stream = _stream_of(dy)
-    ws, nbytes = _layer_scratch(OP_PRODUCT_GRAD_WEIGHT, fr, N, K, mdy, mx, dy, stream)
-    _check(load_library().last_product_grad_weight(fr, N, K, mdy, mx, _activation(activation), mdw, dbias.data_ptr(), ws,
-                                                   nbytes, stream))
+    call, act = load_library().last_product_grad_weight, _activation(activation)
+    _with_scratch(lambda ws, n, stream: call(fr, N, K, mdy, mx, act, mdw, dbias.data_ptr(), ws, n, stream),
+                  OP_PRODUCT_GRAD_WEIGHT, fr, N, K, mdy, mx, dy)
     return dw, dbias
 
 

@@ -28,9 +28,9 @@ struct KeepPlace {
     int n;                           // columns to read: 0 past the end, or where no frame is
 };
 
-__device__ __forceinline__ KeepPlace keep_place(const KeepArgs& a, int d)
+__device__ __forceinline__ KeepPlace keep_place(const KeepArgs& a, unsigned group, int d)
 {
-    const unsigned i = (blockIdx.x * kKeepDeep + d) * 256u + threadIdx.x;
+    const unsigned i = (group * kKeepDeep + d) * 256u + threadIdx.x;
     const unsigned r = i / (unsigned)a.groups;
     KeepPlace p;
     p.row = a.row0 + (int)r;
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a)
     KeepPlace p[kKeepDeep];
     Raw<X> x[kKeepDeep];
 #pragma unroll
-    for (int d = 0; d < kKeepDeep; ++d) p[d] = keep_place(a, d);
+    for (int d = 0; d < kKeepDeep; ++d) p[d] = keep_place(a, blockIdx.x, d);
 #pragma unroll
     for (int d = 0; d < kKeepDeep; ++d) x[d] = raw8<X>(a.x, (size_t)p[d].row * a.px + p[d].h, p[d].n);
 #pragma unroll
@@ -84,12 +84,12 @@ __device__ __forceinline__ void unpack_eight(bool e4m3, const RawEight& r, float
 }
 
 // y = act(kept)
-__global__ __launch_bounds__(256) void kept_values_kernel(KeepArgs a)
+__device__ __forceinline__ void kept_values(const KeepArgs& a, unsigned group)
 {
     KeepPlace p[kKeepDeep];
     RawEight x[kKeepDeep];
 #pragma unroll
-    for (int d = 0; d < kKeepDeep; ++d) p[d] = keep_place(a, d);
+    for (int d = 0; d < kKeepDeep; ++d) p[d] = keep_place(a, group, d);
 #pragma unroll
     for (int d = 0; d < kKeepDeep; ++d) x[d] = raw_eight(a.kept, p[d]);
 #pragma unroll
@@ -101,6 +101,8 @@ __global__ __launch_bounds__(256) void kept_values_kernel(KeepArgs a)
     }
 }
 
+__global__ __launch_bounds__(256) void kept_values_kernel(KeepArgs a) { kept_values(a, blockIdx.x); }
+
 // y = dy act'(kept)
 template <typename X>
 __global__ __launch_bounds__(256) void kept_grad_kernel(KeepArgs a)
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(256) void kept_grad_kernel(KeepArgs a)
     RawEight x[kKeepDeep];
     Raw<X> dy[kKeepDeep];
 #pragma unroll
-    for (int d = 0; d < kKeepDeep; ++d) p[d] = keep_place(a, d);
+    for (int d = 0; d < kKeepDeep; ++d) p[d] = keep_place(a, blockIdx.x, d);
 #pragma unroll
     for (int d = 0; d < kKeepDeep; ++d) {
         x[d] = raw_eight(a.kept, p[d]);

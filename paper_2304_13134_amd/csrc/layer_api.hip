@@ -144,6 +144,35 @@ void launch_norm_grad_on(int s, const NormGradArgs& a, int groups, hipStream_t s
     }
 }
 
+// ---------------------------------------------------------------- 8 bits
+
+// rows of the element-wise calls in launches of at most 2^29 places
+template <typename Launch>
+last_status_t in_pieces(KeepArgs a, long long rows, Launch launch)
+{
+    a.groups = (a.H + kBlock - 1) / kBlock * 4;
+    const long long most = std::max(1ll, (1ll << 29) / a.groups);
+    for (long long r = 0; r < rows; r += most) {
+        a.row0 = (int)r;
+        a.rows = (int)std::min(most, rows - r);
+        launch(a, dim3((unsigned)(((long long)a.rows * a.groups + 256 * kKeepDeep - 1) / (256 * kKeepDeep))));
+    }
+    return hip_done();
+}
+
+KeepArgs kept_values_args(const last_frames_t* f, int H, const last_matrix_t* kept, int act, const last_matrix_t* y)
+{
+    KeepArgs a{};
+    a.frames = frames_of(f);
+    a.H = H;
+    a.y = y->data;
+    a.py = y->pitch;
+    a.act = act;
+    a.ytype = y->type;
+    a.kept = eight_of(kept);
+    return a;
+}
+
 // ---------------------------------------------------------------- products
 
 struct ProductPlan {
@@ -165,7 +194,7 @@ ProductPlan plan_product(bool forward, bool across, long long P, long long Q, lo
     ProductPlan best{0, 1, steps};
     if (forward && P <= 64) return best;
     static const double alone[4] = {0, 0.2, 0.5, 1.2}, shared[4] = {0, 0.4, 0.95, 1.2}, beside[4] = {0, 3.5, 5, 9};
-    static const double by_rows[4] = {0, 1.9, 1.4, 1.15};
+    static const double by_rows[4] = {0, 1.9, 1.2, 1.15};
     double least = 1e30;
     for (int variant = 1; variant <= 3; ++variant) {
         const long long tile = 32 << variant;
@@ -174,10 +203,11 @@ ProductPlan plan_product(bool forward, bool across, long long P, long long Q, lo
             const long long part = std::max(1ll, (steps + splits - 1) / splits);
             if (splits > 1 && (part < 4 || (steps + part - 1) / part != splits)) continue;
             const long long blocks = tiles * splits, at_once = variant == 3 ? 256 : 512;
-            const long long rounds = (blocks + at_once - 1) / at_once, last = blocks - (rounds - 1) * at_once;
             const double factor = across ? by_rows[variant] : 1.0;
-            double us = (rounds - 1) * (part * shared[variant] * factor + beside[variant]);
-            us += part * (last <= 256 ? alone[variant] : shared[variant]) * factor + beside[variant];
+            double us;
+            if (blocks <= 256) us = part * alone[variant] * factor + beside[variant];
+            else if (variant == 3) us = (double)((blocks + 255) / 256) * (part * shared[variant] * factor + beside[variant]);
+            else us = std::max(1.0, (double)blocks / at_once) * (part * shared[variant] * factor + beside[variant]);
             if (splits > 1) us += 4 + (double)splits * P * Q * 8 / 5e6;
             if (us < least) {
                 least = us;
@@ -279,6 +309,11 @@ struct Preparation {
                               (unsigned)((count * (out_pitch / 16) + 255) / 256)};
         a.groups += r.groups;
     }
+    void values(const KeepArgs& k, dim3 grid)
+    {
+        a.values = k;
+        a.values_groups = grid.x;
+    }
     void mask(const last_frames_t* f, long long count, unsigned long long* out)
     {
         a.frames = frames_of(f);
@@ -288,7 +323,8 @@ struct Preparation {
     }
     void launch(hipStream_t st) const
     {
-        if (a.groups + mask_groups) hipLaunchKernelGGL(prepare_kernel, dim3(a.groups + mask_groups), dim3(256), 0, st, a);
+        const unsigned n = a.groups + a.values_groups + mask_groups;
+        if (n) hipLaunchKernelGGL(prepare_kernel, dim3(n), dim3(256), 0, st, a);
     }
 };
 
@@ -405,8 +441,6 @@ last_status_t run_grad_input(Carver& cv, const last_frames_t* f, long long rows,
     return hip_done();
 }
 
-last_status_t run_kept_values(const last_frames_t* f, long long rows, int H, const last_matrix_t* kept, int act, const last_matrix_t* y, hipStream_t st);
-
 last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows, int N, int K, const last_matrix_t* dy, const last_matrix_t* x,
                               int act, const last_matrix_t* dw, float* dbias, hipStream_t st)
 {
@@ -420,7 +454,14 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
         v.type = dy->type;
         v.pitch = packed_pitch(K, dy->type) / 2;
         v.data = cv.take((size_t)(rows * v.pitch * 2));
-        if (cv.base && rows > 0) LAST_TRY(run_kept_values(f, rows, K, x, act, &v, st));
+        if (cv.base && rows > 0) {
+            // in the launch that prepares, but for what is left of rows that are more than one takes
+            KeepArgs all = kept_values_args(f, K, x, act, &v);
+            LAST_TRY(in_pieces(all, rows, [&](const KeepArgs& k, dim3 grid) {
+                if (k.row0 == 0) pre.values(k, grid);
+                else hipLaunchKernelGGL(kept_values_kernel, grid, dim3(256), 0, st, k);
+            }));
+        }
         q = Operand{(const char*)v.data, v.pitch * 2, nullptr, 0};
     } else {
         q = lay_out(cv, pre, x, rows, K);
@@ -455,33 +496,6 @@ last_status_t check_ws(void* ws, size_t have, size_t need)
 {
     if (!ws || ((uintptr_t)ws % kAlign) != 0 || have < need) return LAST_ERR_WORKSPACE;
     return LAST_OK;
-}
-
-// rows of the element-wise calls in launches of at most 2^29 places
-template <typename Launch>
-last_status_t in_pieces(KeepArgs a, long long rows, Launch launch)
-{
-    a.groups = (a.H + kBlock - 1) / kBlock * 4;
-    const long long most = std::max(1ll, (1ll << 29) / a.groups);
-    for (long long r = 0; r < rows; r += most) {
-        a.row0 = (int)r;
-        a.rows = (int)std::min(most, rows - r);
-        launch(a, dim3((unsigned)(((long long)a.rows * a.groups + 256 * kKeepDeep - 1) / (256 * kKeepDeep))));
-    }
-    return hip_done();
-}
-
-last_status_t run_kept_values(const last_frames_t* f, long long rows, int H, const last_matrix_t* kept, int act, const last_matrix_t* y, hipStream_t st)
-{
-    KeepArgs a{};
-    a.frames = frames_of(f);
-    a.H = H;
-    a.y = y->data;
-    a.py = y->pitch;
-    a.act = act;
-    a.ytype = y->type;
-    a.kept = eight_of(kept);
-    return in_pieces(a, rows, [&](const KeepArgs& k, dim3 grid) { hipLaunchKernelGGL(kept_values_kernel, grid, dim3(256), 0, st, k); });
 }
 
 size_t part_bytes(long long rows, int H) { return sizeof(float) * (size_t)norm_grad_groups(rows, H) * H; }
@@ -675,7 +689,9 @@ last_status_t last_kept_values(const last_frames_t* frames, int32_t H, const las
     if (bad_activation(act)) return LAST_ERR_UNSUPPORTED;
     LAST_TRY(check_matrix(kept, H, eight(kept->type)));
     LAST_TRY(check_matrix(y, H, plain(y->type)));
-    return run_kept_values(frames, rows, H, kept, act, y, (hipStream_t)hip_stream);
+    hipStream_t st = (hipStream_t)hip_stream;
+    return in_pieces(kept_values_args(frames, H, kept, act, y), rows,
+                     [&](const KeepArgs& k, dim3 grid) { hipLaunchKernelGGL(kept_values_kernel, grid, dim3(256), 0, st, k); });
 }
 
 last_status_t last_kept_grad(const last_frames_t* frames, int32_t H, const last_matrix_t* dy, const last_matrix_t* kept,

@@ -17,6 +17,7 @@
 // index into a lane.  Out-of-range pieces have an offset that the buffer's bounds check turns into zeros, in memory order
 // that is: rows past the end, frames that do not exist, the rest of the reduction.
 #pragma once
+#include "keep_kernels.hpp"
 #include "layer.hpp"
 
 namespace last {
@@ -850,7 +851,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int sp
 }
 
 // ---- before a product, in one launch: rows of operands laid out at multiples of 16 bytes with zeros behind them, 16 bytes a
-// thread, and which rows exist, a bit each
+// thread; an activation formed again from what was kept; which rows exist, a bit each
 struct PrepareArgs {
     struct Rows {
         const uint8_t* in;
@@ -860,6 +861,8 @@ struct PrepareArgs {
         unsigned groups;                         // workgroups that do it
     } rows[4];
     unsigned groups;                             // of all four
+    KeepArgs values;
+    unsigned values_groups;
     Frames frames;
     int frame_rows;
     unsigned long long* mask;
@@ -868,8 +871,12 @@ struct PrepareArgs {
 __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a)
 {
     unsigned group = blockIdx.x;
+    if (group >= a.groups && group - a.groups < a.values_groups) {
+        kept_values(a.values, group - a.groups);
+        return;
+    }
     if (group >= a.groups) {
-        const int row = (int)((group - a.groups) * 256 + threadIdx.x);
+        const int row = (int)((group - a.groups - a.values_groups) * 256 + threadIdx.x);
         const unsigned long long m = __ballot(row < a.frame_rows && frame_exists(a.frames, row));
         if ((threadIdx.x & (kWave - 1)) == 0 && row < a.frame_rows) a.mask[row >> 6] = m;
         return;
