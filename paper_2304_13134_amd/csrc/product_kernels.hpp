@@ -274,8 +274,9 @@ __device__ __forceinline__ void load_bias(const Epilogue& e, int n, int Q, float
     load8<float>(e.bias, n, e.bias ? Q - n : 0, b);
 }
 
-// Eight columns that are all inside of rows that all exist, the common case, in a loop without a branch around a load or a store, so that
-// no store is waited for (they count with the loads, in order): an extra load is two rows ahead of its use.
+// Eight columns that are all inside of rows that all are, the common case, without a branch around a load or a store, so that no
+// store is waited for (they count with the loads, in order).  What is read beside the sums is sent for four rows at a time, a
+// batch ahead, and also where no frame is, whose results are zeros.
 enum { kRowsPlain = 0, kRowsResidual = 1, kRowsSlope = 2, kRowsKeep = 3, kRowsWide = 4, kRowsEight = 5, kRowsAny = 6 };
 
 __device__ __forceinline__ int rows_kind(const Epilogue& e)
@@ -302,39 +303,35 @@ __device__ __forceinline__ unsigned encode_block(bool e4m3, const float* v, unsi
     return byte;
 }
 
-// m: this lane's first row, every `step`-th of which it has, `count` in all; n: its columns.  get(i, v): the sums of its i-th row.
-template <int KIND, typename Get>
-__device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, int step, int count, const float* bias, Get get)
+// m: this lane's first row, every `step`-th of which it has, COUNT in all, and bit step * i of `exist` tells whether the i-th
+// exists; n: its columns.  get(i, v): the sums of its i-th row.
+template <int KIND, int COUNT, typename Get>
+__device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, int step, unsigned long long exist, const float* bias, Get get)
 {
-    const auto at = [&](int i) { return m + (size_t)(i < count ? i : count - 1) * step; };
+    constexpr bool kExtra = KIND == kRowsResidual || KIND == kRowsSlope;
+    constexpr int kBatch = !kExtra ? 1 : COUNT < 4 ? COUNT : 4;
+    static_assert(COUNT % kBatch == 0, "whole batches");
     struct Extra {
         u4 w;
         unsigned scale;
     };
     const auto extra = [&](int i) {
+        const size_t row = m + (size_t)(i < COUNT ? i : COUNT - 1) * step;
         Extra x{};
-        if constexpr (KIND == kRowsResidual) x.w = *(const u4_any*)((const uint16_t*)e.res + at(i) * e.pres + n);
+        if constexpr (KIND == kRowsResidual) x.w = *(const u4_any*)((const uint16_t*)e.res + row * e.pres + n);
         if constexpr (KIND == kRowsSlope) {
-            const u2 q = *(const u2_any*)(e.kept.q + at(i) * e.kept.pitch + n);
+            const u2 q = *(const u2_any*)(e.kept.q + row * e.kept.pitch + n);
             x.w[0] = q[0];
             x.w[1] = q[1];
-            x.scale = e.kept.scales[at(i) * e.kept.scale_pitch + n / kBlock];
+            x.scale = e.kept.scales[row * e.kept.scale_pitch + n / kBlock];
         }
         return x;
     };
-    Extra x0 = extra(0), x1 = extra(1);
-    float ahead[8];
-    get(0, ahead);
-#pragma unroll 1
-    for (int i = 0; i < count; ++i) {
-        const Extra x = x0;
-        x0 = x1;
-        x1 = extra(i + 2);
+    const auto finish_row = [&](int i, const Extra& x) {
         const size_t row = m + (size_t)i * step;
+        const bool there = exist >> (i * step) & 1;
         float v[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = ahead[u];
-        get(i + 1 < count ? i + 1 : i, ahead);
+        get(i, v);
         if constexpr (KIND == kRowsSlope) {
             float h[8];
             const float sc = scale_value(x.scale);
@@ -346,10 +343,13 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
                 decode4<false>(x.w[1], sc, h + 4);
             }
             times_slope(e.kept_act, h, v);
-        }
+        } else {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] += bias[u];
+            for (int u = 0; u < 8; ++u) v[u] += bias[u];
+        }
         if constexpr (KIND == kRowsKeep) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = there ? v[u] : 0.f;
             unsigned lo, hi;
             const unsigned byte = encode_block(e.kept.e4m3, v, &lo, &hi);
             *(u2_any*)(e.kept.q + row * e.kept.pitch + n) = u2{lo, hi};
@@ -363,6 +363,8 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
 #pragma unroll
             for (int u = 0; u < 8; ++u) v[u] += r[u];
         }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = there ? v[u] : 0.f;
         if constexpr (KIND == kRowsEight) {
             unsigned lo, hi;
             const unsigned byte = encode_block(e.out.e4m3, v, &lo, &hi);
@@ -373,6 +375,18 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
         } else {
             *(u4_any*)((uint16_t*)e.y + row * e.py + n) = pack8(e.type, v);
         }
+    };
+    Extra now[kBatch], next[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) next[j] = extra(j);
+#pragma unroll 1
+    for (int i = 0; i < COUNT; i += kBatch) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) now[j] = next[j];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) next[j] = extra(i + kBatch + j);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) finish_row(i + j, now[j]);
     }
 }
 
@@ -690,13 +704,14 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
         constexpr int kCount = XS * 16 / kRows;
         // blocks in 8 bits need all their lanes, else a lane goes by its own columns
         const int last = kind == kRowsKeep || kind == kRowsEight ? q0 + (wq + 1) * kCols : n + 8;
-        if (rows == ~0ull && last <= a.Q && kind != kRowsAny) {
-            if (kind == kRowsPlain) fast_rows<kRowsPlain>(e, m0, n, kRows, kCount, bias, get_mine);
-            else if (kind == kRowsResidual) fast_rows<kRowsResidual>(e, m0, n, kRows, kCount, bias, get_mine);
-            else if (kind == kRowsSlope) fast_rows<kRowsSlope>(e, m0, n, kRows, kCount, bias, get_mine);
-            else if (kind == kRowsKeep) fast_rows<kRowsKeep>(e, m0, n, kRows, kCount, bias, get_mine);
-            else if (kind == kRowsEight) fast_rows<kRowsEight>(e, m0, n, kRows, kCount, bias, get_mine);
-            else fast_rows<kRowsWide>(e, m0, n, kRows, kCount, bias, get_mine);
+        const unsigned long long exist = rows >> (lane / kLanes);
+        if (first + XS * 16 <= a.P && last <= a.Q && kind != kRowsAny) {
+            if (kind == kRowsPlain) fast_rows<kRowsPlain, kCount>(e, m0, n, kRows, exist, bias, get_mine);
+            else if (kind == kRowsResidual) fast_rows<kRowsResidual, kCount>(e, m0, n, kRows, exist, bias, get_mine);
+            else if (kind == kRowsSlope) fast_rows<kRowsSlope, kCount>(e, m0, n, kRows, exist, bias, get_mine);
+            else if (kind == kRowsKeep) fast_rows<kRowsKeep, kCount>(e, m0, n, kRows, exist, bias, get_mine);
+            else if (kind == kRowsEight) fast_rows<kRowsEight, kCount>(e, m0, n, kRows, exist, bias, get_mine);
+            else fast_rows<kRowsWide, kCount>(e, m0, n, kRows, exist, bias, get_mine);
         } else if (n - c < a.Q) {                            // (some column of the wavefront)
             bool there = rows >> (lane / kLanes) & 1;
             Fetched f = fetch(e, (int)m0, n, a.P, a.Q, there);
