@@ -3,7 +3,8 @@
 //     u = gain dy,  dx = inv (u - s inv^2 mean_h(u s)) + ds,  dgain[h] = sum over rows of dy s inv
 // Both read and write every value once and are bound by memory: a row stays in registers between the sum and its use
 // (8 columns a lane in each of CH places), in one wavefront up to 2048 columns, so that no barrier separates them, and in
-// 4 or 16 wavefronts beyond.
+// 4 or 16 wavefronts beyond.  16384 x 512 in bfloat16 with a residual, three quarters of the frames existing: 10.9 us (59 MB),
+// 2331 x 257 in float32 to 8 bits 7.1 us, one row 2.1 us.
 #pragma once
 #include "layer.hpp"
 
@@ -144,7 +145,7 @@ struct NormGradArgs {
 // they meet in LDS and go out as one row of partial sums a workgroup, added in order by column_sum_kernel.  The next row
 // is sent for before this one is worked on, always, so that the wait for this one is not one for it too: in the place of a
 // row that does not exist this one is read again, from cache.  16384 x 2048 in bfloat16 with ds, three quarters of the frames
-// existing (218 MB): without that, a row a wavefront, 70 us.
+// existing (218 MB): 45 us, and 4.7 us for the sums over the workgroups; without that, a row a wavefront, 70 us.
 template <typename DY, typename S, int WPR, int CH, bool DS>
 __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel(NormGradArgs a)
 {
