@@ -14,6 +14,7 @@ struct KeepArgs {
     Frames frames;
     int row0, rows, H;               // rows row0 .. row0 + rows of the matrices
     int groups;                      // threads of a row: 4 for each block
+    Divisor by_groups;
     const void* x;                   // keep: values; grad: dy
     void* y;                         // values, grad: results
     long long px, py;
@@ -33,7 +34,7 @@ struct KeepPlace {
 __device__ __forceinline__ KeepPlace keep_place(const KeepArgs& a, unsigned group, int d)
 {
     const unsigned i = (group * kKeepDeep + d) * 256u + threadIdx.x;
-    const unsigned r = i / (unsigned)a.groups;
+    const unsigned r = quotient(i, a.by_groups);
     KeepPlace p;
     p.row = a.row0 + (int)r;
     p.h = (int)(i - r * a.groups) * 8;
@@ -53,9 +54,12 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a)
     for (int d = 0; d < kKeepDeep; ++d) x[d] = raw8<X>(a.x, (size_t)p[d].row * a.px + p[d].h, p[d].n);
 #pragma unroll
     for (int d = 0; d < kKeepDeep; ++d) {
-        float v[8];
-        unpack<X>(x[d], v);
-        const unsigned top = quad_max(top8(v));
+        float v[8] = {};
+        unsigned top = 0;
+        if (__any(p[d].n > 0)) {                             // (some frame of the wavefront exists)
+            unpack<X>(x[d], v);
+            top = quad_max(top8(v));
+        }
         if (p[d].in) store_eight(a.kept, p[d].row, p[d].h, a.H - p[d].h, (p[d].h & (kBlock - 1)) == 0, top, v);
     }
 }
@@ -96,9 +100,11 @@ __device__ __forceinline__ void kept_values(const KeepArgs& a, unsigned group)
     for (int d = 0; d < kKeepDeep; ++d) x[d] = raw_eight(a.kept, p[d]);
 #pragma unroll
     for (int d = 0; d < kKeepDeep; ++d) {
-        float v[8];
-        unpack_eight(a.kept.e4m3, x[d], v);                  // (act(0) = 0 for each)
-        activate8(a.act, v);
+        float v[8] = {};
+        if (__any(p[d].n > 0)) {
+            unpack_eight(a.kept.e4m3, x[d], v);              // (act(0) = 0 for each)
+            activate8(a.act, v);
+        }
         store8_as(a.ytype, a.y, (size_t)p[d].row * a.py + p[d].h, p[d].in ? a.H - p[d].h : 0, v);
     }
 }
@@ -121,10 +127,12 @@ __global__ __launch_bounds__(256) void kept_grad_kernel(KeepArgs a)
     }
 #pragma unroll
     for (int d = 0; d < kKeepDeep; ++d) {
-        float h[8], v[8];
-        unpack_eight(a.kept.e4m3, x[d], h);
-        unpack<X>(dy[d], v);
-        times_slope(a.act, h, v);
+        float h[8], v[8] = {};
+        if (__any(p[d].n > 0)) {
+            unpack_eight(a.kept.e4m3, x[d], h);
+            unpack<X>(dy[d], v);
+            times_slope(a.act, h, v);
+        }
         store8_as(a.ytype, a.y, (size_t)p[d].row * a.py + p[d].h, p[d].in ? a.H - p[d].h : 0, v);
     }
 }

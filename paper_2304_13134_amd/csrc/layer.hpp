@@ -29,16 +29,33 @@ struct e4m3_t { uint8_t bits; };
 
 constexpr int kBlock = 32;           // columns that share a scale
 
+// n / d for n < 2^31 as n m 2^-(31 + s) with s = ceil(log2 d), m = ceil(2^(31 + s) / d): m d passes 2^(31 + s) by less than d <= 2^s,
+// so the quotient is off by less than n 2^-31 / d < 1 / d and its integer part is right.  (A division takes some 20 instructions, a
+// quarter of them at a quarter of the rate: as much as the rest of what eight values kept in 8 bits take.)
+struct Divisor {
+    unsigned m, s;
+};
+
+inline Divisor divisor_of(unsigned d)
+{
+    unsigned s = 0;
+    while ((1ull << s) < d) ++s;
+    return Divisor{d ? (unsigned)(((1ull << (31 + s)) + d - 1) / d) : 0u, s};
+}
+
+__device__ __forceinline__ unsigned quotient(unsigned n, const Divisor& d) { return __umulhi(n + n, d.m) >> d.s; }
+
 // rows b T + t of frames; those with t >= len[b] do not exist (lengths below 0 count as 0)
 struct Frames {
     const int* len;                  // null: all exist
     int T;
+    Divisor by;                      // T
 };
 
 __device__ __forceinline__ bool frame_exists(const Frames& f, int row)
 {
     if (!f.len) return true;
-    const int b = (int)((unsigned)row / (unsigned)f.T);
+    const int b = (int)quotient((unsigned)row, f.by);
     return row - b * f.T < f.len[b];
 }
 
@@ -77,21 +94,24 @@ __device__ __forceinline__ unsigned scale_byte(unsigned top)
     return b < 0 ? 0u : (unsigned)b;
 }
 
-// four values times 1 / scale to four codes, to nearest even
+// four values times 1 / scale to four codes, to nearest even; 0 where the block holds a value that is not finite
 template <bool E4M3>
 __device__ __forceinline__ unsigned encode4(const float* v, unsigned byte)
 {
-    if (byte == 255u) return 0u;
     const float m = __uint_as_float((254u - byte) << 23);
+    unsigned r;
     if constexpr (E4M3) {
-        int r = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * m, v[1] * m, 0, false);
-        return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * m, v[3] * m, r, true);
+        r = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(v[0] * m, v[1] * m, 0, false);
+        r = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * m, v[3] * m, (int)r, true);
     } else {
-        unsigned r = 0;
+        // v m is exact and at most 127; added to 1.5 2^23, whose neighbours are 1 apart, it is rounded to an integer, whose last eight
+        // bits are the sum's
+        unsigned c[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r |= ((unsigned)(int)rintf(v[i] * m) & 255u) << (8 * i);
-        return r;
+        for (int i = 0; i < 4; ++i) c[i] = __float_as_uint(__builtin_fmaf(v[i], m, 12582912.f));
+        r = __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u) | __builtin_amdgcn_perm(c[3], c[2], 0x04000c0cu);
     }
+    return byte == 255u ? 0u : r;
 }
 
 template <bool E4M3>

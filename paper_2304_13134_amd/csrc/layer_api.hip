@@ -64,7 +64,7 @@ last_status_t check_matrix(const last_matrix_t* m, long long columns, bool types
         if (rc_ != LAST_OK) return rc_;                 \
     } while (0)
 
-Frames frames_of(const last_frames_t* f) { return Frames{f->lengths, f->T}; }
+Frames frames_of(const last_frames_t* f) { return Frames{f->lengths, f->T, divisor_of((unsigned)f->T)}; }
 
 Eight eight_of(const last_matrix_t* m)
 {
@@ -151,6 +151,7 @@ template <typename Launch>
 last_status_t in_pieces(KeepArgs a, long long rows, Launch launch)
 {
     a.groups = (a.H + kBlock - 1) / kBlock * 4;
+    a.by_groups = divisor_of((unsigned)a.groups);
     const long long most = std::max(1ll, (1ll << 29) / a.groups);
     for (long long r = 0; r < rows; r += most) {
         a.row0 = (int)r;

@@ -286,7 +286,7 @@ __device__ __forceinline__ void load_bias(const Epilogue& e, int n, int Q, float
 // Eight columns that are all inside of rows that all are, the common case, without a branch around a load or a store, so that no
 // store is waited for (they count with the loads, in order).  What is read beside the sums is sent for four rows at a time, a
 // batch ahead, and also where no frame is, whose results are zeros.
-enum { kRowsPlain = 0, kRowsResidual = 1, kRowsSlope = 2, kRowsKeep = 3, kRowsWide = 4, kRowsEight = 5, kRowsAny = 6 };
+enum { kRowsPlain = 0, kRowsResidual = 1, kRowsSlope = 2, kRowsKeep = 3, kRowsWide = 4, kRowsEight = 5, kRowsNone = 6, kRowsAny = 7 };
 
 __device__ __forceinline__ int rows_kind(const Epilogue& e)
 {
@@ -338,6 +338,10 @@ __device__ __forceinline__ void fast_rows(const Epilogue& e, size_t m, int n, in
     };
     const auto finish_row = [&](int i, const Extra& x) {
         const size_t row = m + (size_t)i * step;
+        if constexpr (KIND == kRowsNone) {                   // no frame: nothing to read or to compute
+            *(u4_any*)((uint16_t*)e.y + row * e.py + n) = u4{0, 0, 0, 0};
+            return;
+        }
         const bool there = exist >> (i * step) & 1;
         float v[8];
         get(i, v);
@@ -715,7 +719,8 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
         const int last = kind == kRowsKeep || kind == kRowsEight ? q0 + (wq + 1) * kCols : n + 8;
         const unsigned long long exist = rows >> (lane / kLanes);
         if (first + XS * 16 <= a.P && last <= a.Q && kind != kRowsAny) {
-            if (kind == kRowsPlain) fast_rows<kRowsPlain, kCount>(e, m0, n, kRows, exist, bias, get_mine);
+            if (rows == 0 && kind <= kRowsSlope) fast_rows<kRowsNone, kCount>(e, m0, n, kRows, exist, bias, get_mine);
+            else if (kind == kRowsPlain) fast_rows<kRowsPlain, kCount>(e, m0, n, kRows, exist, bias, get_mine);
             else if (kind == kRowsResidual) fast_rows<kRowsResidual, kCount>(e, m0, n, kRows, exist, bias, get_mine);
             else if (kind == kRowsSlope) fast_rows<kRowsSlope, kCount>(e, m0, n, kRows, exist, bias, get_mine);
             else if (kind == kRowsKeep) fast_rows<kRowsKeep, kCount>(e, m0, n, kRows, exist, bias, get_mine);
