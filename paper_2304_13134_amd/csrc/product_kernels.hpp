@@ -24,7 +24,9 @@
 // library's: 80 % at 1.87, the clock follows the power); LDS 25 %, without bank conflicts.  A step of 128 bytes takes 1.53 us on the
 // whole chip, 1.45 without the reads of LDS, 1.08 without the loads to it, and 1.10 on a chip with 16 such workgroups: what is
 // left is bound by the feed from L2 and memory, 16.8 MB a step.  Tried and slower or the same: four wavefronts of 128 x 128,
-// starting each XCD at another place of the reduction, two buffers for P, whole 512-byte rows of results in a wavefront.
+// tiles of 128 x 256, starting each XCD at another place of the reduction, two buffers for P, whole 512-byte rows of results in a
+// wavefront.  The epilogue's activations are bound by instructions: a slope of silu takes 9 a value, two of them at a quarter of
+// the rate, 8 us a tile of 256 x 256; rows that do not exist skip them.
 #pragma once
 #include "keep_kernels.hpp"
 #include "layer.hpp"

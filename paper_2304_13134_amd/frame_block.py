@@ -3,9 +3,9 @@ the products and the activations kept in 8 bits go together in training and in r
 
     python -m paper_2304_13134_amd.frame_block        # trains a small one through the globally normalised loss
 
-Training keeps, beside the frames themselves, the norm's result and what the activation is applied to, both in 8 bits: 5/8
-of the memory of two 16-bit tensors less, for gradients that differ by the codes' rounding (about 0.7 % of a kept value's
-rms with int8).  Recognition runs the products on 8-bit operands.
+Training keeps, beside the frames themselves, the norm's result and what the activation is applied to, both in 8 bits: 8.25
+bits a value with the scales instead of 16, for gradients that differ by the codes' rounding (0.8 % of a kept value's rms
+with int8, of normal values).  Recognition runs the products on 8-bit operands.
 """
 from __future__ import annotations
 
