@@ -144,8 +144,10 @@ struct NormGradArgs {
 // Every wavefront (WPR = 1) or workgroup goes over its rows and keeps the sums of its columns of dgain in registers;
 // they meet in LDS and go out as one row of partial sums a workgroup, added in order by column_sum_kernel.  The next row
 // is sent for before this one is worked on, always, so that the wait for this one is not one for it too: in the place of a
-// row that does not exist this one is read again, from cache.  16384 x 2048 in bfloat16 with ds, three quarters of the frames
-// existing (218 MB): 45 us, and 4.7 us for the sums over the workgroups; without that, a row a wavefront, 70 us.
+// row that does not exist this one is read again, from cache.  From turn to turn a workgroup moves on by 0.618 of their number,
+// so that one that meets the end of an item does not meet those of all, T being a multiple of that number or close to it.
+// 16384 x 2048 in bfloat16 with ds, three quarters of the frames existing (218 MB): 42 us, and 4.7 us for the sums over the
+// workgroups; in the same place every turn 45 us; a row a wavefront, nothing sent for ahead, 70 us.
 template <typename DY, typename S, int WPR, int CH, bool DS>
 __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel(NormGradArgs a)
 {
@@ -183,16 +185,25 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int k = 0; k < 8; ++k) dg[c][k] = 0.f;
-    const int step = (int)gridDim.x * kRows;
-    const auto exists = [&](int row) { return row < a.rows && frame_exists(a.frames, row); };
-    int row = (int)blockIdx.x * kRows + wave, turn = 0;
-    bool there = exists(row), there_next = exists(row + step);
+    const auto exists = [&](long long row) { return row < a.rows && frame_exists(a.frames, (int)row); };
+    const int groups = (int)gridDim.x, shift = (int)(0.618f * (float)groups);
+    int place = (int)blockIdx.x;
+    long long first = 0;                                     // of the turn that is looked at
+    const auto later = [&]() {
+        first += groups;
+        place += shift;
+        place -= place >= groups ? groups : 0;
+        return (first + place) * kRows + wave;
+    };
+    long long row = (long long)place * kRows + wave, row_next = later();
+    bool there = exists(row), there_next = exists(row_next);
     Row next{};
-    if (row < a.rows) next = get(row);
-    for (; row < a.rows; row += step, ++turn) {
+    if (row < a.rows) next = get((int)row);
+    for (int turn = 0; row < a.rows; ++turn) {
         const Row now = next;
-        next = get(there_next ? row + step : row);
-        const bool there_later = exists(row + 2 * step);
+        next = get((int)(there_next ? row_next : row));
+        const long long row_later = later();
+        const bool there_later = exists(row_later);
         float u[CH][8], s[CH][8];
         float dot = 0.f;
 #pragma unroll
@@ -233,6 +244,8 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel
             for (int k = 0; k < 8; ++k) u[c][k] = there ? u[c][k] : 0.f;
             store8_as(a.dxtype, a.dx, (size_t)row * a.pdx + h, a.H - h, u[c]);
         }
+        row = row_next;
+        row_next = row_later;
         there = there_next;
         there_next = there_later;
     }
