@@ -184,18 +184,19 @@ struct ProductPlan {
 
 // Tiles and shares of a reduction of `steps` steps (128 bytes, or 64 rows).  Up to 64 rows of a forward product go to the
 // kernel that reads w once and keeps nothing in LDS; beyond, the cheapest of what these would take, from measurements on
-// MI355X: a workgroup with a compute unit to itself takes 1.2, 0.5 and 0.2 us a step with tiles of 256, 128 and 64, two
-// that share one 0.95 and 0.4 us a step (tiles of 128 and 64), and 9, 5 and 3.5 us beside its steps; across the rows of
-// both operands a step takes 1.15 to 1.9 times as long (transposing reads).  Tiles of 256 win from a full chip on (16384 x 1024 on
-// 4096: 107 us, with tiles of 128 122), tiles of 64 up to about half a million results (512 x 1024 on 4096: 20 us, 37 and 80).  Shares are
-// written and read in 32 bits at about 5 TB/s and cost a launch: 16384 x 1024 x 4096 rows of weight gradient in 4 shares
-// 161 us, in one 357 us.
-ProductPlan plan_product(bool forward, bool across, long long P, long long Q, long long steps)
+// MI355X: a workgroup with a compute unit to itself takes 1.2, 0.5 and 0.2 us a step with tiles of 256, 128 and 64 (the first 1.5 on a
+// full chip), two that share one 0.95 and 0.4 us (tiles of 128 and 64), three 0.55 (of 64), and 9, 5 and 3.5 us beside its steps;
+// operands that run across the reduction (none, one, both) take up to 1.8 times as long (transposing reads), less where others fill the
+// time.  Tiles of 256 win from a full chip on (16384 x 1024 on 4096: 105 us, with tiles of 128 129), tiles of 64 up to about half a million
+// results (512 x 1024 on 4096: 20 us, 37 and 80).  Shares are written and read in 32 bits at about 5 TB/s and cost a launch:
+// 16384 x 1024 x 4096 rows of weight gradient in 4 shares 152 us, in one 350 us.
+ProductPlan plan_product(bool forward, int across, long long P, long long Q, long long steps)
 {
     ProductPlan best{0, 1, steps};
     if (forward && P <= 64) return best;
-    static const double alone[4] = {0, 0.2, 0.5, 1.2}, shared[4] = {0, 0.4, 0.95, 1.2}, beside[4] = {0, 3.5, 5, 9};
-    static const double by_rows[4] = {0, 1.9, 1.2, 1.15};
+    static const double alone[4] = {0, 0.2, 0.5, 1.2}, two[4] = {0, 0.4, 0.95, 0}, many[4] = {0, 0.55, 0.95, 1.5}, beside[4] = {0, 3.5, 5, 9};
+    static const double alone_by[3][3] = {{0, 1, 1}, {0, 1.4, 1.15}, {0, 1.8, 1.5}};
+    static const double many_by[3][4] = {{0, 1, 1, 1}, {0, 1.05, 1.05, 1}, {0, 1.1, 1.1, 1.15}};
     double least = 1e30;
     for (int variant = 1; variant <= 3; ++variant) {
         const long long tile = 32 << variant;
@@ -203,12 +204,17 @@ ProductPlan plan_product(bool forward, bool across, long long P, long long Q, lo
         for (int splits = 1; splits <= 64; splits *= 2) {
             const long long part = std::max(1ll, (steps + splits - 1) / splits);
             if (splits > 1 && (part < 4 || (steps + part - 1) / part != splits)) continue;
-            const long long blocks = tiles * splits, at_once = variant == 3 ? 256 : 512;
-            const double factor = across ? by_rows[variant] : 1.0;
-            double us;
-            if (blocks <= 256) us = part * alone[variant] * factor + beside[variant];
-            else if (variant == 3) us = (double)((blocks + 255) / 256) * (part * shared[variant] * factor + beside[variant]);
-            else us = std::max(1.0, (double)blocks / at_once) * (part * shared[variant] * factor + beside[variant]);
+            const long long blocks = tiles * splits, at_once = variant == 1 ? 768 : variant == 2 ? 512 : 256;
+            double step, rounds = std::max(1.0, (double)blocks / at_once);
+            if (variant == 3) {
+                step = (alone[3] + (many[3] - alone[3]) * std::min(1.0, blocks / 256.0)) * many_by[across][3];
+                rounds = (double)((blocks + 255) / 256);
+            } else if (blocks <= 256) {
+                step = alone[variant] * alone_by[across][variant];
+            } else {
+                step = (blocks <= 512 ? two : many)[variant] * many_by[across][variant];
+            }
+            double us = rounds * (part * step + beside[variant]);
             if (splits > 1) us += 4 + (double)splits * P * Q * 8 / 5e6;
             if (us < least) {
                 least = us;
@@ -236,7 +242,7 @@ void launch_tiles(ProductArgs a, const ProductPlan& p, hipStream_t st)
     constexpr bool kEight = Elt<E>::size == 1;
     if (p.variant == 3) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 256, 256, 2, 4, kEight ? 2 : 3, 2>), grid, dim3(512), 0, st, a);
     else if (p.variant == 2) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 128, 128, 2, 2, kEight ? 2 : 3, 2>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((product_kernel<E, LP, LQ, 64, 64, 2, 2, 4, 4>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((product_kernel<E, LP, LQ, 64, 64, 2, 2, 3, 3>), grid, dim3(256), 0, st, a);
     if (p.splits > 1) {
         const long long waves = (long long)((a.P + 15) / 16) * ((a.Q + 31) / 32);
         hipLaunchKernelGGL(product_join_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, j, p.splits);
@@ -394,7 +400,7 @@ last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, in
     a.Q = N;
     a.K = bytes;
     a.frames = frames_of(f);
-    const ProductPlan plan = plan_product(true, false, rows, N, (bytes + kStep - 1) / kStep);
+    const ProductPlan plan = plan_product(true, 0, rows, N, (bytes + kStep - 1) / kStep);
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
     pre.launch(st);
@@ -430,7 +436,7 @@ last_status_t run_grad_input(Carver& cv, const last_frames_t* f, long long rows,
     a.K = bytes;
     a.q_rows = N;
     a.frames = frames_of(f);
-    const ProductPlan plan = plan_product(false, false, rows, K, (bytes + kStep - 1) / kStep);
+    const ProductPlan plan = plan_product(false, 1, rows, K, (bytes + kStep - 1) / kStep);
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
     pre.launch(st);
@@ -474,7 +480,7 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
     a.P = N;
     a.Q = K;
     a.K = rows;
-    const ProductPlan plan = plan_product(false, true, N, K, (rows + 63) / 64);
+    const ProductPlan plan = plan_product(false, 2, N, K, (rows + 63) / 64);
     set_plan(cv, a, plan, 64, dbias);
     unsigned long long* mask = f->lengths ? (unsigned long long*)cv.take((size_t)((rows + 63) / 64 * 8)) : nullptr;
     if (!cv.base) return LAST_OK;
