@@ -327,6 +327,34 @@ def test_nan_blocks_and_infinities_stay_in_their_rows():
         assert torch.equal(got[keep], want[keep]) and not torch.isfinite(got[5]).any()
 
 
+@pytest.mark.parametrize("T,N,K", [(261, 320, 128), (833, 512, 2048), (3301, 1024, 1024)])
+@pytest.mark.parametrize("out", ["bf16", "f32", "i8"])
+def test_stretches_without_frames(T, N, K, out):
+    """Tiles and parts of tiles in which no frame is: zeros there, and elsewhere the bits of a call on which all frames exist."""
+    announce("stretches without frames", T, N, K, out)
+    rng = np.random.default_rng(T)
+    n = np.array([T, 0, 64, T // 2, 1], np.int32)
+    there = exists(5, T, n)
+    where = torch.from_numpy(there).cuda()[..., None]
+    x, w, r = draw(rng, (5, T, K), "bf16"), draw(rng, (N, K), "bf16", K ** -0.5), draw(rng, (5, T, N), "bf16" if out in EIGHT else out)
+    kept = lb.last_keep(draw(rng, (5, T, K), "f32"), EIGHT["i8"])
+    dy = draw(rng, (5, T, N), "bf16")
+
+    def call(lengths):
+        type_ = EIGHT.get(out) or TYPES[out]
+        y = lb.last_product(x, w, activation="gelu", lengths=lengths, dtype=type_)[0]
+        return [*(y if out in EIGHT else (y,)),
+                *([] if out in EIGHT else [lb.last_product(x, w, activation="silu", residual=r, lengths=lengths, dtype=type_)[0],
+                                           lb.last_product_grad_input(dy, w, kept=kept, activation="silu", lengths=lengths, dtype=type_)]),
+                *lb.last_product(x, w, lengths=lengths, keep=EIGHT["i8"])[1], *lb.last_keep(x, EIGHT["i8"], lengths=lengths)]
+
+    want = [torch.where(where, v, torch.zeros_like(v)) for v in call(None)]
+    for t in (x, r, dy, kept):
+        spoil(t, there)
+    for v, u in zip(call(dev_lengths(n)), want):
+        assert torch.equal(v, u)
+
+
 @pytest.mark.parametrize("B,T,N,K", PRODUCTS)
 @pytest.mark.parametrize("type_,out,kind,name,lens", [("bf16", "bf16", None, "none", "some"), ("bf16", "bf16", "i8", "silu", "some"), ("f16", "f32", "e4m3", "gelu", "all"),
                                                      ("bf16", "f16", "i8", "tanh", "none"), ("f16", "f16", "e4m3", "relu", "some")])
