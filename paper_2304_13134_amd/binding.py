@@ -195,13 +195,16 @@ def verify_placement(device=None):
 
 def workspace(nbytes, device, least=None):
     """A cached device scratch buffer (grown on demand, 256-byte aligned by the allocator), one per
-    device and stream: calls enqueued on different streams may overlap and must not share scratch.  It is kept until
-    release_workspaces().  Where the card has no room for `nbytes`, one of `least()` bytes, which is not kept."""
+    device and stream: calls enqueued on different streams may overlap and must not share scratch.  It is kept until a
+    larger one takes its place or release_workspaces().  A call under graph capture gets one of the graph's own memory instead,
+    as other temporaries of a capture: the graph writes there on every replay, whatever became of the cached one by then.
+    Where the card has no room for `nbytes`, one of `least()` bytes, which is not kept."""
     index = torch.device(device).index or 0
-    if index not in _placement and not torch.cuda.is_current_stream_capturing():
+    capturing = torch.cuda.is_current_stream_capturing()
+    if index not in _placement and not capturing:
         verify_placement(index)     # once per device, before the first kernel that relies on it
     key = (index, torch.cuda.current_stream().cuda_stream)
-    buf = _workspaces.get(key)
+    buf = None if capturing else _workspaces.get(key)
     if buf is None or buf.numel() < nbytes:
         try:
             buf = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
@@ -210,7 +213,8 @@ def workspace(nbytes, device, least=None):
             if few >= nbytes:
                 raise
             return buf if buf is not None and buf.numel() >= few else torch.empty(few, dtype=torch.uint8, device=device)
-        _workspaces[key] = buf
+        if not capturing:
+            _workspaces[key] = buf
     return buf
 
 
@@ -591,9 +595,9 @@ def _stream_of(t):
 
 def _with_scratch(call, op, frames, N, K, a, b, t):
     """call(workspace address, bytes, stream) for tensor t's device and stream.  The buffer that is there is tried first: the
-    library refuses one that is too small before it enqueues anything."""
+    library refuses one that is too small before it enqueues anything.  (Not under capture, see workspace().)"""
     stream = _stream_of(t)
-    buf = _workspaces.get((t.get_device(), stream))
+    buf = None if torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((t.get_device(), stream))
     if buf is not None:
         code = call(buf.data_ptr(), buf.numel(), stream)
         if code != 5:
