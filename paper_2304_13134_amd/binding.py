@@ -518,14 +518,20 @@ def _pitch(t, name):
     return pitch
 
 
-def _matrix(t, name, rows=None, columns=None):
-    """The packed LastMatrix of a device tensor or a Kept, whose shape is checked against `rows` (leading sizes) and `columns`."""
+def _same_device(t, on, name):
+    if t.get_device() != on:
+        raise ValueError("%s is on another device than the call's other tensors" % name)
+
+
+def _matrix(t, name, on, rows=None, columns=None):
+    """The packed LastMatrix of a tensor or a Kept on device `on`, whose shape is checked against `rows` (leading sizes) and `columns`."""
     codes, scales = t if isinstance(t, Kept) else (t, None)
     type_ = _TYPES.get(codes.dtype) if isinstance(codes, torch.Tensor) else None
     if type_ is None or not codes.is_cuda:
         raise TypeError("%s must be a device tensor of a supported type" % name)
     if (type_ >= 3) != (scales is not None):
         raise TypeError("%s: values in 8 bits are a Kept of codes and scales" % name)
+    _same_device(codes, on, name)
     shape = codes.shape
     if (rows is not None and shape[:-1] != rows) or (columns is not None and shape[-1] != columns):
         raise ValueError("%s has shape %s: expected %s" % (name, tuple(shape), (*(rows or ("...",)), columns)))
@@ -535,35 +541,38 @@ def _matrix(t, name, rows=None, columns=None):
     if not isinstance(scales, torch.Tensor) or not scales.is_cuda or scales.dtype != torch.uint8 \
             or scales.shape != (*shape[:-1], (shape[-1] + 31) // 32):
         raise TypeError("the scales of %s must be device uint8 [..., ceil(columns / 32)]" % name)
+    _same_device(scales, on, "the scales of " + name)
     scale_pitch = scales.shape[-1] if scales.is_contiguous() else _pitch(scales, name)
     return _pack_matrix(codes.data_ptr() or _NO_ROWS, type_, pitch, scales.data_ptr() or _NO_ROWS, scale_pitch)
 
 
-def _opt(t, name, rows, columns):
-    return None if t is None else _matrix(t, name, rows, columns)
+def _opt(t, name, on, rows, columns):
+    return None if t is None else _matrix(t, name, on, rows, columns)
 
 
-def _vector(t, n, name):
+def _vector(t, n, name, on):
     if t is None:
         return None
     _dev_tensor(t, torch.float32, name)
     if t.numel() != n:
         raise ValueError("%s must have %d elements" % (name, n))
+    _same_device(t, on, name)
     return t.data_ptr()
 
 
 def _frames(t, lengths, name):
-    """(packed LastFrames, leading sizes, tensor) of a tensor or Kept [R, H] or [B, T, H]; with lengths it is the latter."""
+    """(packed LastFrames, leading sizes, tensor, its device) of a tensor or Kept [R, H] or [B, T, H]; with lengths it is the latter."""
     t = t[0] if isinstance(t, Kept) else t
     if not isinstance(t, torch.Tensor) or t.dim() not in (2, 3):
         raise TypeError("%s must be a device tensor [rows, columns] or [B, T, columns]" % name)
-    rows = t.shape[:-1]
+    rows, on = t.shape[:-1], t.get_device()
     if lengths is None:
-        return _pack_frames(1, rows[0] if len(rows) == 1 else rows[0] * rows[1], 0), rows, t
+        return _pack_frames(1, rows[0] if len(rows) == 1 else rows[0] * rows[1], 0), rows, t, on
     _dev_tensor(lengths, torch.int32, "lengths")
     if len(rows) != 2 or lengths.shape != rows[:1]:
         raise ValueError("with lengths [B], %s must be [B, T, columns]" % name)
-    return _pack_frames(rows[0], rows[1], lengths.data_ptr()), rows, t
+    _same_device(lengths, on, "lengths")
+    return _pack_frames(rows[0], rows[1], lengths.data_ptr()), rows, t, on
 
 
 def _activation(name):
@@ -588,25 +597,29 @@ def _result(shape, dtype, device, like=None):
     return Kept(t, scales), _pack_matrix(t.data_ptr() or _NO_ROWS, type_, shape[-1], scales.data_ptr() or _NO_ROWS, blocks)
 
 
-def _stream_of(t):
-    """The current stream of the tensor's device."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+def _launch(t, call):
+    """call(stream) with tensor t's device as the current one, on that device's current stream.  (The handle of a default stream
+    is 0 whichever device it is of, and means that of the current device.)"""
+    index = t.get_device()
+    if index == torch._C._cuda_getDevice():
+        return call(torch._C._cuda_getCurrentRawStream(index))
+    with torch.cuda.device(index):
+        return call(torch._C._cuda_getCurrentRawStream(index))
 
 
 def _with_scratch(call, op, frames, N, K, a, b, t):
-    """call(workspace address, bytes, stream) for tensor t's device and stream.  The buffer that is there is tried first: the
-    library refuses one that is too small before it enqueues anything.  (Not under capture, see workspace().)"""
-    stream = _stream_of(t)
-    buf = None if torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((t.get_device(), stream))
-    if buf is not None:
-        code = call(buf.data_ptr(), buf.numel(), stream)
-        if code != 5:
-            return _check(code)
-    nbytes = load_library().last_layer_workspace_bytes(op, frames, N, K, a, b)
-    if nbytes == 0:
-        nbytes = 256                                  # (the call says what is wrong)
-    buf = workspace(nbytes, t.device)
-    _check(call(buf.data_ptr(), buf.numel(), stream))
+    """call(workspace address, bytes, stream) for tensor t's device and its current stream.  The buffer that is there is tried
+    first: the library refuses one that is too small before it enqueues anything.  (Not under capture, see workspace().)"""
+    def launch(stream):
+        buf = None if torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((t.get_device(), stream))
+        if buf is not None:
+            code = call(buf.data_ptr(), buf.numel(), stream)
+            if code != 5:
+                return code
+        nbytes = load_library().last_layer_workspace_bytes(op, frames, N, K, a, b)
+        buf = workspace(nbytes or 256, t.device)      # (where none would do, the call says what is wrong)
+        return call(buf.data_ptr(), buf.numel(), stream)
+    _check(_launch(t, launch))
 
 
 def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=None, keep=None):
@@ -614,10 +627,10 @@ def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=Non
     x), s (None without a residual, where it is x), inv [rows] float32 for the gradient, and, with `keep` torch.int8 or
     torch.float8_e4m3fn, y in 8 bits as a Kept.  With `keep` and no `dtype`, y itself is None.  x: [rows, H], or [B, T, H] with
     lengths [B] of which the frames past the end are zeros in every result."""
-    fr, rows, _ = _frames(x, lengths, "x")
+    fr, rows, _, on = _frames(x, lengths, "x")
     shape, device = x.shape, x.device
     H = shape[-1]
-    mx, mr = _matrix(x, "x"), _opt(residual, "residual", rows, H)
+    mx, mr, g = _matrix(x, "x", on), _opt(residual, "residual", on, rows, H), _vector(gain, H, "gain", on)
     s = y = kept = ms = my = mk = None
     if residual is not None:
         s, ms = _result(shape, x.dtype, device, x)
@@ -626,8 +639,8 @@ def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=Non
     if keep is not None:
         kept, mk = _result(shape, keep, device, x)
     inv = torch.empty(tuple(rows), dtype=torch.float32, device=device)
-    _check(load_library().last_residual_norm(fr, H, mx, mr, _vector(gain, H, "gain"), eps, ms, my, mk, inv.data_ptr() or _NO_ROWS,
-                                             _stream_of(x)))
+    call, i = load_library().last_residual_norm, inv.data_ptr() or _NO_ROWS
+    _check(_launch(x, lambda stream: call(fr, H, mx, mr, g, eps, ms, my, mk, i, stream)))
     return Norm(y, s, inv, kept)
 
 
@@ -635,15 +648,15 @@ def last_residual_norm_grad(dy, s, gain, inv, ds=None, lengths=None, dtype=None)
     """(dx, dgain): the gradient of x and of the residual alike, of `dtype` (default: that of ds, or of s, or, s being a
     Kept, of dy), and dgain [H] float32.  s and inv as last_residual_norm returned them, s maybe in 8 bits (a Kept); ds:
     the gradient that reaches s by other ways."""
-    fr, rows, _ = _frames(dy, lengths, "dy")
+    fr, rows, _, on = _frames(dy, lengths, "dy")
     H, device = dy.shape[-1], dy.device
     if dtype is None:
         dtype = ds.dtype if ds is not None else dy.dtype if isinstance(s, Kept) else s.dtype
-    mdy, ms, mds = _matrix(dy, "dy"), _matrix(s, "s", rows, H), _opt(ds, "ds", rows, H)
+    mdy, ms, mds = _matrix(dy, "dy", on), _matrix(s, "s", on, rows, H), _opt(ds, "ds", on, rows, H)
+    g, i = _vector(gain, H, "gain", on), _vector(inv, dy.numel() // H, "inv", on) or _NO_ROWS
     dx, mdx = _result(dy.shape, dtype, device, dy)
     dgain = torch.empty(H, dtype=torch.float32, device=device)
     call = load_library().last_residual_norm_grad
-    g, i = _vector(gain, H, "gain"), _vector(inv, dy.numel() // H, "inv") or _NO_ROWS
     _with_scratch(lambda ws, n, stream: call(fr, H, mdy, ms, g, i, mds, mdx, dgain.data_ptr(), ws, n, stream),
                   OP_RESIDUAL_NORM_GRAD, fr, 1, H, None, None, dy)
     return dx, dgain
@@ -653,14 +666,14 @@ def last_product(x, w, bias=None, activation="none", residual=None, lengths=None
     """(y, kept): y = act(x w^T + bias) + residual, w [N, K], x [rows, K] or [B, T, K]: both bfloat16, float16, or both a Kept
     of float8_e4m3fn.  `dtype` of y: default that of x (bfloat16 for a Kept); torch.int8 or torch.float8_e4m3fn make it a Kept.
     `keep`: such a type to keep what the activation is applied to in (kept, a Kept), or None."""
-    fr, rows, t = _frames(x, lengths, "x")
+    fr, rows, t, on = _frames(x, lengths, "x")
     N, K = (w[0] if isinstance(w, Kept) else w).shape
-    mx, mw = _matrix(x, "x", rows, K), _matrix(w, "w", (N,), K)
+    mx, mw, b, mr = _matrix(x, "x", on, rows, K), _matrix(w, "w", on, (N,), K), _vector(bias, N, "bias", on), _opt(residual, "residual", on, rows, N)
     shape, device, kept, mk = (*rows, N), t.device, None, None
     y, my = _result(shape, dtype or (torch.bfloat16 if isinstance(x, Kept) else x.dtype), device)
     if keep is not None:
         kept, mk = _result(shape, keep, device)
-    call, b, act, mr = load_library().last_product, _vector(bias, N, "bias"), _activation(activation), _opt(residual, "residual", rows, N)
+    call, act = load_library().last_product, _activation(activation)
     _with_scratch(lambda ws, n, stream: call(fr, N, K, mx, mw, b, act, mr, my, mk, ws, n, stream), OP_PRODUCT, fr, N, K, mx, mw, t)
     return y, kept
 
@@ -668,9 +681,9 @@ def last_product(x, w, bias=None, activation="none", residual=None, lengths=None
 def last_product_grad_input(dy, w, kept=None, activation="none", lengths=None, dtype=None):
     """dx = (dy w) * act'(kept), of `dtype` (default: that of dy): the gradient of a product's input and, with `kept` [.., K],
     through the activation that made this input of what was kept."""
-    fr, rows, _ = _frames(dy, lengths, "dy")
+    fr, rows, _, on = _frames(dy, lengths, "dy")
     N, K = w.shape
-    mdy, mw, mk = _matrix(dy, "dy", rows, N), _matrix(w, "w", (N,), K), _opt(kept, "kept", rows, K)
+    mdy, mw, mk = _matrix(dy, "dy", on, rows, N), _matrix(w, "w", on, (N,), K), _opt(kept, "kept", on, rows, K)
     dx, mdx = _result((*rows, K), dtype or dy.dtype, dy.device)
     call, act = load_library().last_product_grad_input, _activation(activation)
     _with_scratch(lambda ws, n, stream: call(fr, N, K, mdy, mw, mk, act, mdx, ws, n, stream), OP_PRODUCT_GRAD_INPUT, fr, N, K, mdy, mw, dy)
@@ -680,9 +693,9 @@ def last_product_grad_input(dy, w, kept=None, activation="none", lengths=None, d
 def last_product_grad_weight(dy, x, activation="none", lengths=None, dtype=torch.float32):
     """(dw [N, K] of `dtype`, dbias [N] float32): dy^T act(x) and the column sums of dy.  x: of dy's type (activation "none"),
     or a Kept, whose activation is formed again."""
-    fr, rows, _ = _frames(dy, lengths, "dy")
+    fr, rows, _, on = _frames(dy, lengths, "dy")
     N, K, device = dy.shape[-1], (x[0] if isinstance(x, Kept) else x).shape[-1], dy.device
-    mdy, mx = _matrix(dy, "dy"), _matrix(x, "x", rows, K)
+    mdy, mx = _matrix(dy, "dy", on), _matrix(x, "x", on, rows, K)
     dw, mdw = _result((N, K), dtype, device)
     dbias = torch.empty(N, dtype=torch.float32, device=device)
     call, act = load_library().last_product_grad_weight, _activation(activation)
@@ -693,27 +706,30 @@ def last_product_grad_weight(dy, x, activation="none", lengths=None, dtype=torch
 
 def last_keep(x, dtype=torch.int8, lengths=None):
     """x in 8 bits: a Kept of torch.int8 or torch.float8_e4m3fn codes."""
-    fr, _, _ = _frames(x, lengths, "x")
-    mx = _matrix(x, "x")
+    fr, _, _, on = _frames(x, lengths, "x")
+    mx = _matrix(x, "x", on)
     kept, mk = _result(x.shape, dtype, x.device, x)
-    _check(load_library().last_keep(fr, x.shape[-1], mx, mk, _stream_of(x)))
+    call = load_library().last_keep
+    _check(_launch(x, lambda stream: call(fr, x.shape[-1], mx, mk, stream)))
     return kept
 
 
 def last_kept_values(kept, activation="none", lengths=None, dtype=torch.bfloat16):
     """act(kept): what the codes stand for, or the activation formed again from them."""
-    fr, _, t = _frames(kept, lengths, "kept")
-    mk = _matrix(kept, "kept")
+    fr, _, t, on = _frames(kept, lengths, "kept")
+    mk = _matrix(kept, "kept", on)
     y, my = _result(t.shape, dtype, t.device, t)
-    _check(load_library().last_kept_values(fr, t.shape[-1], mk, _activation(activation), my, _stream_of(t)))
+    call, act = load_library().last_kept_values, _activation(activation)
+    _check(_launch(t, lambda stream: call(fr, t.shape[-1], mk, act, my, stream)))
     return y
 
 
 def last_kept_grad(dy, kept, activation, lengths=None, dtype=None):
     """dy * act'(kept), of `dtype` (default: that of dy): the gradient of an activation alone."""
-    fr, rows, _ = _frames(dy, lengths, "dy")
+    fr, rows, _, on = _frames(dy, lengths, "dy")
     H = dy.shape[-1]
-    mdy, mk = _matrix(dy, "dy"), _matrix(kept, "kept", rows, H)
+    mdy, mk = _matrix(dy, "dy", on), _matrix(kept, "kept", on, rows, H)
     dx, mdx = _result(dy.shape, dtype or dy.dtype, dy.device, dy)
-    _check(load_library().last_kept_grad(fr, H, mdy, mk, _activation(activation), mdx, _stream_of(dy)))
+    call, act = load_library().last_kept_grad, _activation(activation)
+    _check(_launch(dy, lambda stream: call(fr, H, mdy, mk, act, mdx, stream)))
     return dx
