@@ -518,9 +518,8 @@ def _pitch(t, name):
     return pitch
 
 
-def _same_device(t, on, name):
-    if t.get_device() != on:
-        raise ValueError("%s is on another device than the call's other tensors" % name)
+def _elsewhere(name):
+    raise ValueError("%s is on another device than the call's other tensors" % name)
 
 
 def _matrix(t, name, on, rows=None, columns=None):
@@ -531,7 +530,8 @@ def _matrix(t, name, on, rows=None, columns=None):
         raise TypeError("%s must be a device tensor of a supported type" % name)
     if (type_ >= 3) != (scales is not None):
         raise TypeError("%s: values in 8 bits are a Kept of codes and scales" % name)
-    _same_device(codes, on, name)
+    if codes.get_device() != on:
+        _elsewhere(name)
     shape = codes.shape
     if (rows is not None and shape[:-1] != rows) or (columns is not None and shape[-1] != columns):
         raise ValueError("%s has shape %s: expected %s" % (name, tuple(shape), (*(rows or ("...",)), columns)))
@@ -541,7 +541,8 @@ def _matrix(t, name, on, rows=None, columns=None):
     if not isinstance(scales, torch.Tensor) or not scales.is_cuda or scales.dtype != torch.uint8 \
             or scales.shape != (*shape[:-1], (shape[-1] + 31) // 32):
         raise TypeError("the scales of %s must be device uint8 [..., ceil(columns / 32)]" % name)
-    _same_device(scales, on, "the scales of " + name)
+    if scales.get_device() != on:
+        _elsewhere("the scales of " + name)
     scale_pitch = scales.shape[-1] if scales.is_contiguous() else _pitch(scales, name)
     return _pack_matrix(codes.data_ptr() or _NO_ROWS, type_, pitch, scales.data_ptr() or _NO_ROWS, scale_pitch)
 
@@ -556,7 +557,8 @@ def _vector(t, n, name, on):
     _dev_tensor(t, torch.float32, name)
     if t.numel() != n:
         raise ValueError("%s must have %d elements" % (name, n))
-    _same_device(t, on, name)
+    if t.get_device() != on:
+        _elsewhere(name)
     return t.data_ptr()
 
 
@@ -571,7 +573,8 @@ def _frames(t, lengths, name):
     _dev_tensor(lengths, torch.int32, "lengths")
     if len(rows) != 2 or lengths.shape != rows[:1]:
         raise ValueError("with lengths [B], %s must be [B, T, columns]" % name)
-    _same_device(lengths, on, "lengths")
+    if lengths.get_device() != on:
+        _elsewhere("lengths")
     return _pack_frames(rows[0], rows[1], lengths.data_ptr()), rows, t, on
 
 
@@ -597,29 +600,31 @@ def _result(shape, dtype, device, like=None):
     return Kept(t, scales), _pack_matrix(t.data_ptr() or _NO_ROWS, type_, shape[-1], scales.data_ptr() or _NO_ROWS, blocks)
 
 
-def _launch(t, call):
-    """call(stream) with tensor t's device as the current one, on that device's current stream.  (The handle of a default stream
-    is 0 whichever device it is of, and means that of the current device.)"""
-    index = t.get_device()
-    if index == torch._C._cuda_getDevice():
-        return call(torch._C._cuda_getCurrentRawStream(index))
-    with torch.cuda.device(index):
-        return call(torch._C._cuda_getCurrentRawStream(index))
+def _launch(on, call, *arguments):
+    """call(*arguments, stream) with device `on` as the current one, on its current stream.  (The handle of a default stream is 0
+    whichever device it is of, and means that of the current device.)"""
+    if on != torch._C._cuda_getDevice():
+        with torch.cuda.device(on):
+            return _launch(on, call, *arguments)
+    _check(call(*arguments, torch._C._cuda_getCurrentRawStream(on)))
 
 
 def _with_scratch(call, op, frames, N, K, a, b, t):
     """call(workspace address, bytes, stream) for tensor t's device and its current stream.  The buffer that is there is tried
     first: the library refuses one that is too small before it enqueues anything.  (Not under capture, see workspace().)"""
-    def launch(stream):
-        buf = None if torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((t.get_device(), stream))
-        if buf is not None:
-            code = call(buf.data_ptr(), buf.numel(), stream)
-            if code != 5:
-                return code
-        nbytes = load_library().last_layer_workspace_bytes(op, frames, N, K, a, b)
-        buf = workspace(nbytes or 256, t.device)      # (where none would do, the call says what is wrong)
-        return call(buf.data_ptr(), buf.numel(), stream)
-    _check(_launch(t, launch))
+    on = t.get_device()
+    if on != torch._C._cuda_getDevice():
+        with torch.cuda.device(on):
+            return _with_scratch(call, op, frames, N, K, a, b, t)
+    stream = torch._C._cuda_getCurrentRawStream(on)
+    buf = None if torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((on, stream))
+    if buf is not None:
+        code = call(buf.data_ptr(), buf.numel(), stream)
+        if code != 5:
+            return _check(code)
+    nbytes = load_library().last_layer_workspace_bytes(op, frames, N, K, a, b)
+    buf = workspace(nbytes or 256, t.device)          # (where none would do, the call says what is wrong)
+    _check(call(buf.data_ptr(), buf.numel(), stream))
 
 
 def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=None, keep=None):
@@ -639,8 +644,7 @@ def last_residual_norm(x, gain, residual=None, lengths=None, eps=1e-5, dtype=Non
     if keep is not None:
         kept, mk = _result(shape, keep, device, x)
     inv = torch.empty(tuple(rows), dtype=torch.float32, device=device)
-    call, i = load_library().last_residual_norm, inv.data_ptr() or _NO_ROWS
-    _check(_launch(x, lambda stream: call(fr, H, mx, mr, g, eps, ms, my, mk, i, stream)))
+    _launch(on, load_library().last_residual_norm, fr, H, mx, mr, g, eps, ms, my, mk, inv.data_ptr() or _NO_ROWS)
     return Norm(y, s, inv, kept)
 
 
@@ -709,8 +713,7 @@ def last_keep(x, dtype=torch.int8, lengths=None):
     fr, _, _, on = _frames(x, lengths, "x")
     mx = _matrix(x, "x", on)
     kept, mk = _result(x.shape, dtype, x.device, x)
-    call = load_library().last_keep
-    _check(_launch(x, lambda stream: call(fr, x.shape[-1], mx, mk, stream)))
+    _launch(on, load_library().last_keep, fr, x.shape[-1], mx, mk)
     return kept
 
 
@@ -719,8 +722,7 @@ def last_kept_values(kept, activation="none", lengths=None, dtype=torch.bfloat16
     fr, _, t, on = _frames(kept, lengths, "kept")
     mk = _matrix(kept, "kept", on)
     y, my = _result(t.shape, dtype, t.device, t)
-    call, act = load_library().last_kept_values, _activation(activation)
-    _check(_launch(t, lambda stream: call(fr, t.shape[-1], mk, act, my, stream)))
+    _launch(on, load_library().last_kept_values, fr, t.shape[-1], mk, _activation(activation), my)
     return y
 
 
@@ -730,6 +732,5 @@ def last_kept_grad(dy, kept, activation, lengths=None, dtype=None):
     H = dy.shape[-1]
     mdy, mk = _matrix(dy, "dy", on), _matrix(kept, "kept", on, rows, H)
     dx, mdx = _result(dy.shape, dtype or dy.dtype, dy.device, dy)
-    call, act = load_library().last_kept_grad, _activation(activation)
-    _check(_launch(dy, lambda stream: call(fr, H, mdy, mk, act, mdx, stream)))
+    _launch(on, load_library().last_kept_grad, fr, H, mdy, mk, _activation(activation), mdx)
     return dx
