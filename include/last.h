@@ -298,7 +298,8 @@ typedef struct {
 
 /* s = x + residual, inv = 1 / sqrt(mean over the H columns of s^2 + eps), y = s * inv * gain.  gain: dev float32 [H], H up
  * to 16384.  residual may be NULL (then s = x); results that are NULL are not written: s (type of x), y (F32, BF16 or F16),
- * kept (y in 8 bits), inv (dev float32 [B*T], what the gradient needs).  x and residual: F32, BF16 or F16, the same. */
+ * kept (y in 8 bits), inv (dev float32 [B*T], what the gradient needs).  x and residual: F32, BF16 or F16, the same.  With
+ * kept, a row and its sum are formed in 64 bits: codes, y and inv are the exact row's, rounded once. */
 last_status_t last_residual_norm(const last_frames_t* frames, int32_t H, const last_matrix_t* x,
                                  const last_matrix_t* residual, const float* gain, float eps,
                                  const last_matrix_t* s, const last_matrix_t* y, const last_matrix_t* kept,

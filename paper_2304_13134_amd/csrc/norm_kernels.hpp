@@ -43,11 +43,12 @@ __device__ __forceinline__ F row_sum(F v, F* red, int turn)
     return v;
 }
 
-// to 32 bits, inexact values to the neighbour whose last bit is 1: rounding that again, to fewer bits, is rounding once
-__device__ __forceinline__ float to_odd(double v)
+// to 32 bits, inexact values to the neighbour whose last bit is 1: rounding that again, to fewer bits, is rounding once.
+// near: v to nearest, which is infinite where v passes what 32 bits hold
+__device__ __forceinline__ float to_odd(double v, float near)
 {
     const float f = __double2float_rz(v);
-    return (double)f == v || !(fabsf(f) < __builtin_huge_valf()) ? f : __uint_as_float(__float_as_uint(f) | 1u);
+    return (double)f == v || !(fabsf(near) < __builtin_huge_valf()) ? near : __uint_as_float(__float_as_uint(f) | 1u);
 }
 
 // KEEP: with the result in 8 bits.  Its codes are those of the exact row: where 32 bits are enough for a result that is
@@ -119,8 +120,16 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_kernel(Norm
         load8<float>(a.gain, h, a.H - h, g);
         if constexpr (KEEP) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[c][k] = there ? to_odd(((double)v[c][k] + (double)rest[c][k]) * inv * (double)g[k]) : 0.f;
+            for (int k = 0; k < 8; ++k) {
+                const double d = there ? ((double)v[c][k] + (double)rest[c][k]) * inv * (double)g[k] : 0.0;
+                g[k] = (float)d;                             // a result in 32 bits is rounded to nearest, the codes and 16 bits once more
+                v[c][k] = to_odd(d, g[k]);
+            }
             store_eight(a.kept, row, h, a.H - h, (lane & 3) == 0, quad_max(top8(v[c])), v[c]);
+            if (a.y && a.ytype == LAST_F32) {
+                store8<float>(a.y, (size_t)row * a.py + h, a.H - h, g);
+                continue;
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[c][k] = there ? v[c][k] * inv * g[k] : 0.f;
