@@ -90,7 +90,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_kernel(Norm
                     const float x = v[c][k], s = x + r[k];
                     if constexpr (KEEP) {
                         const float t = s - x;
-                        rest[c][k] = (x - (s - t)) + (r[k] - t);
+                        rest[c][k] = fabsf(s) < __builtin_huge_valf() ? (x - (s - t)) + (r[k] - t) : 0.f;   // (of an infinity: NaN)
                     }
                     v[c][k] = s;
                 }

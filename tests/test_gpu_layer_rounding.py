@@ -45,3 +45,28 @@ def test_float32_norm_beside_codes_overflows():
     for t in (torch.bfloat16, torch.float16):
         assert torch.equal(torch.isinf(lb.last_residual_norm(x, gain, eps=0.0, dtype=t, keep=torch.int8).y),
                            torch.isinf(lb.last_residual_norm(x, gain, eps=0.0, dtype=t).y))
+
+
+@pytest.mark.parametrize("type_", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("where", ["x", "residual", "sum"])
+def test_infinite_sums_beside_codes(type_, where):
+    """An infinity in x or in the residual, or a sum that passes the type's largest number in 32 bits: NaN in its own place and zeros
+    in the rest of the row, whose inverse root mean square is 0, with codes as without; the codes' other blocks stand for zeros."""
+    announce("infinite sums beside codes", type_, where)
+    x, r = torch.ones(4, 96, device="cuda", dtype=type_), torch.full((4, 96), 0.5, device="cuda", dtype=type_)
+    if where == "sum":
+        if type_ == torch.float16:
+            pytest.skip("sums of float16 stay below the largest float32")
+        x[2, 40] = r[2, 40] = 3e38
+    else:
+        (x if where == "x" else r)[2, 40] = -INF
+    gain = torch.full((96,), 2.0, device="cuda")
+    plain = lb.last_residual_norm(x, gain, residual=r, dtype=torch.float32)
+    got = lb.last_residual_norm(x, gain, residual=r, dtype=torch.float32, keep=torch.int8)
+    assert float(got.inv[2]) == float(plain.inv[2]) == 0.0
+    for y in (plain.y.cpu(), got.y.cpu()):
+        assert torch.isnan(y[2, 40]) and int(torch.isnan(y).sum()) == 1
+        assert not y[2, :40].any() and not y[2, 41:].any()
+    assert torch.equal(got.s.isinf(), plain.s.isinf()) and bool(got.s[2, 40].isinf())
+    k = decode(got.kept)
+    assert np.isnan(k[2, 32:64]).all() and not k[2, :32].any() and not k[2, 64:].any() and np.isfinite(k[[0, 1, 3]]).all()
