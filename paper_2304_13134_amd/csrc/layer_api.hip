@@ -21,6 +21,7 @@ constexpr long long kMaxColumns = 1ll << 20;
 constexpr long long kMaxPitchBytes = 4ll << 20;      // 256 rows of a tile stay within 32-bit offsets
 constexpr int kMaxNormColumns = 16384;
 constexpr size_t kAlign = 256;
+constexpr long long kMaxThreads = 1ll << 31;         // of a launch, which takes fewer than 2^32: what has more to do goes out in pieces
 
 size_t align_up(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
@@ -83,15 +84,20 @@ bool bad_activation(int act) { return act < LAST_ACT_NONE || act > LAST_ACT_TANH
 // ---------------------------------------------------------------- norm
 
 template <typename X, bool KEEP>
-void launch_norm(const NormArgs& a, hipStream_t st)
+void launch_norm(NormArgs a, hipStream_t st)
 {
-    const int four = (a.rows + 3) / 4;
-    if (a.H <= 512) hipLaunchKernelGGL((norm_kernel<X, 1, 1, KEEP>), dim3(four), dim3(256), 0, st, a);
-    else if (a.H <= 1024) hipLaunchKernelGGL((norm_kernel<X, 1, 2, KEEP>), dim3(four), dim3(256), 0, st, a);
-    else if (a.H <= 2048) hipLaunchKernelGGL((norm_kernel<X, 1, 4, KEEP>), dim3(four), dim3(256), 0, st, a);
-    else if (a.H <= 4096) hipLaunchKernelGGL((norm_kernel<X, 4, 2, KEEP>), dim3(a.rows), dim3(256), 0, st, a);
-    else if (a.H <= 8192) hipLaunchKernelGGL((norm_kernel<X, 4, 4, KEEP>), dim3(a.rows), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((norm_kernel<X, 16, 2, KEEP>), dim3(a.rows), dim3(1024), 0, st, a);
+    const int rows = a.rows, most = (int)(kMaxThreads / (a.H <= 2048 ? 64 : a.H <= 8192 ? 256 : 1024));
+    for (int row0 = 0; row0 < rows; row0 = a.rows) {
+        a.row0 = row0;
+        a.rows = rows - row0 < most ? rows : row0 + most;
+        const dim3 each(a.rows - row0), four((a.rows - row0 + 3) / 4);
+        if (a.H <= 512) hipLaunchKernelGGL((norm_kernel<X, 1, 1, KEEP>), four, dim3(256), 0, st, a);
+        else if (a.H <= 1024) hipLaunchKernelGGL((norm_kernel<X, 1, 2, KEEP>), four, dim3(256), 0, st, a);
+        else if (a.H <= 2048) hipLaunchKernelGGL((norm_kernel<X, 1, 4, KEEP>), four, dim3(256), 0, st, a);
+        else if (a.H <= 4096) hipLaunchKernelGGL((norm_kernel<X, 4, 2, KEEP>), each, dim3(256), 0, st, a);
+        else if (a.H <= 8192) hipLaunchKernelGGL((norm_kernel<X, 4, 4, KEEP>), each, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((norm_kernel<X, 16, 2, KEEP>), each, dim3(1024), 0, st, a);
+    }
 }
 
 template <typename X>
@@ -177,7 +183,7 @@ KeepArgs kept_values_args(const last_frames_t* f, int H, const last_matrix_t* ke
 // ---------------------------------------------------------------- products
 
 struct ProductPlan {
-    int variant;                     // 0: few rows, 1: tiles of 64, 2: of 128, 3: of 256
+    int variant;                     // 0: few rows, 1: tiles of 64, 2: of 128, 3: of 256; -1: more results than a launch takes
     int splits;
     long long share;                 // of the reduction, in bytes (kAlong) or rows
 };
@@ -194,6 +200,7 @@ ProductPlan plan_product(bool forward, int across, long long P, long long Q, lon
 {
     ProductPlan best{0, 1, steps};
     if (forward && P <= 64) return best;
+    best.variant = -1;
     static const double alone[4] = {0, 0.2, 0.5, 1.2}, two[4] = {0, 0.4, 0.95, 0}, many[4] = {0, 0.55, 0.95, 1.5}, beside[4] = {0, 3.5, 5, 9};
     static const double alone_by[3][3] = {{0, 1, 1}, {0, 1.4, 1.15}, {0, 1.8, 1.5}};
     static const double many_by[3][4] = {{0, 1, 1, 1}, {0, 1.05, 1.05, 1}, {0, 1.1, 1.1, 1.15}};
@@ -201,6 +208,7 @@ ProductPlan plan_product(bool forward, int across, long long P, long long Q, lon
     for (int variant = 1; variant <= 3; ++variant) {
         const long long tile = 32 << variant;
         const long long tiles = ((P + tile - 1) / tile) * ((Q + tile - 1) / tile);
+        if (tiles * (variant == 3 ? 512 : 256) > kMaxThreads) continue;
         for (int splits = 1; splits <= 64; splits *= 2) {
             const long long part = std::max(1ll, (steps + splits - 1) / splits);
             if (splits > 1 && (part < 4 || (steps + part - 1) / part != splits)) continue;
@@ -328,10 +336,11 @@ struct Preparation {
         a.mask = out;
         mask_groups = (unsigned)((count + 255) / 256);
     }
-    void launch(hipStream_t st) const
+    void launch(hipStream_t st)
     {
-        const unsigned n = a.groups + a.values_groups + mask_groups;
-        if (n) hipLaunchKernelGGL(prepare_kernel, dim3(n), dim3(256), 0, st, a);
+        const unsigned n = a.groups + a.values_groups + mask_groups, most = (unsigned)(kMaxThreads / 256);
+        for (a.first = 0; a.first < n; a.first += most)
+            hipLaunchKernelGGL(prepare_kernel, dim3(std::min(most, n - a.first)), dim3(256), 0, st, a);
     }
 };
 
@@ -401,6 +410,7 @@ last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, in
     a.K = bytes;
     a.frames = frames_of(f);
     const ProductPlan plan = plan_product(true, 0, rows, N, (bytes + kStep - 1) / kStep);
+    if (plan.variant < 0) return LAST_ERR_SHAPE;
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
     pre.launch(st);
@@ -437,6 +447,7 @@ last_status_t run_grad_input(Carver& cv, const last_frames_t* f, long long rows,
     a.q_rows = N;
     a.frames = frames_of(f);
     const ProductPlan plan = plan_product(false, 1, rows, K, (bytes + kStep - 1) / kStep);
+    if (plan.variant < 0) return LAST_ERR_SHAPE;
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
     pre.launch(st);
@@ -481,6 +492,7 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
     a.Q = K;
     a.K = rows;
     const ProductPlan plan = plan_product(false, 2, N, K, (rows + 63) / 64);
+    if (plan.variant < 0) return LAST_ERR_SHAPE;
     set_plan(cv, a, plan, 64, dbias);
     unsigned long long* mask = f->lengths ? (unsigned long long*)cv.take((size_t)((rows + 63) / 64 * 8)) : nullptr;
     if (!cv.base) return LAST_OK;
@@ -499,8 +511,10 @@ bool bad_sizes(long long rows, int N, int K)
     return N < 1 || K < 1 || N > kMaxColumns || K > kMaxColumns || rows * std::max(N, K) > 1ll << 42;
 }
 
+// need 0: sizes that no plan takes (the rest is checked by then)
 last_status_t check_ws(void* ws, size_t have, size_t need)
 {
+    if (need == 0) return LAST_ERR_SHAPE;
     if (!ws || ((uintptr_t)ws % kAlign) != 0 || have < need) return LAST_ERR_WORKSPACE;
     return LAST_OK;
 }
@@ -524,10 +538,11 @@ size_t last_layer_workspace_bytes(int32_t op, const last_frames_t* frames, int32
     if (!types) return 0;
     if (a->pitch < (op == LAST_OP_PRODUCT ? K : N) || b->pitch < K) return 0;
     Carver cv(nullptr);
-    if (op == LAST_OP_PRODUCT) run_product(cv, frames, rows, N, K, a, b, nullptr, 0, nullptr, nullptr, nullptr, nullptr);
-    else if (weight) run_grad_weight(cv, frames, rows, N, K, a, b, 0, nullptr, (float*)kAlign, nullptr);
-    else run_grad_input(cv, frames, rows, N, K, a, b, nullptr, 0, nullptr, nullptr);
-    return std::max(kAlign, cv.used);
+    last_status_t rc;
+    if (op == LAST_OP_PRODUCT) rc = run_product(cv, frames, rows, N, K, a, b, nullptr, 0, nullptr, nullptr, nullptr, nullptr);
+    else if (weight) rc = run_grad_weight(cv, frames, rows, N, K, a, b, 0, nullptr, (float*)kAlign, nullptr);
+    else rc = run_grad_input(cv, frames, rows, N, K, a, b, nullptr, 0, nullptr, nullptr);
+    return rc == LAST_OK ? std::max(kAlign, cv.used) : 0;
 }
 
 last_status_t last_residual_norm(const last_frames_t* frames, int32_t H, const last_matrix_t* x, const last_matrix_t* residual,

@@ -14,7 +14,7 @@ namespace last {
 
 struct NormArgs {
     Frames frames;
-    int rows, H;
+    int row0, rows, H;               // rows row0 .. rows of the matrices
     const void *x, *res;             // res: null, or of the type of x
     const float* gain;
     void *s, *y;                     // each may be null; s of the type of x
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_kernel(Norm
     constexpr int kRows = WPR == 1 ? 4 : 1;                  // rows of a workgroup
     using F = std::conditional_t<KEEP, double, float>;
     __shared__ F red[2 * WPR];
-    const int row = (int)blockIdx.x * kRows + (WPR == 1 ? (int)threadIdx.x / kWave : 0);
+    const int row = a.row0 + (int)blockIdx.x * kRows + (WPR == 1 ? (int)threadIdx.x / kWave : 0);
     const int lane = WPR == 1 ? (int)threadIdx.x % kWave : (int)threadIdx.x;
     if (WPR == 1 && row >= a.rows) return;
     const bool there = frame_exists(a.frames, row);

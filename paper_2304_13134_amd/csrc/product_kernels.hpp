@@ -894,6 +894,7 @@ struct PrepareArgs {
         unsigned groups;                         // workgroups that do it
     } rows[4];
     unsigned groups;                             // of all four
+    unsigned first;                              // of this launch's workgroups
     KeepArgs values;
     unsigned values_groups;
     Frames frames;
@@ -903,7 +904,7 @@ struct PrepareArgs {
 
 __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a)
 {
-    unsigned group = blockIdx.x;
+    unsigned group = a.first + blockIdx.x;
     if (group >= a.groups && group - a.groups < a.values_groups) {
         kept_values(a.values, group - a.groups);
         return;

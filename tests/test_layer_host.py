@@ -158,3 +158,14 @@ def test_the_oracle_of_eight_bits():
         got, scales = lo.encode(v, kind)
         again, s2 = lo.encode(got, kind)
         assert np.array_equal(again, got) and (s2 <= scales).all()
+
+
+def test_more_results_than_a_launch_takes_are_refused(lib):
+    """2^30 rows of 4096 results: even in tiles of 256 x 256 more than 2^32 threads."""
+    fr, x, w, y = ref(frames(1 << 10, 1 << 20)), ref(matrix(pitch=64)), ref(matrix(pitch=64)), ref(matrix(pitch=4096))
+    assert lib.last_layer_workspace_bytes(lb.OP_PRODUCT, fr, 4096, 64, x, w) == 0
+    assert lib.last_product(fr, 4096, 64, x, w, None, 0, None, y, None, ctypes.c_void_p(0x10000), 1 << 40, None) == 2
+    assert lib.last_layer_workspace_bytes(lb.OP_PRODUCT, fr, 64, 64, x, w) > 0
+    big = ref(matrix(pitch=1 << 20))
+    assert lib.last_layer_workspace_bytes(lb.OP_PRODUCT_GRAD_WEIGHT, ref(frames()), 1 << 20, 1 << 20, big, big) == 0
+    assert lib.last_product_grad_weight(ref(frames()), 1 << 20, 1 << 20, big, big, 0, ref(matrix(F32, 1 << 20)), None, ctypes.c_void_p(0x10000), 1 << 50, None) == 2
