@@ -271,7 +271,7 @@ last_status_t last_shortest_path(const last_weights_t* weights, const int32_t* l
  * not read into any result, rows of results are zeros (codes 0, scale bytes 0) and sums over frames pass them by.  Lengths
  * are taken as clamped to [0, T] (the lattice calls on them report a bad one).  T = 0 is allowed.
  *
- * Sums, norms and activations are in float32 (but see last_product for 8-bit operands), each result is rounded once, to
+ * Sums, norms and activations are in float32 (but see last_product for 8-bit operands with results of 16 bits and fewer), each result is rounded once, to
  * nearest even.  Results do not depend on
  * timing: there are no atomics.  Results may not overlap operands, except that the element-wise calls (last_residual_norm,
  * last_residual_norm_grad, last_kept_grad) may write s over x or over residual, dx over dy or over ds, in the same type
@@ -315,8 +315,9 @@ last_status_t last_residual_norm_grad(const last_frames_t* frames, int32_t H, co
                                       void* ws, size_t ws_bytes, void* hip_stream);
 
 /* h = x W^T + bias, y = act(h) + residual.  x: B*T rows of K, w: N rows of K, both BF16, both F16 or both E4M3 (with
- * scales along K).  Sums are float32; those of the 32 products of a block of 8-bit operands are the matrix instruction's,
- * which keeps 13 bits below the largest of them (codes hold 4).  bias (dev float32 [N]) and residual (type of y;
+ * scales along K).  Sums are float32, except that with 8-bit operands and a result of 16 or 8 bits those of the 32 products
+ * of a block are the matrix instruction's, which keeps 13 bits below the largest of them (codes hold 4): a result in F32 is
+ * what has them all, at the rate of 16-bit operands.  bias (dev float32 [N]) and residual (type of y;
  * any of the three plain ones where y is in 8 bits) may be NULL.  y: F32, BF16, F16, or 8 bits (I8, E4M3).  kept (or
  * NULL): h in 8 bits, what the gradient of the activation needs.  Workspace: LAST_OP_PRODUCT, a = x, b = w. */
 last_status_t last_product(const last_frames_t* frames, int32_t N, int32_t K, const last_matrix_t* x,

@@ -9,6 +9,7 @@
 #include "keep_kernels.hpp"
 #include "product_kernels.hpp"
 #include <algorithm>
+#include <type_traits>
 
 using namespace last;
 
@@ -196,7 +197,7 @@ struct ProductPlan {
 // time.  Tiles of 256 win from a full chip on (16384 x 1024 on 4096: 105 us, with tiles of 128 129), tiles of 64 up to about half a million
 // results (512 x 1024 on 4096: 20 us, 37 and 80).  Shares are written and read in 32 bits at about 5 TB/s and cost a launch:
 // 16384 x 1024 x 4096 rows of weight gradient in 4 shares 152 us, in one 350 us.
-ProductPlan plan_product(bool forward, int across, long long P, long long Q, long long steps)
+ProductPlan plan_product(bool forward, int across, long long P, long long Q, long long steps, int largest = 3)
 {
     ProductPlan best{0, 1, steps};
     if (forward && P <= 64) return best;
@@ -205,7 +206,7 @@ ProductPlan plan_product(bool forward, int across, long long P, long long Q, lon
     static const double alone_by[3][3] = {{0, 1, 1}, {0, 1.4, 1.15}, {0, 1.8, 1.5}};
     static const double many_by[3][4] = {{0, 1, 1, 1}, {0, 1.05, 1.05, 1}, {0, 1.1, 1.1, 1.15}};
     double least = 1e30;
-    for (int variant = 1; variant <= 3; ++variant) {
+    for (int variant = 1; variant <= largest; ++variant) {
         const long long tile = 32 << variant;
         const long long tiles = ((P + tile - 1) / tile) * ((Q + tile - 1) / tile);
         if (tiles * (variant == 3 ? 512 : 256) > kMaxThreads) continue;
@@ -248,9 +249,11 @@ void launch_tiles(ProductArgs a, const ProductPlan& p, hipStream_t st)
         a.e = none;
     }
     constexpr bool kEight = Elt<E>::size == 1;
-    if (p.variant == 3) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 256, 256, 2, 4, kEight ? 2 : 3, 2>), grid, dim3(512), 0, st, a);
-    else if (p.variant == 2) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 128, 128, 2, 2, kEight ? 2 : 3, 2>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((product_kernel<E, LP, LQ, 64, 64, 2, 2, 3, 3>), grid, dim3(256), 0, st, a);
+    if constexpr (!std::is_same_v<E, wide_t>) {      // (no registers for widened fragments of 128 x 64 results a wavefront)
+        if (p.variant == 3) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 256, 256, 2, 4, kEight ? 2 : 3, 2>), grid, dim3(512), 0, st, a);
+    }
+    if (p.variant == 2) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 128, 128, 2, 2, kEight ? 2 : 3, 2>), grid, dim3(256), 0, st, a);
+    if (p.variant == 1) hipLaunchKernelGGL((product_kernel<E, LP, LQ, 64, 64, 2, 2, 3, 3>), grid, dim3(256), 0, st, a);
     if (p.splits > 1) {
         const long long waves = (long long)((a.P + 15) / 16) * ((a.Q + 31) / 32);
         hipLaunchKernelGGL(product_join_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, j, p.splits);
@@ -389,8 +392,8 @@ void set_result(Epilogue& e, const last_matrix_t* y, const last_matrix_t* res)
     }
 }
 
-// The call's plan, the same for measuring the workspace and for the call itself.
-last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, int N, int K, const last_matrix_t* x, const last_matrix_t* w,
+// The call's plan, the same for measuring the workspace and for the call itself.  wide: 8-bit operands' products are added in 32 bits.
+last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, int N, int K, const last_matrix_t* x, const last_matrix_t* w, bool wide,
                           const float* bias, int act, const last_matrix_t* res, const last_matrix_t* y, const last_matrix_t* kept, hipStream_t st)
 {
     ProductArgs a{};
@@ -409,7 +412,7 @@ last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, in
     a.Q = N;
     a.K = bytes;
     a.frames = frames_of(f);
-    const ProductPlan plan = plan_product(true, 0, rows, N, (bytes + kStep - 1) / kStep);
+    const ProductPlan plan = plan_product(true, 0, rows, N, (bytes + kStep - 1) / kStep, wide ? 2 : 3);
     if (plan.variant < 0) return LAST_ERR_SHAPE;
     set_plan(cv, a, plan, kStep, nullptr);
     if (!cv.base || rows == 0) return LAST_OK;
@@ -421,10 +424,12 @@ last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, in
     if (plan.variant == 0) {
         if (x->type == LAST_BF16) launch_few<bf16_t>(a, st);
         else if (x->type == LAST_F16) launch_few<f16_t>(a, st);
+        else if (wide) launch_few<wide_t>(a, st);
         else launch_few<e4m3_t>(a, st);
     } else {
         if (x->type == LAST_BF16) launch_tiles<bf16_t, kAlong, kAlong>(a, plan, st);
         else if (x->type == LAST_F16) launch_tiles<f16_t, kAlong, kAlong>(a, plan, st);
+        else if (wide) launch_tiles<wide_t, kAlong, kAlong>(a, plan, st);
         else launch_tiles<e4m3_t, kAlong, kAlong>(a, plan, st);
     }
     return hip_done();
@@ -539,7 +544,14 @@ size_t last_layer_workspace_bytes(int32_t op, const last_frames_t* frames, int32
     if (a->pitch < (op == LAST_OP_PRODUCT ? K : N) || b->pitch < K) return 0;
     Carver cv(nullptr);
     last_status_t rc;
-    if (op == LAST_OP_PRODUCT) rc = run_product(cv, frames, rows, N, K, a, b, nullptr, 0, nullptr, nullptr, nullptr, nullptr);
+    if (op == LAST_OP_PRODUCT) {
+        rc = run_product(cv, frames, rows, N, K, a, b, false, nullptr, 0, nullptr, nullptr, nullptr, nullptr);
+        if (rc == LAST_OK && a->type == LAST_E4M3) {                  // (the type of the result is not known here)
+            Carver wide(nullptr);
+            rc = run_product(wide, frames, rows, N, K, a, b, true, nullptr, 0, nullptr, nullptr, nullptr, nullptr);
+            cv.used = std::max(cv.used, wide.used);
+        }
+    }
     else if (weight) rc = run_grad_weight(cv, frames, rows, N, K, a, b, 0, nullptr, (float*)kAlign, nullptr);
     else rc = run_grad_input(cv, frames, rows, N, K, a, b, nullptr, 0, nullptr, nullptr);
     return rc == LAST_OK ? std::max(kAlign, cv.used) : 0;
@@ -640,7 +652,8 @@ last_status_t last_product(const last_frames_t* frames, int32_t N, int32_t K, co
     if (kept) LAST_TRY(check_matrix(kept, N, eight(kept->type)));
     LAST_TRY(check_ws(ws, ws_bytes, last_layer_workspace_bytes(LAST_OP_PRODUCT, frames, N, K, x, w)));
     Carver cv(ws);
-    return run_product(cv, frames, rows, N, K, x, w, bias, act, residual, y, kept, (hipStream_t)hip_stream);
+    const bool wide = x->type == LAST_E4M3 && y->type == LAST_F32;
+    return run_product(cv, frames, rows, N, K, x, w, wide, bias, act, residual, y, kept, (hipStream_t)hip_stream);
 }
 
 last_status_t last_product_grad_input(const last_frames_t* frames, int32_t N, int32_t K, const last_matrix_t* dy, const last_matrix_t* w,

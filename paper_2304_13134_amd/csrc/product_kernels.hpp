@@ -32,6 +32,8 @@
 #include "keep_kernels.hpp"
 #include "layer.hpp"
 
+#include <type_traits>
+
 namespace last {
 
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
@@ -40,6 +42,10 @@ typedef int i8x __attribute__((ext_vector_type(8)));
 typedef int i4x __attribute__((ext_vector_type(4)));
 
 typedef __attribute__((address_space(3))) void* lds_t;
+
+// e4m3 codes that are multiplied as bfloat16
+struct wide_t { uint8_t bits; };
+template <> struct Elt<wide_t> : EltCodes<true> {};
 
 enum { kAlong = 0, kAcross = 1 };
 constexpr unsigned kNowhere = 0x80000000u;       // beyond every buffer
@@ -200,11 +206,30 @@ __device__ __forceinline__ i8x join8(u4 a, u4 b)
 
 // lane: values 16 g .. and 64 + 16 g .. of 128 of its row or column, and the scale of values 32 g ..  The instruction adds the 32
 // products of a block with 13 bits below the largest (1 + 2^-13 is exact, 1 + 2^-14 is 1) and blocks in 32 bits: at most 32
-// 2^-13 of a block's largest product, typically 2^-16 of the sum's terms, where each code is already 2^-5 off.  Codes turned
-// into bfloat16 would be added in 32 bits throughout, at half the rate and with the conversions on top.
+// 2^-13 of a block's largest product, typically 2^-16 of the sum's terms, where each code is already 2^-5 off.  A choice for results
+// of 16 bits and fewer, whose last bit is 2^-8 or 2^-11; those of 32 bits are of codes turned into bfloat16 (widen).
 __device__ __forceinline__ f4 mfma_scaled(i8x a, i8x b, f4 c, int sa, int sb)
 {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, sa, 0, sb);
+}
+
+// 16 codes and their scale to bfloat16, which holds them (values under 2^-126 as far as its subnormal numbers do): products of
+// these are added in 32 bits throughout, at half the rate of the codes' own and with the conversions on top
+__device__ __forceinline__ void widen(u4 q, unsigned byte, u4* w)
+{
+    const float scale = scale_value(byte);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i >> 1][(i & 1) * 2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[i], scale, false));
+        w[i >> 1][(i & 1) * 2 + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[i], scale, true));
+    }
+}
+
+// a lane's 32 codes of 128; scales: of values 32 (g / 2) .. in the first byte, of 64 + 32 (g / 2) .. in the second
+__device__ __forceinline__ void widen(i8x q, int scales, u4* w)
+{
+    widen(u4{(unsigned)q[0], (unsigned)q[1], (unsigned)q[2], (unsigned)q[3]}, scales & 255, w);
+    widen(u4{(unsigned)q[4], (unsigned)q[5], (unsigned)q[6], (unsigned)q[7]}, scales >> 8, w + 2);
 }
 
 __device__ __forceinline__ u4 across_read(const char* lds, int a0, int a1)
@@ -428,7 +453,7 @@ template <typename E, int LP, int LQ, int BP, int BQ, int WP, int WQ, int SP, in
 __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs a)
 {
     constexpr int kThreads = WP * WQ * kWave;
-    constexpr bool kEight = Elt<E>::size == 1;
+    constexpr bool kEight = Elt<E>::size == 1, kWide = std::is_same_v<E, wide_t>;
     constexpr int NP = BP / WP / 16, NQ = BQ / WQ / 16;                   // accumulators of a wavefront
     using TP = Tile<LP, BP, kThreads>;
     using TQ = Tile<LQ, BQ, kThreads>;
@@ -563,26 +588,44 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
             constexpr int H = NP / 2, kSends = (TP::kLoads + TQ::kLoads + kScaleLoads + H - 1) / H;
             i8x fp[NP], fq[NQ];
             int cp[NP], cq[NQ];
+            u4 vp[kWide ? 4 : 1], vq[kWide ? NQ : 1][kWide ? 4 : 1];      // widened: a row of P, all columns of Q
+            const auto scale_of = [&](int buf, int r) {
+                if constexpr (kWide) return scales[buf][r * 4 + (g >> 1)] | scales[buf][r * 4 + 2 + (g >> 1)] << 8;
+                else return (int)scales[buf][r * 4 + g];
+            };
             const auto take_p = [&](int buf, int x) {
                 const unsigned at = here(at_p + buf * TP::kBytes);
                 fp[x] = join8(read_p(at, 0, x), read_p(at, 1, x));
-                cp[x] = scales[buf][(wp * (BP / WP) + x * 16 + i16) * 4 + g];
+                cp[x] = scale_of(buf, wp * (BP / WP) + x * 16 + i16);
             };
             const auto take_q = [&](int buf, int y) {
                 const unsigned at = here(at_q + buf * TQ::kBytes);
                 fq[y] = join8(read_q(at, 0, y), read_q(at, 1, y));
-                cq[y] = scales[buf][(BP + wq * (BQ / WQ) + y * 16 + i16) * 4 + g];
+                cq[y] = scale_of(buf, BP + wq * (BQ / WQ) + y * 16 + i16);
+            };
+            const auto multiply = [&](int x, int y) {
+                if constexpr (kWide) {
+                    if (y == 0) widen(fp[x], cp[x], vp);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[x][y] = Mfma<bf16_t>::go(vq[y][k], vp[k], acc[x][y]);
+                } else {
+                    acc[x][y] = mfma_scaled(fq[y], fp[x], acc[x][y], cq[y], cp[x]);
+                }
             };
 #pragma unroll
             for (int y = 0; y < NQ; ++y) take_q(0, y);
 #pragma unroll
             for (int x = 0; x < H; ++x) take_p(0, x);
             for (int s = 0; s < steps; ++s) {
+                if constexpr (kWide) {
+#pragma unroll
+                    for (int y = 0; y < NQ; ++y) widen(fq[y], cq[y], vq[y]);
+                }
 #pragma unroll
                 for (int x = 0; x < H; ++x) {
                     take_p(buf_q, H + x);
 #pragma unroll
-                    for (int y = 0; y < NQ; ++y) acc[x][y] = mfma_scaled(fq[y], fp[x], acc[x][y], cq[y], cp[x]);
+                    for (int y = 0; y < NQ; ++y) multiply(x, y);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 arrived<kLater>();
@@ -599,13 +642,13 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
                     take_p(next, x);
                     if (x + 1 < H) {
 #pragma unroll
-                        for (int y = 0; y < NQ; ++y) acc[H + x][y] = mfma_scaled(fq[y], fp[H + x], acc[H + x][y], cq[y], cp[H + x]);
+                        for (int y = 0; y < NQ; ++y) multiply(H + x, y);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
 #pragma unroll
                 for (int y = 0; y < NQ; ++y) {
-                    acc[NP - 1][y] = mfma_scaled(fq[y], fp[NP - 1], acc[NP - 1][y], cq[y], cp[NP - 1]);
+                    multiply(NP - 1, y);
                     take_q(next, y);
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -765,8 +808,8 @@ constexpr int kFewWaves = 8;
 template <typename E, int MT, int QF>
 __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
 {
-    constexpr bool kEight = Elt<E>::size == 1;
-    constexpr int kDeep = kEight && MT * QF >= 8 ? 2 : 4;                 // (steps under way: as many as there are registers for)
+    constexpr bool kEight = Elt<E>::size == 1, kWide = std::is_same_v<E, wide_t>;
+    constexpr int kDeep = kEight && MT * QF >= (kWide ? 4 : 8) ? 2 : 4;                 // (steps under way: as many as there are registers for)
     __shared__ f4 red[kFewWaves][MT][QF][kWave];
     const int lane = (int)threadIdx.x % kWave, g = lane >> 4, i16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -808,27 +851,42 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
                     fp[d][t][h] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(bp, in ? (int)(op[t] + kh) : (int)kNowhere, 0, 0));
             }
             if constexpr (kEight) {
-                const int block = k / kBlock + g;
-                const bool in = block * kBlock < bytes;
+                const auto scale_of = [&](bool there, const uint8_t* row, int block) { return there && block * kBlock < bytes ? (int)row[block] : 0; };
+                const auto scales_of = [&](bool there, const uint8_t* row) {
+                    if constexpr (kWide) return scale_of(there, row, k / kBlock + (g >> 1)) | scale_of(there, row, k / kBlock + 2 + (g >> 1)) << 8;
+                    else return scale_of(there, row, k / kBlock + g);
+                };
 #pragma unroll
-                for (int f = 0; f < QF; ++f) cq[d][f] = in && oq[f] < kNowhere ? a.sq[(q0 + rq[f]) * a.psq + block] : 0;
+                for (int f = 0; f < QF; ++f) cq[d][f] = scales_of(oq[f] < kNowhere, a.sq + (q0 + rq[f]) * a.psq);
 #pragma unroll
-                for (int t = 0; t < MT; ++t) cp[d][t] = in && op[t] < kNowhere ? a.sp[(t * 16 + i16) * a.psp + block] : 0;
+                for (int t = 0; t < MT; ++t) cp[d][t] = scales_of(op[t] < kNowhere, a.sp + (t * 16 + i16) * a.psp);
             }
         }
 #pragma unroll
-        for (int d = 0; d < kDeep; ++d)
+        for (int d = 0; d < kDeep; ++d) {
+            u4 vq[kWide ? QF : 1][kWide ? 4 : 1];
+            if constexpr (kWide) {
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
+                for (int f = 0; f < QF; ++f) widen(join8(fq[d][f][0], fq[d][f][1]), cq[d][f], vq[f]);
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                u4 vp[kWide ? 4 : 1];
+                if constexpr (kWide) widen(join8(fp[d][t][0], fp[d][t][1]), cp[d][t], vp);
 #pragma unroll
                 for (int f = 0; f < QF; ++f) {
-                    if constexpr (kEight) {
+                    if constexpr (kWide) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[t][f] = Mfma<bf16_t>::go(vq[f][j], vp[j], acc[t][f]);
+                    } else if constexpr (kEight) {
                         acc[t][f] = mfma_scaled(join8(fq[d][f][0], fq[d][f][1]), join8(fp[d][t][0], fp[d][t][1]), acc[t][f], cq[d][f], cp[d][t]);
                     } else {
                         acc[t][f] = Mfma<E>::go(fq[d][f][0], fp[d][t][0], acc[t][f]);
                         acc[t][f] = Mfma<E>::go(fq[d][f][1], fp[d][t][1], acc[t][f]);
                     }
                 }
+            }
+        }
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t)
