@@ -402,6 +402,9 @@ last_status_t last_shortest_distance_static(const last_weights_t* weights, const
  *     function for several frames at once).  2 shares the rows of e and the phase barriers between
  *     two frames and doubles the hidden tile in LDS; a shape whose tiles then no longer fit uses 1.
  *     The shortest distance does not depend on it bit for bit.
+ *   LAST_OPT_PRODUCT_TILES (0..3, default 0): tiles of the layer's products: 0 = few rows, or tiles and shares by
+ *     what they cost; 1, 2, 3 = tiles of 64, 128, 256 for all (8-bit operands with a float32 result have none of
+ *     256 and take 128).  last_layer_workspace_bytes follows the setting.
  * last_set_option returns LAST_ERR_UNSUPPORTED for an unknown option or value; last_get_option
  * returns -1 for an unknown option. */
 typedef enum {
@@ -411,7 +414,8 @@ typedef enum {
     LAST_OPT_SPIN_LIMIT = 3,
     LAST_OPT_FUSED_FRAMES_PER_TILE = 4,
     LAST_OPT_FUSED_KEEP_MARGINALS = 5,
-    LAST_OPT_COUNT_ = 6
+    LAST_OPT_PRODUCT_TILES = 6,
+    LAST_OPT_COUNT_ = 7
 } last_option_t;
 last_status_t last_set_option(int32_t option, int32_t value);
 int32_t last_get_option(int32_t option);

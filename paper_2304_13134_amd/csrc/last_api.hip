@@ -38,7 +38,7 @@ using namespace last;
 namespace {
 
 // process-wide settings (last_set_option)
-std::atomic<int> g_opt[LAST_OPT_COUNT_] = {{0}, {0}, {1}, {1 << 20}, {2}, {1}};
+std::atomic<int> g_opt[LAST_OPT_COUNT_] = {{0}, {0}, {1}, {1 << 20}, {2}, {1}, {0}};
 inline int opt(int o) { return g_opt[o].load(std::memory_order_relaxed); }
 
 constexpr size_t kAlign = 256;
@@ -364,8 +364,10 @@ hipError_t g_last_hip_error = hipSuccess;     // diagnostics only: what the last
 
 }  // namespace
 
+// for the calls in layer_api.hip
 namespace last {
-void note_hip_error(hipError_t e) { g_last_hip_error = e; }    // (of the calls in layer_api.hip)
+void note_hip_error(hipError_t e) { g_last_hip_error = e; }
+int option(int o) { return opt(o); }
 }
 
 namespace {
@@ -1200,6 +1202,7 @@ last_status_t last_set_option(int32_t option, int32_t value)
     if (option == LAST_OPT_CLUSTER_VITERBI && (value < 0 || value > 2)) return LAST_ERR_UNSUPPORTED;
     if (option == LAST_OPT_FUSED_FRAMES_PER_TILE && value != 1 && value != 2) return LAST_ERR_UNSUPPORTED;
     if (option == LAST_OPT_FUSED_KEEP_MARGINALS && value != 0 && value != 1) return LAST_ERR_UNSUPPORTED;
+    if (option == LAST_OPT_PRODUCT_TILES && (value < 0 || value > 3)) return LAST_ERR_UNSUPPORTED;
     g_opt[option].store(value, std::memory_order_relaxed);
     return LAST_OK;
 }

@@ -13,7 +13,10 @@
 
 using namespace last;
 
-namespace last { void note_hip_error(hipError_t e); }
+namespace last {
+void note_hip_error(hipError_t e);
+int option(int o);
+}
 
 namespace {
 
@@ -200,7 +203,8 @@ struct ProductPlan {
 ProductPlan plan_product(bool forward, int across, long long P, long long Q, long long steps, int largest = 3)
 {
     ProductPlan best{0, 1, steps};
-    if (forward && P <= 64) return best;
+    const int asked = std::min(option(LAST_OPT_PRODUCT_TILES), largest);
+    if (forward && P <= 64 && !asked) return best;
     best.variant = -1;
     static const double alone[4] = {0, 0.2, 0.5, 1.2}, two[4] = {0, 0.4, 0.95, 0}, many[4] = {0, 0.55, 0.95, 1.5}, beside[4] = {0, 3.5, 5, 9};
     static const double alone_by[3][3] = {{0, 1, 1}, {0, 1.4, 1.15}, {0, 1.8, 1.5}};
@@ -209,6 +213,7 @@ ProductPlan plan_product(bool forward, int across, long long P, long long Q, lon
     for (int variant = 1; variant <= largest; ++variant) {
         const long long tile = 32 << variant;
         const long long tiles = ((P + tile - 1) / tile) * ((Q + tile - 1) / tile);
+        if (asked && variant != asked) continue;
         if (tiles * (variant == 3 ? 512 : 256) > kMaxThreads) continue;
         for (int splits = 1; splits <= 64; splits *= 2) {
             const long long part = std::max(1ll, (steps + splits - 1) / splits);

@@ -169,3 +169,16 @@ def test_more_results_than_a_launch_takes_are_refused(lib):
     big = ref(matrix(pitch=1 << 20))
     assert lib.last_layer_workspace_bytes(lb.OP_PRODUCT_GRAD_WEIGHT, ref(frames()), 1 << 20, 1 << 20, big, big) == 0
     assert lib.last_product_grad_weight(ref(frames()), 1 << 20, 1 << 20, big, big, 0, ref(matrix(F32, 1 << 20)), None, ctypes.c_void_p(0x10000), 1 << 50, None) == 2
+
+
+def test_option_of_tiles(lib):
+    """Values outside of 0 .. 3 are refused; the workspace follows the setting: shares of a long reduction go by the tiles."""
+    fr, m = ref(frames(1, 20000)), ref(matrix(pitch=640))
+    sizes = []
+    for v in (0, 1, 2, 3):
+        assert lib.last_set_option(lb.OPT_PRODUCT_TILES, v) == 0 and lib.last_get_option(lb.OPT_PRODUCT_TILES) == v
+        sizes.append(lib.last_layer_workspace_bytes(lb.OP_PRODUCT_GRAD_WEIGHT, fr, 640, 640, m, m))
+    assert lib.last_set_option(lb.OPT_PRODUCT_TILES, 4) == 6 and lib.last_set_option(lb.OPT_PRODUCT_TILES, -1) == 6
+    assert lib.last_get_option(lb.OPT_PRODUCT_TILES) == 3
+    assert lib.last_set_option(lb.OPT_PRODUCT_TILES, 0) == 0
+    assert sizes[0] in sizes[1:] and len(set(sizes[1:])) > 1 and min(sizes) >= 256, sizes
