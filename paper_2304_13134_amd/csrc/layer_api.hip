@@ -24,6 +24,7 @@ constexpr long long kMaxRows = 1ll << 30;
 constexpr long long kMaxColumns = 1ll << 20;
 constexpr long long kMaxPitchBytes = 4ll << 20;      // 256 rows of a tile stay within 32-bit offsets
 constexpr int kMaxNormColumns = 16384;
+constexpr long long kFewRows = 32;
 constexpr size_t kAlign = 256;
 constexpr long long kMaxThreads = 1ll << 31;         // of a launch, which takes fewer than 2^32: what has more to do goes out in pieces
 
@@ -192,19 +193,23 @@ struct ProductPlan {
     long long share;                 // of the reduction, in bytes (kAlong) or rows
 };
 
-// Tiles and shares of a reduction of `steps` steps (128 bytes, or 64 rows).  Up to 64 rows of a forward product go to the
-// kernel that reads w once and keeps nothing in LDS; beyond, the cheapest of what these would take, from measurements on
+// Tiles and shares of a reduction of `steps` steps (128 bytes, or 64 rows).  Up to 32 rows of a forward product go to the
+// kernel that reads w once and keeps nothing in LDS: 16, 32, 48, 64 rows of 2048 results over 512 terms in bfloat16 take it 4.5, 5.5, 7.1, 7.5 us,
+// of 512 over 2048 6.4, 8.4, 10.9, 12.2, of 1024 over 4096 10.2, 13.8, 19.0, 21.1; tiles of 64 6.5, 10.8 and 11 to 12, whatever the rows (8-bit
+// operands: 4.0 to 5.9, 6.0 to 11.1, 8.5 to 16.8; 5.7, 9.0, 9.3).  Beyond, the cheapest of what these would take, from measurements on
 // MI355X: a workgroup with a compute unit to itself takes 1.2, 0.5 and 0.2 us a step with tiles of 256, 128 and 64 (the first 1.5 on a
 // full chip), two that share one 0.95 and 0.4 us (tiles of 128 and 64), three 0.55 (of 64), and 9, 5 and 3.5 us beside its steps;
 // operands that run across the reduction (none, one, both) take up to 1.8 times as long (transposing reads), less where others fill the
 // time.  Tiles of 256 win from a full chip on (16384 x 1024 on 4096: 105 us, with tiles of 128 129), tiles of 64 up to about half a million
 // results (512 x 1024 on 4096: 20 us, 37 and 80).  Shares are written and read in 32 bits at about 5 TB/s and cost a launch:
-// 16384 x 1024 x 4096 rows of weight gradient in 4 shares 152 us, in one 350 us.
+// 16384 x 1024 x 4096 rows of weight gradient in 4 shares 152 us, in one 350 us.  Measured with operands of 16 bits and without an activation;
+// of 180 products of drawn sizes, 8-bit operands among them, the tiles it names were 1 % slower than the best of the three in
+// the mean, 26 % at worst, and of 20 with activations, residuals and kept sums 1 %, 7 %.
 ProductPlan plan_product(bool forward, int across, long long P, long long Q, long long steps, int largest = 3)
 {
     ProductPlan best{0, 1, steps};
     const int asked = std::min(option(LAST_OPT_PRODUCT_TILES), largest);
-    if (forward && P <= 64 && !asked) return best;
+    if (forward && P <= kFewRows && !asked) return best;
     best.variant = -1;
     static const double alone[4] = {0, 0.2, 0.5, 1.2}, two[4] = {0, 0.4, 0.95, 0}, many[4] = {0, 0.55, 0.95, 1.5}, beside[4] = {0, 3.5, 5, 9};
     static const double alone_by[3][3] = {{0, 1, 1}, {0, 1.4, 1.15}, {0, 1.8, 1.5}};
@@ -268,18 +273,15 @@ void launch_tiles(ProductArgs a, const ProductPlan& p, hipStream_t st)
 template <typename E>
 void launch_few(const ProductArgs& a, hipStream_t st)
 {
-    const int mt = (a.P + 15) / 16;
     // values in 8 bits need the 32 columns of a block in one wavefront
     const bool two = a.e.kept.q || a.e.out.q || a.Q > 16 * 1024;
     const dim3 grid((unsigned)(two ? (a.Q + 31) / 32 : (a.Q + 15) / 16)), block(kFewWaves * kWave);
     if (two) {
-        if (mt == 1) hipLaunchKernelGGL((few_kernel<E, 1, 2>), grid, block, 0, st, a);
-        else if (mt == 2) hipLaunchKernelGGL((few_kernel<E, 2, 2>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((few_kernel<E, 4, 2>), grid, block, 0, st, a);
+        if (a.P <= 16) hipLaunchKernelGGL((few_kernel<E, 1, 2>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((few_kernel<E, 2, 2>), grid, block, 0, st, a);
     } else {
-        if (mt == 1) hipLaunchKernelGGL((few_kernel<E, 1, 1>), grid, block, 0, st, a);
-        else if (mt == 2) hipLaunchKernelGGL((few_kernel<E, 2, 1>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((few_kernel<E, 4, 1>), grid, block, 0, st, a);
+        if (a.P <= 16) hipLaunchKernelGGL((few_kernel<E, 1, 1>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((few_kernel<E, 2, 1>), grid, block, 0, st, a);
     }
 }
 

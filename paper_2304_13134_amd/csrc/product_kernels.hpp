@@ -809,7 +809,7 @@ template <typename E, int MT, int QF>
 __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(ProductArgs a)
 {
     constexpr bool kEight = Elt<E>::size == 1, kWide = std::is_same_v<E, wide_t>;
-    constexpr int kDeep = kEight && MT * QF >= (kWide ? 4 : 8) ? 2 : 4;                 // (steps under way: as many as there are registers for)
+    constexpr int kDeep = kWide && MT * QF >= 4 ? 2 : 4;                 // (steps under way: as many as there are registers for)
     __shared__ f4 red[kFewWaves][MT][QF][kWave];
     const int lane = (int)threadIdx.x % kWave, g = lane >> 4, i16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);

@@ -64,3 +64,11 @@ def test_operands_as_they_come(tiles):
 def test_the_same_results_again_and_captured(tiles):
     layer.test_results_do_not_depend_on_timing()
     layer.test_streams_and_graphs()
+
+
+@pytest.mark.parametrize("rows", [15, 16, 17, 31, 32, 33, 48, 64])
+@pytest.mark.parametrize("N,K", [(48, 200), (260, 1000)])
+@pytest.mark.parametrize("type_,out,name,bias,res,kind,lens", [("bf16", "bf16", "silu", True, True, None, "some"), ("f16", "f32", "gelu", True, False, "i8", "all"),
+                                                              ("e4m3", "bf16", "none", True, True, None, "all"), ("e4m3", "f32", "silu", True, False, "e4m3", "some")])
+def test_rows_around_the_kernel_for_few(rows, N, K, type_, out, name, bias, res, kind, lens):
+    layer.test_product(1, rows, N, K, type_, out, name, bias, res, kind, lens)
