@@ -576,6 +576,8 @@ def _frames(t, lengths, name):
         raise ValueError("with lengths [B], %s must be [B, T, columns]" % name)
     if lengths.get_device() != on:
         _elsewhere("lengths")
+    if rows[0] == 0:
+        return _pack_frames(1, 0, 0), rows, t, on     # (no items: no frames)
     return _pack_frames(rows[0], rows[1], lengths.data_ptr()), rows, t, on
 
 
