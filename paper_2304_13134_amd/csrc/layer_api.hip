@@ -311,8 +311,10 @@ struct Operand {
 
 struct Carver {
     char* base;
-    size_t used = 0;
-    explicit Carver(void* p) : base((char*)p) {}
+    size_t have, used = 0;
+    explicit Carver(void* p, size_t n = 0) : base((char*)p), have(n) {}
+    // a plan that went by another setting of an option than the size that was checked (set in between, by another thread)
+    bool over() const { return base && used > have; }
     char* take(size_t bytes)
     {
         char* p = base ? base + used : nullptr;
@@ -422,6 +424,7 @@ last_status_t run_product(Carver& cv, const last_frames_t* f, long long rows, in
     const ProductPlan plan = plan_product(true, 0, rows, N, (bytes + kStep - 1) / kStep, wide ? 2 : 3);
     if (plan.variant < 0) return LAST_ERR_SHAPE;
     set_plan(cv, a, plan, kStep, nullptr);
+    if (cv.over()) return LAST_ERR_WORKSPACE;
     if (!cv.base || rows == 0) return LAST_OK;
     pre.launch(st);
     a.e.bias = bias;
@@ -461,6 +464,7 @@ last_status_t run_grad_input(Carver& cv, const last_frames_t* f, long long rows,
     const ProductPlan plan = plan_product(false, 1, rows, K, (bytes + kStep - 1) / kStep);
     if (plan.variant < 0) return LAST_ERR_SHAPE;
     set_plan(cv, a, plan, kStep, nullptr);
+    if (cv.over()) return LAST_ERR_WORKSPACE;
     if (!cv.base || rows == 0) return LAST_OK;
     pre.launch(st);
     set_result(a.e, dx, nullptr);
@@ -507,6 +511,7 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
     if (plan.variant < 0) return LAST_ERR_SHAPE;
     set_plan(cv, a, plan, 64, dbias);
     unsigned long long* mask = f->lengths ? (unsigned long long*)cv.take((size_t)((rows + 63) / 64 * 8)) : nullptr;
+    if (cv.over()) return LAST_ERR_WORKSPACE;
     if (!cv.base) return LAST_OK;
     if (mask) pre.mask(f, rows, mask);
     pre.launch(st);
@@ -658,7 +663,7 @@ last_status_t last_product(const last_frames_t* frames, int32_t N, int32_t K, co
     if (residual) LAST_TRY(check_matrix(residual, N, plain(residual->type) && (eight(y->type) || residual->type == y->type)));
     if (kept) LAST_TRY(check_matrix(kept, N, eight(kept->type)));
     LAST_TRY(check_ws(ws, ws_bytes, last_layer_workspace_bytes(LAST_OP_PRODUCT, frames, N, K, x, w)));
-    Carver cv(ws);
+    Carver cv(ws, ws_bytes);
     const bool wide = x->type == LAST_E4M3 && y->type == LAST_F32;
     return run_product(cv, frames, rows, N, K, x, w, wide, bias, act, residual, y, kept, (hipStream_t)hip_stream);
 }
@@ -677,7 +682,7 @@ last_status_t last_product_grad_input(const last_frames_t* frames, int32_t N, in
     LAST_TRY(check_matrix(dx, K, plain(dx->type)));
     if (kept) LAST_TRY(check_matrix(kept, K, eight(kept->type)));
     LAST_TRY(check_ws(ws, ws_bytes, last_layer_workspace_bytes(LAST_OP_PRODUCT_GRAD_INPUT, frames, N, K, dy, w)));
-    Carver cv(ws);
+    Carver cv(ws, ws_bytes);
     return run_grad_input(cv, frames, rows, N, K, dy, w, kept, act, dx, (hipStream_t)hip_stream);
 }
 
@@ -694,7 +699,7 @@ last_status_t last_product_grad_weight(const last_frames_t* frames, int32_t N, i
     LAST_TRY(check_matrix(x, K, eight(x->type) || (x->type == dy->type && act == LAST_ACT_NONE)));
     LAST_TRY(check_matrix(dw, K, plain(dw->type)));
     LAST_TRY(check_ws(ws, ws_bytes, last_layer_workspace_bytes(LAST_OP_PRODUCT_GRAD_WEIGHT, frames, N, K, dy, x)));
-    Carver cv(ws);
+    Carver cv(ws, ws_bytes);
     return run_grad_weight(cv, frames, rows, N, K, dy, x, act, dw, dbias, (hipStream_t)hip_stream);
 }
 
