@@ -483,7 +483,8 @@ last_status_t run_grad_weight(Carver& cv, const last_frames_t* f, long long rows
     const Operand p = lay_out(cv, pre, dy, rows, N);
     Operand q;
     if (eight(x->type)) {
-        // the activation formed again, once, instead of by every tile that reads it
+        // the activation formed again, once, instead of by every tile that reads it; rounded to dy's type, as the product that it was the
+        // input of had it: what dw is the gradient of, whatever the type of dw
         last_matrix_t v{};
         v.type = dy->type;
         v.pitch = packed_pitch(K, dy->type) / 2;

@@ -3,8 +3,10 @@
 //     u = gain dy,  dx = inv (u - s inv^2 mean_h(u s)) + ds,  dgain[h] = sum over rows of dy s inv
 // Both read and write every value once and are bound by memory: a row stays in registers between the sum and its use
 // (8 columns a lane in each of CH places), in one wavefront up to 2048 columns, so that no barrier separates them, and in
-// 4 or 16 wavefronts beyond.  16384 x 512 in bfloat16 with a residual, three quarters of the frames existing: 10.9 us (59 MB),
-// 2331 x 257 in float32 to 8 bits 7.1 us, one row 2.1 us.
+// 4 or 16 wavefronts beyond.  16384 x 512 in bfloat16 with a residual, three quarters of the frames existing: 10.9 us (59 MB), one row
+// 2.1 us; with all frames in float32 23.9 us (134 MB: 5.6 TB/s), 2048 x 16384 in bfloat16 46 us (268 MB: 5.8 TB/s).  To 8 bits: 16384 x 512
+// from bfloat16 22 us (59 MB: 2.7 TB/s, bound by the instructions in 64 bits), 2331 x 257 from float32 7.2 us (a chain of latencies: the
+// row, its sum, a root and a division in 64 bits, the gain).
 #pragma once
 #include "layer.hpp"
 
@@ -156,7 +158,9 @@ struct NormGradArgs {
 // row that does not exist this one is read again, from cache.  From turn to turn a workgroup moves on by 0.618 of their number,
 // so that one that meets the end of an item does not meet those of all, T being a multiple of that number or close to it.
 // 16384 x 2048 in bfloat16 with ds, three quarters of the frames existing (218 MB): 42 us, and 4.7 us for the sums over the
-// workgroups; in the same place every turn 45 us; a row a wavefront, nothing sent for ahead, 70 us.
+// workgroups; in the same place every turn 45 us; a row a wavefront, nothing sent for ahead, 70 us.  With all frames: in float32 105 us
+// (537 MB: 5.1 TB/s), s in 8 bits 46 us (236 MB); 16384 x 512 15.5 us (67 MB), 4096 x 8192 60 us (268 MB: 4.5 TB/s).  Beyond 8192 columns the two
+// rows in registers spill (up to 86 of them): 2048 x 16384 117 us (268 MB: 2.3 TB/s).
 template <typename DY, typename S, int WPR, int CH, bool DS>
 __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * kWave) void norm_grad_kernel(NormGradArgs a)
 {

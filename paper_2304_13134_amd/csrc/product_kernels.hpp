@@ -19,7 +19,8 @@
 //
 // Tiles of 256 x 256 on eight wavefronts of 128 x 64: 128 sums a lane leave registers for one set of fragments and a bit.
 // Measured (16384 x 1024 results, bfloat16): over 1024, 4096, 8192 terms 37, 107, 205 us = 930, 1285, 1340 TFLOP/s; a large library
-// product of these sizes 31, 90, 176 us.  8-bit operands: 28.6, 66, 118 us = 1200, 2080, 2330.  Input gradients as forward; weight
+// product of these sizes 31, 90, 176 us.  8-bit operands: 28.6, 66, 118 us = 1200, 2080, 2330; with results in float32, on tiles of
+// 128 x 128 of widened codes, 8000 x 4096 over 4096 280 us = 960 (145 us = 1850 with results in bfloat16).  Input gradients as forward; weight
 // gradients 4096 x 4096 over 16384 rows 428 us = 1285 TFLOP/s.  The matrix cores are busy 65 % of the cycles at 2.0 GHz (the
 // library's: 80 % at 1.87, the clock follows the power); LDS 25 %, without bank conflicts.  A step of 128 bytes takes 1.53 us on the
 // whole chip, 1.45 without the reads of LDS, 1.08 without the loads to it, and 1.10 on a chip with 16 such workgroups: what is
@@ -801,7 +802,7 @@ __global__ __launch_bounds__(WP * WQ * kWave, 2) void product_kernel(ProductArgs
 
 // ---- few rows: y = act(x w^T + bias) + residual for at most 16 MT rows, bound by the bytes of w, which go from memory to
 // registers once.  One row of 512 x 2048 in bfloat16 4.4 us, four of 4096 x 4096 in 8 bits 7.0 us (2.5 TB/s: a launch, a load, a
-// sum through LDS and a store, one after the other).  A workgroup takes 16 QF columns, its wavefronts every kFewWaves-th 128 bytes of the rows, four (two) such
+// sum through LDS and a store, one after the other), 10.7 us with results in float32.  A workgroup takes 16 QF columns, its wavefronts every kFewWaves-th 128 bytes of the rows, four (two) such
 // steps' loads under way at a time; their sums meet in LDS.
 constexpr int kFewWaves = 8;
 
