@@ -77,3 +77,14 @@ def test_small_and_large_scales(rows, scale):
     x, w = draw(rng, (rows, 96), "f32"), lb.last_keep(draw(rng, (50, 96), "f32"), E4M3)
     want = lb.last_product(lb.last_keep(x, E4M3), w, dtype=torch.float32)[0] * scale
     assert torch.equal(lb.last_product(lb.last_keep(x * scale, E4M3), w, dtype=torch.float32)[0], want)
+
+
+def test_smallest_codes():
+    """Values down to bfloat16's smallest subnormal number are multiplied as they are."""
+    announce("smallest codes")
+    for e in (-125, -127, -130, -133):
+        for rows in (3, 100):
+            x, w = torch.zeros(rows, 32, device="cuda"), torch.zeros(40, 32, device="cuda")
+            x[:, 0], w[:, 0] = 2.0 ** e, 2.0 ** 100
+            y = lb.last_product(lb.last_keep(x, E4M3), lb.last_keep(w, E4M3), dtype=torch.float32)[0]
+            assert torch.equal(y, torch.full((rows, 40), 2.0 ** (e + 100), device="cuda")), e
