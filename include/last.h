@@ -65,6 +65,7 @@
  *   it: up to 96 states it computes such items in the log domain (weights more
  *   than 1040 below the largest of their row count as absent arcs), from 97 to
  *   264 states dist may miss such paths.
+ * 8 (calls on a paged cache): a frame that is written or seen has no page, see last_cache_t.
  * Items with status 1..3 get dist = NaN and zero gradients.
  * Frames t >= len[b] do not exist for item b: their weights are never read
  * into a result, their marginals are 0 and their path entries are -1.
@@ -102,7 +103,10 @@ typedef enum {
     LAST_OP_RESIDUAL_NORM_GRAD = 6,    /* this and the following: last_layer_workspace_bytes */
     LAST_OP_PRODUCT = 7,
     LAST_OP_PRODUCT_GRAD_INPUT = 8,
-    LAST_OP_PRODUCT_GRAD_WEIGHT = 9
+    LAST_OP_PRODUCT_GRAD_WEIGHT = 9,
+    LAST_OP_HEAD_NORM_GRAD = 10,       /* this and the following: last_attention_workspace_bytes */
+    LAST_OP_ATTENTION_GRAD = 11,
+    LAST_OP_CACHED_ATTENTION = 12
 } last_op_t;
 
 /* Context dependency (Section 3): the full n-gram one in closed form (Figure 1a
@@ -356,6 +360,96 @@ last_status_t last_kept_values(const last_frames_t* frames, int32_t H, const las
 last_status_t last_kept_grad(const last_frames_t* frames, int32_t H, const last_matrix_t* dy,
                              const last_matrix_t* kept, last_activation_t act, const last_matrix_t* dx,
                              void* hip_stream);
+
+/* ---- Frames that see each other: attention in the layer, and its streaming form on a paged cache.
+ *
+ * Columns are heads: head h of a matrix has columns h*width .. (h+1)*width - 1.  Queries and results have `heads` of them, keys and
+ * values kv_heads, each of which heads / kv_heads neighbouring query heads share.  width is a multiple of 8 up to 128; with bands,
+ * T is at most 2^28.  Rows, pitches, alignment, lengths and frames that do not exist are as above, so queries, keys and
+ * values may be columns of the one matrix that a product made, and gradients go back to columns of one. */
+typedef struct {
+    int32_t heads, kv_heads, width;
+} last_heads_t;
+
+/* Column i < columns / 2 of a head is rotated with column i + columns / 2 by the angle position * frequencies[i]; the columns from
+ * `columns` on are not.  Frame t of item b has position first[b] + t.  columns: a multiple of 8 up to width, 0 for no rotation.
+ * Angles are formed in 64 bits. */
+typedef struct {
+    int32_t columns;
+    const float* frequencies;  /* dev float32 [columns / 2], radians a frame */
+    const int32_t* first;      /* dev int32 [B], or NULL for 0               */
+} last_rotation_t;
+
+/* Frame t sees frame s if s exists, s <= t + right, and s >= t - left or s < sinks (first frames that stay visible, at most 64).
+ * left, right: -1 for no limit.  scale (> 0): what scores are multiplied with. */
+typedef struct {
+    int32_t left, right, sinks;
+    float scale;
+} last_band_t;
+
+/* Keys and values of streams in pages.  k, v: dev [pages][kv_heads][page][width], BF16 or F16.  Frames j*page .. of item b are on page
+ * table[b][j], 0 <= j < entries; page * entries at most 2^30.  used[b] frames (clamped to [0, 2^30]) are in the cache
+ * before the new ones of a call, which are frames used[b] + t; the caller counts them afterwards.  Entries of pages on which no frame is
+ * written or seen may hold anything.  A frame whose entry is missing (j >= entries) or names no page gives its item
+ * item_status 8: it is not written, and results of frames that see it are NaN. */
+typedef struct {
+    void *k, *v;
+    int32_t type, pages, page, entries;
+    const int32_t* table;      /* dev int32 [B][entries] */
+    const int32_t* used;       /* dev int32 [B]          */
+} last_cache_t;
+
+/* Queries and keys normed by head and rotated: n = x * gain / sqrt(mean over the head's columns of x^2 + eps), or n = x where the
+ * gain is NULL; y = n rotated.  q with yq, k with yk: F32, BF16 or F16, all of one type; either pair may be NULL.  Gains: dev float32
+ * [width].  y may be written over x in the same pitch. */
+last_status_t last_head_norm(const last_frames_t* frames, const last_heads_t* heads, const last_matrix_t* q, const last_matrix_t* k,
+                             const float* gain_q, const float* gain_k, float eps, const last_rotation_t* rotation,
+                             const last_matrix_t* yq, const last_matrix_t* yk, void* hip_stream);
+
+/* The gradient: with dn = dy rotated back, u = gain * dn and inv the norm's factor, dx = inv * (u - x * inv^2 * mean(u * x)) and
+ * dgain[c] = sum over frames and heads of dn * x * inv; where the gain is NULL dx = dn.  q, k: as last_head_norm took them, all
+ * matrices of one type.  Either of (dyq, q, dq) and (dyk, k, dk) may be NULL, and the gains' gradients (dev float32 [width], written).
+ * dx may be written over dy in the same pitch.  Workspace: LAST_OP_HEAD_NORM_GRAD, with a gain's gradient only. */
+last_status_t last_head_norm_grad(const last_frames_t* frames, const last_heads_t* heads, const last_matrix_t* dyq, const last_matrix_t* dyk,
+                                  const last_matrix_t* q, const last_matrix_t* k, const float* gain_q, const float* gain_k, float eps,
+                                  const last_rotation_t* rotation, const last_matrix_t* dq, const last_matrix_t* dk, float* dgain_q,
+                                  float* dgain_k, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* y[t] = sum over the frames s that t sees of P[t][s] v[s], P the softmax of scale * q[t] . k[s] over them; lse (dev float32
+ * [B*T][heads], or NULL): the logarithm of the sum of exponentials, which the gradient needs.  q, k, v, y: all BF16 or all F16.
+ * Scores, sums and statistics are float32; P is rounded to the operands' type before it is multiplied.  What a frame
+ * does not see has no part in its result, infinities and NaN in its place included. */
+last_status_t last_attention(const last_frames_t* frames, const last_heads_t* heads, const last_band_t* band, const last_matrix_t* q,
+                             const last_matrix_t* k, const last_matrix_t* v, const last_matrix_t* y, float* lse, void* hip_stream);
+
+/* The gradients of q, k and v, those of k and v summed over the heads that share them.  y and lse as last_attention returned
+ * them; all matrices of one type, BF16 or F16.  P and dS are rounded to it before they are multiplied.  Frames that do
+ * not exist have no part in it; an infinity or a NaN in a frame that does may come out of the gradients of any of the item's frames.
+ * Workspace: LAST_OP_ATTENTION_GRAD. */
+last_status_t last_attention_grad(const last_frames_t* frames, const last_heads_t* heads, const last_band_t* band, const last_matrix_t* dy,
+                                  const last_matrix_t* q, const last_matrix_t* k, const last_matrix_t* v, const last_matrix_t* y,
+                                  const float* lse, const last_matrix_t* dq, const last_matrix_t* dk, const last_matrix_t* dv, void* ws,
+                                  size_t ws_bytes, void* hip_stream);
+
+/* Keys of new frames, normed and rotated by their positions used[b] + t as by last_head_norm, and their values to the pages of the cache;
+ * with q, its queries to yq in the same launch.  rotation->first is not read.  lengths: how many new frames an item has, 0 among
+ * them.  Nothing else of the pages is touched.  Two items must not write to one page.  item_status (dev int32 [B], or NULL):
+ * 0, or 8. */
+last_status_t last_cache_append(const last_frames_t* frames, const last_heads_t* heads, const last_matrix_t* q, const last_matrix_t* k,
+                                const last_matrix_t* v, const float* gain_q, const float* gain_k, float eps, const last_rotation_t* rotation,
+                                const last_cache_t* cache, const last_matrix_t* yq, int32_t* item_status, void* hip_stream);
+
+/* last_attention of the new frames (at positions used[b] + t) to what is in the cache after last_cache_append, with the same `used`:
+ * used[b] + lengths[b] frames exist.  q, y and the cache: all BF16 or all F16.  Items may share pages.  Workspace:
+ * LAST_OP_CACHED_ATTENTION (with the cache). */
+last_status_t last_cached_attention(const last_frames_t* frames, const last_heads_t* heads, const last_band_t* band, const last_matrix_t* q,
+                                    const last_cache_t* cache, const last_matrix_t* y, int32_t* item_status, void* ws, size_t ws_bytes,
+                                    void* hip_stream);
+
+/* Scratch bytes of a call above (LAST_OP_HEAD_NORM_GRAD ...): band and cache may be NULL where the call has none.  At least 256; 0 on
+ * invalid arguments. */
+size_t last_attention_workspace_bytes(int32_t op, const last_frames_t* frames, const last_heads_t* heads, const last_band_t* band,
+                                      const last_cache_t* cache);
 
 /* For callers that cannot allocate device memory (code under HIP graph capture,
  * tight serving loops, harnesses that forbid hipMalloc): last_shortest_distance

@@ -22,6 +22,7 @@ OP_SHORTEST_DISTANCE, OP_ARC_POSTERIORS, OP_INTERSECT_REFERENCE, OP_SHORTEST_PAT
 OP_LOCAL_LOG_LIKELIHOOD = 4
 OP_LOSS = 5
 OP_RESIDUAL_NORM_GRAD, OP_PRODUCT, OP_PRODUCT_GRAD_INPUT, OP_PRODUCT_GRAD_WEIGHT = 6, 7, 8, 9
+OP_HEAD_NORM_GRAD, OP_ATTENTION_GRAD, OP_CACHED_ATTENTION = 10, 11, 12
 WEIGHTS_DENSE, WEIGHTS_SHARED_EMB = 0, 1
 
 EXPORTS = ["last_workspace_bytes", "last_shortest_distance", "last_arc_posteriors",
@@ -31,7 +32,8 @@ EXPORTS = ["last_workspace_bytes", "last_shortest_distance", "last_arc_posterior
            "last_local_log_likelihood", "last_probe_bandwidth", "last_globally_normalized_loss",
            "last_verify_placement", "last_least_workspace_bytes", "last_residual_norm", "last_residual_norm_grad",
            "last_product", "last_product_grad_input", "last_product_grad_weight", "last_layer_workspace_bytes",
-           "last_keep", "last_kept_values", "last_kept_grad"]
+           "last_keep", "last_kept_values", "last_kept_grad", "last_head_norm", "last_head_norm_grad", "last_attention",
+           "last_attention_grad", "last_cache_append", "last_cached_attention", "last_attention_workspace_bytes"]
 PROBE_READ, PROBE_COPY, PROBE_READ_ROWS, PROBE_READ_COLUMNS = 0, 1, 2, 3
 OPT_FORCE_SOLO, OPT_CLUSTER_GENERATION, OPT_CLUSTER_VITERBI, OPT_SPIN_LIMIT, OPT_FUSED_FRAMES_PER_TILE = 0, 1, 2, 3, 4
 OPT_FUSED_KEEP_MARGINALS = 5
@@ -129,11 +131,19 @@ def load_library():
             ("last_product_grad_weight", [fr, i32, i32, mx, mx, i32, mx, vp, vp, sz, vp]),
             ("last_keep", [fr, i32, mx, mx, vp]),
             ("last_kept_values", [fr, i32, mx, i32, mx, vp]),
-            ("last_kept_grad", [fr, i32, mx, mx, i32, mx, vp])):
+            ("last_kept_grad", [fr, i32, mx, mx, i32, mx, vp]),
+            ("last_head_norm", [fr, vp, mx, mx, vp, vp, f32, vp, mx, mx, vp]),
+            ("last_head_norm_grad", [fr, vp, mx, mx, mx, mx, vp, vp, f32, vp, mx, mx, vp, vp, vp, sz, vp]),
+            ("last_attention", [fr, vp, vp, mx, mx, mx, mx, vp, vp]),
+            ("last_attention_grad", [fr, vp, vp, mx, mx, mx, mx, mx, vp, mx, mx, mx, vp, sz, vp]),
+            ("last_cache_append", [fr, vp, mx, mx, mx, vp, vp, f32, vp, vp, mx, vp, vp]),
+            ("last_cached_attention", [fr, vp, vp, mx, vp, mx, vp, vp, sz, vp])):
         getattr(lib, name).restype = i32
         getattr(lib, name).argtypes = arguments
     lib.last_layer_workspace_bytes.restype = sz
     lib.last_layer_workspace_bytes.argtypes = [i32, fr, i32, i32, mx, mx]
+    lib.last_attention_workspace_bytes.restype = sz
+    lib.last_attention_workspace_bytes.argtypes = [i32, fr, vp, vp, vp]
     lib.last_kernel_variant.restype = i32
     lib.last_kernel_variant.argtypes = [ctypes.POINTER(LastWeights), ctypes.POINTER(LastContext), i32]
     _lib = lib
@@ -613,19 +623,24 @@ def _launch(on, call, *arguments):
 
 
 def _with_scratch(call, op, frames, N, K, a, b, t):
+    """call(workspace address, bytes, stream) for tensor t's device and its current stream, with what last_layer_workspace_bytes asks for."""
+    _with_scratch_of(call, lambda: load_library().last_layer_workspace_bytes(op, frames, N, K, a, b), t)
+
+
+def _with_scratch_of(call, size, t):
     """call(workspace address, bytes, stream) for tensor t's device and its current stream.  The buffer that is there is tried
     first: the library refuses one that is too small before it enqueues anything.  (Not under capture, see workspace().)"""
     on = t.get_device()
     if on != torch._C._cuda_getDevice():
         with torch.cuda.device(on):
-            return _with_scratch(call, op, frames, N, K, a, b, t)
+            return _with_scratch_of(call, size, t)
     stream = torch._C._cuda_getCurrentRawStream(on)
     buf = None if torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((on, stream))
     if buf is not None:
         code = call(buf.data_ptr(), buf.numel(), stream)
         if code != 5:
             return _check(code)
-    nbytes = load_library().last_layer_workspace_bytes(op, frames, N, K, a, b)
+    nbytes = size()
     buf = workspace(nbytes or 256, t.device)          # (where none would do, the call says what is wrong)
     _check(call(buf.data_ptr(), buf.numel(), stream))
 
@@ -737,3 +752,234 @@ def last_kept_grad(dy, kept, activation, lengths=None, dtype=None):
     dx, mdx = _result(dy.shape, dtype or dy.dtype, dy.device, dy)
     _launch(on, load_library().last_kept_grad, fr, H, mdy, mk, _activation(activation), mdx)
     return dx
+
+
+# ---- frames that see each other
+
+_pack_heads = struct.Struct("@iii").pack
+_pack_band = struct.Struct("@iiif").pack
+_pack_rotation = struct.Struct("@iPP").pack
+_pack_cache = struct.Struct("@PPiiiiPP").pack
+
+
+class Rotation(tuple):
+    """How last_head_norm rotates: (frequencies, first), frequencies float32 [columns / 2] in radians a frame, of the columns that are
+    rotated (column i with column i + columns / 2), first int32 [B], the position of each item's frame 0, or None for 0."""
+
+    def __new__(cls, frequencies, first=None):
+        return super().__new__(cls, (frequencies, first))
+
+    frequencies = property(lambda self: self[0])
+    first = property(lambda self: self[1])
+
+
+class Cache(tuple):
+    """Keys and values of streams in pages: (k, v, table, used).  k, v: bfloat16 or float16 [pages, kv_heads, page, width]; table int32
+    [B, entries]: the page of frames j * page .. of an item; used int32 [B]: the frames in the cache before the new ones of a
+    call, which the caller counts up after the calls of a step (used += lengths)."""
+
+    def __new__(cls, k, v, table, used):
+        return super().__new__(cls, (k, v, table, used))
+
+    k = property(lambda self: self[0])
+    v = property(lambda self: self[1])
+    table = property(lambda self: self[2])
+    used = property(lambda self: self[3])
+
+
+def _heads(q, k, width):
+    """(packed LastHeads, heads, kv_heads) of matrices of which one may be None"""
+    if width < 1:
+        raise ValueError("width must be positive")
+    counts = []
+    for t, name in ((q, "q"), (k, "k")):
+        if t is not None and (not isinstance(t, torch.Tensor) or t.dim() < 1 or t.shape[-1] % width != 0 or t.shape[-1] == 0):
+            raise ValueError("%s must be a tensor with whole heads of %d columns" % (name, width))
+        counts.append(None if t is None else t.shape[-1] // width)
+    heads, kv = counts
+    if heads is not None and kv is not None and heads % kv != 0:
+        raise ValueError("%d heads cannot share %d heads of keys evenly" % (heads, kv))
+    return _pack_heads(heads or kv, kv or heads, width), heads, kv
+
+
+def _rotation(rotation, width, B, on):
+    """packed LastRotation or None"""
+    if rotation is None:
+        return None
+    frequencies, first = rotation if isinstance(rotation, Rotation) else (rotation, None)
+    f = _dev_tensor(frequencies, torch.float32, "frequencies")
+    if f.dim() != 1 or 2 * f.shape[0] > width or f.shape[0] % 4 != 0:
+        raise ValueError("frequencies must be [columns / 2] of a multiple of 8 columns, at most %d" % width)
+    if f.get_device() != on:
+        _elsewhere("frequencies")
+    if first is not None:
+        _dev_tensor(first, torch.int32, "first")
+        if first.shape != (B,):
+            raise ValueError("first must be [%d]" % B)
+        if first.get_device() != on:
+            _elsewhere("first")
+    return _pack_rotation(2 * f.shape[0], f.data_ptr() or _NO_ROWS, 0 if first is None else first.data_ptr() or _NO_ROWS)
+
+
+def _items(t, lengths, name):
+    """_frames of a tensor in which frames see each other, or have positions: [B, T, columns], or [T, columns] for one item; and B"""
+    fr, rows, t, on = _frames(t, lengths, name)
+    if len(rows) == 1:
+        return _pack_frames(1, rows[0], 0), rows, on, 1
+    if lengths is None and rows[0] > 0:
+        fr = _pack_frames(rows[0], rows[1], 0)
+    return fr, rows, on, rows[0]
+
+
+def _band(left, right, sinks, scale, width):
+    for n, name in ((left, "left"), (right, "right")):
+        if n is not None and n < 0:
+            raise ValueError("%s must be a number of frames, or None for no limit" % name)
+    if sinks < 0:
+        raise ValueError("sinks must be a number of frames")
+    most = 0x7fffffff
+    return _pack_band(-1 if left is None else min(left, most), -1 if right is None else min(right, most), min(sinks, most),
+                      width ** -0.5 if scale is None else scale)
+
+
+def _out(t, name, like, on, rows):
+    """(tensor to write, its packed LastMatrix): a given one, or a new one of `like`'s shape and type"""
+    if t is None:
+        return _result(like.shape, like.dtype, like.device, like)
+    return t, _matrix(t, name, on, rows, like.shape[-1])
+
+
+def last_head_norm(q, k, width, gain_q=None, gain_k=None, rotation=None, lengths=None, eps=1e-5, out=None):
+    """(yq, yk): queries and keys normed by heads of `width` columns and rotated by their frames' positions.  q, k: [T, columns] or
+    [B, T, columns] of one type, either may be None; gains float32 [width], None: not normed; rotation: a Rotation, frequencies alone
+    (positions from 0), or None.  out: a pair of tensors to write to, which may be q and k themselves."""
+    heads, _, _ = _heads(q, k, width)
+    fr, rows, on, B = _items(q if q is not None else k, lengths, "q" if q is not None else "k")
+    r = _rotation(rotation, width, B, on)
+    g = [_vector(t, width, name, on) for t, name in ((gain_q, "gain_q"), (gain_k, "gain_k"))]
+    x, y, my = [None, None], [None, None], [None, None]
+    for i, (t, name) in enumerate(((q, "q"), (k, "k"))):
+        if t is not None:
+            x[i] = _matrix(t, name, on, rows)
+            y[i], my[i] = _out(out[i] if out is not None else None, "out", t, on, rows)
+    _launch(on, load_library().last_head_norm, fr, heads, x[0], x[1], g[0], g[1], eps, r, my[0], my[1])
+    return y[0], y[1]
+
+
+def last_head_norm_grad(dyq, dyk, q, k, width, gain_q=None, gain_k=None, rotation=None, lengths=None, eps=1e-5, out=None):
+    """(dq, dk, dgain_q, dgain_k) of last_head_norm with the same arguments; the gradients of gains float32 [width], None where the
+    gain is.  Either of dyq, dyk may be None.  out: a pair of tensors to write dq and dk to, which may be dyq and dyk themselves."""
+    heads, _, _ = _heads(dyq, dyk, width)
+    one = dyq if dyq is not None else dyk
+    fr, rows, on, B = _items(one, lengths, "dyq" if dyq is not None else "dyk")
+    r = _rotation(rotation, width, B, on)
+    g, dy, x, dx, mdx, dg = [None, None], [None, None], [None, None], [None, None], [None, None], [None, None]
+    for i, (t, s, gain, end) in enumerate(((dyq, q, gain_q, "q"), (dyk, k, gain_k, "k"))):
+        if t is None:
+            continue
+        dy[i], x[i] = _matrix(t, "dy" + end, on, rows), _matrix(s, end, on, rows, t.shape[-1])
+        g[i] = _vector(gain, width, "gain_" + end, on)
+        dx[i], mdx[i] = _out(out[i] if out is not None else None, "out", t, on, rows)
+        if gain is not None:
+            dg[i] = torch.empty(width, dtype=torch.float32, device=t.device)
+    lib = load_library()
+    _with_scratch_of(lambda ws, n, stream: lib.last_head_norm_grad(fr, heads, dy[0], dy[1], x[0], x[1], g[0], g[1], eps, r, mdx[0], mdx[1],
+                                                                  _ptr(dg[0]), _ptr(dg[1]), ws, n, stream),
+                     lambda: lib.last_attention_workspace_bytes(OP_HEAD_NORM_GRAD, fr, heads, None, None), one)
+    return dx[0], dx[1], dg[0], dg[1]
+
+
+def last_attention(q, k, v, width, left=None, right=0, sinks=0, scale=None, lengths=None):
+    """(y, lse): attention of each frame t to the frames t - left .. t + right of its item and the first `sinks` ones that are no later than
+    t + right (left, right None: no limit), and the logarithms of the softmax sums, float32 [.., heads], for the gradient.  q: [T, columns]
+    or [B, T, columns], k and v with as many heads of `width` columns or fewer, shared evenly: all bfloat16 or all float16, columns of one
+    matrix maybe.  scale: what scores are multiplied with, default width ** -0.5."""
+    heads, n, _ = _heads(q, k, width)
+    fr, rows, on, _ = _items(q, lengths, "q")
+    mq, mk, mv = _matrix(q, "q", on), _matrix(k, "k", on, rows), _matrix(v, "v", on, rows, k.shape[-1])
+    y, my = _result(q.shape, q.dtype, q.device, q)
+    lse = torch.empty((*rows, n), dtype=torch.float32, device=q.device)
+    _launch(on, load_library().last_attention, fr, heads, _band(left, right, sinks, scale, width), mq, mk, mv, my, lse.data_ptr() or _NO_ROWS)
+    return y, lse
+
+
+def last_attention_grad(dy, q, k, v, y, lse, width, left=None, right=0, sinks=0, scale=None, lengths=None, out=None):
+    """(dq, dk, dv) of last_attention with the same arguments, given its results.  They are columns of one new matrix [.., (heads + 2
+    kv_heads) width], as the gradient of one product's result wants them, or go to the three tensors of `out`."""
+    heads, n, kv = _heads(q, k, width)
+    fr, rows, on, _ = _items(q, lengths, "q")
+    mq, mk, mv = _matrix(q, "q", on), _matrix(k, "k", on, rows), _matrix(v, "v", on, rows, k.shape[-1])
+    mdy, my = _matrix(dy, "dy", on, rows, q.shape[-1]), _matrix(y, "y", on, rows, q.shape[-1])
+    l = _vector(lse, q.numel() // width, "lse", on) or _NO_ROWS
+    if out is None:
+        whole = torch.empty((*rows, (n + 2 * kv) * width), dtype=q.dtype, device=q.device)
+        out = whole.split([n * width, kv * width, kv * width], dim=-1)
+    mo = [_matrix(t, name, on, rows, x.shape[-1]) for t, name, x in zip(out, ("dq", "dk", "dv"), (q, k, k))]
+    band, lib = _band(left, right, sinks, scale, width), load_library()
+    _with_scratch_of(lambda ws, m, stream: lib.last_attention_grad(fr, heads, band, mdy, mq, mk, mv, my, l, mo[0], mo[1], mo[2], ws, m, stream),
+                     lambda: lib.last_attention_workspace_bytes(OP_ATTENTION_GRAD, fr, heads, band, None), q)
+    return tuple(out)
+
+
+def _cache(cache, B, on):
+    """packed LastCache"""
+    k, v, table, used = cache
+    for t, name in ((k, "cache.k"), (v, "cache.v")):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float16) or t.dim() != 4 or not t.is_contiguous():
+            raise TypeError("%s must be a contiguous bfloat16 or float16 device tensor [pages, kv_heads, page, width]" % name)
+        if t.get_device() != on:
+            _elsewhere(name)
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("cache.k and cache.v must be alike")
+    _dev_tensor(table, torch.int32, "cache.table")
+    _dev_tensor(used, torch.int32, "cache.used")
+    if table.dim() != 2 or table.shape[0] != B or used.shape != (B,):
+        raise ValueError("cache.table must be [%d, entries] and cache.used [%d]" % (B, B))
+    if table.get_device() != on or used.get_device() != on:
+        _elsewhere("cache.table or cache.used")
+    return _pack_cache(k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[0], k.shape[2], table.shape[1], table.data_ptr() or _NO_ROWS,
+                       used.data_ptr() or _NO_ROWS)
+
+
+def _status_of(item_status, B, t, on):
+    """(address of the call's item_status)"""
+    item_status = _status(item_status, B, t.device)
+    if item_status.numel() < B or item_status.get_device() != on:
+        raise ValueError("item_status must have %d elements on the call's device" % B)
+    return item_status.data_ptr() if B else None
+
+
+def last_cache_append(k, v, cache, q=None, gain_q=None, gain_k=None, frequencies=None, lengths=None, eps=1e-5, item_status=None):
+    """Keys of new frames, normed and rotated as by last_head_norm at positions used + t, and their values into a Cache; with q, returns its
+    queries, normed and rotated by the same call, else None.  k, v: [B, T, kv_heads width] of the cache's type, of which lengths [B] new
+    frames exist.  item_status: see check_item_status()."""
+    width = cache.k.shape[-1]
+    heads, _, kv = _heads(q, k, width)
+    fr, rows, on, B = _items(k, lengths, "k")
+    r = _rotation(frequencies, width, B, on)
+    if kv != cache.k.shape[1]:
+        raise ValueError("k has %d heads, the cache %d" % (kv, cache.k.shape[1]))
+    mk, mv, mc = _matrix(k, "k", on), _matrix(v, "v", on, rows, k.shape[-1]), _cache(cache, B, on)
+    g = [_vector(t, width, name, on) for t, name in ((gain_q, "gain_q"), (gain_k, "gain_k"))]
+    mq = yq = my = None
+    if q is not None:
+        mq = _matrix(q, "q", on, rows)
+        yq, my = _result(q.shape, q.dtype, q.device, q)
+    _launch(on, load_library().last_cache_append, fr, heads, mq, mk, mv, g[0], g[1], eps, r, mc, my, _status_of(item_status, B, k, on))
+    return yq
+
+
+def last_cached_attention(q, cache, left=None, right=0, sinks=0, scale=None, lengths=None, item_status=None):
+    """y: last_attention of new frames, q [B, T, columns] of which lengths [B] exist, at positions cache.used + t, to what a Cache holds after
+    last_cache_append with the same `used`.  item_status: see check_item_status()."""
+    width, kv = cache.k.shape[-1], cache.k.shape[1]
+    if q.shape[-1] % (kv * width) != 0 or q.shape[-1] == 0:
+        raise ValueError("q must have a multiple of the cache's %d heads of %d columns" % (kv, width))
+    heads = _pack_heads(q.shape[-1] // width, kv, width)
+    fr, rows, on, B = _items(q, lengths, "q")
+    mq, mc, band = _matrix(q, "q", on), _cache(cache, B, on), _band(left, right, sinks, scale, width)
+    y, my = _result(q.shape, q.dtype, q.device, q)
+    status, lib = _status_of(item_status, B, q, on), load_library()
+    _with_scratch_of(lambda ws, n, stream: lib.last_cached_attention(fr, heads, band, mq, mc, my, status, ws, n, stream),
+                     lambda: lib.last_attention_workspace_bytes(OP_CACHED_ATTENTION, fr, heads, band, mc), q)
+    return y
