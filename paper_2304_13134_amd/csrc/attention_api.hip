@@ -17,7 +17,7 @@ using namespace last;
 
 namespace {
 
-constexpr int kMostWidth = 128, kMostHeads = 1 << 16, kMostSinks = 64, kMostPage = 1 << 20;
+constexpr int kMostWidth = 128, kMostHeads = 1 << 16, kMostPage = 1 << 20;
 constexpr int kMostFrames = 1 << 28;                  // of an item: sums of two of them and a position stay in 32 bits
 
 last_status_t check_heads(const last_heads_t* h)
@@ -146,34 +146,56 @@ int padded(int width) { return width <= 32 ? 32 : width <= 64 ? 64 : 128; }
         else { constexpr int DP = 128; call; }                      \
     } while (0)
 
+// Heads that share keys go to one XCD together where that gives each as many.
+unsigned heads_together(const AttentionArgs& a) { return a.B * a.kv_heads % 8 == 0 ? (unsigned)(a.heads / a.kv_heads) : 1u; }
+
 template <typename E>
 void launch_attention(AttentionArgs a, hipStream_t st)
 {
-    a.tiles = (unsigned)((a.T + kOwn - 1) / kOwn);
+    const long long own = (long long)((a.T + 255) / 256) * a.heads * a.B;
+    const bool two = false;
+    const int frames = two ? 256 : 128;
+    a.tiles = (unsigned)((a.T + frames - 1) / frames);
+    a.together = heads_together(a);
     in_launches((long long)a.tiles * a.heads * a.B, [&](long long first, dim3 grid) {
         a.first = (unsigned)first;
-        LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((attention_kernel<E, DP>), grid, dim3(256), 0, st, a));
+        if (two) LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((attention_kernel<E, DP, 2>), grid, dim3(256), 0, st, a));
+        else LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((attention_kernel<E, DP, 1>), grid, dim3(256), 0, st, a));
     });
 }
 
-// Shares of the frames that see first ones from beyond the window: a share has at least 512 of them.
-int sink_shares(const Band& band, int T)
+// Chunks of the frames that see first ones from beyond the window: of 256 frames where that makes no more than 64 a head.
+int sink_chunks(const Band& band, int T)
 {
     if (band.sinks == 0 || band.left + 1 >= T) return 0;
-    return std::max(1, std::min(64, (T - band.left) / 512));
+    return std::max(1, std::min(64, (T - band.left - 1 + 255) / 256));
 }
 
 struct GradPlan {
-    int shares;
-    float *delta, *part;
+    int chunks, shares, parts;
+    float *delta, *part, *sums, *kept;
 };
+
+// Heads that share keys go in parts where that makes workgroups enough for four rounds.
+int grad_parts(const last_frames_t* f, const last_heads_t* h)
+{
+    const long long groups = (long long)f->B * h->kv_heads * ((f->T + kOwn - 1) / kOwn) * (padded(h->width) == 128 ? 2 : 1);
+    return (int)std::max(1ll, std::min<long long>(h->heads / h->kv_heads, 1024 / std::max(1ll, groups)));
+}
 
 GradPlan plan_grad(Carver& cv, long long rows, const last_frames_t* f, const last_heads_t* h, const Band& band)
 {
-    GradPlan p;
-    p.shares = sink_shares(band, f->T);
+    GradPlan p{};
+    p.chunks = sink_chunks(band, f->T);
+    p.shares = h->heads / h->kv_heads * p.chunks * 2;
     p.delta = (float*)cv.take(sizeof(float) * (size_t)rows * h->heads);
-    p.part = p.shares ? (float*)cv.take(sizeof(float) * (size_t)f->B * h->kv_heads * p.shares * 2 * kMostSinks * padded(h->width)) : nullptr;
+    if (p.chunks) {
+        const size_t row = sizeof(float) * 2 * kMostSinks * padded(h->width), units = (size_t)f->B * h->kv_heads;
+        p.part = (float*)cv.take(row * units * p.shares);
+        p.sums = (float*)cv.take(row * units);
+    }
+    p.parts = grad_parts(f, h);
+    if (p.parts > 1) p.kept = (float*)cv.take(sizeof(float) * 2 * p.parts * (size_t)rows * h->kv_heads * padded(h->width));
     return p;
 }
 
@@ -193,21 +215,34 @@ void launch_delta(const AttentionArgs& a, hipStream_t st)
 }
 
 template <typename E>
-void launch_attention_grad(AttentionArgs a, hipStream_t st)
+void launch_attention_grad(AttentionArgs a, int chunks, hipStream_t st)
 {
     launch_delta<E>(a, st);
-    if (a.shares) {
-        a.tiles = (unsigned)a.shares;
-        in_launches((long long)a.tiles * a.kv_heads * a.B, [&](long long first, dim3 grid) {
+    a.together = 1;
+    if (chunks) {
+        a.tiles = (unsigned)chunks;
+        in_launches((long long)a.tiles * a.heads * a.B, [&](long long first, dim3 grid) {
             a.first = (unsigned)first;
-            LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_key_kernel<E, DP, true>), grid, dim3(256), 0, st, a));
+            LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_first_kernel<E, DP>), grid, dim3(256), 0, st, a));
+        });
+        in_launches((long long)a.B * a.kv_heads * 2 * a.band.sinks, [&](long long first, dim3 grid) {
+            hipLaunchKernelGGL(first_join_kernel, grid, dim3(128), 0, st, (const float*)a.part, a.sums, a.shares, padded(a.D), a.band.sinks, first);
         });
     }
     a.tiles = (unsigned)((a.T + kOwn - 1) / kOwn);
-    in_launches((long long)a.tiles * a.kv_heads * a.B, [&](long long first, dim3 grid) {
+    a.half = a.tiles * (unsigned)(a.kv_heads * a.parts * a.B);
+    in_launches((long long)a.half * (padded(a.D) == 128 ? 2 : 1), [&](long long first, dim3 grid) {
         a.first = (unsigned)first;
-        LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_key_kernel<E, DP, false>), grid, dim3(256), 0, st, a));
+        if (padded(a.D) == 128) hipLaunchKernelGGL((grad_key_kernel<E, 128, true>), grid, dim3(256), 0, st, a);
+        else if (padded(a.D) == 64) hipLaunchKernelGGL((grad_key_kernel<E, 64, false>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((grad_key_kernel<E, 32, false>), grid, dim3(256), 0, st, a);
     });
+    if (a.parts > 1) {
+        in_launches((2ll * a.B * a.T * a.kv_heads * (padded(a.D) / 4) + 255) / 256, [&](long long first, dim3 grid) {
+            hipLaunchKernelGGL((grad_join_kernel<E>), grid, dim3(256), 0, st, a, padded(a.D), first);
+        });
+    }
+    a.together = heads_together(a);
     in_launches((long long)a.tiles * a.heads * a.B, [&](long long first, dim3 grid) {
         a.first = (unsigned)first;
         LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_query_kernel<E, DP>), grid, dim3(256), 0, st, a));
@@ -433,10 +468,13 @@ last_status_t last_attention_grad(const last_frames_t* frames, const last_heads_
     const GradPlan plan = plan_grad(cv, rows, frames, heads, a.band);
     a.delta = plan.delta;
     a.part = plan.part;
+    a.sums = plan.sums;
     a.shares = plan.shares;
+    a.parts = plan.parts;
+    a.kept = plan.kept;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (type == LAST_BF16) launch_attention_grad<bf16_t>(a, st);
-    else launch_attention_grad<f16_t>(a, st);
+    if (type == LAST_BF16) launch_attention_grad<bf16_t>(a, plan.chunks, st);
+    else launch_attention_grad<f16_t>(a, plan.chunks, st);
     return hip_done();
 }
 

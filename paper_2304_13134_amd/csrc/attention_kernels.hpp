@@ -24,7 +24,8 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 64;            // frames of a tile in LDS
 constexpr int kOwn = 128;            // frames of a workgroup
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMostSinks = 64;       // first frames
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Band {
     int left, right, sinks;
@@ -38,10 +39,13 @@ struct AttentionArgs {
     void *y, *dq, *dk, *dv;
     long long pq, pk, pv, py, pdy, pdq, pdk, pdv;
     float *lse, *delta;              // [B * T][heads]
-    float* part;                     // first frames' sums of dk and dv, see sinks_kernel
+    float *part, *sums;              // first frames' sums of dk and dv (grad_first_kernel, first_join_kernel), or null
     int shares;
+    float* kept;                     // sums of dk and dv of parts of the heads that share them (grad_join_kernel)
+    int parts;
     Band band;
-    unsigned first, tiles;           // of the launch; a workgroup's own frames are tile `id % tiles`
+    unsigned half;                   // workgroups of grad_key_kernel that form keys' gradients alone
+    unsigned first, tiles, together; // of the launch: its first workgroup, tiles of a head, heads that go to one XCD together
 };
 
 template <typename E> struct Mma;
@@ -68,61 +72,95 @@ __device__ __forceinline__ f16x zeros16()
     return v;
 }
 
-// A tile in LDS: rows of DP columns of 16 bits.
+// A tile in LDS: rows of DP columns of 16 bits.  16-byte piece c of row r stands at c ^ spread(r) of its row, so that the 256 bytes that
+// the banks give at a time are different ones for a column of 16 rows (reads along rows) and for four pieces of 4 rows (transposing reads).
 template <int DP> struct Rows {
-    static constexpr int kPitch = DP * 2 + 16;
+    static constexpr int kPitch = DP * 2;
     static constexpr int kBytes = kTile * kPitch;
-    static constexpr int kPieces = DP / 8;                   // of 16 bytes a row
-    static constexpr int kEach = kTile * kPieces / 256;      // of a thread of 256
-    static constexpr int kApart = 256 / kPieces;             // rows between a thread's pieces
-};
-
-// a thread's pieces of a tile, sent for ahead
-template <int DP> struct Sent {
-    u4 v[Rows<DP>::kEach];
-};
-
-// Rows s0 .. s0 + 63 of a head from `p` (its row 0); what `exists(row)` denies and columns beyond D are zeros.
-template <int DP, typename Exists>
-__device__ __forceinline__ void send(Sent<DP>& r, const char* p, long long pitch, int D, int s0, Exists exists)
-{
-    const int c = (int)threadIdx.x % Rows<DP>::kPieces * 8;
-#pragma unroll
-    for (int i = 0; i < Rows<DP>::kEach; ++i) {
-        const int s = s0 + (int)threadIdx.x / Rows<DP>::kPieces + i * Rows<DP>::kApart;
-        r.v[i] = u4{0u, 0u, 0u, 0u};
-        if (c < D && exists(s)) r.v[i] = *(const u4_any*)(p + ((size_t)s * pitch + c) * 2);
+    static __device__ __forceinline__ int spread(int r)
+    {
+        return (r >> 2 & 3) | (DP == 128 ? (r & 3) << 2 : DP == 64 ? (r >> 1 & 1) << 2 : 0);
     }
-}
+};
 
-template <int DP>
-__device__ __forceinline__ void lay(const Sent<DP>& r, char* lds)
-{
-    const int at = (int)threadIdx.x / Rows<DP>::kPieces * Rows<DP>::kPitch + (int)threadIdx.x % Rows<DP>::kPieces * 16;
+// A tile's way from memory to LDS, by THREADS threads: sent for ahead to registers.
+template <int DP, int THREADS> struct Tile {
+    static constexpr int kPieces = DP / 8;                   // of 16 bytes a row
+    static constexpr int kApart = THREADS / kPieces;         // rows between a thread's pieces
+    static constexpr int kEach = kTile / kApart;
+    static_assert(kTile % kApart == 0 && kApart % 16 == 0, "whole tiles, the same spread for a thread's pieces");
+    u4 v[kEach];
+    bool all;
+
+    // Rows s0 .. s0 + 63 of a head from `p` (its row 0).  all_: all of them are there; else what `exists(row)` denies is asked for at row `other`
+    // instead, which exists, and laid as zeros, as are columns beyond D.
+    template <typename Exists>
+    __device__ __forceinline__ void send(const char* p, long long pitch, int D, int s0, bool all_, int other, Exists exists)
+    {
+        const int piece = (int)threadIdx.x % kPieces * 8, c = piece < D ? piece : 0, r = (int)threadIdx.x / kPieces;
+        all = all_ && D == DP;
+        if (all_) {
+            const char* const base = p + (size_t)(unsigned)s0 * pitch * 2;
+            const unsigned off = (unsigned)(r * pitch + c) * 2u;                       // (64 pitches of at most 4 MiB)
 #pragma unroll
-    for (int i = 0; i < Rows<DP>::kEach; ++i) *(u4*)(lds + at + i * Rows<DP>::kApart * Rows<DP>::kPitch) = r.v[i];
-}
+            for (int i = 0; i < kEach; ++i) v[i] = *(const u4_any*)(base + (size_t)i * kApart * pitch * 2 + off);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int s = s0 + r + i * kApart;
+                v[i] = *(const u4_any*)(p + ((size_t)(unsigned)(exists(s) ? s : other) * pitch + c) * 2);
+            }
+        }
+    }
 
-// first operand, rows 32 block .. of the tile, columns 16 k ..
-template <int DP>
-__device__ __forceinline__ u4 along_rows(const char* lds, int block, int k)
-{
-    const int lane = (int)threadIdx.x % kWave;
-    return *(const u4*)(lds + (lane & 31) * Rows<DP>::kPitch + (lane >> 5) * 16 + block * 32 * Rows<DP>::kPitch + k * 32);
-}
+    template <typename Exists>
+    __device__ __forceinline__ void lay(char* lds, int D, int s0, Exists exists) const
+    {
+        const int r = (int)threadIdx.x / kPieces, c = (int)threadIdx.x % kPieces;
+        const int at = r * Rows<DP>::kPitch + (c ^ Rows<DP>::spread(r)) * 16;
+        if (all) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) *(u4*)(lds + at + i * kApart * Rows<DP>::kPitch) = v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const unsigned keep = (c * 8 < D) & exists(s0 + r + i * kApart) ? ~0u : 0u;
+                *(u4*)(lds + at + i * kApart * Rows<DP>::kPitch) = v[i] & u4{keep, keep, keep, keep};
+            }
+        }
+    }
+};
 
-// first operand, columns 32 block .. of the tile, rows 16 k .. in the order of the scores
-template <int DP>
-__device__ __forceinline__ u4 along_columns(const char* lds, int block, int k)
-{
-    typedef __attribute__((address_space(3))) s4* at;
-    const int lane = (int)threadIdx.x % kWave;
-    const char* p = lds + (4 * (lane >> 5) + (lane & 15) / 4) * Rows<DP>::kPitch + ((lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2 +
-                    16 * k * Rows<DP>::kPitch + block * 64;
-    const u2 lo = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)p));
-    const u2 hi = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(p + 8 * Rows<DP>::kPitch)));
-    return u4{lo[0], lo[1], hi[0], hi[1]};
-}
+// First operands from a tile: where a lane reads.
+template <int DP> struct Reads {
+    int rows[DP / 16];               // along rows: of columns 16 k ..
+    int columns[DP / 32][2];         // along columns 32 d ..: rows 4 h .. and 8 + 4 h ..
+    __device__ __forceinline__ void init()
+    {
+        const int lane = (int)threadIdx.x % kWave, h = lane >> 5, r = lane & 31;
+        const int c = 4 * h + (lane & 15) / 4, piece = 2 * (lane >> 4 & 1) + (lane & 3) / 2;
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) rows[k] = r * Rows<DP>::kPitch + ((2 * k + h) ^ Rows<DP>::spread(r)) * 16;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                columns[d][i] = (c + 8 * i) * Rows<DP>::kPitch + ((4 * d + piece) ^ Rows<DP>::spread(c + 8 * i)) * 16 + (lane & 1) * 8;
+    }
+    // rows 32 block .. of the tile, columns 16 k ..
+    __device__ __forceinline__ u4 along_rows(const char* lds, int block, int k) const
+    {
+        return *(const u4*)(lds + rows[k] + block * 32 * Rows<DP>::kPitch);
+    }
+    // columns 32 d .. of the tile, rows 16 k .. in the order of the scores
+    __device__ __forceinline__ u4 along_columns(const char* lds, int d, int k) const
+    {
+        typedef __attribute__((address_space(3))) s4* at;
+        const u2 lo = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(lds + columns[d][0] + 16 * k * Rows<DP>::kPitch)));
+        const u2 hi = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(lds + columns[d][1] + 16 * k * Rows<DP>::kPitch)));
+        return u4{lo[0], lo[1], hi[0], hi[1]};
+    }
+};
 
 // 16 sums of a lane to two second operands
 template <typename E>
@@ -150,6 +188,14 @@ __device__ __forceinline__ void own_rows(const char* p, int D, u4* r)
     }
 }
 
+// Waits for what a loop reads of its own before the loop: where that is left to the first use in it, every turn waits there for all loads under way.
+template <int N>
+__device__ __forceinline__ void have(u4 (&r)[N])
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) asm volatile("" : "+v"(r[k]));
+}
+
 // a lane's own row of results, columns 32 block + result_row(i); zeros of a frame that is not there
 template <typename E, int DP>
 __device__ __forceinline__ void put_rows(char* p, int D, const f16x* acc, float factor, bool there)
@@ -168,7 +214,18 @@ __device__ __forceinline__ void put_rows(char* p, int D, const f16x* acc, float 
         }
 }
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, kWave); }
+// maximum and sum over both halves
+__device__ __forceinline__ float max_of_halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float sum_of_halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
 // frames of an item: lengths as clamped
 __device__ __forceinline__ int frames_of_item(const int* len, int T, int b) { return len ? clamped(len[b], T) : T; }
@@ -212,6 +269,38 @@ __device__ void plain_row(const char* q, int D, float c2, int from, int to, Seen
     *l = sum;
 }
 
+// What a lane's frame sees: [lo, hi) and first frames.  Frames are told apart by one unsigned comparison; first ones only in tiles that have any.
+struct Sight {
+    int lo, hi, sinks;
+    // scores of 32 frames from s0 on; what is not seen becomes `other`
+    __device__ __forceinline__ void apply(f16x& s, int s0, float other) const
+    {
+        const unsigned span = hi > lo ? (unsigned)(hi - lo) : 0u;
+        const int from = s0 + result_row(0) - lo;
+        if (s0 < sinks) {
+            const int end = hi < sinks ? hi : sinks;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int c = 8 * (i >> 2) + (i & 3);
+                s[i] = (unsigned)(from + c) < span || c < end - (s0 + result_row(0)) ? s[i] : other;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = (unsigned)(from + 8 * (i >> 2) + (i & 3)) < span ? s[i] : other;
+        }
+    }
+};
+
+// frame t of an item of len frames, in a band
+__device__ __forceinline__ Sight sight_of(int t, int len, const Band& band)
+{
+    Sight s;
+    s.lo = t - band.left;
+    s.hi = t >= len ? 0 : t + band.right + 1 < len ? t + band.right + 1 : len;
+    s.sinks = band.sinks;
+    return s;
+}
+
 // the running maximum and sum of a lane's frame, its results so far
 template <int DP> struct Softmax {
     f16x acc[DP / 32];
@@ -232,7 +321,7 @@ template <int DP> struct Softmax {
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
-        top = fmaxf(top, other_half(top));
+        top = max_of_halves(top);
         // The maximum is only a reference: as long as no score passes it by a factor of 2^8 the sums keep it, which saves their scaling.
         if (__any((top - m) * c2 > 8.f || (m == LAST_NEG_INF && top > m))) {
             const float higher = fmaxf(m, top), old = m == LAST_NEG_INF ? 0.f : __builtin_amdgcn_exp2f((m - higher) * c2);
@@ -262,7 +351,7 @@ template <int DP> struct Softmax {
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) t += acc[d][i] * 0.f;
-        t += other_half(t);
+        t = sum_of_halves(t);
         return !(t == 0.f);
     }
 };
@@ -273,11 +362,22 @@ struct Place {
     size_t row0;                     // of the item
 };
 
-__device__ __forceinline__ Place place_of(const AttentionArgs& a, int heads)
+// Workgroups i, i + 8, ... run on one XCD: those of a head do, eight heads (or heads that share keys) at a time, so that its keys and values are
+// in one L2; what is left of fewer than eight goes over all.  Those that have most to do where there is no window come first: the last queries, the first keys.
+__device__ __forceinline__ Place place_of(const AttentionArgs& a, unsigned id, int heads, bool keys = false)
 {
     Place p;
-    const unsigned id = a.first + blockIdx.x, hb = id / a.tiles;
-    p.tile = (int)(id % a.tiles);
+    const unsigned units = (unsigned)(a.B * heads) / a.together, per = a.tiles * a.together;
+    unsigned unit, rest;
+    if (id < units / 8 * 8 * per) {
+        unit = id / (8 * per) * 8 + id % 8;
+        rest = id % (8 * per) / 8;
+    } else {
+        unit = id / per;
+        rest = id % per;
+    }
+    const unsigned hb = unit * a.together + rest / a.tiles;
+    p.tile = (int)(keys ? rest % a.tiles : a.tiles - 1 - rest % a.tiles);
     p.head = (int)(hb % (unsigned)heads);
     p.item = (int)(hb / (unsigned)heads);
     p.kv = p.head / (heads / a.kv_heads);
@@ -286,95 +386,114 @@ __device__ __forceinline__ Place place_of(const AttentionArgs& a, int heads)
     return p;
 }
 
-template <typename E, int DP>
-__global__ __launch_bounds__(256) void attention_kernel(AttentionArgs a)
+// NQ: groups of 32 frames of a wavefront, which share what it reads from LDS.
+template <typename E, int DP, int NQ>
+__global__ __launch_bounds__(256, DP * NQ > 128 ? 1 : DP * NQ > 64 ? 2 : 3) void attention_kernel(AttentionArgs a)
 {
-    __shared__ __attribute__((aligned(16))) char lds[2 * Rows<DP>::kBytes];
-    char *const kt = lds, *const vt = lds + Rows<DP>::kBytes;
-    const Place at = place_of(a, a.heads);
+    constexpr int kGroup = 4 * 32 * NQ;
+    __shared__ __attribute__((aligned(16))) char lds[2][2 * Rows<DP>::kBytes];
+    const Place at = place_of(a, a.first + blockIdx.x, a.heads);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x % kWave;
-    const int g0 = at.tile * kOwn, t0 = g0 + wave * 32, t = t0 + (lane & 31);
+    const int g0 = at.tile * kGroup, t0 = g0 + wave * 32 * NQ, t = t0 + (lane & 31);
     const Band band = a.band;
     const float c2 = band.scale * kLog2e;
-    const bool there = t < at.len;
-    const char* const q = (const char*)a.q + (((at.row0 + t) * a.pq) + (size_t)at.head * a.D) * 2;
+    const char* const q = (const char*)a.q + (at.row0 * a.pq + (size_t)at.head * a.D) * 2;
     const char* const k = (const char*)a.k + (at.row0 * a.pk + (size_t)at.kv * a.D) * 2;
     const char* const v = (const char*)a.v + (at.row0 * a.pv + (size_t)at.kv * a.D) * 2;
-    u4 qf[DP / 16];
-    own_rows<DP>(there ? q : nullptr, a.D, qf);
+    u4 qf[NQ][DP / 16];
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) own_rows<DP>(t + 32 * g < at.len ? q + (size_t)(t + 32 * g) * a.pq * 2 : nullptr, a.D, qf[g]);
     // frames that the workgroup's see: first ones, and [lo, hi)
     const int lo = g0 - band.left > 0 ? g0 - band.left : 0;
-    const int hi = g0 >= at.len ? 0 : g0 + kOwn + band.right < at.len ? g0 + kOwn + band.right : at.len;
+    const int hi = g0 >= at.len ? 0 : g0 + kGroup + band.right < at.len ? g0 + kGroup + band.right : at.len;
     const int first_tiles = band.sinks > 0 && hi > 0 ? 1 : 0;
     const int first = lo / kTile > first_tiles ? lo / kTile : first_tiles, last = (hi + kTile - 1) / kTile;
     const int tiles = first_tiles + (last > first ? last - first : 0);
     const auto start = [&](int j) { return (j < first_tiles ? j : first + j - first_tiles) * kTile; };
-    const auto exists = [&](int s) { return s < hi && (s >= lo || s < band.sinks); };
-    const int seen_lo = t - band.left, seen_hi = there ? (t + band.right + 1 < at.len ? t + band.right + 1 : at.len) : 0;
-    Softmax<DP> soft;
-    soft.init();
-    Sent<DP> ks, vs;
-    if (tiles > 0) {
-        send<DP>(ks, k, a.pk, a.D, start(0), exists);
-        send<DP>(vs, v, a.pv, a.D, start(0), exists);
-    }
+    const auto exists = [&](int s) { return (s < hi) & ((s >= lo) | (s < band.sinks)); };
+    Softmax<DP> soft[NQ];
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) soft[g].init();
+    Tile<DP, 256> ks, vs;
+    Reads<DP> reads;
+    reads.init();
+    const auto get = [&](int s0) {
+        const bool all = s0 >= lo && s0 + kTile <= hi;
+        ks.send(k, a.pk, a.D, s0, all, hi - 1, exists);
+        vs.send(v, a.pv, a.D, s0, all, hi - 1, exists);
+    };
+    if (tiles > 0) get(start(0));
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) have(qf[g]);
     for (int j = 0; j < tiles; ++j) {
         const int s0 = start(j);
-        __syncthreads();
-        lay<DP>(ks, kt);
-        lay<DP>(vs, vt);
-        __syncthreads();
-        if (j + 1 < tiles) {
-            send<DP>(ks, k, a.pk, a.D, start(j + 1), exists);
-            send<DP>(vs, v, a.pv, a.D, start(j + 1), exists);
-        }
-        if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + kTile <= t0 - band.left && s0 >= band.sinks)) continue;
-        f16x s[2];
+        char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
+        ks.lay(kt, a.D, s0, exists);
+        vs.lay(vt, a.D, s0, exists);
+        __syncthreads();                             // (the other buffer is written again after the next one)
+        if (j + 1 < tiles) get(start(j + 1));
+        if (s0 >= t0 + 32 * NQ + band.right || t0 >= at.len || (s0 + kTile <= t0 - band.left && s0 >= band.sinks)) continue;
+        const bool all = s0 >= t0 + 32 * NQ - 1 - band.left && s0 + kTile - 1 <= t0 + band.right && s0 + kTile <= at.len && t0 + 32 * NQ <= at.len;
+        f16x s[NQ][2];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-            s[n] = zeros16();
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) s[n] = Mma<E>::go(along_rows<DP>(kt, n, i), qf[i], s[n]);
+            for (int g = 0; g < NQ; ++g) s[g][n] = zeros16();
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                const u4 f = reads.along_rows(kt, n, i);
+#pragma unroll
+                for (int g = 0; g < NQ; ++g) s[g][n] = Mma<E>::go(f, qf[g][i], s[g][n]);
+            }
         }
-        if (!(s0 >= t0 + 31 - band.left && s0 + kTile - 1 <= t0 + band.right && s0 + kTile <= at.len && t0 + 32 <= at.len)) {
+        if (!all) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int g = 0; g < NQ; ++g) {
+                const Sight sight = sight_of(t + 32 * g, at.len, band);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int f = s0 + 32 * n + result_row(i);
-                    s[n][i] = f < seen_hi && (f >= seen_lo || f < band.sinks) ? s[n][i] : LAST_NEG_INF;
-                }
+                for (int n = 0; n < 2; ++n) sight.apply(s[g][n], s0 + 32 * n, LAST_NEG_INF);
+            }
         }
-        soft.template take<2>(s, c2);
+#pragma unroll
+        for (int g = 0; g < NQ; ++g) soft[g].template take<2>(s[g], c2);
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-            u4 p[2];
-            to_operands<E>(s[n], p);
+            u4 p[NQ][2];
+#pragma unroll
+            for (int g = 0; g < NQ; ++g) to_operands<E>(s[g][n], p[g]);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) soft.acc[d] = Mma<E>::go(along_columns<DP>(vt, d, 2 * n + i), p[i], soft.acc[d]);
+                for (int d = 0; d < DP / 32; ++d) {
+                    const u4 f = reads.along_columns(vt, d, 2 * n + i);
+#pragma unroll
+                    for (int g = 0; g < NQ; ++g) soft[g].acc[d] = Mma<E>::go(f, p[g][i], soft[g].acc[d]);
+                }
         }
     }
-    const float l = soft.l + other_half(soft.l);
-    const bool odd = there && soft.not_finite();
-    if (t < a.T && !odd) {
-        char* const y = (char*)a.y + (((at.row0 + t) * a.py) + (size_t)at.head * a.D) * 2;
-        put_rows<E, DP>(y, a.D, soft.acc, 1.f / l, there);
-        if (a.lse && lane < 32) a.lse[(at.row0 + t) * a.heads + at.head] = there ? (soft.m * c2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : 0.f;
-    }
-    for (unsigned long long rows = __ballot(odd) & 0xffffffffull; rows; rows &= rows - 1) {
-        const int tr = t0 + __ffsll(rows) - 1;
-        const int end = tr + band.right + 1 < at.len ? tr + band.right + 1 : at.len;
-        const char* const qr = (const char*)a.q + (((at.row0 + tr) * a.pq) + (size_t)at.head * a.D) * 2;
-        float m, sum, o[2];
-        plain_row<E>(qr, a.D, c2, 0, end, [&](int s) { return s >= tr - band.left || s < band.sinks; },
-                     [&](int s) { return k + (size_t)s * a.pk * 2; }, [&](int s) { return v + (size_t)s * a.pv * 2; }, &m, &sum, o);
-        char* const y = (char*)a.y + (((at.row0 + tr) * a.py) + (size_t)at.head * a.D) * 2;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (lane + 64 * i < a.D) Elt<E>::put(y, lane + 64 * i, o[i] / sum);
-        if (a.lse && lane == 0) a.lse[(at.row0 + tr) * a.heads + at.head] = (m * c2 + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    for (int g = 0; g < NQ; ++g) {
+        const int tg = t + 32 * g;
+        const bool there = tg < at.len;
+        const float l = sum_of_halves(soft[g].l);
+        const bool odd = there && soft[g].not_finite();
+        const size_t row = at.row0 + tg;
+        if (tg < a.T && !odd) {
+            put_rows<E, DP>((char*)a.y + (row * a.py + (size_t)at.head * a.D) * 2, a.D, soft[g].acc, 1.f / l, there);
+            if (a.lse && lane < 32) a.lse[row * a.heads + at.head] = there ? (soft[g].m * c2 + __builtin_amdgcn_logf(l)) * kLn2 : 0.f;
+        }
+        for (unsigned long long rows = __ballot(odd) & 0xffffffffull; rows; rows &= rows - 1) {
+            const int tr = t0 + 32 * g + __ffsll(rows) - 1;
+            const int end = tr + band.right + 1 < at.len ? tr + band.right + 1 : at.len;
+            float m, sum, o[2];
+            plain_row<E>(q + (size_t)tr * a.pq * 2, a.D, c2, 0, end, [&](int s) { return s >= tr - band.left || s < band.sinks; },
+                         [&](int s) { return k + (size_t)s * a.pk * 2; }, [&](int s) { return v + (size_t)s * a.pv * 2; }, &m, &sum, o);
+            char* const y = (char*)a.y + (((at.row0 + tr) * a.py) + (size_t)at.head * a.D) * 2;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (lane + 64 * i < a.D) Elt<E>::put(y, lane + 64 * i, o[i] / sum);
+            if (a.lse && lane == 0) a.lse[(at.row0 + tr) * a.heads + at.head] = (m * c2 + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
     }
 }
 
@@ -401,11 +520,10 @@ __global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, long long f
 
 // The gradient of queries: a wavefront's own frames are queries, the tiles keys and values.
 template <typename E, int DP>
-__global__ __launch_bounds__(256) void grad_query_kernel(AttentionArgs a)
+__global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
 {
-    __shared__ __attribute__((aligned(16))) char lds[2 * Rows<DP>::kBytes];
-    char *const kt = lds, *const vt = lds + Rows<DP>::kBytes;
-    const Place at = place_of(a, a.heads);
+    __shared__ __attribute__((aligned(16))) char lds[2][2 * Rows<DP>::kBytes];
+    const Place at = place_of(a, a.first + blockIdx.x, a.heads);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x % kWave;
     const int g0 = at.tile * kOwn, t0 = g0 + wave * 32, t = t0 + (lane & 31);
     const Band band = a.band;
@@ -417,33 +535,37 @@ __global__ __launch_bounds__(256) void grad_query_kernel(AttentionArgs a)
     u4 qf[DP / 16], df[DP / 16];
     own_rows<DP>(there ? (const char*)a.q + (row * a.pq + (size_t)at.head * a.D) * 2 : nullptr, a.D, qf);
     own_rows<DP>(there ? (const char*)a.dy + (row * a.pdy + (size_t)at.head * a.D) * 2 : nullptr, a.D, df);
-    const float l2 = there ? a.lse[row * a.heads + at.head] * kLog2e : 0.f, delta = there ? a.delta[row * a.heads + at.head] : 0.f;
+    float l2 = there ? a.lse[row * a.heads + at.head] * kLog2e : 0.f, delta = there ? a.delta[row * a.heads + at.head] : 0.f;
     const int lo = g0 - band.left > 0 ? g0 - band.left : 0;
     const int hi = g0 >= at.len ? 0 : g0 + kOwn + band.right < at.len ? g0 + kOwn + band.right : at.len;
     const int first_tiles = band.sinks > 0 && hi > 0 ? 1 : 0;
     const int first = lo / kTile > first_tiles ? lo / kTile : first_tiles, last = (hi + kTile - 1) / kTile;
     const int tiles = first_tiles + (last > first ? last - first : 0);
     const auto start = [&](int j) { return (j < first_tiles ? j : first + j - first_tiles) * kTile; };
-    const auto exists = [&](int s) { return s < hi && (s >= lo || s < band.sinks); };
-    const int seen_lo = t - band.left, seen_hi = there ? (t + band.right + 1 < at.len ? t + band.right + 1 : at.len) : 0;
+    const auto exists = [&](int s) { return (s < hi) & ((s >= lo) | (s < band.sinks)); };
+    const Sight sight = sight_of(t, at.len, band);
     f16x acc[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) acc[d] = zeros16();
-    Sent<DP> ks, vs;
-    if (tiles > 0) {
-        send<DP>(ks, k, a.pk, a.D, start(0), exists);
-        send<DP>(vs, v, a.pv, a.D, start(0), exists);
-    }
+    Tile<DP, 256> ks, vs;
+    Reads<DP> reads;
+    reads.init();
+    const auto get = [&](int s0) {
+        const bool all = s0 >= lo && s0 + kTile <= hi;
+        ks.send(k, a.pk, a.D, s0, all, hi - 1, exists);
+        vs.send(v, a.pv, a.D, s0, all, hi - 1, exists);
+    };
+    if (tiles > 0) get(start(0));
+    have(qf);
+    have(df);
+    asm volatile("" : "+v"(l2), "+v"(delta));
     for (int j = 0; j < tiles; ++j) {
         const int s0 = start(j);
+        char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
+        ks.lay(kt, a.D, s0, exists);
+        vs.lay(vt, a.D, s0, exists);
         __syncthreads();
-        lay<DP>(ks, kt);
-        lay<DP>(vs, vt);
-        __syncthreads();
-        if (j + 1 < tiles) {
-            send<DP>(ks, k, a.pk, a.D, start(j + 1), exists);
-            send<DP>(vs, v, a.pv, a.D, start(j + 1), exists);
-        }
+        if (j + 1 < tiles) get(start(j + 1));
         if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + kTile <= t0 - band.left && s0 >= band.sinks)) continue;
         const bool all = s0 >= t0 + 31 - band.left && s0 + kTile - 1 <= t0 + band.right && s0 + kTile <= at.len && t0 + 32 <= at.len;
 #pragma unroll
@@ -451,158 +573,295 @@ __global__ __launch_bounds__(256) void grad_query_kernel(AttentionArgs a)
             f16x s = zeros16(), p = zeros16();
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) {
-                s = Mma<E>::go(along_rows<DP>(kt, n, i), qf[i], s);
-                p = Mma<E>::go(along_rows<DP>(vt, n, i), df[i], p);
+                s = Mma<E>::go(reads.along_rows(kt, n, i), qf[i], s);
+                p = Mma<E>::go(reads.along_rows(vt, n, i), df[i], p);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c2, -l2)) * (p[i] - delta);
-                const int f = s0 + 32 * n + result_row(i);
-                s[i] = all || (f < seen_hi && (f >= seen_lo || f < band.sinks)) ? e : 0.f;
+                s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c2, -l2)) * (p[i] - delta);
             }
+            if (!all) sight.apply(s, s0 + 32 * n, 0.f);
             u4 d[2];
             to_operands<E>(s, d);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int x = 0; x < DP / 32; ++x) acc[x] = Mma<E>::go(along_columns<DP>(kt, x, 2 * n + i), d[i], acc[x]);
+                for (int x = 0; x < DP / 32; ++x) acc[x] = Mma<E>::go(reads.along_columns(kt, x, 2 * n + i), d[i], acc[x]);
         }
     }
     if (t < a.T) put_rows<E, DP>((char*)a.dq + (row * a.pdq + (size_t)at.head * a.D) * 2, a.D, acc, band.scale, there);
 }
 
-// The gradients of keys and values: a wavefront's own frames are keys, the tiles queries and their dy, of all heads that share
-// the keys.  SINKS: the part that first frames s < sinks have in frames t > s + left, a share of these a workgroup; its sums go to
-// `part`, [item][kv head][share][2][64][DP], and are added by the workgroup that has these frames for its own.
-template <typename E, int DP, bool SINKS>
-__global__ __launch_bounds__(256) void grad_key_kernel(AttentionArgs a)
+// What a tile of 64 queries and their dy adds to the gradients of a wavefront's 32 keys (DK) and values (DV); of blocks FROM .. TO - 1 of its 32 queries.
+template <typename E, int DP, bool DK, bool DV>
+__device__ __forceinline__ void key_tile(const char* qt, const char* yt, const float* st, const Reads<DP>& reads, const u4 (&kf)[DP / 16],
+                                         const u4 (&vf)[DP / 16], float c2, bool all, const Sight& sight, int t0, int from, int to, f16x* dk, f16x* dv)
 {
-    __shared__ __attribute__((aligned(16))) char lds[2 * Rows<DP>::kBytes];
-    __shared__ float stats[2][kTile];
-    char *const qt = lds, *const yt = lds + Rows<DP>::kBytes;
-    const Place at = place_of(a, a.kv_heads);
+    const int h = (int)threadIdx.x % kWave >> 5;
+    // (both gradients' sums and operands leave no registers for two blocks at a time)
+    constexpr int kAtOnce = DK && DV ? 1 : 2;
+#pragma unroll kAtOnce
+    for (int n = from; n < to; ++n) {
+        f16x p = zeros16(), e = zeros16();
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            p = Mma<E>::go(reads.along_rows(qt, n, i), kf[i], p);
+            if constexpr (DK) e = Mma<E>::go(reads.along_rows(yt, n, i), vf[i], e);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const f4 l2 = *(const f4*)&st[32 * n + 2 * i + 4 * h];
+            f4 delta{};
+            if constexpr (DK) delta = *(const f4*)&st[kTile + 32 * n + 2 * i + 4 * h];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                p[i + x] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i + x], c2, -l2[x]));
+                if constexpr (DK) e[i + x] = p[i + x] * (e[i + x] - delta[x]);
+            }
+        }
+        if (!all) {
+            if constexpr (DV) sight.apply(p, t0 + 32 * n, 0.f);
+            if constexpr (DK) sight.apply(e, t0 + 32 * n, 0.f);
+        }
+        u4 f[2];
+        if constexpr (DV) {
+            to_operands<E>(p, f);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) dv[d] = Mma<E>::go(reads.along_columns(yt, d, 2 * n + i), f[i], dv[d]);
+        }
+        if constexpr (DK) {
+            to_operands<E>(e, f);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) dk[d] = Mma<E>::go(reads.along_columns(qt, d, 2 * n + i), f[i], dk[d]);
+        }
+    }
+}
+
+// The gradients of keys (DK) and values (DV): a wavefront's own frames are keys, the tiles queries and their dy, of the heads that share the keys, or
+// of a part of them, whose sums grad_join_kernel adds.
+template <typename E, int DP, bool DK, bool DV>
+__device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at, char (*lds)[2 * Rows<DP>::kBytes], float (*stats)[2][kTile])
+{
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x % kWave;
     const Band band = a.band;
-    const int g0 = SINKS ? 0 : at.tile * kOwn, s0 = g0 + wave * 32, s = s0 + (lane & 31);
+    const int g0 = at.tile * kOwn, s0 = g0 + wave * 32, s = s0 + (lane & 31);
     const float c2 = band.scale * kLog2e;
-    const bool there = s < at.len && (!SINKS || s < band.sinks);
+    const bool there = s < at.len;
     const size_t row = at.row0 + s;
-    const int group = a.heads / a.kv_heads;
+    const int group = a.heads / a.kv_heads, part = at.head % a.parts;
+    const int from = at.kv * group + group * part / a.parts, to = at.kv * group + group * (part + 1) / a.parts;
     u4 kf[DP / 16], vf[DP / 16];
     own_rows<DP>(there ? (const char*)a.k + (row * a.pk + (size_t)at.kv * a.D) * 2 : nullptr, a.D, kf);
-    own_rows<DP>(there ? (const char*)a.v + (row * a.pv + (size_t)at.kv * a.D) * 2 : nullptr, a.D, vf);
+    if constexpr (DK) own_rows<DP>(there ? (const char*)a.v + (row * a.pv + (size_t)at.kv * a.D) * 2 : nullptr, a.D, vf);
     // frames that see the workgroup's
-    int lo = g0 - band.right > 0 ? g0 - band.right : 0;
-    int hi = g0 >= at.len ? 0 : (long long)g0 + kOwn + band.left < at.len ? g0 + kOwn + band.left : at.len;
-    if (SINKS) {
-        lo = band.left + 1 < at.len ? band.left + 1 : at.len;
-        hi = at.len;
-    }
-    int first = lo / kTile, last = (hi + kTile - 1) / kTile;
-    if (SINKS) {
-        const int n = last > first ? last - first : 0;
-        last = first + (int)((long long)n * (at.tile + 1) / a.shares);
-        first = first + (int)((long long)n * at.tile / a.shares);
-    }
-    const int per = last > first ? last - first : 0, tiles = per * group;
-    const auto exists = [&](int t) { return t >= lo && t < hi; };
-    // t sees s: s - right <= t, t <= s + left (or, of first frames, beyond)
-    const int seen_lo = SINKS ? s + band.left + 1 : s - band.right;
-    const int seen_hi = !there ? 0 : SINKS ? at.len : (long long)s + band.left + 1 < at.len ? s + band.left + 1 : at.len;
-    const bool idle = SINKS ? s0 >= band.sinks : s0 >= at.len;
+    const int lo = g0 - band.right > 0 ? g0 - band.right : 0;
+    const int hi = g0 >= at.len ? 0 : (long long)g0 + kOwn + band.left < at.len ? g0 + kOwn + band.left : at.len;
+    const int first = lo / kTile, last = (hi + kTile - 1) / kTile;
+    const int per = last > first ? last - first : 0, tiles = per * (to - from);
+    const auto exists = [&](int t) { return (t >= lo) & (t < hi); };
+    // t sees s: s - right <= t <= s + left
+    const Sight sight{s - band.right, !there ? 0 : (long long)s + band.left + 1 < at.len ? s + band.left + 1 : at.len, 0};
     f16x dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zeros16();
-    Sent<DP> qs, ys;
+    Tile<DP, 256> qs, ys;
+    Reads<DP> reads;
+    reads.init();
     float stat = 0.f;
+    // Turn j is tile first + j % per of head from + j / per.  Formed anew each time with both gradients, counted with one: what leaves the compiler
+    // registers (16 x 1024, 8 heads of 64 columns in a band 80.5 us, counted 85; 2 x 4096, 16 heads of 128 626 us, counted 594).
+    constexpr bool kCount = !(DK && DV);
+    int head_next = from, t_next = first, t_now = first;
     const auto get = [&](int j) {
-        const int head = at.kv * group + j / per, t0 = (first + j % per) * kTile;
-        send<DP>(qs, (const char*)a.q + (at.row0 * a.pq + (size_t)head * a.D) * 2, a.pq, a.D, t0, exists);
-        send<DP>(ys, (const char*)a.dy + (at.row0 * a.pdy + (size_t)head * a.D) * 2, a.pdy, a.D, t0, exists);
+        const int head = kCount ? head_next : from + j / per, t0 = (kCount ? t_next : first + j % per) * kTile;
+        const bool all = t0 >= lo && t0 + kTile <= hi;
+        qs.send((const char*)a.q + (at.row0 * a.pq + (size_t)head * a.D) * 2, a.pq, a.D, t0, all, hi - 1, exists);
+        ys.send((const char*)a.dy + (at.row0 * a.pdy + (size_t)head * a.D) * 2, a.pdy, a.D, t0, all, hi - 1, exists);
         const int t = t0 + (int)threadIdx.x % kTile;
         stat = 0.f;
         if (threadIdx.x < 2 * kTile && exists(t)) {
             const size_t i = (at.row0 + t) * a.heads + head;
-            stat = threadIdx.x < kTile ? a.lse[i] * kLog2e : a.delta[i];
+            stat = *(threadIdx.x < kTile ? a.lse + i : a.delta + i);
+        }
+        if (kCount && ++t_next == last) {
+            t_next = first;
+            ++head_next;
         }
     };
     if (tiles > 0) get(0);
+    have(kf);
+    if constexpr (DK) have(vf);
     for (int j = 0; j < tiles; ++j) {
-        const int t0 = (first + j % per) * kTile;
-        __syncthreads();
-        lay<DP>(qs, qt);
-        lay<DP>(ys, yt);
-        if (threadIdx.x < 2 * kTile) stats[threadIdx.x / kTile][threadIdx.x % kTile] = stat;
+        const int t0 = (kCount ? t_now : first + j % per) * kTile;
+        if (kCount) t_now = t_now + 1 == last ? first : t_now + 1;
+        char *const qt = lds[j & 1], *const yt = qt + Rows<DP>::kBytes;
+        float* const st = stats[j & 1][0];
+        qs.lay(qt, a.D, t0, exists);
+        ys.lay(yt, a.D, t0, exists);
+        if (threadIdx.x < 2 * kTile) st[threadIdx.x] = threadIdx.x < kTile ? stat * kLog2e : stat;
         __syncthreads();
         if (j + 1 < tiles) get(j + 1);
-        if (idle || t0 + kTile <= s0 - band.right || (!SINKS && t0 > (long long)s0 + 31 + band.left)) continue;
-        const bool all = !SINKS && t0 >= s0 + 31 - band.right && t0 + kTile - 1 <= (long long)s0 + band.left && t0 + kTile <= at.len && s0 + 32 <= at.len;
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            f16x p = zeros16(), e = zeros16();
-#pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
-                p = Mma<E>::go(along_rows<DP>(qt, n, i), kf[i], p);
-                e = Mma<E>::go(along_rows<DP>(yt, n, i), vf[i], e);
-            }
-            const int h = lane >> 5;
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const f4 l2 = *(const f4*)&stats[0][32 * n + 2 * i + 4 * h], delta = *(const f4*)&stats[1][32 * n + 2 * i + 4 * h];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int f = t0 + 32 * n + result_row(i + x);
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i + x], c2, -l2[x]));
-                    const bool sees = all || (f >= seen_lo && f < seen_hi);
-                    p[i + x] = sees ? w : 0.f;
-                    e[i + x] = sees ? w * (e[i + x] - delta[x]) : 0.f;
-                }
-            }
-            u4 pf[2], ef[2];
-            to_operands<E>(p, pf);
-            to_operands<E>(e, ef);
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) {
-                    dv[d] = Mma<E>::go(along_columns<DP>(yt, d, 2 * n + i), pf[i], dv[d]);
-                    dk[d] = Mma<E>::go(along_columns<DP>(qt, d, 2 * n + i), ef[i], dk[d]);
-                }
-        }
+        if (s0 >= at.len || t0 + kTile <= s0 - band.right || t0 > (long long)s0 + 31 + band.left) continue;
+        const bool all = t0 >= s0 + 31 - band.right && t0 + kTile - 1 <= (long long)s0 + band.left && t0 + kTile <= at.len && s0 + 32 <= at.len;
+        key_tile<E, DP, DK, DV>(qt, yt, st, reads, kf, vf, c2, all, sight, t0, 0, 2, dk, dv);
     }
-    const size_t all_parts = ((size_t)at.item * a.kv_heads + at.kv) * a.shares;
-    if constexpr (SINKS) {
-        if (s >= 64) return;
-        float* const out = a.part + ((all_parts + at.tile) * 2 * 64 + s) * DP;
+    if (s >= a.T) return;
+    if (a.parts > 1) {
+        if (!there) return;
+        const size_t at_k = (((size_t)part * a.B * a.T + row) * a.kv_heads + at.kv) * DP, to_v = (size_t)a.parts * a.B * a.T * a.kv_heads * DP;
+        const auto keep = [&](float* out, const f16x* sums) {
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) *(f4*)(out + 32 * d + result_row(i)) = f4{sums[d][i], sums[d][i + 1], sums[d][i + 2], sums[d][i + 3]};
+        };
+        if constexpr (DK) keep(a.kept + at_k, dk);
+        if constexpr (DV) keep(a.kept + to_v + at_k, dv);
+        return;
+    }
+    // what frames beyond the window add to first ones
+    const auto add_first = [&](f16x* sums, int which) {
+        if (!a.part || !(there && s < band.sinks)) return;
+        const float* const in = a.sums + ((((size_t)at.item * a.kv_heads + at.kv) * 2 + which) * kMostSinks + s) * DP;
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                *(f4*)(out + 32 * d + result_row(i)) = f4{dk[d][i], dk[d][i + 1], dk[d][i + 2], dk[d][i + 3]};
-                *(f4*)(out + 64 * DP + 32 * d + result_row(i)) = f4{dv[d][i], dv[d][i + 1], dv[d][i + 2], dv[d][i + 3]};
+                const f4 x = *(const f4*)(in + 32 * d + result_row(i));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sums[d][i + c] += x[c];
             }
-    } else {
-        if (a.part && s < band.sinks && there) {
-            for (int share = 0; share < a.shares; ++share) {
-                const float* const in = a.part + ((all_parts + share) * 2 * 64 + s) * DP;
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const f4 x = *(const f4*)(in + 32 * d + result_row(i)), z = *(const f4*)(in + 64 * DP + 32 * d + result_row(i));
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            dk[d][i + c] += x[c];
-                            dv[d][i + c] += z[c];
-                        }
-                    }
-            }
-        }
-        if (s < a.T) {
-            put_rows<E, DP>((char*)a.dk + (row * a.pdk + (size_t)at.kv * a.D) * 2, a.D, dk, band.scale, there);
-            put_rows<E, DP>((char*)a.dv + (row * a.pdv + (size_t)at.kv * a.D) * 2, a.D, dv, 1.f, there);
-        }
+    };
+    if constexpr (DK) {
+        add_first(dk, 0);
+        put_rows<E, DP>((char*)a.dk + (row * a.pdk + (size_t)at.kv * a.D) * 2, a.D, dk, band.scale, there);
     }
+    if constexpr (DV) {
+        add_first(dv, 1);
+        put_rows<E, DP>((char*)a.dv + (row * a.pdv + (size_t)at.kv * a.D) * 2, a.D, dv, 1.f, there);
+    }
+}
+
+// APART: workgroups of a second half form the values' gradients, those of the first the keys', since both sums and operands of 128 columns do not leave
+// registers for two wavefronts on a SIMD; the scores are formed twice, which is a product of five.
+template <typename E, int DP, bool APART>
+__global__ __launch_bounds__(256, 2) void grad_key_kernel(AttentionArgs a)
+{
+    __shared__ __attribute__((aligned(16))) char lds[2][2 * Rows<DP>::kBytes];
+    __shared__ float stats[2][2][kTile];
+    const unsigned id = a.first + blockIdx.x;
+    if constexpr (APART) {
+        if (id >= a.half) grad_key<E, DP, false, true>(a, place_of(a, id - a.half, a.kv_heads * a.parts, true), lds, stats);
+        else grad_key<E, DP, true, false>(a, place_of(a, id, a.kv_heads * a.parts, true), lds, stats);
+    } else {
+        grad_key<E, DP, true, true>(a, place_of(a, id, a.kv_heads * a.parts, true), lds, stats);
+    }
+}
+
+// The part that first frames s < sinks have in frames t > s + left: a workgroup takes a chunk of these of one head, a wavefront 32 first frames and half
+// of each tile.  Sums go to `part`, [item][kv head][share][2][64][DP], a share for each head of the group, chunk and half.
+template <typename E, int DP>
+__global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void grad_first_kernel(AttentionArgs a)
+{
+    __shared__ __attribute__((aligned(16))) char lds[2][2 * Rows<DP>::kBytes];
+    __shared__ float stats[2][2][kTile];
+    const Place at = place_of(a, a.first + blockIdx.x, a.heads);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x % kWave;
+    const Band band = a.band;
+    const int s0 = wave % 2 * 32, s = s0 + (lane & 31), half = wave / 2, group = a.heads / a.kv_heads;
+    const float c2 = band.scale * kLog2e;
+    const bool there = s < at.len && s < band.sinks;
+    const size_t row = at.row0 + s;
+    u4 kf[DP / 16], vf[DP / 16];
+    own_rows<DP>(there ? (const char*)a.k + (row * a.pk + (size_t)at.kv * a.D) * 2 : nullptr, a.D, kf);
+    own_rows<DP>(there ? (const char*)a.v + (row * a.pv + (size_t)at.kv * a.D) * 2 : nullptr, a.D, vf);
+    const int lo = band.left + 1 < at.len ? band.left + 1 : at.len, hi = at.len;
+    const int all_first = lo / kTile, n = lo < hi ? (hi + kTile - 1) / kTile - all_first : 0;
+    const int first = all_first + (int)((long long)n * at.tile / (int)a.tiles), last = all_first + (int)((long long)n * (at.tile + 1) / (int)a.tiles);
+    const auto exists = [&](int t) { return (t >= lo) & (t < hi); };
+    const Sight sight{s + band.left + 1, there ? at.len : 0, 0};
+    f16x dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = zeros16();
+    Tile<DP, 256> qs, ys;
+    Reads<DP> reads;
+    reads.init();
+    float stat = 0.f;
+    const auto get = [&](int t0) {
+        const bool all = t0 >= lo && t0 + kTile <= hi;
+        qs.send((const char*)a.q + (at.row0 * a.pq + (size_t)at.head * a.D) * 2, a.pq, a.D, t0, all, hi - 1, exists);
+        ys.send((const char*)a.dy + (at.row0 * a.pdy + (size_t)at.head * a.D) * 2, a.pdy, a.D, t0, all, hi - 1, exists);
+        const int t = t0 + (int)threadIdx.x % kTile;
+        stat = 0.f;
+        if (threadIdx.x < 2 * kTile && exists(t)) {
+            const size_t i = (at.row0 + t) * a.heads + at.head;
+            stat = *(threadIdx.x < kTile ? a.lse + i : a.delta + i);
+        }
+    };
+    if (first < last) get(first * kTile);
+    have(kf);
+    have(vf);
+    for (int j = first; j < last; ++j) {
+        const int t0 = j * kTile;
+        char *const qt = lds[j & 1], *const yt = qt + Rows<DP>::kBytes;
+        float* const st = stats[j & 1][0];
+        qs.lay(qt, a.D, t0, exists);
+        ys.lay(yt, a.D, t0, exists);
+        if (threadIdx.x < 2 * kTile) st[threadIdx.x] = threadIdx.x < kTile ? stat * kLog2e : stat;
+        __syncthreads();
+        if (j + 1 < last) get(t0 + kTile);
+        if (s0 >= band.sinks) continue;
+        key_tile<E, DP, true, true>(qt, yt, st, reads, kf, vf, c2, false, sight, t0, half, half + 1, dk, dv);
+    }
+    if (s >= band.sinks) return;
+    const int share = ((at.head % group) * (int)a.tiles + at.tile) * 2 + half;
+    float* const out = a.part + ((((size_t)at.item * a.kv_heads + at.kv) * a.shares + share) * 2 * kMostSinks + s) * DP;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            *(f4*)(out + 32 * d + result_row(i)) = f4{dk[d][i], dk[d][i + 1], dk[d][i + 2], dk[d][i + 3]};
+            *(f4*)(out + kMostSinks * DP + 32 * d + result_row(i)) = f4{dv[d][i], dv[d][i + 1], dv[d][i + 2], dv[d][i + 3]};
+        }
+}
+
+// Gradients of keys and values from the parts' sums [2][part][row][kv head][DP], in order: four columns a thread.
+template <typename E>
+__global__ __launch_bounds__(256) void grad_join_kernel(AttentionArgs a, int DP, long long first)
+{
+    const int fours = DP / 4;
+    const long long i = (first + blockIdx.x) * 256 + threadIdx.x, units = (long long)a.B * a.T * a.kv_heads;
+    const long long u = i / fours;
+    const int c = (int)(i - u * fours) * 4;
+    if (u >= 2 * units || c >= a.D) return;
+    const int which = u >= units ? 1 : 0;
+    const long long unit = u - which * units, row = unit / a.kv_heads;
+    const int kv = (int)(unit - row * a.kv_heads), b = (int)(row / a.T), s = (int)(row - (long long)b * a.T);
+    f4 v{};
+    if (s < frames_of_item(a.len, a.T, b)) {
+        for (int part = 0; part < a.parts; ++part) v += *(const f4*)(a.kept + (((size_t)which * a.parts + part) * units + unit) * DP + c);
+        if (a.part && s < a.band.sinks) v += *(const f4*)(a.sums + ((((size_t)b * a.kv_heads + kv) * 2 + which) * kMostSinks + s) * DP + c);
+        if (which == 0) v *= a.band.scale;
+    }
+    const float x[4] = {v[0], v[1], v[2], v[3]};
+    store4<E>(which ? a.dv : a.dk, (size_t)row * (which ? a.pdv : a.pdk) + (size_t)kv * a.D + c, x);
+}
+
+// sums [item][kv head][2][64][DP] of the shares, in order; a workgroup a row
+__global__ __launch_bounds__(128) void first_join_kernel(const float* part, float* sums, int shares, int DP, int sinks, long long first)
+{
+    const long long i = first + blockIdx.x, unit = i / (2 * sinks);
+    const int r = (int)(i - unit * 2 * sinks), which = r / sinks, s = r - which * sinks, c = (int)threadIdx.x;
+    if (c >= DP) return;
+    const float* in = part + ((size_t)unit * shares * 2 * kMostSinks + (size_t)which * kMostSinks + s) * DP + c;
+    float t = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < shares; ++k) t += in[(size_t)k * 2 * kMostSinks * DP];
+    sums[(((size_t)unit * 2 + which) * kMostSinks + s) * DP + c] = t;
 }
 
 }  // namespace last

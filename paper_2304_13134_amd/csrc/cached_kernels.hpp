@@ -85,12 +85,14 @@ __global__ __launch_bounds__(256) void cached_kernel(CachedArgs a)
         }
         return p;
     };
-    const int seen_lo = used + t - band.left, seen_hi = there ? (used + t + band.right + 1 < total ? used + t + band.right + 1 : total) : 0;
+    const Sight sight{used + t - band.left, !there ? 0 : used + t + band.right + 1 < total ? used + t + band.right + 1 : total, sinks};
     u4 qf[DP / 16];
     own_rows<DP>(there ? (const char*)a.q + ((row0 + t) * a.pq + (size_t)head * a.D) * 2 : nullptr, a.D, qf);
     Softmax<DP> soft;
     soft.init();
     char* const vt = lds + wave * CachedRows<DP>::kBytes;
+    Reads<DP> reads;
+    reads.init();
     u4 kf[DP / 16], vf[DP / 16];
     const auto get = [&](int j) {
         const PageRow p = find(start(j) + (lane & 31));
@@ -114,13 +116,9 @@ __global__ __launch_bounds__(256) void cached_kernel(CachedArgs a)
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) s = Mma<E>::go(kf[i], qf[i], s);
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) *(u4*)(vt + (lane & 31) * Rows<DP>::kPitch + 32 * i + 16 * h) = vf[i];
+        for (int i = 0; i < DP / 16; ++i) *(u4*)(vt + reads.rows[i]) = vf[i];
         if (j + 4 < end) get(j + 4);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int f = s0 + result_row(i);
-            s[i] = f < seen_hi && (f >= seen_lo || f < sinks) ? s[i] : LAST_NEG_INF;
-        }
+        sight.apply(s, s0, LAST_NEG_INF);
         soft.template take<1>(&s, c2);
         u4 p[2];
         to_operands<E>(s, p);
@@ -128,11 +126,11 @@ __global__ __launch_bounds__(256) void cached_kernel(CachedArgs a)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) soft.acc[d] = Mma<E>::go(along_columns<DP>(vt, d, i), p[i], soft.acc[d]);
+            for (int d = 0; d < DP / 32; ++d) soft.acc[d] = Mma<E>::go(reads.along_columns(vt, d, i), p[i], soft.acc[d]);
         asm volatile("" ::: "memory");
     }
     // the four wavefronts' sums, relative to the largest maximum, in a fixed order
-    float l = soft.l + other_half(soft.l);
+    float l = sum_of_halves(soft.l);
     if (lane < 32) {
         all_m[wave][lane] = soft.m;
         all_l[wave][lane] = l;
