@@ -387,7 +387,7 @@ typedef struct {
     float scale;
 } last_band_t;
 
-/* Keys and values of streams in pages.  k, v: dev [pages][kv_heads][page][width], BF16 or F16.  Frames j*page .. of item b are on page
+/* Keys and values of streams in pages.  k, v: dev [pages][kv_heads][page][width], BF16 or F16, 16-byte aligned.  Frames j*page .. of item b are on page
  * table[b][j], 0 <= j < entries; page * entries at most 2^30.  used[b] frames (clamped to [0, 2^30]) are in the cache
  * before the new ones of a call, which are frames used[b] + t; the caller counts them afterwards.  Entries of pages on which no frame is
  * written or seen may hold anything.  A frame whose entry is missing (j >= entries) or names no page gives its item

@@ -57,7 +57,7 @@ last_status_t check_cache(const last_cache_t* c, const last_heads_t* h, int T)
     if (!c || !c->k || !c->v || !c->table || !c->used) return LAST_ERR_NULL;
     if (c->pages < 1 || c->page < 1 || c->page > kMostPage || c->entries < 1) return LAST_ERR_SHAPE;
     if ((long long)c->page * c->entries > kMostUsed || T > kMostFrames) return LAST_ERR_SHAPE;
-    if ((uintptr_t)c->k % size_of(c->type) != 0 || (uintptr_t)c->v % size_of(c->type) != 0) return LAST_ERR_SHAPE;
+    if ((uintptr_t)c->k % 16 != 0 || (uintptr_t)c->v % 16 != 0) return LAST_ERR_SHAPE;
     (void)h;
     return LAST_OK;
 }
@@ -152,15 +152,15 @@ unsigned heads_together(const AttentionArgs& a) { return a.B * a.kv_heads % 8 ==
 template <typename E>
 void launch_attention(AttentionArgs a, hipStream_t st)
 {
-    const long long own = (long long)((a.T + 255) / 256) * a.heads * a.B;
-    const bool two = false;
-    const int frames = two ? 256 : 128;
+    const long long groups = (long long)((a.T + kOwn - 1) / kOwn) * a.heads * a.B;
+    const bool halves = groups <= 512;
+    const int frames = halves ? kOwn / 2 : kOwn;
     a.tiles = (unsigned)((a.T + frames - 1) / frames);
     a.together = heads_together(a);
     in_launches((long long)a.tiles * a.heads * a.B, [&](long long first, dim3 grid) {
         a.first = (unsigned)first;
-        if (two) LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((attention_kernel<E, DP, 2>), grid, dim3(256), 0, st, a));
-        else LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((attention_kernel<E, DP, 1>), grid, dim3(256), 0, st, a));
+        if (halves) LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((attention_kernel<E, DP, true>), grid, dim3(256), 0, st, a));
+        else LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((attention_kernel<E, DP, false>), grid, dim3(256), 0, st, a));
     });
 }
 
@@ -249,7 +249,7 @@ void launch_attention_grad(AttentionArgs a, int chunks, hipStream_t st)
     });
 }
 
-// Blocks of 32 rows, and over how many workgroups a block's frames are split: so that there are some 512, each with at least
+// Blocks of 32 rows, and over how many workgroups a block's frames are split: so that there are some 1024, each with at least
 // 256 frames if the window or the table lets there be as many.
 struct CachedPlan {
     int row_blocks, splits;
@@ -264,7 +264,7 @@ CachedPlan plan_cached(Carver& cv, long long rows, const last_frames_t* f, const
     const long long groups = (long long)f->B * h->kv_heads * p.row_blocks;
     long long seen = (long long)c->page * c->entries;
     if (band->left >= 0) seen = std::min(seen, (long long)band->left + band->sinks + 33);
-    p.splits = (int)std::max(1ll, std::min({512 / std::max(1ll, groups), seen / 256, 128ll}));
+    p.splits = (int)std::max(1ll, std::min({1024ll / std::max(1ll, groups), seen / 256, (long long)kMostSplits}));
     p.part = p.part_ml = nullptr;
     if (p.splits > 1) {
         p.part = (float*)cv.take(sizeof(float) * (size_t)rows * h->heads * p.splits * h->width);
@@ -281,8 +281,8 @@ void launch_cached(CachedArgs a, hipStream_t st)
         LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((cached_kernel<E, DP>), grid, dim3(256), 0, st, a));
     });
     if (a.splits == 1) return;
-    in_launches(((long long)a.B * a.T * a.heads + 3) / 4, [&](long long first, dim3 grid) {
-        hipLaunchKernelGGL((cached_join_kernel<E>), grid, dim3(256), 0, st, a, first * 4);
+    in_launches((long long)a.B * a.T * a.heads, [&](long long first, dim3 grid) {
+        hipLaunchKernelGGL((cached_join_kernel<E>), grid, dim3(256), 0, st, a, first);
     });
 }
 

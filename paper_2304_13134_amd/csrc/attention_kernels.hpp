@@ -124,7 +124,7 @@ template <int DP, int THREADS> struct Tile {
         } else {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const unsigned keep = (c * 8 < D) & exists(s0 + r + i * kApart) ? ~0u : 0u;
+                const unsigned keep = ((c * 8 < D) & exists(s0 + r + i * kApart)) ? ~0u : 0u;
                 *(u4*)(lds + at + i * kApart * Rows<DP>::kPitch) = v[i] & u4{keep, keep, keep, keep};
             }
         }
@@ -386,23 +386,27 @@ __device__ __forceinline__ Place place_of(const AttentionArgs& a, unsigned id, i
     return p;
 }
 
-// NQ: groups of 32 frames of a wavefront, which share what it reads from LDS.
-template <typename E, int DP, int NQ>
-__global__ __launch_bounds__(256, DP * NQ > 128 ? 1 : DP * NQ > 64 ? 2 : 3) void attention_kernel(AttentionArgs a)
+// HALVES: a workgroup has 64 frames instead of 128, and two wavefronts for each 32 of them, one for either half of each tile, whose sums are joined at the end:
+// twice as many workgroups of half the length.
+template <typename E, int DP, bool HALVES>
+__global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(AttentionArgs a)
 {
-    constexpr int kGroup = 4 * 32 * NQ;
+    constexpr int kGroup = HALVES ? 64 : 128, kBlocks = HALVES ? 1 : 2;
     __shared__ __attribute__((aligned(16))) char lds[2][2 * Rows<DP>::kBytes];
+    __shared__ float stats[HALVES ? 2 : 1][2][32];
     const Place at = place_of(a, a.first + blockIdx.x, a.heads);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x % kWave;
-    const int g0 = at.tile * kGroup, t0 = g0 + wave * 32 * NQ, t = t0 + (lane & 31);
+    const int half = HALVES ? wave / 2 : 0;
+    const int g0 = at.tile * kGroup, t0 = g0 + (HALVES ? wave % 2 : wave) * 32, t = t0 + (lane & 31);
     const Band band = a.band;
     const float c2 = band.scale * kLog2e;
+    const bool there = t < at.len;
+    const size_t row = at.row0 + t;
     const char* const q = (const char*)a.q + (at.row0 * a.pq + (size_t)at.head * a.D) * 2;
     const char* const k = (const char*)a.k + (at.row0 * a.pk + (size_t)at.kv * a.D) * 2;
     const char* const v = (const char*)a.v + (at.row0 * a.pv + (size_t)at.kv * a.D) * 2;
-    u4 qf[NQ][DP / 16];
-#pragma unroll
-    for (int g = 0; g < NQ; ++g) own_rows<DP>(t + 32 * g < at.len ? q + (size_t)(t + 32 * g) * a.pq * 2 : nullptr, a.D, qf[g]);
+    u4 qf[DP / 16];
+    own_rows<DP>(there ? q + (size_t)t * a.pq * 2 : nullptr, a.D, qf);
     // frames that the workgroup's see: first ones, and [lo, hi)
     const int lo = g0 - band.left > 0 ? g0 - band.left : 0;
     const int hi = g0 >= at.len ? 0 : g0 + kGroup + band.right < at.len ? g0 + kGroup + band.right : at.len;
@@ -411,9 +415,9 @@ __global__ __launch_bounds__(256, DP * NQ > 128 ? 1 : DP * NQ > 64 ? 2 : 3) void
     const int tiles = first_tiles + (last > first ? last - first : 0);
     const auto start = [&](int j) { return (j < first_tiles ? j : first + j - first_tiles) * kTile; };
     const auto exists = [&](int s) { return (s < hi) & ((s >= lo) | (s < band.sinks)); };
-    Softmax<DP> soft[NQ];
-#pragma unroll
-    for (int g = 0; g < NQ; ++g) soft[g].init();
+    const Sight sight = sight_of(t, at.len, band);
+    Softmax<DP> soft;
+    soft.init();
     Tile<DP, 256> ks, vs;
     Reads<DP> reads;
     reads.init();
@@ -423,77 +427,82 @@ __global__ __launch_bounds__(256, DP * NQ > 128 ? 1 : DP * NQ > 64 ? 2 : 3) void
         vs.send(v, a.pv, a.D, s0, all, hi - 1, exists);
     };
     if (tiles > 0) get(start(0));
-#pragma unroll
-    for (int g = 0; g < NQ; ++g) have(qf[g]);
+    have(qf);
     for (int j = 0; j < tiles; ++j) {
-        const int s0 = start(j);
+        const int tile0 = start(j), s0 = tile0 + 32 * half;
         char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
-        ks.lay(kt, a.D, s0, exists);
-        vs.lay(vt, a.D, s0, exists);
+        ks.lay(kt, a.D, tile0, exists);
+        vs.lay(vt, a.D, tile0, exists);
         __syncthreads();                             // (the other buffer is written again after the next one)
         if (j + 1 < tiles) get(start(j + 1));
-        if (s0 >= t0 + 32 * NQ + band.right || t0 >= at.len || (s0 + kTile <= t0 - band.left && s0 >= band.sinks)) continue;
-        const bool all = s0 >= t0 + 32 * NQ - 1 - band.left && s0 + kTile - 1 <= t0 + band.right && s0 + kTile <= at.len && t0 + 32 * NQ <= at.len;
-        f16x s[NQ][2];
+        if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + 32 * kBlocks <= t0 - band.left && s0 >= band.sinks)) continue;
+        const bool all = s0 >= t0 + 31 - band.left && s0 + 32 * kBlocks - 1 <= t0 + band.right && s0 + 32 * kBlocks <= at.len && t0 + 32 <= at.len;
+        f16x s[kBlocks];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < kBlocks; ++n) {
+            s[n] = zeros16();
 #pragma unroll
-            for (int g = 0; g < NQ; ++g) s[g][n] = zeros16();
-#pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
-                const u4 f = reads.along_rows(kt, n, i);
-#pragma unroll
-                for (int g = 0; g < NQ; ++g) s[g][n] = Mma<E>::go(f, qf[g][i], s[g][n]);
-            }
+            for (int i = 0; i < DP / 16; ++i) s[n] = Mma<E>::go(reads.along_rows(kt, half + n, i), qf[i], s[n]);
         }
         if (!all) {
 #pragma unroll
-            for (int g = 0; g < NQ; ++g) {
-                const Sight sight = sight_of(t + 32 * g, at.len, band);
-#pragma unroll
-                for (int n = 0; n < 2; ++n) sight.apply(s[g][n], s0 + 32 * n, LAST_NEG_INF);
-            }
+            for (int n = 0; n < kBlocks; ++n) sight.apply(s[n], s0 + 32 * n, LAST_NEG_INF);
         }
+        soft.template take<kBlocks>(s, c2);
 #pragma unroll
-        for (int g = 0; g < NQ; ++g) soft[g].template take<2>(s[g], c2);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            u4 p[NQ][2];
-#pragma unroll
-            for (int g = 0; g < NQ; ++g) to_operands<E>(s[g][n], p[g]);
+        for (int n = 0; n < kBlocks; ++n) {
+            u4 p[2];
+            to_operands<E>(s[n], p);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) {
-                    const u4 f = reads.along_columns(vt, d, 2 * n + i);
-#pragma unroll
-                    for (int g = 0; g < NQ; ++g) soft[g].acc[d] = Mma<E>::go(f, p[g][i], soft[g].acc[d]);
-                }
+                for (int d = 0; d < DP / 32; ++d) soft.acc[d] = Mma<E>::go(reads.along_columns(vt, d, 2 * (half + n) + i), p[i], soft.acc[d]);
         }
     }
+    float l = sum_of_halves(soft.l);
+    if constexpr (HALVES) {
+        // the second half's sums, relative to the larger maximum
+        float* const sums = (float*)lds[0] + wave % 2 * (DP / 32 * 16 * kWave);
+        __syncthreads();
+        if (half == 1) {
 #pragma unroll
-    for (int g = 0; g < NQ; ++g) {
-        const int tg = t + 32 * g;
-        const bool there = tg < at.len;
-        const float l = sum_of_halves(soft[g].l);
-        const bool odd = there && soft[g].not_finite();
-        const size_t row = at.row0 + tg;
-        if (tg < a.T && !odd) {
-            put_rows<E, DP>((char*)a.y + (row * a.py + (size_t)at.head * a.D) * 2, a.D, soft[g].acc, 1.f / l, there);
-            if (a.lse && lane < 32) a.lse[row * a.heads + at.head] = there ? (soft[g].m * c2 + __builtin_amdgcn_logf(l)) * kLn2 : 0.f;
-        }
-        for (unsigned long long rows = __ballot(odd) & 0xffffffffull; rows; rows &= rows - 1) {
-            const int tr = t0 + 32 * g + __ffsll(rows) - 1;
-            const int end = tr + band.right + 1 < at.len ? tr + band.right + 1 : at.len;
-            float m, sum, o[2];
-            plain_row<E>(q + (size_t)tr * a.pq * 2, a.D, c2, 0, end, [&](int s) { return s >= tr - band.left || s < band.sinks; },
-                         [&](int s) { return k + (size_t)s * a.pk * 2; }, [&](int s) { return v + (size_t)s * a.pv * 2; }, &m, &sum, o);
-            char* const y = (char*)a.y + (((at.row0 + tr) * a.py) + (size_t)at.head * a.D) * 2;
+            for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (lane + 64 * i < a.D) Elt<E>::put(y, lane + 64 * i, o[i] / sum);
-            if (a.lse && lane == 0) a.lse[(at.row0 + tr) * a.heads + at.head] = (m * c2 + __builtin_amdgcn_logf(sum)) * kLn2;
+                for (int i = 0; i < 16; ++i) sums[(d * 16 + i) * kWave + lane] = soft.acc[d][i];
+            if (lane < 32) {
+                stats[wave % 2][0][lane] = soft.m;
+                stats[wave % 2][1][lane] = l;
+            }
         }
+        __syncthreads();
+        if (half == 1) return;
+        const float m1 = stats[wave % 2][0][lane & 31], l1 = stats[wave % 2][1][lane & 31];
+        const float m = fmaxf(soft.m, m1), by = m == LAST_NEG_INF ? 0.f : m;
+        const float f0 = __builtin_amdgcn_exp2f((soft.m - by) * c2), f1 = __builtin_amdgcn_exp2f((m1 - by) * c2);
+        soft.m = m;
+        l = l * f0 + l1 * f1;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) soft.acc[d][i] = soft.acc[d][i] * f0 + sums[(d * 16 + i) * kWave + lane] * f1;
+        soft.l = l;
+    }
+    const bool odd = there && soft.not_finite();
+    if (t < a.T && !odd) {
+        put_rows<E, DP>((char*)a.y + (row * a.py + (size_t)at.head * a.D) * 2, a.D, soft.acc, 1.f / l, there);
+        if (a.lse && lane < 32) a.lse[row * a.heads + at.head] = there ? (soft.m * c2 + __builtin_amdgcn_logf(l)) * kLn2 : 0.f;
+    }
+    for (unsigned long long rows = __ballot(odd) & 0xffffffffull; rows; rows &= rows - 1) {
+        const int tr = t0 + __ffsll(rows) - 1;
+        const int end = tr + band.right + 1 < at.len ? tr + band.right + 1 : at.len;
+        float m, sum, o[2];
+        plain_row<E>(q + (size_t)tr * a.pq * 2, a.D, c2, 0, end, [&](int s) { return s >= tr - band.left || s < band.sinks; },
+                     [&](int s) { return k + (size_t)s * a.pk * 2; }, [&](int s) { return v + (size_t)s * a.pv * 2; }, &m, &sum, o);
+        char* const y = (char*)a.y + (((at.row0 + tr) * a.py) + (size_t)at.head * a.D) * 2;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (lane + 64 * i < a.D) Elt<E>::put(y, lane + 64 * i, o[i] / sum);
+        if (a.lse && lane == 0) a.lse[(at.row0 + tr) * a.heads + at.head] = (m * c2 + __builtin_amdgcn_logf(sum)) * kLn2;
     }
 }
 

@@ -118,7 +118,7 @@ def test_attention_refuses(lib):
 
 
 BAD_CACHES = [(None, 1), (cache(k=None), 1), (cache(v=None), 1), (cache(table=None), 1), (cache(used=None), 1), (cache(pages=0), 2), (cache(page=0), 2),
-              (cache(entries=0), 2), (cache(page=1 << 20, entries=1 << 11), 2), (cache(page=(1 << 20) + 1), 2), (cache(k=0x10001), 2), (cache(type=F16), 6),
+              (cache(entries=0), 2), (cache(page=1 << 20, entries=1 << 11), 2), (cache(page=(1 << 20) + 1), 2), (cache(k=0x10001), 2), (cache(v=0x20008), 2), (cache(type=F16), 6),
               (cache(type=F32), 6), (cache(type=I8), 6)]
 
 
