@@ -80,7 +80,7 @@ Band band_of(const last_band_t* b, int T)
     return Band{within(b->left), within(b->right), b->sinks, b->scale};
 }
 
-HeadSide side_of(const last_matrix_t* x, const last_matrix_t* y, const float* gain, int heads, bool turned)
+HeadSide side_of(const last_matrix_t* x, const last_matrix_t* y, const float* gain, int heads)
 {
     HeadSide s{};
     s.x = x->data;
@@ -88,23 +88,30 @@ HeadSide side_of(const last_matrix_t* x, const last_matrix_t* y, const float* ga
     if (y) { s.y = y->data; s.py = y->pitch; }
     s.gain = gain;
     s.heads = heads;
-    s.turned = turned;
     return s;
 }
 
-template <typename E>
-void launch_heads(HeadArgs a, hipStream_t st)
+template <typename E, int LN>
+void launch_heads(const HeadArgs& a, hipStream_t st)
 {
-    const int lanes = a.D / 8, at_once = lanes > 8 ? 4 : lanes > 4 ? 8 : lanes > 2 ? 16 : lanes > 1 ? 32 : 64;
-    const int heads = a.side[0].heads + a.side[1].heads + a.side[2].heads, passes = (heads + at_once - 1) / at_once;
+    int groups = 0;
+    for (const HeadSide& side : a.side) groups += (side.heads + kWave / LN - 1) / (kWave / LN);
     // A wavefront takes all heads of a frame, whose angles it forms once, but where that leaves compute units without work.
-    a.split = (int)std::max(1ll, std::min<long long>(passes, 4096 / a.rows));
-    const dim3 grid((unsigned)std::min<long long>(((long long)a.rows * a.split + 3) / 4, 2048)), block(256);
-    if (at_once == 4) hipLaunchKernelGGL((heads_kernel<E, 16>), grid, block, 0, st, a);
-    else if (at_once == 8) hipLaunchKernelGGL((heads_kernel<E, 8>), grid, block, 0, st, a);
-    else if (at_once == 16) hipLaunchKernelGGL((heads_kernel<E, 4>), grid, block, 0, st, a);
-    else if (at_once == 32) hipLaunchKernelGGL((heads_kernel<E, 2>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((heads_kernel<E, 1>), grid, block, 0, st, a);
+    const int split = (int)std::max(1ll, std::min<long long>(groups, 4096 / a.rows));
+    const dim3 grid((unsigned)std::min<long long>(((long long)a.rows + 3) / 4, 2048), (unsigned)split);
+    if (a.cache.table) hipLaunchKernelGGL((heads_kernel<E, LN, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((heads_kernel<E, LN, false>), grid, dim3(256), 0, st, a);
+}
+
+template <typename E>
+void launch_heads(const HeadArgs& a, hipStream_t st)
+{
+    const int lanes = a.D / 8;
+    if (lanes > 8) launch_heads<E, 16>(a, st);
+    else if (lanes > 4) launch_heads<E, 8>(a, st);
+    else if (lanes > 2) launch_heads<E, 4>(a, st);
+    else if (lanes > 1) launch_heads<E, 2>(a, st);
+    else launch_heads<E, 1>(a, st);
 }
 
 void launch_heads_of(int type, const HeadArgs& a, hipStream_t st)
@@ -324,12 +331,12 @@ last_status_t last_head_norm(const last_frames_t* frames, const last_heads_t* he
     if (q) {
         LAST_TRY(check_matrix(q, (long long)heads->heads * heads->width, plain(type)));
         LAST_TRY(check_matrix(yq, (long long)heads->heads * heads->width, yq->type == type));
-        a.side[0] = side_of(q, yq, gain_q, heads->heads, true);
+        a.side[0] = side_of(q, yq, gain_q, heads->heads);
     }
     if (k) {
         LAST_TRY(check_matrix(k, (long long)heads->kv_heads * heads->width, plain(type) && k->type == type));
         LAST_TRY(check_matrix(yk, (long long)heads->kv_heads * heads->width, yk->type == type));
-        a.side[1] = side_of(k, yk, gain_k, heads->kv_heads, true);
+        a.side[1] = side_of(k, yk, gain_k, heads->kv_heads);
     }
     if (rows == 0) return LAST_OK;
     a.frames = frames_of(frames);
@@ -496,11 +503,11 @@ last_status_t last_cache_append(const last_frames_t* frames, const last_heads_t*
     if (q) {
         LAST_TRY(check_matrix(q, cq, q->type == type));
         LAST_TRY(check_matrix(yq, cq, yq->type == type));
-        a.side[0] = side_of(q, yq, gain_q, heads->heads, true);
+        a.side[0] = side_of(q, yq, gain_q, heads->heads);
     }
-    a.side[1] = side_of(k, nullptr, gain_k, heads->kv_heads, true);
+    a.side[1] = side_of(k, nullptr, gain_k, heads->kv_heads);
     a.side[1].pages = (char*)cache->k;
-    a.side[2] = side_of(v, nullptr, nullptr, heads->kv_heads, false);
+    a.side[2] = side_of(v, nullptr, nullptr, heads->kv_heads);
     a.side[2].pages = (char*)cache->v;
     a.frames = frames_of(frames);
     a.rows = (int)rows;

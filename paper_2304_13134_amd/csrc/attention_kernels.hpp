@@ -227,8 +227,8 @@ __device__ __forceinline__ float sum_of_halves(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// frames of an item: lengths as clamped
-__device__ __forceinline__ int frames_of_item(const int* len, int T, int b) { return len ? clamped(len[b], T) : T; }
+// frames of an item, which is the same one for all lanes: lengths as clamped
+__device__ __forceinline__ int frames_of_item(const int* len, int T, int b) { return len ? clamped(same_for_all(len, b), T) : T; }
 
 template <typename E> __device__ __forceinline__ float value_at(const char* p, int c)
 {
@@ -516,7 +516,7 @@ __global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, long long f
     const long long row = i / a.heads;
     const int head = (int)(i - row * a.heads), b = (int)(row / a.T), c = 8 * lane;
     float sum = 0.f;
-    if ((int)(row - (long long)b * a.T) < frames_of_item(a.len, a.T, b) && c < a.D) {
+    if ((int)(row - (long long)b * a.T) < (a.len ? clamped(a.len[b], a.T) : a.T) && c < a.D) {
         float x[8], z[8];
         load8<E>(a.dy, (size_t)row * a.pdy + (size_t)head * a.D + c, 8, x);
         load8<E>(a.y, (size_t)row * a.py + (size_t)head * a.D + c, 8, z);
@@ -851,7 +851,7 @@ __global__ __launch_bounds__(256) void grad_join_kernel(AttentionArgs a, int DP,
     const long long unit = u - which * units, row = unit / a.kv_heads;
     const int kv = (int)(unit - row * a.kv_heads), b = (int)(row / a.T), s = (int)(row - (long long)b * a.T);
     f4 v{};
-    if (s < frames_of_item(a.len, a.T, b)) {
+    if (s < (a.len ? clamped(a.len[b], a.T) : a.T)) {
         for (int part = 0; part < a.parts; ++part) v += *(const f4*)(a.kept + (((size_t)which * a.parts + part) * units + unit) * DP + c);
         if (a.part && s < a.band.sinks) v += *(const f4*)(a.sums + ((((size_t)b * a.kv_heads + kv) * 2 + which) * kMostSinks + s) * DP + c);
         if (which == 0) v *= a.band.scale;

@@ -19,7 +19,6 @@ struct HeadSide {
     long long py;
     const float* gain;               // null: not normed
     int heads;
-    int turned;                      // whether it is rotated
     char* pages;
 };
 
@@ -44,16 +43,22 @@ struct HeadArgs {
     float eps;
     Turn turn;
     HeadSide side[3];
-    int sides, split;                // wavefronts a frame
     Pages cache;
     int* status;                     // [B] or null
 };
 
 constexpr int kMostUsed = 1 << 30;   // positions stay in 32 bits
 
+// p[i] where both are the same for all lanes: by the scalar unit, whose loads wait for no others
+__device__ __forceinline__ int same_for_all(const int* p, int i)
+{
+    typedef const __attribute__((address_space(4))) int* at;
+    return *((at)(uintptr_t)p + i);
+}
+
 __device__ __forceinline__ int used_frames(const int* used, int b)
 {
-    const int n = used[b];
+    const int n = same_for_all(used, b);
     return n < 0 ? 0 : n > kMostUsed ? kMostUsed : n;
 }
 
@@ -76,8 +81,9 @@ __device__ __forceinline__ void sine_cosine(double t, float* sine, float* cosine
     const double f = t - floor(t), k = rint(f * 4.0);
     const int quarter = (int)k;
     const float x = (float)((f - k * 0.25) * 6.283185307179586), s = x * x;
-    const float sn = x * (1.f + s * (-1.6666667e-1f + s * (8.3333333e-3f + s * (-1.9841270e-4f + s * 2.7557319e-6f))));
-    const float cs = 1.f + s * (-0.5f + s * (4.1666667e-2f + s * (-1.3888889e-3f + s * 2.4801587e-5f)));
+    float sn = __builtin_fmaf(s, 2.7557319e-6f, -1.9841270e-4f), cs = __builtin_fmaf(s, 2.4801587e-5f, -1.3888889e-3f);
+    sn = x * __builtin_fmaf(s, __builtin_fmaf(s, __builtin_fmaf(s, sn, 8.3333333e-3f), -1.6666667e-1f), 1.f);
+    cs = __builtin_fmaf(s, __builtin_fmaf(s, __builtin_fmaf(s, cs, 4.1666667e-2f), -0.5f), 1.f);
     const float a = quarter & 1 ? cs : sn, b = quarter & 1 ? sn : cs;
     *sine = quarter & 2 ? -a : a;
     *cosine = (quarter + 1) & 2 ? -b : b;
@@ -139,6 +145,22 @@ __device__ __forceinline__ void store4(void* p, size_t i, const float* v)
     else *(u2_two*)((uint16_t*)p + i) = u2{f16_pair(v[0], v[1]), f16_pair(v[2], v[3])};
 }
 
+// 1 / sqrt(v), to an ulp (the instruction knows no subnormal numbers)
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const bool small = v < 0x1p-64f;
+    const float r = __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v);
+    return small ? r * 0x1p32f : r;
+}
+
+// in one instruction each: `p` is the same for all lanes
+template <typename E>
+__device__ __forceinline__ void get8(const char* p, unsigned o0, unsigned o1, Four<E>* r)
+{
+    r[0] = raw4<E>(p + o0, 0);
+    r[1] = raw4<E>(p + o1, 0);
+}
+
 template <int LN>
 __device__ __forceinline__ float head_sum(float v)
 {
@@ -147,36 +169,59 @@ __device__ __forceinline__ float head_sum(float v)
     return v;
 }
 
-// the angles of a frame: of the lane's four pairs
-__device__ __forceinline__ void angles(const double* turns, double position, bool turned, float* sn, float* cs)
+// The angles of a frame: a lane forms one pair's, and has its own four from LDS (`turned`: 2 x 64 floats of the wavefront's).
+struct Angles {
+    float frequency;                 // of the pair that the lane forms
+    float* at;
+    __device__ __forceinline__ void init(const Turn& t, float* lds)
+    {
+        const int lane = (int)threadIdx.x % kWave;
+        at = lds + (int)threadIdx.x / kWave * 2 * kWave;
+        frequency = lane < t.R / 2 ? t.frequencies[lane] : 0.f;
+    }
+    __device__ __forceinline__ void get(double position, const HeadLane& of, float* sn, float* cs) const
+    {
+        const int lane = (int)threadIdx.x % kWave;
+        float s, c;
+        sine_cosine(position * ((double)frequency * 0.15915494309189535), &s, &c);
+        asm volatile("" ::: "memory");
+        at[lane] = s;
+        at[kWave + lane] = c;
+        asm volatile("" ::: "memory");                       // (one wavefront's accesses to LDS stay in order)
+        const f4 x = *(const f4*)(at + (of.turned ? of.c0 : 0)), y = *(const f4*)(at + kWave + (of.turned ? of.c0 : 0));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sn[k] = of.turned ? x[k] : 0.f;
+            cs[k] = of.turned ? y[k] : 1.f;
+        }
+    }
+};
+
+// (two instructions: a compute unit takes about 33 clocks for one that addresses memory by lane, whatever its width, and sixteen of a value each
+// were most of a wavefront's)
+__device__ __forceinline__ void load_gain(const float* gain, const HeadLane& at, float* g)
 {
+    f4 a{1.f, 1.f, 1.f, 1.f}, b = a;
+    if (gain && at.here) {
+        a = *(const f4_any*)(gain + at.c0);
+        b = *(const f4_any*)(gain + at.c1);
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        sn[k] = 0.f;
-        cs[k] = 1.f;
-        if (turned) sine_cosine(position * turns[k], &sn[k], &cs[k]);
+        g[k] = a[k];
+        g[4 + k] = b[k];
     }
 }
 
-__device__ __forceinline__ void own_turns(const Turn& t, const HeadLane& at, double* turns)
-{
-#pragma unroll
-    for (int k = 0; k < 4; ++k) turns[k] = at.turned ? (double)t.frequencies[at.c0 + k] * 0.15915494309189535 : 0.0;
-}
-
-__device__ __forceinline__ void load_gain(const float* gain, const HeadLane& at, float* g)
-{
-#pragma unroll
-    for (int k = 0; k < 8; ++k) g[k] = gain && at.here ? gain[(k < 4 ? at.c0 : at.c1 - 4) + k] : 1.f;
-}
-
+// (which products are fused is written out, here and in the sums, so that a row has the same bits from every kernel)
 __device__ __forceinline__ void rotate8(const float* sn, const float* cs, float sign, float* v)
 {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const float a = v[k], b = v[4 + k], s = sign * sn[k];
-        v[k] = a * cs[k] - b * s;
-        v[4 + k] = b * cs[k] + a * s;
+        v[k] = __builtin_fmaf(a, cs[k], -(b * s));
+        v[4 + k] = __builtin_fmaf(b, cs[k], a * s);
+        asm("" : "+v"(v[k]), "+v"(v[4 + k]));                // (else they may be rounded to 16 bits in the same instruction, or not)
     }
 }
 
@@ -187,30 +232,39 @@ __global__ void no_frames_kernel(int* status, int B)
     if (b < B) status[b] = kItemOk;
 }
 
-// LN: lanes of a head.  A unit of work is every split-th group of 64 / LN heads of a frame.
-template <typename E, int LN>
+// LN: lanes of a head.  A group is 64 / LN heads of a frame, of queries, keys or values alone, so that pointers are the same for all lanes; a wavefront
+// takes every split-th group of a frame.  PAGES: keys and values go to the pages of a cache.  The code is kept short: with four groups unrolled, and
+// loads sent for ahead, its 17 KB took longer to arrive than a frame does.
+// 16384 x 16 heads of 64 in bfloat16, three quarters of the frames existing (59 MB): 13 us, of which the memory takes 9
+template <typename E, int LN, bool PAGES>
 __global__ __launch_bounds__(256) void heads_kernel(HeadArgs a)
 {
     constexpr int kAtOnce = kWave / LN;
+    constexpr unsigned kSize = Elt<E>::size;
+    __shared__ __attribute__((aligned(16))) float lds[4 * 2 * kWave];
     const int lane = (int)threadIdx.x % LN, group = (int)threadIdx.x % kWave / LN;
-    const int wave = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), waves = (int)gridDim.x * 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)threadIdx.x / kWave), waves = (int)gridDim.x * 4;
     const HeadLane at(lane, a.D, a.turn.R);
-    double turns[4];
-    own_turns(a.turn, at, turns);
+    const unsigned o0 = (unsigned)(group * a.D + at.c0) * kSize, o1 = (unsigned)(group * a.D + at.c1) * kSize;
+    const HeadSide s0 = a.side[0], s1 = a.side[1], s2 = a.side[2];
+    const int g0 = (s0.heads + kAtOnce - 1) / kAtOnce, g1 = g0 + (s1.heads + kAtOnce - 1) / kAtOnce;
+    const int groups = g1 + (PAGES ? (s2.heads + kAtOnce - 1) / kAtOnce : 0), part = (int)blockIdx.y, split = (int)gridDim.y;
+    Angles angles;
+    angles.init(a.turn, lds);
     float gq[8], gk[8];
-    load_gain(a.side[0].gain, at, gq);
-    load_gain(a.side[1].gain, at, gk);
-    const int n0 = a.side[0].heads, n1 = n0 + a.side[1].heads, n2 = n1 + a.side[2].heads;
-    for (long long unit = wave; unit < (long long)a.rows * a.split; unit += waves) {
-        const int row = a.split == 1 ? (int)unit : (int)(unit / a.split), part = (int)(unit - (long long)row * a.split);
+    load_gain(s0.gain, at, gq);
+    load_gain(s1.gain, at, gk);
+    const float by_width = 1.f / (float)a.D;
+    for (int row = wave; row < a.rows; row += waves) {
         const int b = (int)quotient((unsigned)row, a.frames.by), t = row - b * a.frames.T;
-        const int exist = a.frames.len ? a.frames.len[b] : a.frames.T;
+        const int exist = a.frames.len ? same_for_all(a.frames.len, b) : a.frames.T;
         const bool there = t < exist;
-        const int first = a.turn.first ? a.turn.first[b] : 0;
+        double position = t;
         int page = 0, in_page = 0;
-        if (a.cache.table) {
+        if constexpr (PAGES) {
             const int used = used_frames(a.cache.used, b);
             page = page_of(a.cache, b, used + t, &in_page);
+            position += used;
             if (a.status && t == 0 && part == 0) {
                 // every page that the item's new frames go to
                 int bad = 0, n = clamped(exist, a.frames.T), r;
@@ -218,42 +272,44 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadArgs a)
                 const bool any = __any(bad);
                 if (threadIdx.x % kWave == 0) a.status[b] = any ? kItemBadPage : kItemOk;
             }
+        } else if (a.turn.first) {
+            position += same_for_all(a.turn.first, b);
         }
         float sn[4], cs[4];
-        angles(turns, (double)(a.cache.table ? used_frames(a.cache.used, b) : first) + t, at.turned, sn, cs);
-        for (int h0 = part * kAtOnce; h0 < n2; h0 += a.split * kAtOnce) {
-            const int head = h0 + group;
-            const int which = head < n0 ? 0 : head < n1 ? 1 : 2;
-            const HeadSide& s = a.side[which];
-            const int h = head - (which == 0 ? 0 : which == 1 ? n0 : n1);
-            const bool on = head < n2 && at.here;
+#pragma unroll 1
+        for (int i = part; i < groups; i += split) {
+            const bool of_q = i < g0, of_k = !of_q && i < g1;
+            const int h = (of_q ? i : of_k ? i - g0 : i - g1) * kAtOnce, heads = of_q ? s0.heads : of_k ? s1.heads : s2.heads;
+            const bool on = at.here && group < heads - h;
+            const size_t column = (size_t)h * a.D;
+            Four<E> x[2]{};
+            if (there && on)
+                get8<E>((const char*)(of_q ? s0.x : of_k ? s1.x : s2.x) + ((size_t)row * (of_q ? s0.px : of_k ? s1.px : s2.px) + column) * kSize, o0, o1, x);
+            if (i == part) angles.get(position, at, sn, cs);
             float v[8];
+            unpack4<E>(x[0], v);
+            unpack4<E>(x[1], v + 4);
+            if (of_q || of_k) {
+                if (of_q ? s0.gain : s1.gain) {
+                    float sum = 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = 0.f;
-            if (on && there) {
-                const size_t x = (size_t)row * s.px + (size_t)h * a.D;
-                unpack4<E>(raw4<E>(s.x, x + at.c0), v);
-                unpack4<E>(raw4<E>(s.x, x + at.c1), v + 4);
+                    for (int c = 0; c < 8; ++c) sum = __builtin_fmaf(v[c], v[c], sum);
+                    float inv = inverse_root(__builtin_fmaf(head_sum<LN>(sum), by_width, a.eps));
+                    inv = there ? inv : 0.f;                 // (a frame that is not there has zeros)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) v[c] *= inv * (of_q ? gq[c] : gk[c]);
+                }
+                rotate8(sn, cs, 1.f, v);
             }
-            float sum = 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum += v[k] * v[k];
-            sum = head_sum<LN>(sum);
             if (!on) continue;
-            if (there && s.gain) {
-                const float inv = 1.f / sqrtf(sum / (float)a.D + a.eps);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] *= inv * (which == 0 ? gq[k] : gk[k]);
-            }
-            if (there && s.turned) rotate8(sn, cs, 1.f, v);
-            if (s.y) {
-                const size_t y = (size_t)row * s.py + (size_t)h * a.D;
-                store4<E>(s.y, y + at.c0, v);
-                store4<E>(s.y, y + at.c1, v + 4);
+            if (!PAGES || of_q) {
+                char* const y = (char*)(of_q ? s0.y : s1.y) + ((size_t)row * (of_q ? s0.py : s1.py) + column) * kSize;
+                store4<E>(y + o0, 0, v);
+                store4<E>(y + o1, 0, v + 4);
             } else if (there && page >= 0) {
-                const size_t y = (((size_t)page * s.heads + h) * a.cache.page + in_page) * a.D;
-                store4<E>(s.pages, y + at.c0, v);
-                store4<E>(s.pages, y + at.c1, v + 4);
+                char* const y = (of_k ? s1.pages : s2.pages) + (((size_t)page * heads + h + group) * a.cache.page + in_page) * a.D * kSize;
+                store4<E>(y, at.c0, v);
+                store4<E>(y, at.c1, v + 4);
             }
         }
     }
@@ -276,66 +332,80 @@ struct HeadGradArgs {
     float* part;                     // [workgroups][2][D] partial sums of the gains' gradients, or null
 };
 
+// 16384 x 20 heads of 128 in bfloat16, three quarters of the frames existing (210 MB): 43 us (4.9 TB/s)
 template <typename E, int LN>
 __global__ __launch_bounds__(256) void heads_grad_kernel(HeadGradArgs a)
 {
     constexpr int kAtOnce = kWave / LN;
+    constexpr unsigned kSize = Elt<E>::size;
+    __shared__ __attribute__((aligned(16))) float lds[4 * 2 * kWave];
     const int lane = (int)threadIdx.x % LN, group = (int)threadIdx.x % kWave / LN;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const HeadLane at(lane, a.D, a.turn.R);
-    double turns[4];
-    own_turns(a.turn, at, turns);
-    float g[2][8], dg[2][8];
-    load_gain(a.side[0].gain, at, g[0]);
-    load_gain(a.side[1].gain, at, g[1]);
+    const unsigned o0 = (unsigned)(group * a.D + at.c0) * kSize, o1 = (unsigned)(group * a.D + at.c1) * kSize;
+    const HeadGradSide s0 = a.side[0], s1 = a.side[1];
+    Angles angles;
+    angles.init(a.turn, lds);
+    float gq[8], gk[8], dgq[8], dgk[8];
+    load_gain(s0.gain, at, gq);
+    load_gain(s1.gain, at, gk);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) dg[0][k] = dg[1][k] = 0.f;
-    const int n0 = a.side[0].heads, n1 = n0 + a.side[1].heads;
+    for (int k = 0; k < 8; ++k) dgq[k] = dgk[k] = 0.f;
+    const float by_width = 1.f / (float)a.D;
+    const int g0 = (s0.heads + kAtOnce - 1) / kAtOnce, groups = g0 + (s1.heads + kAtOnce - 1) / kAtOnce;
+    // u = dy rotated back to dx, d[k] += what the gain's gradient gets
+    // (lanes without a head have zeros, and no factor: it would be infinite without an eps)
+    const auto norm_grad = [&](float* u, const float* x, const float* gain, float* d, bool on) {
+        float sum = 0.f, dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += x[k] * x[k];
+        float inv = inverse_root(head_sum<LN>(sum) * by_width + a.eps);
+        inv = on ? inv : 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            d[k] += u[k] * (x[k] * inv);
+            u[k] *= gain[k];
+            dot += u[k] * x[k];
+        }
+        const float m = inv * inv * (head_sum<LN>(dot) * by_width);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) u[k] = inv * (u[k] - x[k] * m);
+    };
     for (long long r = (long long)blockIdx.x * 4 + wave; r < a.rows; r += (long long)gridDim.x * 4) {
-        const int row = (int)r, b = (int)quotient((unsigned)row, a.frames.by), t = row - b * a.frames.T;
-        const bool there = frame_exists(a.frames, row);
+        const int row = __builtin_amdgcn_readfirstlane((int)r), b = (int)quotient((unsigned)row, a.frames.by), t = row - b * a.frames.T;
+        const bool there = t < (a.frames.len ? same_for_all(a.frames.len, b) : a.frames.T);
+        const double position = (double)(a.turn.first ? same_for_all(a.turn.first, b) : 0) + t;
         float sn[4], cs[4];
-        angles(turns, (double)(a.turn.first ? a.turn.first[b] : 0) + t, at.turned, sn, cs);
-        for (int h0 = 0; h0 < n1; h0 += kAtOnce) {
-            const int head = h0 + group, which = head < n0 ? 0 : 1;
-            const HeadGradSide& s = a.side[which];
-            const int h = head - (which ? n0 : 0);
-            const bool on = head < n1 && at.here;
+#pragma unroll 1
+        for (int i = 0; i < groups; ++i) {
+            const bool of_q = i < g0;
+            const int h = (of_q ? i : i - g0) * kAtOnce;
+            const bool on = at.here && group < (of_q ? s0.heads : s1.heads) - h;
+            const size_t column = (size_t)h * a.D;
+            Four<E> raw[4]{};
+            if (there && on) {
+                get8<E>((const char*)(of_q ? s0.dy : s1.dy) + ((size_t)row * (of_q ? s0.pdy : s1.pdy) + column) * kSize, o0, o1, raw);
+                if (of_q ? s0.gain : s1.gain)
+                    get8<E>((const char*)(of_q ? s0.x : s1.x) + ((size_t)row * (of_q ? s0.px : s1.px) + column) * kSize, o0, o1, raw + 2);
+            }
+            if (i == 0) angles.get(position, at, sn, cs);
             float u[8], x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) u[k] = x[k] = 0.f;
-            if (on && there) {
-                const size_t i = (size_t)row * s.pdy + (size_t)h * a.D, j = (size_t)row * s.px + (size_t)h * a.D;
-                unpack4<E>(raw4<E>(s.dy, i + at.c0), u);
-                unpack4<E>(raw4<E>(s.dy, i + at.c1), u + 4);
-                if (s.gain) {
-                    unpack4<E>(raw4<E>(s.x, j + at.c0), x);
-                    unpack4<E>(raw4<E>(s.x, j + at.c1), x + 4);
-                }
+            unpack4<E>(raw[0], u);
+            unpack4<E>(raw[1], u + 4);
+            unpack4<E>(raw[2], x);
+            unpack4<E>(raw[3], x + 4);
+            if (there) {
                 rotate8(sn, cs, -1.f, u);
+                if (of_q) {
+                    if (s0.gain) norm_grad(u, x, gq, dgq, on);
+                } else {
+                    if (s1.gain) norm_grad(u, x, gk, dgk, on);
+                }
             }
-            float sum = 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum += x[k] * x[k];
-            const float inv = 1.f / sqrtf(head_sum<LN>(sum) / (float)a.D + a.eps);
-            float dot = 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float d = on && there && s.gain ? u[k] * x[k] * inv : 0.f;
-                dg[0][k] += which == 0 ? d : 0.f;
-                dg[1][k] += which == 1 ? d : 0.f;
-                u[k] *= which == 0 ? g[0][k] : g[1][k];
-                dot += u[k] * x[k];
-            }
-            const float m = inv * inv * (head_sum<LN>(dot) / (float)a.D);
             if (!on) continue;
-            if (s.gain) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) u[k] = there ? inv * (u[k] - x[k] * m) : 0.f;
-            }
-            const size_t i = (size_t)row * s.pdx + (size_t)h * a.D;
-            store4<E>(s.dx, i + at.c0, u);
-            store4<E>(s.dx, i + at.c1, u + 4);
+            char* const dx = (char*)(of_q ? s0.dx : s1.dx) + ((size_t)row * (of_q ? s0.pdx : s1.pdx) + column) * kSize;
+            store4<E>(dx + o0, 0, u);
+            store4<E>(dx + o1, 0, u + 4);
         }
     }
     if (!a.part) return;
@@ -345,7 +415,7 @@ __global__ __launch_bounds__(256) void heads_grad_kernel(HeadGradArgs a)
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            float v = dg[i][k];
+            float v = i == 0 ? dgq[k] : dgk[k];
 #pragma unroll
             for (int o = LN; o < kWave; o <<= 1) v += __shfl_xor(v, o, kWave);
             if (group == 0) red[wave][i][lane * 8 + k] = v;
