@@ -71,12 +71,16 @@ class FrameModel:
 
     def loss_and_gradients(self, x, lengths, refs, ref_lengths):
         """(loss [B], gradients by parameter) of frames x [B, T, H]."""
+        return self.loss_of_frames(x, lengths, refs, ref_lengths)[:2]
+
+    def loss_of_frames(self, x, lengths, refs, ref_lengths):
+        """(loss [B], gradients by parameter, gradient of x)"""
         y, saved = self.block.forward(x, lengths)
         f = lb.last_residual_norm(y, self.gain, lengths=lengths)
         dist, num, (df, de, dW) = lb.last_globally_normalized_loss(lb.SharedEmb(f.y, self.e, self.W), lengths, refs, ref_lengths, order=2)
         dy, dgain = lb.last_residual_norm_grad(df, y, self.gain, f.inv, lengths=lengths)
-        _, grads = self.block.backward(dy, saved, lengths)
-        return dist - num, [(self.gain, dgain), (self.e, de), (self.W, dW)] + [(p, grads[k]) for k, p in self.block.parameters().items()]
+        dx, grads = self.block.backward(dy, saved, lengths)
+        return dist - num, [(self.gain, dgain), (self.e, de), (self.W, dW)] + [(p, grads[k]) for k, p in self.block.parameters().items()], dx
 
     def step(self, x, lengths, refs, ref_lengths, rate=0.002):
         """One step down the gradient; the mean loss before it."""
