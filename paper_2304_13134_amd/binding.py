@@ -787,16 +787,17 @@ class Cache(tuple):
     used = property(lambda self: self[3])
 
 
+def _heads_of(t, name, width):
+    n = t.shape[-1] if isinstance(t, torch.Tensor) and t.dim() > 0 else 0
+    if width < 1 or n == 0 or n % width != 0:
+        raise ValueError("%s must be a tensor with whole heads of %d columns" % (name, width))
+    return n // width
+
+
 def _heads(q, k, width):
     """(packed LastHeads, heads, kv_heads) of matrices of which one may be None"""
-    if width < 1:
-        raise ValueError("width must be positive")
-    counts = []
-    for t, name in ((q, "q"), (k, "k")):
-        if t is not None and (not isinstance(t, torch.Tensor) or t.dim() < 1 or t.shape[-1] % width != 0 or t.shape[-1] == 0):
-            raise ValueError("%s must be a tensor with whole heads of %d columns" % (name, width))
-        counts.append(None if t is None else t.shape[-1] // width)
-    heads, kv = counts
+    heads = None if q is None else _heads_of(q, "q", width)
+    kv = None if k is None else _heads_of(k, "k", width)
     if heads is not None and kv is not None and heads % kv != 0:
         raise ValueError("%d heads cannot share %d heads of keys evenly" % (heads, kv))
     return _pack_heads(heads or kv, kv or heads, width), heads, kv
@@ -823,20 +824,16 @@ def _rotation(rotation, width, B, on):
 
 def _items(t, lengths, name):
     """_frames of a tensor in which frames see each other, or have positions: [B, T, columns], or [T, columns] for one item; and B"""
+    if lengths is None and isinstance(t, torch.Tensor) and t.dim() == 3:
+        rows = t.shape[:2]
+        return _pack_frames(max(1, rows[0]), rows[1] if rows[0] else 0, 0), rows, t.get_device(), rows[0]
     fr, rows, t, on = _frames(t, lengths, name)
-    if len(rows) == 1:
-        return _pack_frames(1, rows[0], 0), rows, on, 1
-    if lengths is None and rows[0] > 0:
-        fr = _pack_frames(rows[0], rows[1], 0)
-    return fr, rows, on, rows[0]
+    return fr, rows, on, rows[0] if len(rows) == 2 else 1
 
 
 def _band(left, right, sinks, scale, width):
-    for n, name in ((left, "left"), (right, "right")):
-        if n is not None and n < 0:
-            raise ValueError("%s must be a number of frames, or None for no limit" % name)
-    if sinks < 0:
-        raise ValueError("sinks must be a number of frames")
+    if (left is not None and left < 0) or (right is not None and right < 0) or sinks < 0:
+        raise ValueError("left and right must be numbers of frames, or None for no limit, and sinks one")
     most = 0x7fffffff
     return _pack_band(-1 if left is None else min(left, most), -1 if right is None else min(right, most), min(sinks, most),
                       width ** -0.5 if scale is None else scale)
@@ -921,8 +918,8 @@ def last_attention_grad(dy, q, k, v, y, lse, width, left=None, right=0, sinks=0,
     return tuple(out)
 
 
-def _cache(cache, B, on):
-    """packed LastCache"""
+def _refuse_cache(cache, B, on):
+    """Raises what is wrong with a Cache that _cache does not take."""
     k, v, table, used = cache
     for t, name in ((k, "cache.k"), (v, "cache.v")):
         if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float16) or t.dim() != 4 or not t.is_contiguous():
@@ -935,16 +932,31 @@ def _cache(cache, B, on):
     _dev_tensor(used, torch.int32, "cache.used")
     if table.dim() != 2 or table.shape[0] != B or used.shape != (B,):
         raise ValueError("cache.table must be [%d, entries] and cache.used [%d]" % (B, B))
-    if table.get_device() != on or used.get_device() != on:
-        _elsewhere("cache.table or cache.used")
-    return _pack_cache(k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[0], k.shape[2], table.shape[1], table.data_ptr() or _NO_ROWS,
+    _elsewhere("cache.table or cache.used")
+
+
+def _cache(cache, B, on):
+    """packed LastCache (checked at once: a fifth of the time of a short call otherwise)"""
+    k, v, table, used = cache
+    try:
+        shape, dtype, rows = k.shape, k.dtype, table.shape
+        if not (on >= 0 and len(shape) == 4 and (dtype is torch.bfloat16 or dtype is torch.float16) and v.dtype is dtype and v.shape == shape
+                and k.is_contiguous() and v.is_contiguous() and k.get_device() == on and v.get_device() == on
+                and len(rows) == 2 and rows[0] == B and used.shape == (B,) and table.dtype is torch.int32 and used.dtype is torch.int32
+                and table.is_contiguous() and used.is_contiguous() and table.get_device() == on and used.get_device() == on):
+            _refuse_cache(cache, B, on)
+    except AttributeError:
+        raise TypeError("a Cache holds four device tensors") from None
+    return _pack_cache(k.data_ptr(), v.data_ptr(), _TYPES[dtype], shape[0], shape[2], rows[1], table.data_ptr() or _NO_ROWS,
                        used.data_ptr() or _NO_ROWS)
 
 
 def _status_of(item_status, B, t, on):
     """(address of the call's item_status)"""
-    item_status = _status(item_status, B, t.device)
-    if item_status.numel() < B or item_status.get_device() != on:
+    global last_item_status
+    if item_status is None:
+        last_item_status = item_status = torch.empty(B, dtype=torch.int32, device=t.device)
+    elif _dev_tensor(item_status, torch.int32, "item_status").numel() < B or item_status.get_device() != on:
         raise ValueError("item_status must have %d elements on the call's device" % B)
     return item_status.data_ptr() if B else None
 
@@ -953,12 +965,12 @@ def last_cache_append(k, v, cache, q=None, gain_q=None, gain_k=None, frequencies
     """Keys of new frames, normed and rotated as by last_head_norm at positions used + t, and their values into a Cache; with q, returns its
     queries, normed and rotated by the same call, else None.  k, v: [B, T, kv_heads width] of the cache's type, of which lengths [B] new
     frames exist.  item_status: see check_item_status()."""
-    width = cache.k.shape[-1]
+    _, held, _, width = cache[0].shape
     heads, _, kv = _heads(q, k, width)
     fr, rows, on, B = _items(k, lengths, "k")
     r = _rotation(frequencies, width, B, on)
-    if kv != cache.k.shape[1]:
-        raise ValueError("k has %d heads, the cache %d" % (kv, cache.k.shape[1]))
+    if kv != held:
+        raise ValueError("k has %d heads, the cache %d" % (kv, held))
     mk, mv, mc = _matrix(k, "k", on), _matrix(v, "v", on, rows, k.shape[-1]), _cache(cache, B, on)
     g = [_vector(t, width, name, on) for t, name in ((gain_q, "gain_q"), (gain_k, "gain_k"))]
     mq = yq = my = None
@@ -972,10 +984,11 @@ def last_cache_append(k, v, cache, q=None, gain_q=None, gain_k=None, frequencies
 def last_cached_attention(q, cache, left=None, right=0, sinks=0, scale=None, lengths=None, item_status=None):
     """y: last_attention of new frames, q [B, T, columns] of which lengths [B] exist, at positions cache.used + t, to what a Cache holds after
     last_cache_append with the same `used`.  item_status: see check_item_status()."""
-    width, kv = cache.k.shape[-1], cache.k.shape[1]
-    if q.shape[-1] % (kv * width) != 0 or q.shape[-1] == 0:
+    _, kv, _, width = cache[0].shape
+    columns = q.shape[-1]
+    if columns % (kv * width) != 0 or columns == 0:
         raise ValueError("q must have a multiple of the cache's %d heads of %d columns" % (kv, width))
-    heads = _pack_heads(q.shape[-1] // width, kv, width)
+    heads = _pack_heads(columns // width, kv, width)
     fr, rows, on, B = _items(q, lengths, "q")
     mq, mc, band = _matrix(q, "q", on), _cache(cache, B, on), _band(left, right, sinks, scale, width)
     y, my = _result(q.shape, q.dtype, q.device, q)
