@@ -207,24 +207,14 @@ GradPlan plan_grad(Carver& cv, long long rows, const last_frames_t* f, const las
 }
 
 template <typename E>
-void launch_delta(const AttentionArgs& a, hipStream_t st)
-{
-    const int lanes = a.D / 8, ln = lanes > 8 ? 16 : lanes > 4 ? 8 : lanes > 2 ? 4 : lanes > 1 ? 2 : 1;
-    const long long per = 256 / ln, groups = ((long long)a.B * a.T * a.heads + per - 1) / per;
-    in_launches(groups, [&](long long first, dim3 grid) {
-        const long long from = first * per;
-        if (ln == 16) hipLaunchKernelGGL((delta_kernel<E, 16>), grid, dim3(256), 0, st, a, from);
-        else if (ln == 8) hipLaunchKernelGGL((delta_kernel<E, 8>), grid, dim3(256), 0, st, a, from);
-        else if (ln == 4) hipLaunchKernelGGL((delta_kernel<E, 4>), grid, dim3(256), 0, st, a, from);
-        else if (ln == 2) hipLaunchKernelGGL((delta_kernel<E, 2>), grid, dim3(256), 0, st, a, from);
-        else hipLaunchKernelGGL((delta_kernel<E, 1>), grid, dim3(256), 0, st, a, from);
-    });
-}
-
-template <typename E>
 void launch_attention_grad(AttentionArgs a, int chunks, hipStream_t st)
 {
-    launch_delta<E>(a, st);
+    a.tiles = (unsigned)((a.T + kOwn - 1) / kOwn);
+    a.together = heads_together(a);
+    in_launches((long long)a.tiles * a.heads * a.B, [&](long long first, dim3 grid) {
+        a.first = (unsigned)first;
+        LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_query_kernel<E, DP>), grid, dim3(256), 0, st, a));
+    });
     a.together = 1;
     if (chunks) {
         a.tiles = (unsigned)chunks;
@@ -249,11 +239,6 @@ void launch_attention_grad(AttentionArgs a, int chunks, hipStream_t st)
             hipLaunchKernelGGL((grad_join_kernel<E>), grid, dim3(256), 0, st, a, padded(a.D), first);
         });
     }
-    a.together = heads_together(a);
-    in_launches((long long)a.tiles * a.heads * a.B, [&](long long first, dim3 grid) {
-        a.first = (unsigned)first;
-        LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_query_kernel<E, DP>), grid, dim3(256), 0, st, a));
-    });
 }
 
 // Blocks of 32 rows, and over how many workgroups a block's frames are split: so that there are some 1024, each with at least

@@ -38,7 +38,7 @@ struct AttentionArgs {
     const void *q, *k, *v, *dy;
     void *y, *dq, *dk, *dv;
     long long pq, pk, pv, py, pdy, pdq, pdk, pdv;
-    float *lse, *delta;              // [B * T][heads]
+    float *lse, *delta;              // [B * T][heads]; delta of frames that exist
     float *part, *sums;              // first frames' sums of dk and dv (grad_first_kernel, first_join_kernel), or null
     int shares;
     float* kept;                     // sums of dk and dv of parts of the heads that share them (grad_join_kernel)
@@ -506,28 +506,23 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
     }
 }
 
-// delta[t][head] = dy . y, 0 where there is no frame: eight columns a lane, LN lanes a head
-template <typename E, int LN>
-__global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, long long first)
+// a lane's own row's scalar product of two rows of 16 bits that both halves have alternate pieces of
+template <typename E, int N>
+__device__ __forceinline__ float row_product(const u4 (&x)[N], const u4 (&y)[N])
 {
-    const int lane = (int)threadIdx.x % LN;
-    const long long i = first + ((long long)blockIdx.x * 256 + threadIdx.x) / LN;
-    if (i >= (long long)a.B * a.T * a.heads) return;
-    const long long row = i / a.heads;
-    const int head = (int)(i - row * a.heads), b = (int)(row / a.T), c = 8 * lane;
     float sum = 0.f;
-    if ((int)(row - (long long)b * a.T) < (a.len ? clamped(a.len[b], a.T) : a.T) && c < a.D) {
-        float x[8], z[8];
-        load8<E>(a.dy, (size_t)row * a.pdy + (size_t)head * a.D + c, 8, x);
-        load8<E>(a.y, (size_t)row * a.py + (size_t)head * a.D + c, 8, z);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum += x[k] * z[k];
+    for (int k = 0; k < N; ++k) {
+        float a[8], b[8];
+        unpack<E>(Raw<E>{x[k]}, a);
+        unpack<E>(Raw<E>{y[k]}, b);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sum = __builtin_fmaf(a[c], b[c], sum);
     }
-    sum = head_sum<LN>(sum);
-    if (lane == 0) a.delta[i] = sum;
+    return sum_of_halves(sum);
 }
 
-// The gradient of queries: a wavefront's own frames are queries, the tiles keys and values.
+// The gradient of queries: a wavefront's own frames are queries, the tiles keys and values.  It comes first, and leaves delta for the others.
 template <typename E, int DP>
 __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
 {
@@ -544,7 +539,13 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
     u4 qf[DP / 16], df[DP / 16];
     own_rows<DP>(there ? (const char*)a.q + (row * a.pq + (size_t)at.head * a.D) * 2 : nullptr, a.D, qf);
     own_rows<DP>(there ? (const char*)a.dy + (row * a.pdy + (size_t)at.head * a.D) * 2 : nullptr, a.D, df);
-    float l2 = there ? a.lse[row * a.heads + at.head] * kLog2e : 0.f, delta = there ? a.delta[row * a.heads + at.head] : 0.f;
+    float l2 = there ? a.lse[row * a.heads + at.head] * kLog2e : 0.f, delta;
+    {
+        u4 yf[DP / 16];
+        own_rows<DP>(there ? (const char*)a.y + (row * a.py + (size_t)at.head * a.D) * 2 : nullptr, a.D, yf);
+        delta = row_product<E>(df, yf);
+        if (there && lane < 32) a.delta[row * a.heads + at.head] = delta;
+    }
     const int lo = g0 - band.left > 0 ? g0 - band.left : 0;
     const int hi = g0 >= at.len ? 0 : g0 + kOwn + band.right < at.len ? g0 + kOwn + band.right : at.len;
     const int first_tiles = band.sinks > 0 && hi > 0 ? 1 : 0;
