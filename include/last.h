@@ -364,9 +364,9 @@ last_status_t last_kept_grad(const last_frames_t* frames, int32_t H, const last_
 /* ---- Frames that see each other: attention in the layer, and its streaming form on a paged cache.
  *
  * Columns are heads: head h of a matrix has columns h*width .. (h+1)*width - 1.  Queries and results have `heads` of them, keys and
- * values kv_heads, each of which heads / kv_heads neighbouring query heads share.  width is a multiple of 8 up to 128; with bands,
- * T is at most 2^28.  Rows, pitches, alignment, lengths and frames that do not exist are as above, so queries, keys and
- * values may be columns of the one matrix that a product made, and gradients go back to columns of one. */
+ * values kv_heads, each of which heads / kv_heads neighbouring query heads share.  width is a multiple of 8 up to 128; T is at most
+ * 2^28, and with bands B * T * heads is less than 2^31.  Rows, pitches, alignment, lengths and frames that do not exist are as
+ * above, so queries, keys and values may be columns of the one matrix that a product made, and gradients go back to columns of one. */
 typedef struct {
     int32_t heads, kv_heads, width;
 } last_heads_t;
@@ -423,7 +423,8 @@ last_status_t last_attention(const last_frames_t* frames, const last_heads_t* he
                              const last_matrix_t* k, const last_matrix_t* v, const last_matrix_t* y, float* lse, void* hip_stream);
 
 /* The gradients of q, k and v, those of k and v summed over the heads that share them.  y and lse as last_attention returned
- * them; all matrices of one type, BF16 or F16.  P and dS are rounded to it before they are multiplied.  Frames that do
+ * them; all matrices of one type, BF16 or F16.  P and dS are rounded to it before they are multiplied (in F16 a dS
+ * beyond 65504, for instance of a loss scaled too far, is infinite).  Frames that do
  * not exist have no part in it; an infinity or a NaN in a frame that does may come out of the gradients of any of the item's frames.
  * Workspace: LAST_OP_ATTENTION_GRAD. */
 last_status_t last_attention_grad(const last_frames_t* frames, const last_heads_t* heads, const last_band_t* band, const last_matrix_t* dy,
@@ -433,7 +434,7 @@ last_status_t last_attention_grad(const last_frames_t* frames, const last_heads_
 
 /* Keys of new frames, normed and rotated by their positions used[b] + t as by last_head_norm, and their values to the pages of the cache;
  * with q, its queries to yq in the same launch.  rotation->first is not read.  lengths: how many new frames an item has, 0 among
- * them.  Nothing else of the pages is touched.  Two items must not write to one page.  item_status (dev int32 [B], or NULL):
+ * them.  Nothing else of the pages is touched.  No two entries of the table that frames are written by may name one page.  item_status (dev int32 [B], or NULL):
  * 0, or 8. */
 last_status_t last_cache_append(const last_frames_t* frames, const last_heads_t* heads, const last_matrix_t* q, const last_matrix_t* k,
                                 const last_matrix_t* v, const float* gain_q, const float* gain_k, float eps, const last_rotation_t* rotation,

@@ -29,11 +29,12 @@ last_status_t check_heads(const last_heads_t* h)
     return LAST_OK;
 }
 
-last_status_t check_items(const last_frames_t* f, const last_heads_t* h, long long* rows)
+// seen: of a call in which frames see each other, whose workgroups, at most one for each head of each frame, are numbered in 32 bits
+last_status_t check_items(const last_frames_t* f, const last_heads_t* h, bool seen, long long* rows)
 {
     LAST_TRY(check_frames(f, rows));
     LAST_TRY(check_heads(h));
-    if (f->T > kMostFrames || *rows * h->heads > 1ll << 36 || (long long)f->T * h->heads > 1ll << 30) return LAST_ERR_SHAPE;
+    if (f->T > kMostFrames || *rows * h->heads > (seen ? (1ll << 31) - 1 : 1ll << 36) || (long long)f->T * h->heads > 1ll << 30) return LAST_ERR_SHAPE;
     return LAST_OK;
 }
 
@@ -286,7 +287,7 @@ size_t last_attention_workspace_bytes(int32_t op, const last_frames_t* frames, c
                                       const last_cache_t* cache)
 {
     long long rows;
-    if (check_items(frames, heads, &rows) != LAST_OK) return 0;
+    if (check_items(frames, heads, op != LAST_OP_HEAD_NORM_GRAD, &rows) != LAST_OK) return 0;
     Carver cv(nullptr);
     if (op == LAST_OP_HEAD_NORM_GRAD) {
         cv.take(sizeof(float) * 2 * (size_t)head_grad_groups(rows) * heads->width);
@@ -307,7 +308,7 @@ last_status_t last_head_norm(const last_frames_t* frames, const last_heads_t* he
                              const last_matrix_t* yq, const last_matrix_t* yk, void* hip_stream)
 {
     long long rows;
-    LAST_TRY(check_items(frames, heads, &rows));
+    LAST_TRY(check_items(frames, heads, false, &rows));
     if ((!q && !k) || (q && !yq) || (k && !yk)) return LAST_ERR_NULL;
     if (!(eps >= 0.f)) return LAST_ERR_SHAPE;
     LAST_TRY(check_rotation(rotation, heads->width));
@@ -340,7 +341,7 @@ last_status_t last_head_norm_grad(const last_frames_t* frames, const last_heads_
                                   float* dgain_k, void* ws, size_t ws_bytes, void* hip_stream)
 {
     long long rows;
-    LAST_TRY(check_items(frames, heads, &rows));
+    LAST_TRY(check_items(frames, heads, false, &rows));
     if ((!dyq && !dyk) || (dyq && (!dq || !q)) || (dyk && (!dk || !k))) return LAST_ERR_NULL;
     if ((dgain_q && (!gain_q || !dyq)) || (dgain_k && (!gain_k || !dyk))) return LAST_ERR_NULL;
     if (!(eps >= 0.f)) return LAST_ERR_SHAPE;
@@ -383,7 +384,7 @@ last_status_t last_attention(const last_frames_t* frames, const last_heads_t* he
                              const last_matrix_t* k, const last_matrix_t* v, const last_matrix_t* y, float* lse, void* hip_stream)
 {
     long long rows;
-    LAST_TRY(check_items(frames, heads, &rows));
+    LAST_TRY(check_items(frames, heads, true, &rows));
     if (!q || !k || !v || !y) return LAST_ERR_NULL;
     LAST_TRY(check_band(band));
     const long long cq = (long long)heads->heads * heads->width, ck = (long long)heads->kv_heads * heads->width;
@@ -421,7 +422,7 @@ last_status_t last_attention_grad(const last_frames_t* frames, const last_heads_
                                   size_t ws_bytes, void* hip_stream)
 {
     long long rows;
-    LAST_TRY(check_items(frames, heads, &rows));
+    LAST_TRY(check_items(frames, heads, true, &rows));
     if (!dy || !q || !k || !v || !y || !lse || !dq || !dk || !dv) return LAST_ERR_NULL;
     LAST_TRY(check_band(band));
     const long long cq = (long long)heads->heads * heads->width, ck = (long long)heads->kv_heads * heads->width;
@@ -475,7 +476,7 @@ last_status_t last_cache_append(const last_frames_t* frames, const last_heads_t*
                                 const last_cache_t* cache, const last_matrix_t* yq, int32_t* item_status, void* hip_stream)
 {
     long long rows;
-    LAST_TRY(check_items(frames, heads, &rows));
+    LAST_TRY(check_items(frames, heads, false, &rows));
     if (!k || !v || (q && !yq)) return LAST_ERR_NULL;
     if (!(eps >= 0.f)) return LAST_ERR_SHAPE;
     LAST_TRY(check_rotation(rotation, heads->width));
@@ -515,7 +516,7 @@ last_status_t last_cached_attention(const last_frames_t* frames, const last_head
                                     void* hip_stream)
 {
     long long rows;
-    LAST_TRY(check_items(frames, heads, &rows));
+    LAST_TRY(check_items(frames, heads, true, &rows));
     if (!q || !y) return LAST_ERR_NULL;
     LAST_TRY(check_band(band));
     LAST_TRY(check_cache(cache, heads, frames->T));

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256, 2) void cached_kernel(CachedArgs a)
         const int page = page_of(a.cache, b, s, &x);
         return page < 0 ? -1 : (long long)((((size_t)page * a.kv_heads + kv) * a.cache.page + x) * a.D);
     };
-    const Sight sight{used + t - band.left, !there ? 0 : used + t + band.right + 1 < total ? used + t + band.right + 1 : total, sinks};
+    const Sight sight{used + t - band.left > 0 ? used + t - band.left : 0, !there ? 0 : used + t + band.right + 1 < total ? used + t + band.right + 1 : total, sinks};
     Softmax<DP> soft;
     soft.init();
     char *const qt = lds, *const kt = lds + (1 + wave * 2) * C::kBytes, *const vt = kt + C::kBytes;

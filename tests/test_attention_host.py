@@ -110,6 +110,8 @@ def test_attention_refuses(lib):
             assert f(k=m) == code and f(v=m) == code and f(y=m) == code
         assert f(q=matrix(F32), k=matrix(F32), v=matrix(F32), y=matrix(F32)) == 6
         assert f(fr=frames(T=0)) == 0 and f(fr=frames(1, (1 << 28) + 1)) == 2
+        # workgroups are numbered in 32 bits
+        assert f(fr=frames(1 << 19, 1 << 6), h=Heads(64, 64, 8), q=matrix(pitch=512), k=matrix(pitch=512), v=matrix(pitch=512), y=matrix(pitch=512)) == 2
         for missing in ("q", "k", "v", "y"):
             assert f(**{missing: None}) == 1
     for missing in ("dy", "lse", "dq", "dk", "dv"):
@@ -144,6 +146,7 @@ def test_cache_calls_refuse(lib):
         assert append(k=m) == code and append(v=m) == code and append(yq=m) == code and attend(y=m) == code
     assert append(k=None) == 1 and append(v=None) == 1 and append(yq=None) == 1 and append(q=None, yq=None) == 0 and append(eps=-1.0) == 2
     assert append(r=Rotated(8, None, None), fr=frames()) == 1 and append(r=Rotated(100, 0x1000, None)) == 2
+    assert attend(fr=frames(1 << 19, 1 << 6), h=Heads(64, 64, 8)) == 2
     assert attend(q=None) == 1 and attend(y=None) == 1 and attend(ws=None) == 5 and attend(n=16) == 5
 
 
@@ -162,6 +165,9 @@ def test_workspaces(lib):
     for c, code in BAD_CACHES:
         assert code == 6 or size(ops[2], c=c) == 0
     assert size(ops[0], b=None, c=None) >= 256 and size(ops[1], c=None) >= 256
+    many = {"fr": frames(1 << 19, 1 << 6), "h": Heads(64, 64, 8)}
+    assert size(ops[0], **many) > 0 and size(ops[1], **many) == 0 and size(ops[2], **many) == 0
+    assert size(ops[1], fr=frames((1 << 19) - 1, 1 << 6), h=Heads(64, 64, 8)) > 0
     assert size(0) == 0 and size(lb.OP_PRODUCT) == 0 and size(13) == 0
     assert size(ops[1], fr=frames(1, 4096), b=Band(100, 0, 4, 1)) > size(ops[1], fr=frames(1, 4096), b=Band(100, 0, 0, 1))
 
