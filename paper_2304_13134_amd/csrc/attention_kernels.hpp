@@ -72,6 +72,11 @@ __device__ __forceinline__ f16x zeros16()
     return v;
 }
 
+// A value that a branch changes, in the registers where the other way has it: else the compiler lets the branch write others, and copies on the way
+// that does not change it, which is the usual one.
+template <typename V>
+__device__ __forceinline__ void in_place(V& v) { asm volatile("" : "+v"(v)); }
+
 // A tile in LDS: rows of DP columns of 16 bits.  16-byte piece c of row r stands at c ^ spread(r) of its row, so that the 256 bytes that
 // the banks give at a time are different ones for a column of 16 rows (reads along rows) and for four pieces of 4 rows (transposing reads).
 template <int DP> struct Rows {
@@ -114,20 +119,20 @@ template <int DP, int THREADS> struct Tile {
     }
 
     template <typename Exists>
-    __device__ __forceinline__ void lay(char* lds, int D, int s0, Exists exists) const
+    __device__ __forceinline__ void lay(char* lds, int D, int s0, Exists exists)
     {
         const int r = (int)threadIdx.x / kPieces, c = (int)threadIdx.x % kPieces;
         const int at = r * Rows<DP>::kPitch + (c ^ Rows<DP>::spread(r)) * 16;
-        if (all) {
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) *(u4*)(lds + at + i * kApart * Rows<DP>::kPitch) = v[i];
-        } else {
+        if (!all) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 const unsigned keep = ((c * 8 < D) & exists(s0 + r + i * kApart)) ? ~0u : 0u;
-                *(u4*)(lds + at + i * kApart * Rows<DP>::kPitch) = v[i] & u4{keep, keep, keep, keep};
+                v[i] &= u4{keep, keep, keep, keep};
+                in_place(v[i]);
             }
         }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) *(u4*)(lds + at + i * kApart * Rows<DP>::kPitch) = v[i];
     }
 };
 
@@ -323,7 +328,7 @@ template <int DP> struct Softmax {
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
         top = max_of_halves(top);
         // The maximum is only a reference: as long as no score passes it by a factor of 2^8 the sums keep it, which saves their scaling.
-        if (__any((top - m) * c2 > 8.f || (m == LAST_NEG_INF && top > m))) {
+        if (__any(((top - m) * c2 > 8.f) | ((m == LAST_NEG_INF) & (top > m)))) {
             const float higher = fmaxf(m, top), old = m == LAST_NEG_INF ? 0.f : __builtin_amdgcn_exp2f((m - higher) * c2);
             m = higher;
             l *= old;
@@ -333,15 +338,15 @@ template <int DP> struct Softmax {
                 for (int i = 0; i < 16; ++i) acc[d][i] *= old;
         }
         const float by = m == LAST_NEG_INF ? 0.f : m * c2;
-        float sum = 0.f;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], c2, -by));
-                sum += s[n][i];
+                sum[i % 4] += s[n][i];
             }
-        l += sum;
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
     // whether a result is no number (or would be for another frame's sake)
     __device__ __forceinline__ bool not_finite() const
@@ -444,9 +449,14 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) s[n] = Mma<E>::go(reads.along_rows(kt, half + n, i), qf[i], s[n]);
         }
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n) in_place(s[n]);
         if (!all) {
 #pragma unroll
-            for (int n = 0; n < kBlocks; ++n) sight.apply(s[n], s0 + 32 * n, LAST_NEG_INF);
+            for (int n = 0; n < kBlocks; ++n) {
+                sight.apply(s[n], s0 + 32 * n, LAST_NEG_INF);
+                in_place(s[n]);
+            }
         }
         soft.template take<kBlocks>(s, c2);
 #pragma unroll
@@ -590,7 +600,11 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
             for (int i = 0; i < 16; ++i) {
                 s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c2, -l2)) * (p[i] - delta);
             }
-            if (!all) sight.apply(s, s0 + 32 * n, 0.f);
+            in_place(s);
+            if (!all) {
+                sight.apply(s, s0 + 32 * n, 0.f);
+                in_place(s);
+            }
             u4 d[2];
             to_operands<E>(s, d);
 #pragma unroll
@@ -629,9 +643,13 @@ __device__ __forceinline__ void key_tile(const char* qt, const char* yt, const f
                 if constexpr (DK) e[i + x] = p[i + x] * (e[i + x] - delta[x]);
             }
         }
+        if constexpr (DV) in_place(p);
+        if constexpr (DK) in_place(e);
         if (!all) {
             if constexpr (DV) sight.apply(p, t0 + 32 * n, 0.f);
             if constexpr (DK) sight.apply(e, t0 + 32 * n, 0.f);
+            if constexpr (DV) in_place(p);
+            if constexpr (DK) in_place(e);
         }
         u4 f[2];
         if constexpr (DV) {
