@@ -15,6 +15,7 @@
 #pragma once
 #include "heads_kernels.hpp"
 #include "layer.hpp"
+#include <type_traits>
 
 namespace last {
 
@@ -102,14 +103,11 @@ template <int DP, int THREADS> struct Tile {
     template <typename Exists>
     __device__ __forceinline__ void send(const char* p, long long pitch, int D, int s0, bool all_, int other, Exists exists)
     {
-        const int piece = (int)threadIdx.x % kPieces * 8, c = piece < D ? piece : 0, r = (int)threadIdx.x / kPieces;
         all = all_ && D == DP;
         if (all_) {
-            const char* const base = p + (size_t)(unsigned)s0 * pitch * 2;
-            const unsigned off = (unsigned)(r * pitch + c) * 2u;                       // (64 pitches of at most 4 MiB)
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) v[i] = *(const u4_any*)(base + (size_t)i * kApart * pitch * 2 + off);
+            send_all(p, pitch, D, s0);
         } else {
+            const int piece = (int)threadIdx.x % kPieces * 8, c = piece < D ? piece : 0, r = (int)threadIdx.x / kPieces;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 const int s = s0 + r + i * kApart;
@@ -117,12 +115,19 @@ template <int DP, int THREADS> struct Tile {
             }
         }
     }
+    __device__ __forceinline__ void send_all(const char* p, long long pitch, int D, int s0)
+    {
+        const int piece = (int)threadIdx.x % kPieces * 8, c = piece < D ? piece : 0, r = (int)threadIdx.x / kPieces;
+        const char* const base = p + (size_t)(unsigned)s0 * pitch * 2;
+        const unsigned off = (unsigned)(r * pitch + c) * 2u;                       // (64 pitches of at most 4 MiB)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = *(const u4_any*)(base + (size_t)i * kApart * pitch * 2 + off);
+    }
 
     template <typename Exists>
     __device__ __forceinline__ void lay(char* lds, int D, int s0, Exists exists)
     {
         const int r = (int)threadIdx.x / kPieces, c = (int)threadIdx.x % kPieces;
-        const int at = r * Rows<DP>::kPitch + (c ^ Rows<DP>::spread(r)) * 16;
         if (!all) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
@@ -131,8 +136,24 @@ template <int DP, int THREADS> struct Tile {
                 in_place(v[i]);
             }
         }
+        lay(lds);
+    }
+    __device__ __forceinline__ void lay(char* lds) const
+    {
+        const int r = (int)threadIdx.x / kPieces, c = (int)threadIdx.x % kPieces;
+        const int at = r * Rows<DP>::kPitch + (c ^ Rows<DP>::spread(r)) * 16;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) *(u4*)(lds + at + i * kApart * Rows<DP>::kPitch) = v[i];
+    }
+    // zeros in columns beyond D
+    __device__ __forceinline__ void clear(int D)
+    {
+        const unsigned keep = (int)threadIdx.x % kPieces * 8 < D ? ~0u : 0u;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            v[i] &= u4{keep, keep, keep, keep};
+            in_place(v[i]);
+        }
     }
 };
 
@@ -278,11 +299,12 @@ __device__ void plain_row(const char* q, int D, float c2, int from, int to, Seen
 struct Sight {
     int lo, hi, sinks;
     // scores of 32 frames from s0 on; what is not seen becomes `other`
+    template <bool FIRSTS = true>
     __device__ __forceinline__ void apply(f16x& s, int s0, float other) const
     {
         const unsigned span = hi > lo ? (unsigned)(hi - lo) : 0u;
         const int from = s0 + result_row(0) - lo;
-        if (s0 < sinks) {
+        if (FIRSTS && s0 < sinks) {
             const int end = hi < sinks ? hi : sinks;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -317,9 +339,9 @@ template <int DP> struct Softmax {
         m = LAST_NEG_INF;
         l = 0.f;
     }
-    // scores of N blocks of 32 frames, -inf where not seen, become probabilities relative to m
+    // raises m to the maximum of scores of N blocks of 32 frames, -inf where not seen, if they pass it
     template <int N>
-    __device__ __forceinline__ void take(f16x* s, float c2)
+    __device__ __forceinline__ void raise(const f16x* s, float c2)
     {
         float top = s[0][0];
 #pragma unroll
@@ -333,11 +355,24 @@ template <int DP> struct Softmax {
             m = higher;
             l *= old;
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d)
+            for (int d = 0; d < DP / 32; ++d) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[d][i] *= old;
+                in_place(acc[d]);
+            }
         }
-        const float by = m == LAST_NEG_INF ? 0.f : m * c2;
+    }
+    // the scores become probabilities relative to m
+    template <int N>
+    __device__ __forceinline__ void take(f16x* s, float c2)
+    {
+        raise<N>(s, c2);
+        l += powers<N>(s, c2, m == LAST_NEG_INF ? 0.f : m * c2);
+    }
+    // scores become probabilities relative to an exponent; their sum
+    template <int N>
+    __device__ __forceinline__ float powers(f16x* s, float c2, float by) const
+    {
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -346,7 +381,7 @@ template <int DP> struct Softmax {
                 s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], c2, -by));
                 sum[i % 4] += s[n][i];
             }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        return (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
     // whether a result is no number (or would be for another frame's sake)
     __device__ __forceinline__ bool not_finite() const
@@ -391,6 +426,34 @@ __device__ __forceinline__ Place place_of(const AttentionArgs& a, unsigned id, i
     return p;
 }
 
+// The order of a workgroup's tiles: first those of which some of its frames see not all, in order, then in a loop of its own, which looks at no limits, the
+// others, tiles low .. low + full - 1.  (Limits looked at for each tile: a third of the vector instructions of a tile that needs none, since
+// the compiler forms masks before it branches, and copies what they may change.)
+struct Order {
+    int firsts, first, low, full, some;          // firsts: 1 if tile 0 is there for first frames, before those from `first` on
+    // own frames [g0, end) see, or are seen by, frames from - t .. to + t, of which [lo, hi) are there for any of them
+    __device__ __forceinline__ Order(int g0, int end, long long from, long long to, int lo, int hi, int len, int firsts_)
+    {
+        firsts = hi > 0 ? firsts_ : 0;
+        first = lo / kTile > firsts ? lo / kTile : firsts;
+        const int last = (hi + kTile - 1) / kTile, tiles = firsts + (last > first ? last - first : 0);
+        const long long all_from = end - 1 - from, all_to = g0 + to + 1;
+        low = all_from > 0 ? (int)((all_from + kTile - 1) / kTile) : 0;
+        low = low > first ? low : first;
+        const int high = (int)(all_to < len ? all_to : len) / kTile;
+        full = last > first && high > low ? high - low : 0;
+        some = tiles - full;
+    }
+    __device__ __forceinline__ int tiles() const { return some + full; }
+    // where tile i of the order begins
+    __device__ __forceinline__ int start(int i) const
+    {
+        if (i < firsts) return i * kTile;
+        const int n = i - firsts + first;
+        return (i >= some ? low + i - some : n < low ? n : n + full) * kTile;
+    }
+};
+
 // HALVES: a workgroup has 64 frames instead of 128, and two wavefronts for each 32 of them, one for either half of each tile, whose sums are joined at the end:
 // twice as many workgroups of half the length.
 template <typename E, int DP, bool HALVES>
@@ -415,10 +478,8 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
     // frames that the workgroup's see: first ones, and [lo, hi)
     const int lo = g0 - band.left > 0 ? g0 - band.left : 0;
     const int hi = g0 >= at.len ? 0 : g0 + kGroup + band.right < at.len ? g0 + kGroup + band.right : at.len;
-    const int first_tiles = band.sinks > 0 && hi > 0 ? 1 : 0;
-    const int first = lo / kTile > first_tiles ? lo / kTile : first_tiles, last = (hi + kTile - 1) / kTile;
-    const int tiles = first_tiles + (last > first ? last - first : 0);
-    const auto start = [&](int j) { return (j < first_tiles ? j : first + j - first_tiles) * kTile; };
+    const Order order(g0, g0 + kGroup < at.len ? g0 + kGroup : at.len, band.left, band.right, lo, hi, at.len, band.sinks > 0);
+    const int some = order.some, tiles = order.tiles();
     const auto exists = [&](int s) { return (s < hi) & ((s >= lo) | (s < band.sinks)); };
     const Sight sight = sight_of(t, at.len, band);
     Softmax<DP> soft;
@@ -431,34 +492,9 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
         ks.send(k, a.pk, a.D, s0, all, hi - 1, exists);
         vs.send(v, a.pv, a.D, s0, all, hi - 1, exists);
     };
-    if (tiles > 0) get(start(0));
+    if (tiles > 0) get(order.start(0));
     have(qf);
-    for (int j = 0; j < tiles; ++j) {
-        const int tile0 = start(j), s0 = tile0 + 32 * half;
-        char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
-        ks.lay(kt, a.D, tile0, exists);
-        vs.lay(vt, a.D, tile0, exists);
-        __syncthreads();                             // (the other buffer is written again after the next one)
-        if (j + 1 < tiles) get(start(j + 1));
-        if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + 32 * kBlocks <= t0 - band.left && s0 >= band.sinks)) continue;
-        const bool all = s0 >= t0 + 31 - band.left && s0 + 32 * kBlocks - 1 <= t0 + band.right && s0 + 32 * kBlocks <= at.len && t0 + 32 <= at.len;
-        f16x s[kBlocks];
-#pragma unroll
-        for (int n = 0; n < kBlocks; ++n) {
-            s[n] = zeros16();
-#pragma unroll
-            for (int i = 0; i < DP / 16; ++i) s[n] = Mma<E>::go(reads.along_rows(kt, half + n, i), qf[i], s[n]);
-        }
-#pragma unroll
-        for (int n = 0; n < kBlocks; ++n) in_place(s[n]);
-        if (!all) {
-#pragma unroll
-            for (int n = 0; n < kBlocks; ++n) {
-                sight.apply(s[n], s0 + 32 * n, LAST_NEG_INF);
-                in_place(s[n]);
-            }
-        }
-        soft.template take<kBlocks>(s, c2);
+    const auto multiply = [&](const char* vt, f16x* s) {
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n) {
             u4 p[2];
@@ -468,6 +504,67 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d) soft.acc[d] = Mma<E>::go(reads.along_columns(vt, d, 2 * (half + n) + i), p[i], soft.acc[d]);
         }
+    };
+    const auto scores = [&](const char* kt, f16x* s) {
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n) s[n] = zeros16();
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+            for (int n = 0; n < kBlocks; ++n) s[n] = Mma<E>::go(reads.along_rows(kt, half + n, i), qf[i], s[n]);
+    };
+    for (int j = 0; j < some; ++j) {
+        const int tile0 = order.start(j), s0 = tile0 + 32 * half;
+        char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
+        ks.lay(kt, a.D, tile0, exists);
+        vs.lay(vt, a.D, tile0, exists);
+        __syncthreads();                             // (the other buffer is written again after the next one)
+        if (j + 1 < tiles) get(order.start(j + 1));
+        if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + 32 * kBlocks <= t0 - band.left && s0 >= band.sinks)) continue;
+        f16x s[kBlocks];
+        scores(kt, s);
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n) sight.apply(s[n], s0 + 32 * n, LAST_NEG_INF);
+        soft.template take<kBlocks>(s, c2);
+        multiply(vt, s);
+    }
+    // Relative to the reference there is, without a look at the maximum.  Where that gives a sum that is none (no reference yet: the exponent is
+    // -inf) or beyond 2^15, which a type of 16 bits holds, the loop is left to raise the reference, and entered again with the same tile.
+    const bool whole = a.D == DP;
+    float by = soft.m * c2;
+    bool raised = false;
+    for (int j = some; j < tiles;) {
+        char *kt = lds[j & 1], *vt = kt + Rows<DP>::kBytes;
+        f16x s[kBlocks];
+        for (; j < tiles; ++j) {
+            kt = lds[j & 1];
+            vt = kt + Rows<DP>::kBytes;
+            if (!raised) {
+                if (!whole) {
+                    ks.clear(a.D);
+                    vs.clear(a.D);
+                }
+                ks.lay(kt);
+                vs.lay(vt);
+                __syncthreads();
+                if (j + 1 < tiles) {
+                    const int s0 = (order.low + j + 1 - some) * kTile;
+                    ks.send_all(k, a.pk, a.D, s0);
+                    vs.send_all(v, a.pv, a.D, s0);
+                }
+            }
+            scores(kt, s);
+            const float sum = soft.template powers<kBlocks>(s, c2, by);
+            if (!raised && __any(!(sum <= 0x1p15f))) break;
+            raised = false;
+            soft.l += sum;
+            multiply(vt, s);
+        }
+        if (j >= tiles) break;
+        scores(kt, s);
+        soft.template raise<kBlocks>(s, c2);
+        by = soft.m == LAST_NEG_INF ? 0.f : soft.m * c2;
+        raised = true;
     }
     float l = sum_of_halves(soft.l);
     if constexpr (HALVES) {
@@ -558,10 +655,8 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
     }
     const int lo = g0 - band.left > 0 ? g0 - band.left : 0;
     const int hi = g0 >= at.len ? 0 : g0 + kOwn + band.right < at.len ? g0 + kOwn + band.right : at.len;
-    const int first_tiles = band.sinks > 0 && hi > 0 ? 1 : 0;
-    const int first = lo / kTile > first_tiles ? lo / kTile : first_tiles, last = (hi + kTile - 1) / kTile;
-    const int tiles = first_tiles + (last > first ? last - first : 0);
-    const auto start = [&](int j) { return (j < first_tiles ? j : first + j - first_tiles) * kTile; };
+    const Order order(g0, g0 + kOwn < at.len ? g0 + kOwn : at.len, band.left, band.right, lo, hi, at.len, band.sinks > 0);
+    const int some = order.some, tiles = order.tiles();
     const auto exists = [&](int s) { return (s < hi) & ((s >= lo) | (s < band.sinks)); };
     const Sight sight = sight_of(t, at.len, band);
     f16x acc[DP / 32];
@@ -575,19 +670,11 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
         ks.send(k, a.pk, a.D, s0, all, hi - 1, exists);
         vs.send(v, a.pv, a.D, s0, all, hi - 1, exists);
     };
-    if (tiles > 0) get(start(0));
+    if (tiles > 0) get(order.start(0));
     have(qf);
     have(df);
     asm volatile("" : "+v"(l2), "+v"(delta));
-    for (int j = 0; j < tiles; ++j) {
-        const int s0 = start(j);
-        char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
-        ks.lay(kt, a.D, s0, exists);
-        vs.lay(vt, a.D, s0, exists);
-        __syncthreads();
-        if (j + 1 < tiles) get(start(j + 1));
-        if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + kTile <= t0 - band.left && s0 >= band.sinks)) continue;
-        const bool all = s0 >= t0 + 31 - band.left && s0 + kTile - 1 <= t0 + band.right && s0 + kTile <= at.len && t0 + 32 <= at.len;
+    const auto turn = [&](const char* kt, const char* vt, auto limits, bool all, int s0) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             f16x s = zeros16(), p = zeros16();
@@ -600,10 +687,12 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
             for (int i = 0; i < 16; ++i) {
                 s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c2, -l2)) * (p[i] - delta);
             }
-            in_place(s);
-            if (!all) {
-                sight.apply(s, s0 + 32 * n, 0.f);
+            if constexpr (limits) {
                 in_place(s);
+                if (!all) {
+                    sight.apply(s, s0 + 32 * n, 0.f);
+                    in_place(s);
+                }
             }
             u4 d[2];
             to_operands<E>(s, d);
@@ -612,18 +701,46 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
 #pragma unroll
                 for (int x = 0; x < DP / 32; ++x) acc[x] = Mma<E>::go(reads.along_columns(kt, x, 2 * n + i), d[i], acc[x]);
         }
+    };
+    for (int j = 0; j < some; ++j) {
+        const int s0 = order.start(j);
+        char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
+        ks.lay(kt, a.D, s0, exists);
+        vs.lay(vt, a.D, s0, exists);
+        __syncthreads();
+        if (j + 1 < tiles) get(order.start(j + 1));
+        if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + kTile <= t0 - band.left && s0 >= band.sinks)) continue;
+        const bool all = s0 >= t0 + 31 - band.left && s0 + kTile - 1 <= t0 + band.right && s0 + kTile <= at.len;
+        turn(kt, vt, std::true_type{}, all, s0);
+    }
+    for (int j = some; j < tiles; ++j) {
+        char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
+        if (a.D != DP) {
+            ks.clear(a.D);
+            vs.clear(a.D);
+        }
+        ks.lay(kt);
+        vs.lay(vt);
+        __syncthreads();
+        if (j + 1 < tiles) {
+            const int s0 = (order.low + j + 1 - some) * kTile;
+            ks.send_all(k, a.pk, a.D, s0);
+            vs.send_all(v, a.pv, a.D, s0);
+        }
+        turn(kt, vt, std::false_type{}, true, 0);
     }
     if (t < a.T) put_rows<E, DP>((char*)a.dq + (row * a.pdq + (size_t)at.head * a.D) * 2, a.D, acc, band.scale, there);
 }
 
-// What a tile of 64 queries and their dy adds to the gradients of a wavefront's 32 keys (DK) and values (DV); of blocks FROM .. TO - 1 of its 32 queries.
-template <typename E, int DP, bool DK, bool DV>
+// What a tile of 64 queries and their dy adds to the gradients of a wavefront's 32 keys (DK) and values (DV); of blocks from .. to - 1 of its 32 queries.
+// LIMITS: not all of them may see the wavefront's.
+template <typename E, int DP, bool DK, bool DV, bool LIMITS>
 __device__ __forceinline__ void key_tile(const char* qt, const char* yt, const float* st, const Reads<DP>& reads, const u4 (&kf)[DP / 16],
-                                         const u4 (&vf)[DP / 16], float c2, bool all, const Sight& sight, int t0, int from, int to, f16x* dk, f16x* dv)
+                                         const u4 (&vf)[DP / 16], float c2, const Sight& sight, int t0, int from, int to, f16x* dk, f16x* dv)
 {
     const int h = (int)threadIdx.x % kWave >> 5;
     // (both gradients' sums and operands leave no registers for two blocks at a time)
-    constexpr int kAtOnce = DK && DV ? 1 : 2;
+    constexpr int kAtOnce = 1;
 #pragma unroll kAtOnce
     for (int n = from; n < to; ++n) {
         f16x p = zeros16(), e = zeros16();
@@ -643,13 +760,9 @@ __device__ __forceinline__ void key_tile(const char* qt, const char* yt, const f
                 if constexpr (DK) e[i + x] = p[i + x] * (e[i + x] - delta[x]);
             }
         }
-        if constexpr (DV) in_place(p);
-        if constexpr (DK) in_place(e);
-        if (!all) {
-            if constexpr (DV) sight.apply(p, t0 + 32 * n, 0.f);
-            if constexpr (DK) sight.apply(e, t0 + 32 * n, 0.f);
-            if constexpr (DV) in_place(p);
-            if constexpr (DK) in_place(e);
+        if constexpr (LIMITS) {
+            if constexpr (DV) sight.apply<false>(p, t0 + 32 * n, 0.f);
+            if constexpr (DK) sight.apply<false>(e, t0 + 32 * n, 0.f);
         }
         u4 f[2];
         if constexpr (DV) {
@@ -688,8 +801,8 @@ __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at
     // frames that see the workgroup's
     const int lo = g0 - band.right > 0 ? g0 - band.right : 0;
     const int hi = g0 >= at.len ? 0 : (long long)g0 + kOwn + band.left < at.len ? g0 + kOwn + band.left : at.len;
-    const int first = lo / kTile, last = (hi + kTile - 1) / kTile;
-    const int per = last > first ? last - first : 0, tiles = per * (to - from);
+    const Order order(g0, g0 + kOwn < at.len ? g0 + kOwn : at.len, band.right, band.left, lo, hi, at.len, 0);
+    const int some = order.some;
     const auto exists = [&](int t) { return (t >= lo) & (t < hi); };
     // t sees s: s - right <= t <= s + left
     const Sight sight{s - band.right, !there ? 0 : (long long)s + band.left + 1 < at.len ? s + band.left + 1 : at.len, 0};
@@ -700,42 +813,68 @@ __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at
     Reads<DP> reads;
     reads.init();
     float stat = 0.f;
-    // Turn j is tile first + j % per of head from + j / per.  Formed anew each time with both gradients, counted with one: what leaves the compiler
-    // registers (16 x 1024, 8 heads of 64 columns in a band 80.5 us, counted 85; 2 x 4096, 16 heads of 128 626 us, counted 594).
-    constexpr bool kCount = !(DK && DV);
-    int head_next = from, t_next = first, t_now = first;
-    const auto get = [&](int j) {
-        const int head = kCount ? head_next : from + j / per, t0 = (kCount ? t_next : first + j % per) * kTile;
+    const auto get_stat = [&](int head, int t) {
+        const size_t i = (at.row0 + t) * a.heads + head;
+        stat = *(threadIdx.x < kTile ? a.lse + i : a.delta + i);
+    };
+    const auto lay_stat = [&](float* st) {
+        if (threadIdx.x < 2 * kTile) st[threadIdx.x] = threadIdx.x < kTile ? stat * kLog2e : stat;
+    };
+    const auto get = [&](int head, int t0) {
         const bool all = t0 >= lo && t0 + kTile <= hi;
         qs.send((const char*)a.q + (at.row0 * a.pq + (size_t)head * a.D) * 2, a.pq, a.D, t0, all, hi - 1, exists);
         ys.send((const char*)a.dy + (at.row0 * a.pdy + (size_t)head * a.D) * 2, a.pdy, a.D, t0, all, hi - 1, exists);
         const int t = t0 + (int)threadIdx.x % kTile;
         stat = 0.f;
-        if (threadIdx.x < 2 * kTile && exists(t)) {
-            const size_t i = (at.row0 + t) * a.heads + head;
-            stat = *(threadIdx.x < kTile ? a.lse + i : a.delta + i);
-        }
-        if (kCount && ++t_next == last) {
-            t_next = first;
-            ++head_next;
-        }
+        if (threadIdx.x < 2 * kTile && exists(t)) get_stat(head, t);
     };
-    if (tiles > 0) get(0);
+    // (of all heads first the tiles of which not all is seen, then the others)
+    const int turns = some * (to - from), all_turns = order.full * (to - from);
+    if (turns + all_turns > 0) get(from, order.start(0));
     have(kf);
     if constexpr (DK) have(vf);
-    for (int j = 0; j < tiles; ++j) {
-        const int t0 = (kCount ? t_now : first + j % per) * kTile;
-        if (kCount) t_now = t_now + 1 == last ? first : t_now + 1;
+    int head = from, i = 0;
+    for (int j = 0; j < turns; ++j) {
+        const int t0 = order.start(i);
         char *const qt = lds[j & 1], *const yt = qt + Rows<DP>::kBytes;
         float* const st = stats[j & 1][0];
         qs.lay(qt, a.D, t0, exists);
         ys.lay(yt, a.D, t0, exists);
-        if (threadIdx.x < 2 * kTile) st[threadIdx.x] = threadIdx.x < kTile ? stat * kLog2e : stat;
+        lay_stat(st);
         __syncthreads();
-        if (j + 1 < tiles) get(j + 1);
+        if (++i == some) {
+            i = 0;
+            ++head;
+        }
+        const bool more = j + 1 < turns;
+        if (more || all_turns > 0) get(more ? head : from, more ? order.start(i) : order.low * kTile);
         if (s0 >= at.len || t0 + kTile <= s0 - band.right || t0 > (long long)s0 + 31 + band.left) continue;
-        const bool all = t0 >= s0 + 31 - band.right && t0 + kTile - 1 <= (long long)s0 + band.left && t0 + kTile <= at.len && s0 + 32 <= at.len;
-        key_tile<E, DP, DK, DV>(qt, yt, st, reads, kf, vf, c2, all, sight, t0, 0, 2, dk, dv);
+        key_tile<E, DP, DK, DV, true>(qt, yt, st, reads, kf, vf, c2, sight, t0, 0, 2, dk, dv);
+    }
+    head = from;
+    i = 0;
+    for (int j = turns; j < turns + all_turns; ++j) {
+        char *const qt = lds[j & 1], *const yt = qt + Rows<DP>::kBytes;
+        float* const st = stats[j & 1][0];
+        if (a.D != DP) {
+            qs.clear(a.D);
+            ys.clear(a.D);
+        }
+        qs.lay(qt);
+        ys.lay(yt);
+        lay_stat(st);
+        __syncthreads();
+        if (++i == order.full) {
+            i = 0;
+            ++head;
+        }
+        if (j + 1 < turns + all_turns) {
+            const int t0 = (order.low + i) * kTile;
+            qs.send_all((const char*)a.q + (at.row0 * a.pq + (size_t)head * a.D) * 2, a.pq, a.D, t0);
+            ys.send_all((const char*)a.dy + (at.row0 * a.pdy + (size_t)head * a.D) * 2, a.pdy, a.D, t0);
+            if (threadIdx.x < 2 * kTile) get_stat(head, t0 + (int)threadIdx.x % kTile);
+        }
+        key_tile<E, DP, DK, DV, false>(qt, yt, st, reads, kf, vf, c2, sight, 0, 0, 2, dk, dv);
     }
     if (s >= a.T) return;
     if (a.parts > 1) {
@@ -843,7 +982,7 @@ __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void grad_first_kernel(Atte
         __syncthreads();
         if (j + 1 < last) get(t0 + kTile);
         if (s0 >= band.sinks) continue;
-        key_tile<E, DP, true, true>(qt, yt, st, reads, kf, vf, c2, false, sight, t0, half, half + 1, dk, dv);
+        key_tile<E, DP, true, true, true>(qt, yt, st, reads, kf, vf, c2, sight, t0, half, half + 1, dk, dv);
     }
     if (s >= band.sinks) return;
     const int share = ((at.head % group) * (int)a.tiles + at.tile) * 2 + half;

@@ -86,6 +86,61 @@ def test_scales_and_large_scores(scale):
         assert_within(x, w, rounded(e, w, "bf16"), name)
 
 
+MANY = [  # of more than 512 workgroups of 128 frames, which have one wavefront for 32 frames
+    (44, 300, 4, 2, 64, None, None, 0, "f16", True, 0),
+    (70, 260, 4, 1, 40, 100, 20, 5, "bf16", True, 1),
+    (66, 520, 2, 1, 128, 300, 0, 3, "bf16", True, 0),
+    (130, 400, 1, 1, 24, None, 0, 0, "f16", False, 0),
+]
+
+
+@pytest.mark.parametrize("grows", [0.0, 3.0])
+@pytest.mark.parametrize("case", MANY, ids=str)
+def test_many_workgroups(case, grows):
+    """Also with scores that pass the ones before them by more than what sums are kept relative to, again and again."""
+    announce(case, grows)
+    q, k, v, dy, n, there, band = inputs(case)
+    if grows:
+        k *= torch.linspace(0.1, grows, case[1], device="cuda")[:, None].to(k.dtype)
+    D, kind, scale = case[4], case[8], 2.0 if grows else case[4] ** -0.5
+    want, e, L, eL = whole_attention(f64(q), f64(k), f64(v), D, n, *band.values(), scale, kind)
+    for x in (q, k, v):
+        spoil(x, there)
+    y, lse = lb.last_attention(q, k, v, D, lengths=dev(n), scale=scale, **band)
+    assert_within(lse, L, eL, "lse")
+    assert_within(y, want, rounded(e, want, kind), "y")
+    for x in (q, k, v):
+        x[torch.from_numpy(~there).cuda()] = 0
+    want = whole_attention_grad(*(f64(x) for x in (dy, q, k, v, y, lse)), D, n, *band.values(), scale, kind)
+    for x in (q, k, v, dy, y):
+        spoil(x, there)
+    got = lb.last_attention_grad(dy, q, k, v, y, lse, D, lengths=dev(n), scale=scale, **band)
+    for x, (w, e), name in zip(got, want, ("dq", "dk", "dv")):
+        assert_within(x, w, rounded(e, w, kind), name)
+
+
+@pytest.mark.parametrize("B", [2, 70])
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+def test_a_bad_key_that_many_see(B, bad):
+    """A frame of item 1 with a NaN or an infinity in its key, in a tile that others see whole: theirs are NaN, or what they are without it where the
+    score is -inf; other items' results are what they are."""
+    case = (B, 400, 2, 1, 64, 200, 50, 0, "bf16", False, 0)
+    announce("bad key", B, bad)
+    q, k, v, _, n, there, band = inputs(case)
+    y0, l0 = lb.last_attention(q, k, v, 64, **band)
+    k[1, 130, 7] = float(bad)
+    y, lse = lb.last_attention(q, k, v, 64, **band)
+    one = torch.ones(B, dtype=torch.bool, device="cuda")
+    one[1] = False
+    assert torch.equal(y[one], y0[one]) and torch.equal(lse[one], l0[one])
+    t = torch.arange(400, device="cuda")
+    sees = (130 <= t + 50) & (130 >= t - 200)
+    assert torch.equal(lse[1, ~sees], l0[1, ~sees]) and torch.equal(y[1, ~sees], y0[1, ~sees])
+    heads = torch.isnan(y[1].view(400, 2, 64)).any(-1)
+    assert torch.equal(heads, torch.isnan(y[1].view(400, 2, 64)).all(-1)) and torch.equal(heads, torch.isnan(lse[1]))
+    assert bool(heads[sees].all()) if bad == "nan" else bool((heads[sees] == (q[1, sees].view(-1, 2, 64)[:, :, 7] >= 0)).all())
+
+
 @pytest.mark.parametrize("bad", ["nan value", "nan key", "inf value", "inf key"])
 @pytest.mark.parametrize("width", [40, 128])
 def test_what_is_not_seen_has_no_part(bad, width):
