@@ -456,6 +456,10 @@ struct Order {
 
 // HALVES: a workgroup has 64 frames instead of 128, and two wavefronts for each 32 of them, one for either half of each tile, whose sums are joined at the end:
 // twice as many workgroups of half the length.
+// A tile of 64 columns is 16 products of 32 clocks for a SIMD, and 120 vector instructions beside them, 32 of them exponentials of 8 clocks.  Of 128
+// columns: 900 TF (8 x 2048 frames, 16 heads, all seen; the matrix cores are busy 38% of the time, at 1.8 GHz); of 64: 670 TF (64 x 1024, 8 heads).
+// Measured and left: 64 frames a wavefront, half the LDS reads but one wavefront a SIMD (8192 frames, 16 heads of 128: 182 us, so 110); a
+// block of 32 of the tile at a time (16 x 1000, 8 heads of 64: 59 us, so 53).
 template <typename E, int DP, bool HALVES>
 __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(AttentionArgs a)
 {
@@ -629,7 +633,9 @@ __device__ __forceinline__ float row_product(const u4 (&x)[N], const u4 (&y)[N])
     return sum_of_halves(sum);
 }
 
-// The gradient of queries: a wavefront's own frames are queries, the tiles keys and values.  It comes first, and leaves delta for the others.
+// The gradient of queries: a wavefront's own frames are queries, the tiles keys and values.  It comes first, and leaves delta for the others (a kernel of its
+// own for delta: 7 us of 81 at 16 x 1024 frames, 8 heads of 64 in a band).  Three products a tile; 230 us at 2 x 4096, 16 heads of 128 that see 2047
+// back (670 TF).
 template <typename E, int DP>
 __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
 {
@@ -783,7 +789,8 @@ __device__ __forceinline__ void key_tile(const char* qt, const char* yt, const f
 }
 
 // The gradients of keys (DK) and values (DV): a wavefront's own frames are keys, the tiles queries and their dy, of the heads that share the keys, or
-// of a part of them, whose sums grad_join_kernel adds.
+// of a part of them, whose sums grad_join_kernel adds (1 x 4096, 16 heads of 128 on one: the whole gradient 2522 us undivided, 411 in 16 parts).  No
+// atomics: every sum has one order.
 template <typename E, int DP, bool DK, bool DV>
 __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at, char (*lds)[2 * Rows<DP>::kBytes], float (*stats)[2][kTile])
 {
@@ -914,7 +921,8 @@ __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at
 }
 
 // APART: workgroups of a second half form the values' gradients, those of the first the keys', since both sums and operands of 128 columns do not leave
-// registers for two wavefronts on a SIMD; the scores are formed twice, which is a product of five.
+// registers for two wavefronts on a SIMD; the scores are formed twice, which is a product of five (8 x 2048 frames, 16 heads: the whole gradient
+// 1503 us with both in one, 1185 apart).  370 us at 2 x 4096, 16 heads that see 2047 back: 690 TF with the scores counted twice.
 template <typename E, int DP, bool APART>
 __global__ __launch_bounds__(256, 2) void grad_key_kernel(AttentionArgs a)
 {
@@ -930,7 +938,8 @@ __global__ __launch_bounds__(256, 2) void grad_key_kernel(AttentionArgs a)
 }
 
 // The part that first frames s < sinks have in frames t > s + left: a workgroup takes a chunk of these of one head, a wavefront 32 first frames and half
-// of each tile.  Sums go to `part`, [item][kv head][share][2][64][DP], a share for each head of the group, chunk and half.
+// of each tile (in grad_key_kernel's workgroup of the first frames, which then goes over all of the item, 146 us at 2 x 4096; here 24, and 5 for the
+// join).  Sums go to `part`, [item][kv head][share][2][64][DP], a share for each head of the group, chunk and half.
 template <typename E, int DP>
 __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void grad_first_kernel(AttentionArgs a)
 {
@@ -996,7 +1005,8 @@ __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void grad_first_kernel(Atte
         }
 }
 
-// Gradients of keys and values from the parts' sums [2][part][row][kv head][DP], in order: four columns a thread.
+// Gradients of keys and values from the parts' sums [2][part][row][kv head][DP], in order: four columns a thread.  Bound by reading them: 15 us for two
+// parts of 8192 x 4 heads of 128 (75 MB).
 template <typename E>
 __global__ __launch_bounds__(256) void grad_join_kernel(AttentionArgs a, int DP, long long first)
 {
