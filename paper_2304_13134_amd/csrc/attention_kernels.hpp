@@ -498,39 +498,49 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
     };
     if (tiles > 0) get(order.start(0));
     have(qf);
-    const auto multiply = [&](const char* vt, f16x* s) {
+    // N blocks of 32 of a tile's frames, from block `n0` on
+    const auto scores = [&](const char* kt, int n0, auto N, f16x* s) {
 #pragma unroll
-        for (int n = 0; n < kBlocks; ++n) {
+        for (int n = 0; n < N; ++n) s[n] = zeros16();
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[n] = Mma<E>::go(reads.along_rows(kt, n0 + n, i), qf[i], s[n]);
+    };
+    const auto multiply = [&](const char* vt, int n0, auto N, f16x* s) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
             u4 p[2];
             to_operands<E>(s[n], p);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) soft.acc[d] = Mma<E>::go(reads.along_columns(vt, d, 2 * (half + n) + i), p[i], soft.acc[d]);
+                for (int d = 0; d < DP / 32; ++d) soft.acc[d] = Mma<E>::go(reads.along_columns(vt, d, 2 * (n0 + n) + i), p[i], soft.acc[d]);
         }
     };
-    const auto scores = [&](const char* kt, f16x* s) {
-#pragma unroll
-        for (int n = 0; n < kBlocks; ++n) s[n] = zeros16();
-#pragma unroll
-        for (int i = 0; i < DP / 16; ++i)
-#pragma unroll
-            for (int n = 0; n < kBlocks; ++n) s[n] = Mma<E>::go(reads.along_rows(kt, half + n, i), qf[i], s[n]);
-    };
+    typedef std::integral_constant<int, 1> One;
+    typedef std::integral_constant<int, kBlocks> All;
     for (int j = 0; j < some; ++j) {
-        const int tile0 = order.start(j), s0 = tile0 + 32 * half;
+        const int s0 = order.start(j);
         char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
-        ks.lay(kt, a.D, tile0, exists);
-        vs.lay(vt, a.D, tile0, exists);
+        ks.lay(kt, a.D, s0, exists);
+        vs.lay(vt, a.D, s0, exists);
         __syncthreads();                             // (the other buffer is written again after the next one)
         if (j + 1 < tiles) get(order.start(j + 1));
-        if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + 32 * kBlocks <= t0 - band.left && s0 >= band.sinks)) continue;
-        f16x s[kBlocks];
-        scores(kt, s);
-#pragma unroll
-        for (int n = 0; n < kBlocks; ++n) sight.apply(s[n], s0 + 32 * n, LAST_NEG_INF);
-        soft.template take<kBlocks>(s, c2);
-        multiply(vt, s);
+        if (t0 >= at.len) continue;
+        // blocks of which anything is seen
+        const auto unseen = [&](int n) { return s0 + 32 * n >= t0 + 32 + band.right || (s0 + 32 * n + 32 <= t0 - band.left && s0 + 32 * n >= band.sinks); };
+        int n = HALVES ? half : 0, end = HALVES ? half + 1 : 2;
+        if (unseen(n)) ++n;
+        if (n < end && unseen(end - 1)) --end;
+#pragma unroll 1
+        for (; n < end; ++n) {
+            f16x s;
+            scores(kt, n, One{}, &s);
+            sight.apply(s, s0 + 32 * n, LAST_NEG_INF);
+            soft.template take<1>(&s, c2);
+            multiply(vt, n, One{}, &s);
+        }
     }
     // Relative to the reference there is, without a look at the maximum.  Where that gives a sum that is none (no reference yet: the exponent is
     // -inf) or beyond 2^15, which a type of 16 bits holds, the loop is left to raise the reference, and entered again with the same tile.
@@ -557,15 +567,15 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
                     vs.send_all(v, a.pv, a.D, s0);
                 }
             }
-            scores(kt, s);
+            scores(kt, half, All{}, s);
             const float sum = soft.template powers<kBlocks>(s, c2, by);
             if (!raised && __any(!(sum <= 0x1p15f))) break;
             raised = false;
             soft.l += sum;
-            multiply(vt, s);
+            multiply(vt, half, All{}, s);
         }
         if (j >= tiles) break;
-        scores(kt, s);
+        scores(kt, half, All{}, s);
         soft.template raise<kBlocks>(s, c2);
         by = soft.m == LAST_NEG_INF ? 0.f : soft.m * c2;
         raised = true;
@@ -680,9 +690,10 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
     have(qf);
     have(df);
     asm volatile("" : "+v"(l2), "+v"(delta));
-    const auto turn = [&](const char* kt, const char* vt, auto limits, bool all, int s0) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
+    const auto turn = [&](const char* kt, const char* vt, auto limits, bool all, int s0, int from, int to) {
+        constexpr int kAtOnce = limits ? 1 : 2;
+#pragma unroll kAtOnce
+        for (int n = from; n < to; ++n) {
             f16x s = zeros16(), p = zeros16();
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) {
@@ -717,7 +728,8 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
         if (j + 1 < tiles) get(order.start(j + 1));
         if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + kTile <= t0 - band.left && s0 >= band.sinks)) continue;
         const bool all = s0 >= t0 + 31 - band.left && s0 + kTile - 1 <= t0 + band.right && s0 + kTile <= at.len;
-        turn(kt, vt, std::true_type{}, all, s0);
+        const int from = s0 + 32 <= t0 - band.left && s0 >= band.sinks ? 1 : 0, to = s0 + 32 >= t0 + 32 + band.right ? 1 : 2;
+        turn(kt, vt, std::true_type{}, all, s0, from, to);
     }
     for (int j = some; j < tiles; ++j) {
         char *const kt = lds[j & 1], *const vt = kt + Rows<DP>::kBytes;
@@ -733,7 +745,7 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
             ks.send_all(k, a.pk, a.D, s0);
             vs.send_all(v, a.pv, a.D, s0);
         }
-        turn(kt, vt, std::false_type{}, true, 0);
+        turn(kt, vt, std::false_type{}, true, 0, 0, 2);
     }
     if (t < a.T) put_rows<E, DP>((char*)a.dq + (row * a.pdq + (size_t)at.head * a.D) * 2, a.D, acc, band.scale, there);
 }
@@ -856,7 +868,8 @@ __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at
         const bool more = j + 1 < turns;
         if (more || all_turns > 0) get(more ? head : from, more ? order.start(i) : order.low * kTile);
         if (s0 >= at.len || t0 + kTile <= s0 - band.right || t0 > (long long)s0 + 31 + band.left) continue;
-        key_tile<E, DP, DK, DV, true>(qt, yt, st, reads, kf, vf, c2, sight, t0, 0, 2, dk, dv);
+        const int from_block = t0 + 32 <= s0 - band.right ? 1 : 0, to_block = t0 + 32 > (long long)s0 + 31 + band.left ? 1 : 2;
+        key_tile<E, DP, DK, DV, true>(qt, yt, st, reads, kf, vf, c2, sight, t0, from_block, to_block, dk, dv);
     }
     head = from;
     i = 0;
