@@ -571,6 +571,7 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
             const float sum = soft.template powers<kBlocks>(s, c2, by);
             if (!raised && __any(!(sum <= 0x1p15f))) break;
             raised = false;
+            by = soft.m * c2;                        // (again -inf where all scores were)
             soft.l += sum;
             multiply(vt, half, All{}, s);
         }

@@ -141,6 +141,21 @@ def test_a_bad_key_that_many_see(B, bad):
     assert bool(heads[sees].all()) if bad == "nan" else bool((heads[sees] == (q[1, sees].view(-1, 2, 64)[:, :, 7] >= 0)).all())
 
 
+@pytest.mark.parametrize("B", [1, 150])
+def test_scores_of_minus_infinity_first(B):
+    """Three tiles of keys whose scores are -inf, which have no part, before scores that are far below zero: the others' result, as when they are alone."""
+    announce("-inf first", B)
+    T, D, none = 400, 64, 192
+    q, k, v, _, n, _, _ = inputs((B, T, 1, 1, D, None, None, 0, "bf16", False, 0))
+    q[..., 7], q[..., 8], k[:, :none, 7], k[:, none:, 7], k[:, :, 8] = 1, 4, float("-inf"), 0, -100
+    y, lse = lb.last_attention(q, k, v, D, right=None, scale=1.0)
+    some = T - none
+    want, e, L, eL = whole_attention(f64(q[:1, :some]), f64(k[:1, none:]), f64(v[:1, none:]), D, n, None, None, 0, 1.0, "bf16")
+    assert_within(lse[:1, :some], L, eL, "lse")
+    assert_within(y[:1, :some], want, rounded(e, want, "bf16"), "y")
+    assert bool(torch.isfinite(y).all()) and bool(torch.isfinite(lse).all())
+
+
 @pytest.mark.parametrize("bad", ["nan value", "nan key", "inf value", "inf key"])
 @pytest.mark.parametrize("width", [40, 128])
 def test_what_is_not_seen_has_no_part(bad, width):
