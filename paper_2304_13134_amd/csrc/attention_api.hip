@@ -157,13 +157,14 @@ int padded(int width) { return width <= 32 ? 32 : width <= 64 ? 64 : 128; }
 // Heads that share keys go to one XCD together where that gives each as many.
 unsigned heads_together(const AttentionArgs& a) { return a.B * a.kv_heads % 8 == 0 ? (unsigned)(a.heads / a.kv_heads) : 1u; }
 
+// Two wavefronts for 32 frames where there are no more than two workgroups of 128 a compute unit: 1 x 4096, 16 heads of 128 on one (512 workgroups)
+// 133 -> 111 us, 1 x 2048, 8 of 64 36 -> 29; of 1024 workgroups 16 x 1000, 8 of 64 48 -> 53, 1 x 8192, 16 of 128 109 -> 130.
+bool in_halves(const AttentionArgs& a) { return (long long)((a.T + kOwn - 1) / kOwn) * a.heads * a.B <= 512; }
+
 template <typename E>
 void launch_attention(AttentionArgs a, hipStream_t st)
 {
-    // Two wavefronts for 32 frames where there are no more than two workgroups a compute unit: 1 x 4096, 16 heads of 128 on one (512 workgroups of
-    // 128 frames) 133 -> 111 us, 1 x 2048, 8 of 64 36 -> 29; of 1024 workgroups 16 x 1000, 8 of 64 48 -> 53, 1 x 8192, 16 of 128 109 -> 130.
-    const long long groups = (long long)((a.T + kOwn - 1) / kOwn) * a.heads * a.B;
-    const bool halves = groups <= 512;
+    const bool halves = in_halves(a);
     const int frames = halves ? kOwn / 2 : kOwn;
     a.tiles = (unsigned)((a.T + frames - 1) / frames);
     a.together = heads_together(a);
@@ -213,11 +214,14 @@ GradPlan plan_grad(Carver& cv, long long rows, const last_frames_t* f, const las
 template <typename E>
 void launch_attention_grad(AttentionArgs a, int chunks, hipStream_t st)
 {
-    a.tiles = (unsigned)((a.T + kOwn - 1) / kOwn);
+    const bool halves = in_halves(a);
+    const int frames = halves ? kOwn / 2 : kOwn;
+    a.tiles = (unsigned)((a.T + frames - 1) / frames);
     a.together = heads_together(a);
     in_launches((long long)a.tiles * a.heads * a.B, [&](long long first, dim3 grid) {
         a.first = (unsigned)first;
-        LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_query_kernel<E, DP>), grid, dim3(256), 0, st, a));
+        if (halves) LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_query_kernel<E, DP, true>), grid, dim3(256), 0, st, a));
+        else LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_query_kernel<E, DP, false>), grid, dim3(256), 0, st, a));
     });
     a.together = 1;
     if (chunks) {

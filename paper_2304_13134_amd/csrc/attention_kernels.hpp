@@ -647,13 +647,15 @@ __device__ __forceinline__ float row_product(const u4 (&x)[N], const u4 (&y)[N])
 // The gradient of queries: a wavefront's own frames are queries, the tiles keys and values.  It comes first, and leaves delta for the others (a kernel of its
 // own for delta: 7 us of 81 at 16 x 1024 frames, 8 heads of 64 in a band).  Three products a tile; 230 us at 2 x 4096, 16 heads of 128 that see 2047
 // back (670 TF).
-template <typename E, int DP>
+template <typename E, int DP, bool HALVES>
 __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
 {
+    constexpr int kGroup = HALVES ? 64 : kOwn;
     __shared__ __attribute__((aligned(16))) char lds[2][2 * Rows<DP>::kBytes];
     const Place at = place_of(a, a.first + blockIdx.x, a.heads);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x % kWave;
-    const int g0 = at.tile * kOwn, t0 = g0 + wave * 32, t = t0 + (lane & 31);
+    const int half = HALVES ? wave / 2 : 0;
+    const int g0 = at.tile * kGroup, t0 = g0 + (HALVES ? wave % 2 : wave) * 32, t = t0 + (lane & 31);
     const Band band = a.band;
     const float c2 = band.scale * kLog2e;
     const bool there = t < at.len;
@@ -668,11 +670,11 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
         u4 yf[DP / 16];
         own_rows<DP>(there ? (const char*)a.y + (row * a.py + (size_t)at.head * a.D) * 2 : nullptr, a.D, yf);
         delta = row_product<E>(df, yf);
-        if (there && lane < 32) a.delta[row * a.heads + at.head] = delta;
+        if (there && lane < 32 && half == 0) a.delta[row * a.heads + at.head] = delta;
     }
     const int lo = g0 - band.left > 0 ? g0 - band.left : 0;
-    const int hi = g0 >= at.len ? 0 : g0 + kOwn + band.right < at.len ? g0 + kOwn + band.right : at.len;
-    const Order order(g0, g0 + kOwn < at.len ? g0 + kOwn : at.len, band.left, band.right, lo, hi, at.len, band.sinks > 0);
+    const int hi = g0 >= at.len ? 0 : g0 + kGroup + band.right < at.len ? g0 + kGroup + band.right : at.len;
+    const Order order(g0, g0 + kGroup < at.len ? g0 + kGroup : at.len, band.left, band.right, lo, hi, at.len, band.sinks > 0);
     const int some = order.some, tiles = order.tiles();
     const auto exists = [&](int s) { return (s < hi) & ((s >= lo) | (s < band.sinks)); };
     const Sight sight = sight_of(t, at.len, band);
@@ -692,7 +694,7 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
     have(df);
     asm volatile("" : "+v"(l2), "+v"(delta));
     const auto turn = [&](const char* kt, const char* vt, auto limits, bool all, int s0, int from, int to) {
-        constexpr int kAtOnce = limits ? 1 : 2;
+        constexpr int kAtOnce = limits || HALVES ? 1 : 2;
 #pragma unroll kAtOnce
         for (int n = from; n < to; ++n) {
             f16x s = zeros16(), p = zeros16();
@@ -729,7 +731,11 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
         if (j + 1 < tiles) get(order.start(j + 1));
         if (s0 >= t0 + 32 + band.right || t0 >= at.len || (s0 + kTile <= t0 - band.left && s0 >= band.sinks)) continue;
         const bool all = s0 >= t0 + 31 - band.left && s0 + kTile - 1 <= t0 + band.right && s0 + kTile <= at.len;
-        const int from = s0 + 32 <= t0 - band.left && s0 >= band.sinks ? 1 : 0, to = s0 + 32 >= t0 + 32 + band.right ? 1 : 2;
+        int from = s0 + 32 <= t0 - band.left && s0 >= band.sinks ? 1 : 0, to = s0 + 32 >= t0 + 32 + band.right ? 1 : 2;
+        if (HALVES) {
+            from = from > half ? from : half;
+            to = to < half + 1 ? to : half + 1;
+        }
         turn(kt, vt, std::true_type{}, all, s0, from, to);
     }
     for (int j = some; j < tiles; ++j) {
@@ -746,7 +752,23 @@ __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
             ks.send_all(k, a.pk, a.D, s0);
             vs.send_all(v, a.pv, a.D, s0);
         }
-        turn(kt, vt, std::false_type{}, true, 0, 0, 2);
+        turn(kt, vt, std::false_type{}, true, 0, half, HALVES ? half + 1 : 2);
+    }
+    if constexpr (HALVES) {
+        float* const sums = (float*)lds[0] + wave % 2 * (DP / 32 * 16 * kWave);
+        __syncthreads();
+        if (half == 1) {
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums[(d * 16 + i) * kWave + lane] = acc[d][i];
+        }
+        __syncthreads();
+        if (half == 1) return;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] += sums[(d * 16 + i) * kWave + lane];
     }
     if (t < a.T) put_rows<E, DP>((char*)a.dq + (row * a.pdq + (size_t)at.head * a.D) * 2, a.D, acc, band.scale, there);
 }
