@@ -187,11 +187,21 @@ struct GradPlan {
     float *delta, *part, *sums, *kept;
 };
 
-// Heads that share keys go in parts where there are fewer than 1024 workgroups, two rounds of what fits: 1 x 4096, 16 heads of 128 on one 411 us (503 with
-// 512), 2 x 4096, 16 on four 567 (582 in one part).
+long long key_groups(int B, int T, int kv_heads, int width)
+{
+    return (long long)B * kv_heads * ((T + kOwn - 1) / kOwn) * (padded(width) == 128 ? 2 : 1);
+}
+
+// Two wavefronts for 32 keys where there is no more than one workgroup of 128 a compute unit: 1 x 2048, 8 heads of 64 on one 71 -> 60 us, 1 x 700, 8 of
+// 64 31 -> 27; of 512 workgroups 2 x 4096, 16 of 128 on four 571 -> 599.
+bool keys_in_halves(long long groups) { return groups <= 256; }
+
+// Heads that share keys go in parts where there are fewer than 1024 workgroups, two rounds of what fits: before halves 1 x 4096, 16 heads of 128 on one 411
+// us (503 with 512 workgroups, 2522 in one part), 2 x 4096, 16 on four 567 (582 in one part).
 int grad_parts(const last_frames_t* f, const last_heads_t* h)
 {
-    const long long groups = (long long)f->B * h->kv_heads * ((f->T + kOwn - 1) / kOwn) * (padded(h->width) == 128 ? 2 : 1);
+    long long groups = key_groups(f->B, f->T, h->kv_heads, h->width);
+    if (keys_in_halves(groups)) groups *= 2;
     return (int)std::max(1ll, std::min<long long>(h->heads / h->kv_heads, 1024 / std::max(1ll, groups)));
 }
 
@@ -234,13 +244,14 @@ void launch_attention_grad(AttentionArgs a, int chunks, hipStream_t st)
             hipLaunchKernelGGL(first_join_kernel, grid, dim3(128), 0, st, (const float*)a.part, a.sums, a.shares, padded(a.D), a.band.sinks, first);
         });
     }
-    a.tiles = (unsigned)((a.T + kOwn - 1) / kOwn);
+    const bool keys_halved = keys_in_halves(key_groups(a.B, a.T, a.kv_heads, a.D));
+    const int keys = keys_halved ? kOwn / 2 : kOwn;
+    a.tiles = (unsigned)((a.T + keys - 1) / keys);
     a.half = a.tiles * (unsigned)(a.kv_heads * a.parts * a.B);
     in_launches((long long)a.half * (padded(a.D) == 128 ? 2 : 1), [&](long long first, dim3 grid) {
         a.first = (unsigned)first;
-        if (padded(a.D) == 128) hipLaunchKernelGGL((grad_key_kernel<E, 128, true>), grid, dim3(256), 0, st, a);
-        else if (padded(a.D) == 64) hipLaunchKernelGGL((grad_key_kernel<E, 64, false>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((grad_key_kernel<E, 32, false>), grid, dim3(256), 0, st, a);
+        if (keys_halved) LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_key_kernel<E, DP, DP == 128, true>), grid, dim3(256), 0, st, a));
+        else LAST_BY_WIDTH(a.D, hipLaunchKernelGGL((grad_key_kernel<E, DP, DP == 128, false>), grid, dim3(256), 0, st, a));
     });
     if (a.parts > 1) {
         in_launches((2ll * a.B * a.T * a.kv_heads * (padded(a.D) / 4) + 255) / 256, [&](long long first, dim3 grid) {

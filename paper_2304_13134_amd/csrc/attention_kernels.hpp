@@ -824,14 +824,16 @@ __device__ __forceinline__ void key_tile(const char* qt, const char* yt, const f
 }
 
 // The gradients of keys (DK) and values (DV): a wavefront's own frames are keys, the tiles queries and their dy, of the heads that share the keys, or
-// of a part of them, whose sums grad_join_kernel adds (1 x 4096, 16 heads of 128 on one: the whole gradient 2522 us undivided, 411 in 16 parts).  No
+// of a part of them, whose sums grad_join_kernel adds (1 x 4096, 16 heads of 128 on one: the whole gradient 2522 us undivided, 434 in 16 parts).  No
 // atomics: every sum has one order.
-template <typename E, int DP, bool DK, bool DV>
+template <typename E, int DP, bool DK, bool DV, bool HALVES>
 __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at, char (*lds)[2 * Rows<DP>::kBytes], float (*stats)[2][kTile])
 {
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x % kWave;
     const Band band = a.band;
-    const int g0 = at.tile * kOwn, s0 = g0 + wave * 32, s = s0 + (lane & 31);
+    constexpr int kGroup = HALVES ? 64 : kOwn;
+    const int half = HALVES ? wave / 2 : 0;
+    const int g0 = at.tile * kGroup, s0 = g0 + (HALVES ? wave % 2 : wave) * 32, s = s0 + (lane & 31);
     const float c2 = band.scale * kLog2e;
     const bool there = s < at.len;
     const size_t row = at.row0 + s;
@@ -842,8 +844,8 @@ __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at
     if constexpr (DK) own_rows<DP>(there ? (const char*)a.v + (row * a.pv + (size_t)at.kv * a.D) * 2 : nullptr, a.D, vf);
     // frames that see the workgroup's
     const int lo = g0 - band.right > 0 ? g0 - band.right : 0;
-    const int hi = g0 >= at.len ? 0 : (long long)g0 + kOwn + band.left < at.len ? g0 + kOwn + band.left : at.len;
-    const Order order(g0, g0 + kOwn < at.len ? g0 + kOwn : at.len, band.right, band.left, lo, hi, at.len, 0);
+    const int hi = g0 >= at.len ? 0 : (long long)g0 + kGroup + band.left < at.len ? g0 + kGroup + band.left : at.len;
+    const Order order(g0, g0 + kGroup < at.len ? g0 + kGroup : at.len, band.right, band.left, lo, hi, at.len, 0);
     const int some = order.some;
     const auto exists = [&](int t) { return (t >= lo) & (t < hi); };
     // t sees s: s - right <= t <= s + left
@@ -891,7 +893,11 @@ __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at
         const bool more = j + 1 < turns;
         if (more || all_turns > 0) get(more ? head : from, more ? order.start(i) : order.low * kTile);
         if (s0 >= at.len || t0 + kTile <= s0 - band.right || t0 > (long long)s0 + 31 + band.left) continue;
-        const int from_block = t0 + 32 <= s0 - band.right ? 1 : 0, to_block = t0 + 32 > (long long)s0 + 31 + band.left ? 1 : 2;
+        int from_block = t0 + 32 <= s0 - band.right ? 1 : 0, to_block = t0 + 32 > (long long)s0 + 31 + band.left ? 1 : 2;
+        if (HALVES) {
+            from_block = from_block > half ? from_block : half;
+            to_block = to_block < half + 1 ? to_block : half + 1;
+        }
         key_tile<E, DP, DK, DV, true>(qt, yt, st, reads, kf, vf, c2, sight, t0, from_block, to_block, dk, dv);
     }
     head = from;
@@ -917,7 +923,28 @@ __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at
             ys.send_all((const char*)a.dy + (at.row0 * a.pdy + (size_t)head * a.D) * 2, a.pdy, a.D, t0);
             if (threadIdx.x < 2 * kTile) get_stat(head, t0 + (int)threadIdx.x % kTile);
         }
-        key_tile<E, DP, DK, DV, false>(qt, yt, st, reads, kf, vf, c2, sight, 0, 0, 2, dk, dv);
+        key_tile<E, DP, DK, DV, false>(qt, yt, st, reads, kf, vf, c2, sight, 0, half, HALVES ? half + 1 : 2, dk, dv);
+    }
+    if constexpr (HALVES) {
+        const auto join = [&](float* all, f16x* sums) {
+            float* const other = all + wave % 2 * (DP / 32 * 16 * kWave);
+            if (half == 1) {
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) other[(d * 16 + i) * kWave + lane] = sums[d][i];
+            }
+            __syncthreads();
+            if (half == 1) return;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums[d][i] += other[(d * 16 + i) * kWave + lane];
+        };
+        __syncthreads();
+        if constexpr (DK) join((float*)lds[0], dk);
+        if constexpr (DV) join((float*)lds[1], dv);
+        if (half == 1) return;
     }
     if (s >= a.T) return;
     if (a.parts > 1) {
@@ -956,20 +983,20 @@ __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at
     }
 }
 
-// APART: workgroups of a second half form the values' gradients, those of the first the keys', since both sums and operands of 128 columns do not leave
+// HALVES: as in attention_kernel.  APART: workgroups of a second half form the values' gradients, those of the first the keys', since both sums and operands of 128 columns do not leave
 // registers for two wavefronts on a SIMD; the scores are formed twice, which is a product of five (8 x 2048 frames, 16 heads: the whole gradient
 // 1503 us with both in one, 1185 apart).  370 us at 2 x 4096, 16 heads that see 2047 back: 690 TF with the scores counted twice.
-template <typename E, int DP, bool APART>
+template <typename E, int DP, bool APART, bool HALVES>
 __global__ __launch_bounds__(256, 2) void grad_key_kernel(AttentionArgs a)
 {
     __shared__ __attribute__((aligned(16))) char lds[2][2 * Rows<DP>::kBytes];
     __shared__ float stats[2][2][kTile];
     const unsigned id = a.first + blockIdx.x;
     if constexpr (APART) {
-        if (id >= a.half) grad_key<E, DP, false, true>(a, place_of(a, id - a.half, a.kv_heads * a.parts, true), lds, stats);
-        else grad_key<E, DP, true, false>(a, place_of(a, id, a.kv_heads * a.parts, true), lds, stats);
+        if (id >= a.half) grad_key<E, DP, false, true, HALVES>(a, place_of(a, id - a.half, a.kv_heads * a.parts, true), lds, stats);
+        else grad_key<E, DP, true, false, HALVES>(a, place_of(a, id, a.kv_heads * a.parts, true), lds, stats);
     } else {
-        grad_key<E, DP, true, true>(a, place_of(a, id, a.kv_heads * a.parts, true), lds, stats);
+        grad_key<E, DP, true, true, HALVES>(a, place_of(a, id, a.kv_heads * a.parts, true), lds, stats);
     }
 }
 
