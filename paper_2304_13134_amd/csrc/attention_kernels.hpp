@@ -456,8 +456,8 @@ struct Order {
 
 // HALVES: a workgroup has 64 frames instead of 128, and two wavefronts for each 32 of them, one for either half of each tile, whose sums are joined at the end:
 // twice as many workgroups of half the length.
-// A tile of 64 columns is 16 products of 32 clocks for a SIMD, and 120 vector instructions beside them, 32 of them exponentials of 8 clocks.  Of 128
-// columns: 900 TF (8 x 2048 frames, 16 heads, all seen; the matrix cores are busy 38% of the time, at 1.8 GHz); of 64: 670 TF (64 x 1024, 8 heads).
+// A tile of 64 columns is 16 products of 32 clocks for a SIMD, and 133 vector instructions beside them, 32 of them exponentials of 8 clocks.  Of 128
+// columns: 900 TF (8 x 2048 frames, 16 heads, all seen; the matrix cores are busy 42% of the time, at 1.8 GHz); of 64: 670 TF (64 x 1024, 8 heads; 38%).
 // Measured and left: 64 frames a wavefront, half the LDS reads but one wavefront a SIMD (8192 frames, 16 heads of 128: 182 us, so 110); a
 // block of 32 of the tile at a time (16 x 1000, 8 heads of 64: 59 us, so 53).
 template <typename E, int DP, bool HALVES>
