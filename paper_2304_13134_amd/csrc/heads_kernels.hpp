@@ -289,13 +289,13 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadArgs a)
             float v[8];
             unpack4<E>(x[0], v);
             unpack4<E>(x[1], v + 4);
-            if (of_q || of_k) {
+            // (a frame that is not there keeps its zeros, whatever the gains and frequencies are)
+            if (there && (of_q || of_k)) {
                 if (of_q ? s0.gain : s1.gain) {
                     float sum = 0.f;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) sum = __builtin_fmaf(v[c], v[c], sum);
-                    float inv = inverse_root(__builtin_fmaf(head_sum<LN>(sum), by_width, a.eps));
-                    inv = there ? inv : 0.f;                 // (a frame that is not there has zeros)
+                    const float inv = inverse_root(__builtin_fmaf(head_sum<LN>(sum), by_width, a.eps));
 #pragma unroll
                     for (int c = 0; c < 8; ++c) v[c] *= inv * (of_q ? gq[c] : gk[c]);
                 }
