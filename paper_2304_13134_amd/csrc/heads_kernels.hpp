@@ -275,6 +275,20 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadArgs a)
         } else if (a.turn.first) {
             position += same_for_all(a.turn.first, b);
         }
+        // (a frame that is not there has zeros, whatever the gains and frequencies are)
+        if (!there) {
+            const float zeros[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int i = part; i < (PAGES ? g0 : g1); i += split) {
+                const bool of_q = i < g0;
+                const int h = (of_q ? i : i - g0) * kAtOnce;
+                if (!at.here || group >= (of_q ? s0.heads : s1.heads) - h) continue;
+                char* const y = (char*)(of_q ? s0.y : s1.y) + ((size_t)row * (of_q ? s0.py : s1.py) + (size_t)h * a.D) * kSize;
+                store4<E>(y + o0, 0, zeros);
+                store4<E>(y + o1, 0, zeros);
+            }
+            continue;
+        }
         float sn[4], cs[4];
 #pragma unroll 1
         for (int i = part; i < groups; i += split) {
@@ -283,14 +297,13 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadArgs a)
             const bool on = at.here && group < heads - h;
             const size_t column = (size_t)h * a.D;
             Four<E> x[2]{};
-            if (there && on)
+            if (on)
                 get8<E>((const char*)(of_q ? s0.x : of_k ? s1.x : s2.x) + ((size_t)row * (of_q ? s0.px : of_k ? s1.px : s2.px) + column) * kSize, o0, o1, x);
             if (i == part) angles.get(position, at, sn, cs);
             float v[8];
             unpack4<E>(x[0], v);
             unpack4<E>(x[1], v + 4);
-            // (a frame that is not there keeps its zeros, whatever the gains and frequencies are)
-            if (there && (of_q || of_k)) {
+            if (of_q || of_k) {
                 if (of_q ? s0.gain : s1.gain) {
                     float sum = 0.f;
 #pragma unroll
@@ -306,7 +319,7 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadArgs a)
                 char* const y = (char*)(of_q ? s0.y : s1.y) + ((size_t)row * (of_q ? s0.py : s1.py) + column) * kSize;
                 store4<E>(y + o0, 0, v);
                 store4<E>(y + o1, 0, v + 4);
-            } else if (there && page >= 0) {
+            } else if (page >= 0) {
                 char* const y = (of_k ? s1.pages : s2.pages) + (((size_t)page * heads + h + group) * a.cache.page + in_page) * a.D * kSize;
                 store4<E>(y, at.c0, v);
                 store4<E>(y, at.c1, v + 4);
