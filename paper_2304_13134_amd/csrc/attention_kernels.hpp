@@ -256,41 +256,80 @@ __device__ __forceinline__ float sum_of_halves(float v)
 // frames of an item, which is the same one for all lanes: lengths as clamped
 __device__ __forceinline__ int frames_of_item(const int* len, int T, int b) { return len ? clamped(same_for_all(len, b), T) : T; }
 
-template <typename E> __device__ __forceinline__ float value_at(const char* p, int c)
+// where a frame's keys and values are; null: nowhere, which makes NaN of what sees it
+struct KeyValue {
+    const char *k, *v;
+};
+
+// lane j's pointer
+__device__ __forceinline__ const char* of_lane(const char* p, int j)
 {
-    if constexpr (Elt<E>::type == LAST_BF16) return bf16_to_float(((const uint16_t*)p)[c]);
-    else return (float)((const _Float16*)p)[c];
+    const uintptr_t at = (uintptr_t)p;
+    const unsigned lo = (unsigned)__shfl((int)(unsigned)at, j, kWave), hi = (unsigned)__shfl((int)(unsigned)(at >> 32), j, kWave);
+    return (const char*)((uintptr_t)lo | (uintptr_t)hi << 32);
 }
 
-// One frame's attention without matrix cores, by a wavefront, the head's columns over its lanes.  The products of the kernels multiply what is not
-// seen by zero, which is no number for an infinity or a NaN; rows that come out so are formed again here, over what they see alone.
-// seen(s): whether s in [from, to) is; row(p, s): where its keys and values are.
-template <typename E, typename Seen, typename KeyRow, typename ValueRow>
-__device__ void plain_row(const char* q, int D, float c2, int from, int to, Seen seen, KeyRow key, ValueRow value, float* m, float* l, float* o)
+// One frame's attention without matrix cores, by a wavefront, to frames [from0, to0) and then [from, to).  The products of the kernels multiply what is not
+// seen by zero, which is no number for an infinity or a NaN; rows that come out so are formed again here, over what they see alone.  64 frames at a
+// time: scores with a frame a lane, then eight columns of a frame a lane; o: columns 8 (lane % (DP / 8)) ...  It ends where the sum is no number (a NaN
+// in the query or a key that is seen, a score of +inf), which all results then are.  A bad frame makes such rows of all that see it, 32 of them one
+// after the other, and each waits for its loads, so that many are under way at once: 8192 frames, 8 heads of 64, an infinite value among all that a frame
+// sees: 7.8 ms (46 with four frames' values under way), a NaN key 0.2, neither 0.13.
+template <typename E, int DP, typename Where>
+__device__ void plain_row(const char* q, int D, float c2, int from0, int to0, int from, int to, Where where, float* m, float* l, float* o)
 {
+    constexpr int kPieces = DP / 8, kAtOnce = kWave / kPieces, kAhead = kPieces < 8 ? kPieces : 8;
     const int lane = (int)threadIdx.x % kWave;
-    float x[2], top = LAST_NEG_INF, sum = 0.f;
-    o[0] = o[1] = 0.f;
+    const int piece = lane % kPieces, row = lane / kPieces, column = piece * 8 < D ? piece * 8 : 0;
+    float top = LAST_NEG_INF, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) x[i] = lane + 64 * i < D ? value_at<E>(q, lane + 64 * i) : 0.f;
-    for (int s = from; s < to; ++s) {
-        if (!seen(s)) continue;
-        const char *k = key(s), *v = value(s);
-        float dot = 0.f, w[2] = {0.f, 0.f};
+    for (int k = 0; k < 8; ++k) o[k] = 0.f;
+    for (int part = 0; part < 2 && sum == sum; ++part) {
+        const int end = part ? to : to0;
+        for (int s0 = part ? from : from0; s0 < end; s0 += kWave) {
+            const int n = end - s0 < kWave ? end - s0 : kWave;
+            const KeyValue at = where(s0 + (lane < n ? lane : n - 1));
+            float dot = 0.f;
+            if (at.k) {
+#pragma unroll kAhead
+                for (int j = 0; j < kPieces; ++j) {
+                    const int c = j * 8 < D ? j * 8 : 0;
+                    float x[8], y[8];
+                    unpack<E>(Raw<E>{*(const u4_any*)(q + c * 2)}, x);
+                    unpack<E>(Raw<E>{*(const u4_any*)(at.k + c * 2)}, y);
+                    float t = dot;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (lane + 64 * i < D) {
-                dot += x[i] * (k ? value_at<E>(k, lane + 64 * i) : __uint_as_float(0x7fc00000u));
-                w[i] = v ? value_at<E>(v, lane + 64 * i) : 0.f;
+                    for (int k = 0; k < 8; ++k) t = __builtin_fmaf(x[k], y[k], t);
+                    dot = j * 8 < D ? t : dot;
+                }
             }
-        dot = wave_sum(dot);
-        const float higher = fmaxf(top, dot), by = higher == LAST_NEG_INF ? 0.f : higher;
-        const float old = __builtin_amdgcn_exp2f((top - by) * c2), p = __builtin_amdgcn_exp2f((dot - by) * c2);
-        top = higher;
-        sum = sum * old + p;
+            dot = lane >= n ? LAST_NEG_INF : at.k ? dot : __uint_as_float(0x7fc00000u);
+            const float higher = fmaxf(top, wave_max(dot)), by = higher == LAST_NEG_INF ? 0.f : higher;
+            const float old = __builtin_amdgcn_exp2f((top - by) * c2), p = __builtin_amdgcn_exp2f((dot - by) * c2);
+            top = higher;
+            sum = sum * old + wave_sum(p);
+            if (__any(!(sum == sum))) break;
+            u4 w[kPieces];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) o[i] = o[i] * old + p * w[i];
+            for (int i = 0; i < kPieces; ++i) w[i] = *(const u4_any*)(of_lane(at.v, row + i * kAtOnce) + column * 2);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] *= old;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int r = row + i * kAtOnce;
+                const unsigned keep = r < n ? ~0u : 0u;
+                const float pr = __shfl(p, r, kWave);
+                float v[8];
+                unpack<E>(Raw<E>{w[i] & u4{keep, keep, keep, keep}}, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(pr, v[k], o[k]);
+            }
+        }
     }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int x = kPieces; x < kWave; x <<= 1) o[k] += __shfl_xor(o[k], x, kWave);
     *m = top;
     *l = sum;
 }
@@ -617,13 +656,15 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
     for (unsigned long long rows = __ballot(odd) & 0xffffffffull; rows; rows &= rows - 1) {
         const int tr = t0 + __ffsll(rows) - 1;
         const int end = tr + band.right + 1 < at.len ? tr + band.right + 1 : at.len;
-        float m, sum, o[2];
-        plain_row<E>(q + (size_t)tr * a.pq * 2, a.D, c2, 0, end, [&](int s) { return s >= tr - band.left || s < band.sinks; },
-                     [&](int s) { return k + (size_t)s * a.pk * 2; }, [&](int s) { return v + (size_t)s * a.pv * 2; }, &m, &sum, o);
+        float m, sum, o[8];
+        const int firsts = band.sinks < end ? band.sinks : end, from = tr - band.left > firsts ? tr - band.left : firsts;
+        plain_row<E, DP>(q + (size_t)tr * a.pq * 2, a.D, c2, 0, firsts, from, end, [&](int s) { return KeyValue{k + (size_t)s * a.pk * 2, v + (size_t)s * a.pv * 2}; },
+                     &m, &sum, o);
         char* const y = (char*)a.y + (((at.row0 + tr) * a.py) + (size_t)at.head * a.D) * 2;
+        if (lane < DP / 8 && lane * 8 < a.D) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (lane + 64 * i < a.D) Elt<E>::put(y, lane + 64 * i, o[i] / sum);
+            for (int c = 0; c < 8; ++c) Elt<E>::put(y, lane * 8 + c, o[c] / sum);
+        }
         if (a.lse && lane == 0) a.lse[(at.row0 + tr) * a.heads + at.head] = (m * c2 + __builtin_amdgcn_logf(sum)) * kLn2;
     }
 }

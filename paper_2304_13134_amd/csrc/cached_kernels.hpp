@@ -252,21 +252,25 @@ __global__ __launch_bounds__(256, 2) void cached_kernel(CachedArgs a)
     }
     for (unsigned long long bits = __ballot(odd) & 0xffffffffull; bits; bits &= bits - 1) {
         const int rr = rb * 32 + __ffsll(bits) - 1, tr = rr / group, hr = kv * group + rr % group, at = used + tr;
-        const int to = at + band.right + 1 < total ? at + band.right + 1 : total, stop = start(end - 1) + 32;
-        const auto where = [&](const char* base, int s) -> const char* {
-            const long long p = row_of(s);
-            return p >= 0 ? base + p * 2 : nullptr;
-        };
-        float pm, pl, o[2];
-        plain_row<E>((const char*)a.q + ((row0 + tr) * a.pq + (size_t)hr * a.D) * 2, a.D, c2, start(begin), to < stop ? to : stop,
-                     [&](int s) { return s >= at - band.left || s < sinks; }, [&](int s) { return where(a.k, s); },
-                     [&](int s) { return where(a.v, s); }, &pm, &pl, o);
+        // of what the row sees, the split's blocks: first frames and the others
+        const int start0 = start(begin), stop = start(end - 1) + 32, last_seen = at + band.right + 1 < total ? at + band.right + 1 : total;
+        const int to = last_seen < stop ? last_seen : stop, firsts = sinks < to ? sinks : to;
+        const int low = at - band.left > firsts ? at - band.left : firsts;
+        float pm, pl, o[8];
+        plain_row<E, DP>((const char*)a.q + ((row0 + tr) * a.pq + (size_t)hr * a.D) * 2, a.D, c2, start0, firsts, low > start0 ? low : start0, to,
+                     [&](int s) {
+                         const long long p = row_of(s);
+                         return p >= 0 ? KeyValue{a.k + p * 2, a.v + p * 2} : KeyValue{nullptr, nullptr};
+                     },
+                     &pm, &pl, o);
+        if (lane < DP / 8 && lane * 8 < a.D) {
+            char* const y = (char*)a.y + ((row0 + tr) * a.py + (size_t)hr * a.D) * 2;
+            float* const out = a.part + ((part_row + rr) * a.splits + split) * a.D;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int c = lane + 64 * i;
-            if (c >= a.D) continue;
-            if (a.splits == 1) Elt<E>::put((char*)a.y + ((row0 + tr) * a.py + (size_t)hr * a.D) * 2, c, o[i] / pl);
-            else a.part[((part_row + rr) * a.splits + split) * a.D + c] = o[i];
+            for (int c = 0; c < 8; ++c) {
+                if (a.splits == 1) Elt<E>::put(y, lane * 8 + c, o[c] / pl);
+                else out[lane * 8 + c] = o[c];
+            }
         }
         if (a.splits > 1 && lane == 0) {
             float* const ml = a.part_ml + ((part_row + rr) * a.splits + split) * 2;
