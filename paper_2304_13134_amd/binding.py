@@ -622,25 +622,23 @@ def _launch(on, call, *arguments):
     _check(call(*arguments, torch._C._cuda_getCurrentRawStream(on)))
 
 
-def _with_scratch(call, op, frames, N, K, a, b, t):
-    """call(workspace address, bytes, stream) for tensor t's device and its current stream, with what last_layer_workspace_bytes asks for."""
-    _with_scratch_of(call, lambda: load_library().last_layer_workspace_bytes(op, frames, N, K, a, b), t)
-
-
-def _with_scratch_of(call, size, t):
-    """call(workspace address, bytes, stream) for tensor t's device and its current stream.  The buffer that is there is tried
-    first: the library refuses one that is too small before it enqueues anything.  (Not under capture, see workspace().)"""
+def _with_scratch(call, op, *sizes):
+    """call(workspace address, bytes, stream) for the device and the current stream of the tensor that `sizes` ends with; the others are
+    what the scratch bytes of `op` depend on.  The buffer that is there is tried first: the library refuses one that is too small before it
+    enqueues anything.  (Not under capture, see workspace().)"""
+    t = sizes[-1]
     on = t.get_device()
     if on != torch._C._cuda_getDevice():
         with torch.cuda.device(on):
-            return _with_scratch_of(call, size, t)
+            return _with_scratch(call, op, *sizes)
     stream = torch._C._cuda_getCurrentRawStream(on)
     buf = None if torch._C._cuda_isCurrentStreamCapturing() else _workspaces.get((on, stream))
     if buf is not None:
         code = call(buf.data_ptr(), buf.numel(), stream)
         if code != 5:
             return _check(code)
-    nbytes = size()
+    lib = load_library()
+    nbytes = (lib.last_layer_workspace_bytes if op < OP_HEAD_NORM_GRAD else lib.last_attention_workspace_bytes)(op, *sizes[:-1])
     buf = workspace(nbytes or 256, t.device)          # (where none would do, the call says what is wrong)
     _check(call(buf.data_ptr(), buf.numel(), stream))
 
@@ -880,9 +878,9 @@ def last_head_norm_grad(dyq, dyk, q, k, width, gain_q=None, gain_k=None, rotatio
         if gain is not None:
             dg[i] = torch.empty(width, dtype=torch.float32, device=t.device)
     lib = load_library()
-    _with_scratch_of(lambda ws, n, stream: lib.last_head_norm_grad(fr, heads, dy[0], dy[1], x[0], x[1], g[0], g[1], eps, r, mdx[0], mdx[1],
-                                                                  _ptr(dg[0]), _ptr(dg[1]), ws, n, stream),
-                     lambda: lib.last_attention_workspace_bytes(OP_HEAD_NORM_GRAD, fr, heads, None, None), one)
+    _with_scratch(lambda ws, n, stream: lib.last_head_norm_grad(fr, heads, dy[0], dy[1], x[0], x[1], g[0], g[1], eps, r, mdx[0], mdx[1],
+                                                               _ptr(dg[0]), _ptr(dg[1]), ws, n, stream),
+                  OP_HEAD_NORM_GRAD, fr, heads, None, None, one)
     return dx[0], dx[1], dg[0], dg[1]
 
 
@@ -913,8 +911,8 @@ def last_attention_grad(dy, q, k, v, y, lse, width, left=None, right=0, sinks=0,
         out = whole.split([n * width, kv * width, kv * width], dim=-1)
     mo = [_matrix(t, name, on, rows, x.shape[-1]) for t, name, x in zip(out, ("dq", "dk", "dv"), (q, k, k))]
     band, lib = _band(left, right, sinks, scale, width), load_library()
-    _with_scratch_of(lambda ws, m, stream: lib.last_attention_grad(fr, heads, band, mdy, mq, mk, mv, my, l, mo[0], mo[1], mo[2], ws, m, stream),
-                     lambda: lib.last_attention_workspace_bytes(OP_ATTENTION_GRAD, fr, heads, band, None), q)
+    _with_scratch(lambda ws, m, stream: lib.last_attention_grad(fr, heads, band, mdy, mq, mk, mv, my, l, mo[0], mo[1], mo[2], ws, m, stream),
+                  OP_ATTENTION_GRAD, fr, heads, band, None, q)
     return tuple(out)
 
 
@@ -993,6 +991,6 @@ def last_cached_attention(q, cache, left=None, right=0, sinks=0, scale=None, len
     mq, mc, band = _matrix(q, "q", on), _cache(cache, B, on), _band(left, right, sinks, scale, width)
     y, my = _result(q.shape, q.dtype, q.device, q)
     status, lib = _status_of(item_status, B, q, on), load_library()
-    _with_scratch_of(lambda ws, n, stream: lib.last_cached_attention(fr, heads, band, mq, mc, my, status, ws, n, stream),
-                     lambda: lib.last_attention_workspace_bytes(OP_CACHED_ATTENTION, fr, heads, band, mc), q)
+    _with_scratch(lambda ws, n, stream: lib.last_cached_attention(fr, heads, band, mq, mc, my, status, ws, n, stream),
+                  OP_CACHED_ATTENTION, fr, heads, band, mc, q)
     return y
