@@ -364,9 +364,10 @@ last_status_t last_kept_grad(const last_frames_t* frames, int32_t H, const last_
 /* ---- Frames that see each other: attention in the layer, and its streaming form on a paged cache.
  *
  * Columns are heads: head h of a matrix has columns h*width .. (h+1)*width - 1.  Queries and results have `heads` of them, keys and
- * values kv_heads, each of which heads / kv_heads neighbouring query heads share.  width is a multiple of 8 up to 128; T is at most
- * 2^28, and with bands B * T * heads is less than 2^31.  Rows, pitches, alignment, lengths and frames that do not exist are as
- * above, so queries, keys and values may be columns of the one matrix that a product made, and gradients go back to columns of one. */
+ * values kv_heads, each of which heads / kv_heads neighbouring query heads share.  width is a multiple of 8 up to 128, heads is at most
+ * 65536, T at most 2^28, T * heads at most 2^30 and B * T * heads at most 2^36, or less than 2^31 in calls with a band.  Rows, pitches,
+ * alignment, lengths and frames that do not exist are as above, so queries, keys and values may be columns of the one matrix that a product
+ * made, and gradients go back to columns of one. */
 typedef struct {
     int32_t heads, kv_heads, width;
 } last_heads_t;
@@ -388,7 +389,7 @@ typedef struct {
 } last_band_t;
 
 /* Keys and values of streams in pages.  k, v: dev [pages][kv_heads][page][width], BF16 or F16, 16-byte aligned.  Frames j*page .. of item b are on page
- * table[b][j], 0 <= j < entries; page * entries at most 2^30.  used[b] frames (clamped to [0, 2^30]) are in the cache
+ * table[b][j], 0 <= j < entries; page is at most 2^20, page * entries at most 2^30.  used[b] frames (clamped to [0, 2^30]) are in the cache
  * before the new ones of a call, which are frames used[b] + t; the caller counts them afterwards.  Entries of pages on which no frame is
  * written or seen may hold anything.  A frame whose entry is missing (j >= entries) or names no page gives its item
  * item_status 8: it is not written, and results of frames that see it are NaN. */
@@ -417,7 +418,8 @@ last_status_t last_head_norm_grad(const last_frames_t* frames, const last_heads_
 
 /* y[t] = sum over the frames s that t sees of P[t][s] v[s], P the softmax of scale * q[t] . k[s] over them; lse (dev float32
  * [B*T][heads], or NULL): the logarithm of the sum of exponentials, which the gradient needs.  q, k, v, y: all BF16 or all F16.
- * Scores, sums and statistics are float32; P is rounded to the operands' type before it is multiplied.  What a frame
+ * Scores, sums and statistics are float32; P, relative to some value near the row's largest, is rounded to the operands' type before it is multiplied
+ * (in F16 terms smaller than 2^-14 of the largest have fewer than 11 digits, and those up to 2^-25 of it are in the sum alone).  What a frame
  * does not see has no part in its result, infinities and NaN in its place included.  Rows that these reach are formed a second time without
  * the matrix cores, which takes longer (here and in last_cached_attention): with an infinite value that all of 8192 frames see, causal,
  * 8 heads of 64, a call takes 8 ms and not 0.13; with a NaN or a score of +inf, which end such a row, 0.2. */
@@ -425,9 +427,10 @@ last_status_t last_attention(const last_frames_t* frames, const last_heads_t* he
                              const last_matrix_t* k, const last_matrix_t* v, const last_matrix_t* y, float* lse, void* hip_stream);
 
 /* The gradients of q, k and v, those of k and v summed over the heads that share them.  y and lse as last_attention returned
- * them; all matrices of one type, BF16 or F16.  P and dS are rounded to it before they are multiplied (in F16 a dS
- * beyond 65504, for instance of a loss scaled too far, is infinite).  Frames that do
- * not exist have no part in it; an infinity or a NaN in a frame that does may come out of the gradients of any of the item's frames.
+ * them; all matrices of one type, BF16 or F16.  P and dS are rounded to it before they are multiplied: in F16 a dS
+ * beyond 65504 (of a loss scaled too far) is infinite, and a P (relative to its row's sum) or a dS has fewer than 11 digits below 2^-14 and is
+ * zero up to 2^-25 (of a loss that is not scaled up, or where a row is shared by more than 16384 frames).  Frames that do not exist have no part
+ * in it; an infinity or a NaN in a frame that does may come out of the gradients of any of the item's frames.
  * Workspace: LAST_OP_ATTENTION_GRAD. */
 last_status_t last_attention_grad(const last_frames_t* frames, const last_heads_t* heads, const last_band_t* band, const last_matrix_t* dy,
                                   const last_matrix_t* q, const last_matrix_t* k, const last_matrix_t* v, const last_matrix_t* y,

@@ -29,7 +29,8 @@ last_status_t check_heads(const last_heads_t* h)
     return LAST_OK;
 }
 
-// seen: of a call in which frames see each other, whose workgroups, at most one for each head of each frame, are numbered in 32 bits
+// seen: of a call in which frames see each other, whose workgroups, at most one for each head of each frame, are numbered in 32 bits; an item's heads of
+// frames in blocks of 32 are counted in 31
 last_status_t check_items(const last_frames_t* f, const last_heads_t* h, bool seen, long long* rows)
 {
     LAST_TRY(check_frames(f, rows));
@@ -53,13 +54,12 @@ last_status_t check_band(const last_band_t* b)
     return b->sinks > kMostSinks ? LAST_ERR_UNSUPPORTED : LAST_OK;
 }
 
-last_status_t check_cache(const last_cache_t* c, const last_heads_t* h, int T)
+last_status_t check_cache(const last_cache_t* c)
 {
     if (!c || !c->k || !c->v || !c->table || !c->used) return LAST_ERR_NULL;
     if (c->pages < 1 || c->page < 1 || c->page > kMostPage || c->entries < 1) return LAST_ERR_SHAPE;
-    if ((long long)c->page * c->entries > kMostUsed || T > kMostFrames) return LAST_ERR_SHAPE;
+    if ((long long)c->page * c->entries > kMostUsed) return LAST_ERR_SHAPE;
     if ((uintptr_t)c->k % 16 != 0 || (uintptr_t)c->v % 16 != 0) return LAST_ERR_SHAPE;
-    (void)h;
     return LAST_OK;
 }
 
@@ -313,7 +313,7 @@ size_t last_attention_workspace_bytes(int32_t op, const last_frames_t* frames, c
         if (check_band(band) != LAST_OK) return 0;
         plan_grad(cv, rows, frames, heads, band_of(band, frames->T));
     } else if (op == LAST_OP_CACHED_ATTENTION) {
-        if (check_band(band) != LAST_OK || check_cache(cache, heads, frames->T) != LAST_OK) return 0;
+        if (check_band(band) != LAST_OK || check_cache(cache) != LAST_OK) return 0;
         plan_cached(cv, rows, frames, heads, band, cache);
     } else {
         return 0;
@@ -498,7 +498,7 @@ last_status_t last_cache_append(const last_frames_t* frames, const last_heads_t*
     if (!k || !v || (q && !yq)) return LAST_ERR_NULL;
     if (!(eps >= 0.f)) return LAST_ERR_SHAPE;
     LAST_TRY(check_rotation(rotation, heads->width));
-    LAST_TRY(check_cache(cache, heads, frames->T));
+    LAST_TRY(check_cache(cache));
     const long long cq = (long long)heads->heads * heads->width, ck = (long long)heads->kv_heads * heads->width;
     const int type = cache->type;
     HeadArgs a{};
@@ -537,7 +537,7 @@ last_status_t last_cached_attention(const last_frames_t* frames, const last_head
     LAST_TRY(check_items(frames, heads, true, &rows));
     if (!q || !y) return LAST_ERR_NULL;
     LAST_TRY(check_band(band));
-    LAST_TRY(check_cache(cache, heads, frames->T));
+    LAST_TRY(check_cache(cache));
     const long long cq = (long long)heads->heads * heads->width;
     const int type = cache->type;
     LAST_TRY(check_matrix(q, cq, half_width(type) && q->type == type));
