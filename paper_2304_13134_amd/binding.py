@@ -573,6 +573,13 @@ def _vector(t, n, name, on):
     return t.data_ptr()
 
 
+def _needed(t, n, name, on):
+    """_vector of one that a call reads: not None, though it may have no elements"""
+    if t is None:
+        raise TypeError("%s must be a device tensor" % name)
+    return _vector(t, n, name, on) or _NO_ROWS
+
+
 def _frames(t, lengths, name):
     """(packed LastFrames, leading sizes, tensor, its device) of a tensor or Kept [R, H] or [B, T, H]; with lengths it is the latter."""
     t = t[0] if isinstance(t, Kept) else t
@@ -673,7 +680,7 @@ def last_residual_norm_grad(dy, s, gain, inv, ds=None, lengths=None, dtype=None)
     if dtype is None:
         dtype = ds.dtype if ds is not None else dy.dtype if isinstance(s, Kept) else s.dtype
     mdy, ms, mds = _matrix(dy, "dy", on), _matrix(s, "s", on, rows, H), _opt(ds, "ds", on, rows, H)
-    g, i = _vector(gain, H, "gain", on), _vector(inv, dy.numel() // H, "inv", on) or _NO_ROWS
+    g, i = _vector(gain, H, "gain", on), _needed(inv, dy.numel() // H, "inv", on)
     dx, mdx = _result(dy.shape, dtype, device, dy)
     dgain = torch.empty(H, dtype=torch.float32, device=device)
     call = load_library().last_residual_norm_grad
@@ -905,7 +912,7 @@ def last_attention_grad(dy, q, k, v, y, lse, width, left=None, right=0, sinks=0,
     fr, rows, on, _ = _items(q, lengths, "q")
     mq, mk, mv = _matrix(q, "q", on), _matrix(k, "k", on, rows), _matrix(v, "v", on, rows, k.shape[-1])
     mdy, my = _matrix(dy, "dy", on, rows, q.shape[-1]), _matrix(y, "y", on, rows, q.shape[-1])
-    l = _vector(lse, q.numel() // width, "lse", on) or _NO_ROWS
+    l = _needed(lse, q.numel() // width, "lse", on)
     if out is None:
         whole = torch.empty((*rows, (n + 2 * kv) * width), dtype=q.dtype, device=q.device)
         out = whole.split([n * width, kv * width, kv * width], dim=-1)
