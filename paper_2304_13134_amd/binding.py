@@ -801,6 +801,8 @@ def _heads_of(t, name, width):
 
 def _heads(q, k, width):
     """(packed LastHeads, heads, kv_heads) of matrices of which one may be None"""
+    if q is None and k is None:
+        raise TypeError("queries and keys cannot both be None")
     heads = None if q is None else _heads_of(q, "q", width)
     kv = None if k is None else _heads_of(k, "k", width)
     if heads is not None and kv is not None and heads % kv != 0:
@@ -923,6 +925,10 @@ def last_attention_grad(dy, q, k, v, y, lse, width, left=None, right=0, sinks=0,
     return tuple(out)
 
 
+def _no_cache():
+    raise TypeError("a Cache holds four device tensors, the first two [pages, kv_heads, page, width]") from None
+
+
 def _refuse_cache(cache, B, on):
     """Raises what is wrong with a Cache that _cache does not take."""
     k, v, table, used = cache
@@ -970,7 +976,12 @@ def last_cache_append(k, v, cache, q=None, gain_q=None, gain_k=None, frequencies
     """Keys of new frames, normed and rotated as by last_head_norm at positions used + t, and their values into a Cache; with q, returns its
     queries, normed and rotated by the same call, else None.  k, v: [B, T, kv_heads width] of the cache's type, of which lengths [B] new
     frames exist.  item_status: see check_item_status()."""
-    _, held, _, width = cache[0].shape
+    try:
+        _, held, _, width = cache[0].shape
+    except (AttributeError, IndexError, TypeError, ValueError):
+        _no_cache()
+    if k is None:
+        raise TypeError("k must be a device tensor")
     heads, _, kv = _heads(q, k, width)
     fr, rows, on, B = _items(k, lengths, "k")
     r = _rotation(frequencies, width, B, on)
@@ -989,11 +1000,14 @@ def last_cache_append(k, v, cache, q=None, gain_q=None, gain_k=None, frequencies
 def last_cached_attention(q, cache, left=None, right=0, sinks=0, scale=None, lengths=None, item_status=None):
     """y: last_attention of new frames, q [B, T, columns] of which lengths [B] exist, at positions cache.used + t, to what a Cache holds after
     last_cache_append with the same `used`.  item_status: see check_item_status()."""
-    _, kv, _, width = cache[0].shape
-    columns = q.shape[-1]
-    if columns % (kv * width) != 0 or columns == 0:
+    try:
+        _, kv, _, width = cache[0].shape
+    except (AttributeError, IndexError, TypeError, ValueError):
+        _no_cache()
+    n = _heads_of(q, "q", width)
+    if kv == 0 or n % kv != 0:
         raise ValueError("q must have a multiple of the cache's %d heads of %d columns" % (kv, width))
-    heads = _pack_heads(columns // width, kv, width)
+    heads = _pack_heads(n, kv, width)
     fr, rows, on, B = _items(q, lengths, "q")
     mq, mc, band = _matrix(q, "q", on), _cache(cache, B, on), _band(left, right, sinks, scale, width)
     y, my = _result(q.shape, q.dtype, q.device, q)
