@@ -260,8 +260,8 @@ void launch_attention_grad(AttentionArgs a, int chunks, hipStream_t st)
     }
 }
 
-// Blocks of 32 rows, and over how many workgroups a block's frames are split: so that there are some 1024, each with at least
-// 256 frames if the window or the table lets there be as many.
+// Blocks of 32 rows, and over how many workgroups a block's frames are split: so that there are some 1024, each with at least 256 frames of the window, or of
+// what the table has room for where there is none (how many there are is known on the device alone; a split without frames ends at once).
 struct CachedPlan {
     int row_blocks, splits;
     float *part, *part_ml;

@@ -496,7 +496,9 @@ struct Order {
 // HALVES: a workgroup has 64 frames instead of 128, and two wavefronts for each 32 of them, one for either half of each tile, whose sums are joined at the end:
 // twice as many workgroups of half the length.
 // A tile of 64 columns is 16 products of 32 clocks for a SIMD, and 133 vector instructions beside them, 32 of them exponentials of 8 clocks.  Of 128
-// columns: 900 TF (8 x 2048 frames, 16 heads, all seen; the matrix cores are busy 42% of the time, at 1.8 GHz); of 64: 670 TF (64 x 1024, 8 heads; 38%).
+// columns: 900 TF (8 x 2048 frames, 16 heads, all seen; the matrix cores are busy 42% of the time, at 1.8 GHz); of 64: 660 TF (64 x 1024, 8 heads; 38%).
+// At 128 columns neither the vector units (0.08 instructions a clock) nor LDS (31 %) is what that waits for, but the order of a wavefront's work: products, exponentials
+// and products of a tile one after the other, nothing of the next one meanwhile.
 // Measured and left: 64 frames a wavefront, half the LDS reads but one wavefront a SIMD (8192 frames, 16 heads of 128: 182 us, so 110); a
 // block of 32 of the tile at a time (16 x 1000, 8 heads of 64: 59 us, so 53).
 template <typename E, int DP, bool HALVES>
@@ -686,8 +688,9 @@ __device__ __forceinline__ float row_product(const u4 (&x)[N], const u4 (&y)[N])
 }
 
 // The gradient of queries: a wavefront's own frames are queries, the tiles keys and values.  It comes first, and leaves delta for the others (a kernel of its
-// own for delta: 7 us of 81 at 16 x 1024 frames, 8 heads of 64 in a band).  Three products a tile; 230 us at 2 x 4096, 16 heads of 128 that see 2047
-// back (670 TF).
+// own for delta: 7 us of 81 at 16 x 1024 frames, 8 heads of 64 in a band).  Three products a tile; 225 to 242 us at 2 x 4096, 16 heads of 128 that see 2047
+// back (660 TF), bound by waits for LDS: with 253 registers in use nothing is read more than a product ahead (43 complete waits among 48 products).  In float16
+// 128 columns spill 196 registers: the whole gradient 677 us where it is 560 in bfloat16.
 template <typename E, int DP, bool HALVES>
 __global__ __launch_bounds__(256, 2) void grad_query_kernel(AttentionArgs a)
 {
@@ -822,8 +825,7 @@ __device__ __forceinline__ void key_tile(const char* qt, const char* yt, const f
 {
     const int h = (int)threadIdx.x % kWave >> 5;
     // (both gradients' sums and operands leave no registers for two blocks at a time)
-    constexpr int kAtOnce = 1;
-#pragma unroll kAtOnce
+#pragma unroll 1
     for (int n = from; n < to; ++n) {
         f16x p = zeros16(), e = zeros16();
 #pragma unroll
@@ -1026,7 +1028,8 @@ __device__ __forceinline__ void grad_key(const AttentionArgs& a, const Place& at
 
 // HALVES: as in attention_kernel.  APART: workgroups of a second half form the values' gradients, those of the first the keys', since both sums and operands of 128 columns do not leave
 // registers for two wavefronts on a SIMD; the scores are formed twice, which is a product of five (8 x 2048 frames, 16 heads: the whole gradient
-// 1503 us with both in one, 1185 apart).  370 us at 2 x 4096, 16 heads that see 2047 back: 690 TF with the scores counted twice.
+// 1503 us with both in one, 1185 apart).  368 to 389 us at 2 x 4096, 16 heads that see 2047 back: 660 TF with the scores counted twice; bound by waits for LDS
+// (25 among 24 products).  HALVES and APART spill 14 registers (15 in float16).
 template <typename E, int DP, bool APART, bool HALVES>
 __global__ __launch_bounds__(256, 2) void grad_key_kernel(AttentionArgs a)
 {
