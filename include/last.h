@@ -420,9 +420,9 @@ last_status_t last_head_norm_grad(const last_frames_t* frames, const last_heads_
  * [B*T][heads], or NULL): the logarithm of the sum of exponentials, which the gradient needs.  q, k, v, y: all BF16 or all F16.
  * Scores, sums and statistics are float32; P, relative to some value near the row's largest, is rounded to the operands' type before it is multiplied
  * (in F16 terms smaller than 2^-14 of the largest have fewer than 11 digits, and those up to 2^-25 of it are in the sum alone).  What a frame
- * does not see has no part in its result, infinities and NaN in its place included.  Rows that these reach are formed a second time without
- * the matrix cores, which takes longer (here and in last_cached_attention): with an infinite value that all of 8192 frames see, causal,
- * 8 heads of 64, a call takes 8 ms and not 0.13; with a NaN or a score of +inf, which end such a row, 0.2. */
+ * does not see has no part in its result, infinities and NaN in its place included.  Rows that infinities or NaN in v reach are formed a second time
+ * without the matrix cores, which takes longer (here and in last_cached_attention): with an infinite value that all of 8192 frames see,
+ * causal, 8 heads of 64, a call takes 8 ms and not 0.13. */
 last_status_t last_attention(const last_frames_t* frames, const last_heads_t* heads, const last_band_t* band, const last_matrix_t* q,
                              const last_matrix_t* k, const last_matrix_t* v, const last_matrix_t* y, float* lse, void* hip_stream);
 

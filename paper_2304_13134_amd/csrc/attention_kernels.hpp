@@ -270,11 +270,11 @@ __device__ __forceinline__ const char* of_lane(const char* p, int j)
 }
 
 // One frame's attention without matrix cores, by a wavefront, to frames [from0, to0) and then [from, to).  The products of the kernels multiply what is not
-// seen by zero, which is no number for an infinity or a NaN; rows that come out so are formed again here, over what they see alone.  64 frames at a
-// time: scores with a frame a lane, then eight columns of a frame a lane; o: columns 8 (lane % (DP / 8)) ...  It ends where the sum is no number (a NaN
-// in the query or a key that is seen, a score of +inf), which all results then are.  A bad frame makes such rows of all that see it, 32 of them one
-// after the other, and each waits for its loads, so that many are under way at once: 8192 frames, 8 heads of 64, an infinite value among all that a frame
-// sees: 7.8 ms (46 with four frames' values under way), a NaN key 0.2, neither 0.13.
+// seen by zero, which is no number for an infinite value or a NaN; rows that come out so, though their sums of probabilities are numbers, are formed again
+// here, over what they see alone.  64 frames at a time: scores with a frame a lane, then eight columns of a frame a lane; o: columns 8 (lane % (DP / 8)) ...
+// It ends should the sum be no number, which all results then are.  A bad value makes such rows of all that see it, 32 of them one after the other, and
+// each waits for its loads, so that many are under way at once: 8192 frames, 8 heads of 64, an infinite value among all that a frame sees: 7.8 ms (46 with
+// four frames' values under way), 0.13 without.
 template <typename E, int DP, typename Where>
 __device__ void plain_row(const char* q, int D, float c2, int from0, int to0, int from, int to, Where where, float* m, float* l, float* o)
 {
@@ -425,7 +425,7 @@ template <int DP> struct Softmax {
     // whether a result is no number (or would be for another frame's sake)
     __device__ __forceinline__ bool not_finite() const
     {
-        float t = l * 0.f;
+        float t = 0.f;
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -648,9 +648,9 @@ __global__ __launch_bounds__(256, DP == 128 ? 2 : 3) void attention_kernel(Atten
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) soft.acc[d][i] = soft.acc[d][i] * f0 + sums[(d * 16 + i) * kWave + lane] * f1;
-        soft.l = l;
     }
-    const bool odd = there && soft.not_finite();
+    // (a sum has no part of what is not seen: one that is no number makes a row that is none, as it stands)
+    const bool odd = there && l == l && soft.not_finite();
     if (t < a.T && !odd) {
         put_rows<E, DP>((char*)a.y + (row * a.py + (size_t)at.head * a.D) * 2, a.D, soft.acc, 1.f / l, there);
         if (a.lse && lane < 32) a.lse[row * a.heads + at.head] = there ? (soft.m * c2 + __builtin_amdgcn_logf(l)) * kLn2 : 0.f;

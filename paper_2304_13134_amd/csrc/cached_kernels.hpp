@@ -228,9 +228,7 @@ __global__ __launch_bounds__(256, 2) void cached_kernel(CachedArgs a)
         }
     }
     if (wave > 0) return;
-    soft.m = m;
-    soft.l = h ? 0.f : l;
-    const bool odd = there && soft.not_finite();
+    const bool odd = there && l == l && soft.not_finite();   // (as in attention_kernel)
     const size_t part_row = ((size_t)b * a.kv_heads + kv) * rows;
     if (r < rows && !odd) {
         if (a.splits == 1) {

@@ -90,10 +90,10 @@ def milliseconds(call):
     return min(times)
 
 
-@pytest.mark.parametrize("T,D,left,s", [(16384, 64, None, 0), (1 << 20, 8, 20, (1 << 20) - 30)])
+@pytest.mark.parametrize("T,D,left,s", [(16384, 64, None, 0), (16384, 64, None, 16000), (16384, 128, 5000, 16300), (1 << 20, 8, 20, (1 << 20) - 30)])
 def test_a_bad_key_on_a_long_item(T, D, left, s):
-    """All that see the key are NaN, the others have the bits that they have without it.  A walk through all earlier frames for each row, or on to the last
-    one after the first NaN, would take tens of milliseconds; an ordinary call takes 0.05 to 0.2."""
+    """All that see the key are NaN, the others have the bits that they have without it, and it takes no longer: a walk through all earlier frames for each row
+    would take tens of milliseconds, an ordinary call takes 0.05 to 0.2."""
     announce("bad key, long", T, D, left)
     rng = np.random.default_rng(1)
     q, k, v = (draw(rng, (1, T, D), "bf16") for _ in range(3))
@@ -106,7 +106,7 @@ def test_a_bad_key_on_a_long_item(T, D, left, s):
     assert torch.equal(y[0, ~sees], y0[0, ~sees]) and torch.equal(lse[0, ~sees], l0[0, ~sees])
     ms = milliseconds(lambda: lb.last_attention(q, k, v, D, left=left))
     print("milliseconds", ms, flush=True)
-    assert ms < 20
+    assert ms < 2
 
 
 def test_a_bad_key_in_a_long_cache():
@@ -126,4 +126,4 @@ def test_a_bad_key_in_a_long_cache():
     lb.check_item_status()
     ms = milliseconds(call)
     print("milliseconds", ms, flush=True)
-    assert ms < 20
+    assert ms < 2
