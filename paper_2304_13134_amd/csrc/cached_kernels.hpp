@@ -248,7 +248,9 @@ __global__ __launch_bounds__(256, 2) void cached_kernel(CachedArgs a)
             }
         }
     }
-    for (unsigned long long bits = __ballot(odd) & 0xffffffffull; bits; bits &= bits - 1) {
+    unsigned long long bits = __ballot(odd) & 0xffffffffull;
+    if (__builtin_expect(bits == 0, 1)) return;              // (the usual end before that code, not behind it: 8 x 16 new frames 14.5 -> 14.2 us)
+    for (; bits; bits &= bits - 1) {
         const int rr = rb * 32 + __ffsll(bits) - 1, tr = rr / group, hr = kv * group + rr % group, at = used + tr;
         // of what the row sees, the split's blocks: first frames and the others
         const int start0 = start(begin), stop = start(end - 1) + 32, last_seen = at + band.right + 1 < total ? at + band.right + 1 : total;
